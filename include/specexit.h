@@ -65,6 +65,7 @@ typedef enum { SPECEXIT_KV_CONTIG = 0, SPECEXIT_KV_PAGED = 1 } specexit_kv_layou
 #define SPECEXIT_STATUS_BAD_PAGE   2 /* page id outside 0 .. n_pages-1                            */
 #define SPECEXIT_STATUS_BAD_TOKEN  3 /* token id outside 0 .. vocab-1                             */
 #define SPECEXIT_STATUS_BAD_NODE   4 /* node id / path entry outside its block                    */
+#define SPECEXIT_STATUS_BAD_SETTING 5 /* specexit_sample: top_k between SPECEXIT_SAMPLE_MAX_K and V */
 #define SPECEXIT_MAX_NQ 64
 #define SPECEXIT_MAX_TOP_B 4 /* ranked continuations a tree-drafting row can report */
 #define SPECEXIT_N_SIGNALS 3
@@ -121,6 +122,26 @@ typedef struct {
   int32_t page_size, max_pages_per_seq;
   int64_t l_max, n_pages;
 } specexit_kv_view;
+
+/* One layer's K/V cache in 8 bits: a row (one entry of one KV head, head_dim values) is head_dim
+ * e4m3 codes (the finite-only format: 448 the largest, 0x7F / 0xFF NaN) and one scale byte s, 1..254,
+ * and stands for code * 2^(s - 127).
+ *   CONTIG: k, v are [B, n_kv_heads, l_max, head_dim] bytes, k_scale, v_scale [B, n_kv_heads, l_max];
+ *           l_max a multiple of 16.
+ *   PAGED : k, v are [n_pages, n_kv_heads, page_size, head_dim] bytes, k_scale, v_scale
+ *           [n_pages, n_kv_heads, page_size]; page_table as in specexit_kv_view, page_size any
+ *           multiple of 16.
+ * All four pointers are 16-byte aligned. */
+typedef struct {
+  uint32_t struct_size;
+  int32_t layout;        /* specexit_kv_layout */
+  int32_t n_kv_heads, head_dim;
+  void *k, *v;
+  void *k_scale, *v_scale;
+  const int32_t *page_table;
+  int32_t page_size, max_pages_per_seq;
+  int64_t l_max, n_pages;
+} specexit_quant_kv_view;
 
 /* Exit controller settings.  Defaults of the paper: alpha 0.1 (Appendix, EWMA);
  * confidence > 0.8, progress > 0.3, remaining < 200 for the combined rule, or
@@ -340,6 +361,70 @@ int32_t specexit_kv_compact(const specexit_kv_view *kv, int32_t n_layers, int64_
                             const int32_t *last_node /*[B]*/, const void *block_hidden /*[B,n_q,D] or NULL*/,
                             int32_t D, void *hidden_next /*[B,D]*/, uint32_t flags, void *stream);
 
+/* ---- the 8-bit cache: rows written (the target's cache entries of a prompt or a block) ----
+ * Row (b, t, h) of k_rows / v_rows - token t of sequence b lies (b * T + t) * token_stride elements
+ * behind the pointer, head h of it h * head_dim further on; dtype - is stored at entry pos[b] + t for
+ * t < count[b] (count NULL: T; at most T of them).  token_stride >= n_kv_heads * head_dim, so that the rows may lie
+ * in the output of a fused projection.  With amax = m * 2^E the largest finite magnitude of a row,
+ * 1 <= m < 2, its scale byte is max(1, E + 127 - 8 + (m > 1.75)): the least power of two that brings
+ * the row within 448 (2^-126 for a row of zeros); its codes are the nearest e4m3 numbers to value / scale, ties
+ * to even; values that are not finite become NaN codes.  Rows past count[b] and entries outside the
+ * cache are left as they are (the latter are reported).  No two sequences of a call may share entries that it
+ * writes.  Pointers and strides are multiples of 16 bytes. */
+int32_t specexit_quant_kv_write(const specexit_quant_kv_view *kv, int32_t dtype, int32_t B, int32_t T,
+                                const void *k_rows, const void *v_rows, int64_t token_stride,
+                                const int32_t *pos /*[B]*/, const int32_t *count /*[B] or NULL*/,
+                                uint32_t flags, void *stream);
+
+/* ---- stage 2 over the 8-bit cache: specexit_verify_attn with such a view (Alg. 1) ----
+ * Arguments, masks and limits as there; dtype is that of q and out.  The queries and the
+ * cache's numbers are multiplied as they are: nothing is rounded but sums (fp32), probabilities
+ * (16 bits; fp32: 24) and the output.  Entries that a row does not see may hold anything, NaN
+ * included; a row that sees nothing (an empty context and an empty mask word) is all zeros. */
+int32_t specexit_quant_verify_attn(const specexit_quant_kv_view *kv, int32_t dtype, int32_t B, int32_t n_q,
+                                   int32_t n_q_heads, const void *q, const int32_t *ctx_len /*[B]*/,
+                                   const uint64_t *mask /*[B,n_q] or NULL*/, float scale, void *out,
+                                   void *workspace, size_t workspace_bytes, uint32_t flags, void *stream);
+size_t specexit_quant_verify_attn_workspace_bytes(const specexit_quant_kv_view *kv, int32_t dtype, int32_t B,
+                                                  int32_t n_q, int32_t n_q_heads);
+
+/* ---- after the round, 8-bit cache: specexit_kv_compact for such a view ----
+ * Codes and scales of the accepted path move; layers lie layer_stride_bytes apart in k and v and
+ * scale_stride_bytes apart in k_scale and v_scale.  dtype is that of block_hidden / hidden_next.  A row whose page id
+ * lies outside the pool is neither read nor written. */
+int32_t specexit_quant_kv_compact(const specexit_quant_kv_view *kv, int32_t n_layers, int64_t layer_stride_bytes,
+                                  int64_t scale_stride_bytes, int32_t B, int32_t n_q, const int32_t *ctx_len /*[B]*/,
+                                  const int32_t *accept_path /*[B,n_q]*/, const int32_t *accept_len /*[B]*/,
+                                  int32_t dtype, const int32_t *last_node /*[B]*/,
+                                  const void *block_hidden /*[B,n_q,D] or NULL*/, int32_t D,
+                                  void *hidden_next /*[B,D]*/, uint32_t flags, void *stream);
+
+/* ---- stage 3, sampled: a token per row of logits from a given uniform number (Alg. 1 samples the
+ * target's token) ----
+ * logits [M, ld] in dtype (ld >= V; specexit_lmhead_argmax writes fp32 ones to logits_dbg).  Row r takes
+ * entry r / rows_per_seq of temperature, top_k, top_p and min_p (each may be NULL = off):
+ *   weight w_i = exp((l_i - max l) / temperature), 0 where it is below 2^-40; a temperature below
+ *   2^-10 (0 included) means the best token, lowest index on ties; it is forced to at most 2^96;
+ *   top_k  the k best tokens, by (logit descending, index ascending); k < 1 or k >= V: all;
+ *          k between SPECEXIT_SAMPLE_MAX_K and V is forced to that and reported;
+ *   top_p  of those, the ones whose better ones sum to less than top_p times their sum, at least the best; >= 1: all;
+ *   min_p  of those, the ones with w_i >= min_p (forced to at most 1).
+ * token[r] is the lowest index whose cumulative weight over kept indices is above u[r] times
+ * the kept weights' sum (u in [0, 1), forced into it); prob[r] (may be NULL) its share of that sum.  NaN logits are never
+ * drawn; if one is +infinity, only such ones are; a row without any logit above -infinity gives token -1 and
+ * prob 0.  Weights are 64-bit numbers and their sums fixed-point ones, so that a draw is the same
+ * whatever the launch shape, and a border between two tokens, or of a filter, is met to 1e-12 of the sum.
+ * The drafts of specexit_draft_step and _tree_level are not drawn, so handing
+ * these tokens to specexit_accept_exit as target_argmax accepts a draft with the target's own
+ * probability of it and leaves the output distributed as without drafts. */
+#define SPECEXIT_SAMPLE_MAX_K 1024
+#define SPECEXIT_SAMPLE_MAX_V 262144
+int32_t specexit_sample(int32_t dtype, int32_t M, int32_t V, const void *logits /*[M,ld]*/, int64_t ld,
+                        int32_t rows_per_seq, const float *temperature, const int32_t *top_k, const float *top_p,
+                        const float *min_p, const float *u /*[M]*/, int32_t *token /*[M]*/, float *prob /*[M] or NULL*/,
+                        void *workspace, size_t workspace_bytes, uint32_t flags, void *stream);
+size_t specexit_sample_workspace_bytes(int32_t dtype, int32_t M, int32_t V);
+
 /* ---- measurement aid -------------------------------------------------------------------
  * Hands the library n pairs of caller-owned hipEvent_t ([host] arrays of handles).  From then
  * on, each launch of the named kernel records the next unused pair around that one kernel (for
@@ -366,7 +451,7 @@ int32_t specexit_copy_probe(const void *src, void *dst, size_t bytes, int32_t no
 
 /* ---- scratch sizes, one query for every call ------------------------------------------------
  * Bytes of workspace that call `op` needs for B sequences and n_q block entries (draft tree level:
- * n_q = W rows per sequence; LM head: M = B * n_q rows).  `desc` is a [host] struct of the op's
+ * n_q = W rows per sequence; LM head and sampling: M = B * n_q rows).  `desc` is a [host] struct of the op's
  * query type below (first field struct_size); 0 is returned for shapes the call would reject and
  * for ops that use no scratch.  The per-call *_workspace_bytes functions give the same numbers. */
 #define SPECEXIT_OP_DRAFT_STEP       0 /* desc: specexit_draft_query                        */
@@ -375,6 +460,10 @@ int32_t specexit_copy_probe(const void *src, void *dst, size_t bytes, int32_t no
 #define SPECEXIT_OP_ACCEPT_EXIT      3 /* no scratch: 0                                     */
 #define SPECEXIT_OP_DRAFT_TREE_LEVEL 4 /* desc: specexit_draft_query (top_b used)           */
 #define SPECEXIT_OP_KV_COMPACT       5 /* no scratch: 0                                     */
+#define SPECEXIT_OP_QUANT_VERIFY_ATTN 6 /* desc: specexit_quant_attn_query                  */
+#define SPECEXIT_OP_SAMPLE           7 /* desc: specexit_sample_query                       */
+#define SPECEXIT_OP_QUANT_KV_WRITE   8 /* no scratch: 0                                     */
+#define SPECEXIT_OP_QUANT_KV_COMPACT 9 /* no scratch: 0                                     */
 typedef struct {
   uint32_t struct_size;
   const specexit_model_desc *desc;
@@ -390,6 +479,15 @@ typedef struct {
   uint32_t struct_size;
   int32_t dtype, hidden, vocab, n_extra;
 } specexit_lmhead_query;
+typedef struct {
+  uint32_t struct_size;
+  const specexit_quant_kv_view *kv;
+  int32_t dtype, n_q_heads;
+} specexit_quant_attn_query;
+typedef struct {
+  uint32_t struct_size;
+  int32_t dtype, vocab;
+} specexit_sample_query;
 size_t specexit_workspace_bytes(int32_t op, const void *desc, int32_t B, int32_t n_q);
 
 const char *specexit_last_error(void); /* [host] thread-local, never NULL */

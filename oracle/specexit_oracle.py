@@ -572,3 +572,79 @@ def kv_compact(k, v, ctx_len, accept_path, accept_len, page_table=None, page_siz
         return k_new, v_new
     hidden_next = np.stack([block_hidden[b, int(last_node[b])] for b in range(B)])
     return k_new, v_new, hidden_next
+
+
+# ---------------------------------------------------------------------------
+# the 8-bit cache and sampled tokens
+# ---------------------------------------------------------------------------
+
+def _e4m3_values() -> np.ndarray:
+    """The 256 numbers of the finite-only e4m3 format: sign, four exponent bits of bias 7, three mantissa bits; no infinities, one NaN a sign."""
+    out = np.empty(256, dtype=F64)
+    for c in range(256):
+        e, m = c >> 3 & 15, c & 7
+        x = np.ldexp(m, -9) if e == 0 else np.ldexp(8 + m, e - 10)
+        out[c] = np.nan if c & 127 == 127 else (-x if c & 128 else x)
+    return out
+
+
+E4M3 = _e4m3_values()
+
+
+def quant_rows(x: np.ndarray):
+    """Rows [.., d] -> (codes uint8 [.., d], scale bytes uint8 [..]): the least power of two 2^(s - 127), s >= 1, that brings the row's finite
+    values within 448; the nearest code, ties to the even one; values that are not finite become NaN codes with their sign."""
+    x = np.asarray(x, dtype=F64)
+    ok = np.isfinite(x)
+    amax = np.where(ok, np.abs(x), 0.0).max(axis=-1)
+    s = np.ones(amax.shape, np.int64)
+    live = amax > 0
+    s[live] = np.maximum(1, np.frexp(amax[live] / 448.0)[1] + 127 - (np.frexp(amax[live] / 448.0)[0] == 0.5))
+    y = np.where(ok, np.abs(x), 0.0) * np.ldexp(1.0, 127 - s)[..., None]
+    grid = E4M3[:127]
+    hi = np.clip(np.searchsorted(grid, y), 1, 126)
+    lo = hi - 1
+    down, up = y - grid[lo], grid[hi] - y
+    code = np.where((down < up) | ((down == up) & (lo % 2 == 0)), lo, hi)
+    code = np.where(ok, code, 127) + 128 * np.signbit(x)
+    return code.astype(np.uint8), s.astype(np.uint8)
+
+
+def dequant_rows(codes: np.ndarray, scale: np.ndarray) -> np.ndarray:
+    return E4M3[codes] * np.ldexp(1.0, scale.astype(np.int64) - 127)[..., None]
+
+
+SAMPLE_FLOOR = 2.0 ** -40
+
+
+def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """One token of one row from one uniform number; (token, its share of the kept weights, kept indices).
+
+    weights exp((l - max) / T), none below 2^-40 of the best; T below 2^-10: the best token; then top-k by (logit descending, index ascending), top-p
+    (tokens whose better ones sum to less than top_p of what top-k left), min-p; then the first index at which the kept weights' running sum
+    is above u times their sum.  A row without a logit above -infinity: (-1, 0, none)."""
+    l = np.asarray(logits, dtype=F64)
+    l = np.where(np.isnan(l), -np.inf, l)
+    best = l.max()
+    if best == -np.inf:
+        return -1, 0.0, np.empty(0, np.int64)
+    if not temperature >= 2.0 ** -10:
+        temperature, top_k = 1.0, 1
+    with np.errstate(invalid="ignore"):
+        w = np.exp(np.where(l == best, 0.0, (l - best) / min(float(temperature), 2.0 ** 96)))
+    order = [int(i) for i in np.lexsort((np.arange(l.size), -l)) if w[i] >= SAMPLE_FLOOR]
+    if 1 <= top_k < l.size:
+        order = order[:top_k]
+    if top_p < 1.0:
+        total, run, kept = float(w[order].sum()), 0.0, []
+        for i in order:
+            if kept and not run < top_p * total:
+                break
+            kept.append(i)
+            run += float(w[i])
+        order = kept
+    floor = 0.0 if np.isnan(min_p) else min(float(min_p), 1.0)
+    keep = np.array(sorted(i for i in order if w[i] >= floor), dtype=np.int64)
+    run = np.cumsum(w[keep])
+    j = min(int(np.searchsorted(run, float(u) * run[-1], side="right")), keep.size - 1)
+    return int(keep[j]), float(w[keep[j]] / run[-1]), keep

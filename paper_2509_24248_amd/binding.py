@@ -28,6 +28,8 @@ EXPORTS = [
     "specexit_graph_begin", "specexit_graph_end", "specexit_graph_launch", "specexit_graph_kernels", "specexit_graph_destroy",
     "specexit_workspace_prepare", "specexit_accept_exit", "specexit_kv_compact", "specexit_last_error", "specexit_version", "specexit_profile_events", "specexit_copy_probe",
     "specexit_workspace_bytes", "specexit_set_dev_status", "specexit_lmhead_argmax_noalloc",
+    "specexit_quant_kv_write", "specexit_quant_verify_attn", "specexit_quant_verify_attn_workspace_bytes",
+    "specexit_quant_kv_compact", "specexit_sample", "specexit_sample_workspace_bytes",
 ]
 PROF_DRAFT_HEAD_GEMM, PROF_LMHEAD_GEMM, PROF_VERIFY_ATTN, PROF_DRAFT_ATTN = 0, 1, 2, 3
 PROF_DRAFT_PROJ_IN, PROF_DRAFT_PROJ_OUT = 4, 5
@@ -36,7 +38,10 @@ SMOOTH_WORDS = 48
 FLAG_WORKSPACE_PREPARED = 1
 FLAG_VALIDATE = 2
 STATUS_OK, STATUS_BAD_LENGTH, STATUS_BAD_PAGE, STATUS_BAD_TOKEN, STATUS_BAD_NODE = 0, 1, 2, 3, 4
+STATUS_BAD_SETTING = 5
 OP_DRAFT_STEP, OP_VERIFY_ATTN, OP_LMHEAD_ARGMAX, OP_ACCEPT_EXIT, OP_DRAFT_TREE_LEVEL, OP_KV_COMPACT = 0, 1, 2, 3, 4, 5
+OP_QUANT_VERIFY_ATTN, OP_SAMPLE, OP_QUANT_KV_WRITE, OP_QUANT_KV_COMPACT = 6, 7, 8, 9
+SAMPLE_MAX_K, SAMPLE_MAX_V = 1024, 262144
 
 
 class SpecExitError(RuntimeError):
@@ -67,6 +72,13 @@ class KVView(C.Structure):
                 ("l_max", C.c_int64), ("n_pages", C.c_int64)]
 
 
+class QuantKVView(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("layout", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("page_table", C.c_void_p), ("page_size", C.c_int32), ("max_pages_per_seq", C.c_int32),
+                ("l_max", C.c_int64), ("n_pages", C.c_int64)]
+
+
 class ExitCfg(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("alpha", C.c_float), ("thr_conf", C.c_float),
                 ("thr_prog", C.c_float), ("thr_rem", C.c_float), ("signal_mask", C.c_uint32),
@@ -86,6 +98,14 @@ class AttnQuery(C.Structure):
 class LmHeadQuery(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("hidden", C.c_int32), ("vocab", C.c_int32),
                 ("n_extra", C.c_int32)]
+
+
+class QuantAttnQuery(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("kv", C.POINTER(QuantKVView)), ("dtype", C.c_int32), ("n_q_heads", C.c_int32)]
+
+
+class SampleQuery(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("vocab", C.c_int32)]
 
 
 def _load() -> C.CDLL:
@@ -141,6 +161,19 @@ def _load() -> C.CDLL:
     lib.specexit_profile_events.argtypes = [i32, C.POINTER(vp), C.POINTER(vp), i32]
     lib.specexit_workspace_bytes.restype = sz
     lib.specexit_workspace_bytes.argtypes = [i32, vp, i32, i32]
+    lib.specexit_quant_kv_write.restype = i32
+    lib.specexit_quant_kv_write.argtypes = [C.POINTER(QuantKVView), i32, i32, i32, vp, vp, C.c_int64, vp, vp, u32, vp]
+    lib.specexit_quant_verify_attn_workspace_bytes.restype = sz
+    lib.specexit_quant_verify_attn_workspace_bytes.argtypes = [C.POINTER(QuantKVView), i32, i32, i32, i32]
+    lib.specexit_quant_verify_attn.restype = i32
+    lib.specexit_quant_verify_attn.argtypes = [C.POINTER(QuantKVView), i32, i32, i32, i32, vp, vp, vp, f32, vp, vp, sz, u32, vp]
+    lib.specexit_quant_kv_compact.restype = i32
+    lib.specexit_quant_kv_compact.argtypes = [C.POINTER(QuantKVView), i32, C.c_int64, C.c_int64, i32, i32, vp, vp, vp, i32, vp, vp, i32,
+                                              vp, u32, vp]
+    lib.specexit_sample_workspace_bytes.restype = sz
+    lib.specexit_sample_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.specexit_sample.restype = i32
+    lib.specexit_sample.argtypes = [i32, i32, i32, vp, C.c_int64, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, u32, vp]
     lib.specexit_set_dev_status.restype = i32
     lib.specexit_set_dev_status.argtypes = [vp]
     return lib
@@ -222,6 +255,33 @@ def kv_view(k: torch.Tensor, v: torch.Tensor, page_table: Optional[torch.Tensor]
         kv.page_size, kv.max_pages_per_seq = k.shape[2], page_table.shape[1]
         kv.l_max, kv.n_pages = page_table.shape[1] * k.shape[2], k.shape[0]
     kv._keep = (k, v, page_table)      # the view holds raw addresses: keep their tensors alive with it
+    return kv
+
+
+def quant_kv_view(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                  page_table: Optional[torch.Tensor] = None) -> QuantKVView:
+    """8-bit cache; k, v hold e4m3 codes (uint8 or float8_e4m3fn), k_scale, v_scale a scale byte per row (uint8).
+    contiguous: k, v [B, Hkv, l_max, d], scales [B, Hkv, l_max]; paged: k, v [n_pages, Hkv, page_size, d], scales
+    [n_pages, Hkv, page_size], page_table [B, max_pages] int32."""
+    for t in (k, v, k_scale, v_scale):
+        assert t.is_cuda and t.is_contiguous() and t.element_size() == 1
+    assert k.shape == v.shape and k_scale.shape == v_scale.shape == k.shape[:3]
+    kv = QuantKVView()
+    kv.struct_size = C.sizeof(QuantKVView)
+    kv.n_kv_heads, kv.head_dim = k.shape[1], k.shape[3]
+    kv.k, kv.v, kv.k_scale, kv.v_scale = k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr()
+    if page_table is None:
+        kv.layout = KV_CONTIG
+        kv.page_table = None
+        kv.page_size, kv.max_pages_per_seq = 16, 0
+        kv.l_max, kv.n_pages = k.shape[2], 0
+    else:
+        assert page_table.dtype == torch.int32 and page_table.is_cuda and page_table.is_contiguous()
+        kv.layout = KV_PAGED
+        kv.page_table = page_table.data_ptr()
+        kv.page_size, kv.max_pages_per_seq = k.shape[2], page_table.shape[1]
+        kv.l_max, kv.n_pages = page_table.shape[1] * k.shape[2], k.shape[0]
+    kv._keep = (k, v, k_scale, v_scale, page_table)
     return kv
 
 
@@ -404,3 +464,63 @@ def specexit_set_dev_status(word: Optional[torch.Tensor]) -> None:
     if word is not None:
         assert word.is_cuda and word.dtype == torch.int32 and word.numel() >= 1
     _check(LIB.specexit_set_dev_status(None if word is None else C.c_void_p(word.data_ptr())))
+
+
+def _token_stride(rows: torch.Tensor, B: int, T: int, kv: QuantKVView) -> int:
+    """rows: [B, T, Hkv, d], heads and values consecutive, tokens evenly apart (a slice of a fused projection's output will do)."""
+    assert rows.is_cuda and tuple(rows.shape) == (B, T, kv.n_kv_heads, kv.head_dim)
+    sb, st, sh, sd = rows.stride()
+    step = st if T > 1 else sb if B > 1 else kv.n_kv_heads * kv.head_dim
+    assert sd == 1 and (sh == kv.head_dim or kv.n_kv_heads == 1) and (sb == T * step or B == 1), "tokens must lie evenly apart"
+    return step
+
+
+def specexit_quant_kv_write(kv: QuantKVView, dtype: int, B: int, T: int, k_rows, v_rows, pos, count=None, flags: int = 0,
+                            stream=None) -> None:
+    step = _token_stride(k_rows, B, T, kv)
+    assert _token_stride(v_rows, B, T, kv) == step
+    _check(LIB.specexit_quant_kv_write(C.byref(kv), dtype, B, T, C.c_void_p(k_rows.data_ptr()), C.c_void_p(v_rows.data_ptr()), step,
+                                       _ptr(pos), _ptr(count), flags, _stream(stream)))
+
+
+def specexit_quant_verify_attn_workspace_bytes(kv: QuantKVView, dtype: int, B: int, n_q: int, n_q_heads: int) -> int:
+    return int(LIB.specexit_quant_verify_attn_workspace_bytes(C.byref(kv), dtype, B, n_q, n_q_heads))
+
+
+def specexit_quant_verify_attn(kv: QuantKVView, dtype: int, B: int, n_q: int, n_q_heads: int, q, ctx_len, mask, scale: float,
+                               out, workspace, flags: int = 0, stream=None) -> None:
+    wp, wb = _ws_args(workspace)
+    _check(LIB.specexit_quant_verify_attn(C.byref(kv), dtype, B, n_q, n_q_heads, _ptr(q), _ptr(ctx_len), _ptr(mask),
+                                          C.c_float(scale), _ptr(out), wp, wb, flags, _stream(stream)))
+
+
+def specexit_quant_kv_compact(kv: QuantKVView, n_layers: int, layer_stride_bytes: int, scale_stride_bytes: int, B: int, n_q: int,
+                              ctx_len, accept_path, accept_len, dtype: int = BF16, last_node=None, block_hidden=None, D: int = 0,
+                              hidden_next=None, flags: int = 0, stream=None) -> None:
+    _check(LIB.specexit_quant_kv_compact(C.byref(kv), n_layers, layer_stride_bytes, scale_stride_bytes, B, n_q, _ptr(ctx_len),
+                                         _ptr(accept_path), _ptr(accept_len), dtype, _ptr(last_node), _ptr(block_hidden), D,
+                                         _ptr(hidden_next), flags, _stream(stream)))
+
+
+def specexit_sample_workspace_bytes(dtype: int, M: int, V: int) -> int:
+    return int(LIB.specexit_sample_workspace_bytes(dtype, M, V))
+
+
+def specexit_sample(dtype: int, M: int, V: int, logits, u, token, prob=None, temperature=None, top_k=None, top_p=None, min_p=None,
+                    rows_per_seq: int = 1, workspace=None, flags: int = 0, stream=None) -> None:
+    """logits: [M, >= V], rows evenly apart (a slice of wider rows will do)."""
+    assert logits.is_cuda and logits.dim() == 2 and logits.shape[0] == M and logits.shape[1] >= V and logits.stride(1) == 1
+    ld = logits.stride(0) if M > 1 else logits.shape[1]
+    wp, wb = _ws_args(workspace)
+    _check(LIB.specexit_sample(dtype, M, V, C.c_void_p(logits.data_ptr()), ld, rows_per_seq, _ptr(temperature), _ptr(top_k),
+                               _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(token), _ptr(prob), wp, wb, flags, _stream(stream)))
+
+
+def quant_attn_query(kv: QuantKVView, dtype: int, n_q_heads: int) -> QuantAttnQuery:
+    q = QuantAttnQuery(C.sizeof(QuantAttnQuery), C.pointer(kv), dtype, n_q_heads)
+    q._keep = kv
+    return q
+
+
+def sample_query(dtype: int, vocab: int) -> SampleQuery:
+    return SampleQuery(C.sizeof(SampleQuery), dtype, vocab)

@@ -48,7 +48,8 @@ int num_cus() {
 // device status word of this host thread (specexit_set_dev_status); used by calls that pass
 // SPECEXIT_FLAG_VALIDATE
 static_assert(kStatusBadLength == SPECEXIT_STATUS_BAD_LENGTH && kStatusBadPage == SPECEXIT_STATUS_BAD_PAGE &&
-              kStatusBadToken == SPECEXIT_STATUS_BAD_TOKEN && kStatusBadNode == SPECEXIT_STATUS_BAD_NODE,
+              kStatusBadToken == SPECEXIT_STATUS_BAD_TOKEN && kStatusBadNode == SPECEXIT_STATUS_BAD_NODE &&
+              kStatusBadSetting == SPECEXIT_STATUS_BAD_SETTING,
               "status codes of the ABI and of the kernels differ");
 thread_local int32_t* g_dev_status = nullptr;
 int* status_for(uint32_t flags) { return (flags & SPECEXIT_FLAG_VALIDATE) ? g_dev_status : nullptr; }
@@ -153,6 +154,84 @@ int32_t fill_attn(AttnArgs& a, const specexit_kv_view* kv, int32_t B, int32_t n_
   a.n_pages = a.paged ? kv->n_pages : 0;
   if (a.l_max < n_q) return fail(SPECEXIT_EINVAL, "%s: the cache holds %lld entries per sequence, fewer than the block's %d", who, static_cast<long long>(a.l_max), n_q);
   if (!attn_plan(a, num_cus())) return fail(SPECEXIT_EUNSUPPORTED, "%s: %d sequences x %d KV heads x %lld cache entries is more than one call can split", who, B, a.Hkv, static_cast<long long>(a.l_max));
+  return SPECEXIT_OK;
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// --------------------------------------------------------------------------- 8-bit cache
+int32_t fill_quant_kv(QuantKv& q, const specexit_quant_kv_view* kv, const char* who) {
+  if (!kv || kv->struct_size != sizeof(specexit_quant_kv_view)) return fail(SPECEXIT_EINVAL, "%s: quantised kv view missing or of another ABI size", who);
+  if (!kv->k || !kv->v || !kv->k_scale || !kv->v_scale) return fail(SPECEXIT_EINVAL, "%s: kv or scale pointers are null", who);
+  if (!aligned16(kv->k) || !aligned16(kv->v) || !aligned16(kv->k_scale) || !aligned16(kv->v_scale))
+    return fail(SPECEXIT_EINVAL, "%s: codes and scales must be 16-byte aligned", who);
+  if (kv->head_dim != 64 && kv->head_dim != 128) return fail(SPECEXIT_EUNSUPPORTED, "%s: head_dim %d not in {64,128}", who, kv->head_dim);
+  if (kv->n_kv_heads < 1) return fail(SPECEXIT_EINVAL, "%s: n_kv_heads < 1", who);
+  memset(&q, 0, sizeof(q));
+  if (kv->layout == SPECEXIT_KV_PAGED) {
+    if (!kv->page_table) return fail(SPECEXIT_EINVAL, "%s: paged layout without page_table", who);
+    if (kv->page_size < 16 || kv->page_size % 16) return fail(SPECEXIT_EUNSUPPORTED, "%s: page_size %d is not a multiple of 16", who, kv->page_size);
+    if (kv->max_pages_per_seq < 1 || kv->n_pages < 1) return fail(SPECEXIT_EINVAL, "%s: empty page pool", who);
+    q.paged = 1;
+    q.page_table = kv->page_table;
+    q.page_size = kv->page_size;
+    q.max_pages = kv->max_pages_per_seq;
+    q.l_max = static_cast<int64_t>(kv->max_pages_per_seq) * kv->page_size;
+    q.n_pages = kv->n_pages;
+  } else if (kv->layout == SPECEXIT_KV_CONTIG) {
+    if (kv->l_max < 16 || kv->l_max % 16) return fail(SPECEXIT_EUNSUPPORTED, "%s: l_max %lld is not a multiple of 16", who, static_cast<long long>(kv->l_max));
+    q.page_size = 16;
+    q.l_max = kv->l_max;
+  } else {
+    return fail(SPECEXIT_EINVAL, "%s: unknown kv layout %d", who, kv->layout);
+  }
+  if (q.l_max > 0x7fffffff) return fail(SPECEXIT_EUNSUPPORTED, "%s: more than 2^31 - 1 entries per sequence", who);
+  q.k = kv->k; q.v = kv->v; q.ks = kv->k_scale; q.vs = kv->v_scale;
+  q.Hkv = kv->n_kv_heads;
+  return SPECEXIT_OK;
+}
+
+int32_t fill_quant_attn(QuantAttnArgs& a, const specexit_quant_kv_view* kv, int32_t dtype, int32_t B, int32_t n_q, int32_t n_q_heads) {
+  const char* who = "quant_verify_attn";
+  QuantKv q;
+  int32_t rc = fill_quant_kv(q, kv, who);
+  if (rc) return rc;
+  if (!dtype_ok(dtype)) return fail(SPECEXIT_EINVAL, "%s: unknown dtype %d", who, dtype);
+  if (B < 1) return fail(SPECEXIT_EINVAL, "%s: B < 1", who);
+  if (n_q < 1 || n_q > SPECEXIT_MAX_NQ) return fail(SPECEXIT_EINVAL, "%s: n_q %d outside 1..64", who, n_q);
+  if (n_q_heads < 1 || n_q_heads % q.Hkv) return fail(SPECEXIT_EINVAL, "%s: n_q_heads %d is not a multiple of n_kv_heads %d", who, n_q_heads, q.Hkv);
+  if (static_cast<int64_t>(n_q_heads / q.Hkv) * n_q > 128) return fail(SPECEXIT_EUNSUPPORTED, "%s: more than 128 query rows per KV head", who);
+  if (B > 1024) return fail(SPECEXIT_EUNSUPPORTED, "%s: more than 1024 sequences in one call", who);
+  memset(&a, 0, sizeof(a));
+  a.dtype = dtype;
+  a.paged = q.paged;
+  a.k = q.k; a.v = q.v; a.ks = q.ks; a.vs = q.vs;
+  a.page_table = q.page_table;
+  a.page_size = q.page_size;
+  a.max_pages = q.max_pages;
+  a.l_max = q.l_max;
+  a.n_pages = q.n_pages;
+  a.B = B;
+  a.n_q = a.n_blk = a.mask_stride = n_q;
+  a.Hq = n_q_heads;
+  a.Hkv = q.Hkv;
+  a.d = kv->head_dim;
+  if (a.l_max < n_q) return fail(SPECEXIT_EINVAL, "%s: the cache holds %lld entries per sequence, fewer than the block's %d", who, static_cast<long long>(a.l_max), n_q);
+  if (!quant_attn_plan(a, num_cus())) return fail(SPECEXIT_EUNSUPPORTED, "%s: %d sequences x %d KV heads x %lld cache entries is more than one call can split", who, B, a.Hkv, static_cast<long long>(a.l_max));
+  return SPECEXIT_OK;
+}
+
+int32_t fill_sample(SampleArgs& a, int32_t dtype, int32_t M, int32_t V) {
+  if (!dtype_ok(dtype)) return fail(SPECEXIT_EINVAL, "sample: unknown dtype %d", dtype);
+  if (M < 1 || M > 65535) return fail(SPECEXIT_EINVAL, "sample: M %d outside 1..65535", M);
+  if (V < 1) return fail(SPECEXIT_EINVAL, "sample: V < 1");
+  if (V > SPECEXIT_SAMPLE_MAX_V) return fail(SPECEXIT_EUNSUPPORTED, "sample: V %d above %d", V, SPECEXIT_SAMPLE_MAX_V);
+  static_assert(kSampleMaxK == SPECEXIT_SAMPLE_MAX_K && kSampleMaxSegs * 512 == SPECEXIT_SAMPLE_MAX_V, "limits of the ABI and of the kernels differ");
+  memset(&a, 0, sizeof(a));
+  a.f32 = dtype == SPECEXIT_F32;
+  a.M = M;
+  a.V = V;
+  sample_plan(a);
   return SPECEXIT_OK;
 }
 
@@ -625,8 +704,20 @@ size_t specexit_workspace_bytes(int32_t op, const void* desc, int32_t B, int32_t
       if (!q || q->struct_size != sizeof(*q) || B < 1 || n_q < 1) return 0;
       return specexit_lmhead_argmax_workspace_bytes(q->dtype, B * n_q, q->hidden, q->vocab, q->n_extra);
     }
+    case SPECEXIT_OP_QUANT_VERIFY_ATTN: {
+      const specexit_quant_attn_query* q = static_cast<const specexit_quant_attn_query*>(desc);
+      if (!q || q->struct_size != sizeof(*q)) return 0;
+      return specexit_quant_verify_attn_workspace_bytes(q->kv, q->dtype, B, n_q, q->n_q_heads);
+    }
+    case SPECEXIT_OP_SAMPLE: {
+      const specexit_sample_query* q = static_cast<const specexit_sample_query*>(desc);
+      if (!q || q->struct_size != sizeof(*q) || B < 1 || n_q < 1 || static_cast<int64_t>(B) * n_q > 65535) return 0;
+      return specexit_sample_workspace_bytes(q->dtype, B * n_q, q->vocab);
+    }
     case SPECEXIT_OP_ACCEPT_EXIT:
     case SPECEXIT_OP_KV_COMPACT:
+    case SPECEXIT_OP_QUANT_KV_WRITE:
+    case SPECEXIT_OP_QUANT_KV_COMPACT:
       return 0;   // these calls use no scratch memory
     default:
       fail(SPECEXIT_EINVAL, "workspace_bytes: unknown op %d", op);
@@ -1065,6 +1156,118 @@ int32_t specexit_kv_compact(const specexit_kv_view* kv, int32_t n_layers, int64_
   if (!kv_compact_supported(a)) return fail(SPECEXIT_EUNSUPPORTED, "kv_compact: block of %d nodes with %d-byte rows", n_q, a.row_bytes);
   if (kv->n_kv_heads > 65535 || B > 65535 || n_layers > 65535) return fail(SPECEXIT_EUNSUPPORTED, "kv_compact: grid too large");
   return check_hip(launch_kv_compact(a, static_cast<hipStream_t>(stream)), "kv_compact");
+}
+
+int32_t specexit_quant_kv_write(const specexit_quant_kv_view* kv, int32_t dtype, int32_t B, int32_t T, const void* k_rows,
+                                const void* v_rows, int64_t token_stride, const int32_t* pos, const int32_t* count,
+                                uint32_t flags, void* stream) {
+  QuantWriteArgs a;
+  memset(&a, 0, sizeof(a));
+  int32_t rc = fill_quant_kv(a.kv, kv, "quant_kv_write");
+  if (rc) return rc;
+  if (!dtype_ok(dtype)) return fail(SPECEXIT_EINVAL, "quant_kv_write: unknown dtype %d", dtype);
+  if (B < 1 || T < 1) return fail(SPECEXIT_EINVAL, "quant_kv_write: B or T < 1");
+  if (!k_rows || !v_rows || !pos) return fail(SPECEXIT_EINVAL, "quant_kv_write: a required pointer is null");
+  if (token_stride < static_cast<int64_t>(kv->n_kv_heads) * kv->head_dim) return fail(SPECEXIT_EINVAL, "quant_kv_write: token stride %lld is less than a token's rows", static_cast<long long>(token_stride));
+  if (!aligned16(k_rows) || !aligned16(v_rows) || token_stride * esize(dtype) % 16)
+    return fail(SPECEXIT_EINVAL, "quant_kv_write: rows must be 16-byte aligned");
+  a.f32 = dtype == SPECEXIT_F32;
+  a.d = kv->head_dim;
+  a.B = B; a.T = T;
+  a.k = k_rows; a.v = v_rows; a.token_stride = token_stride;
+  a.pos = pos; a.count = count;
+  a.status = status_for(flags);
+  if (!quant_write_plan(a)) return fail(SPECEXIT_EUNSUPPORTED, "quant_kv_write: %d sequences x %d tokens x %d KV heads is more than one call takes", B, T, kv->n_kv_heads);
+  return check_hip(launch_quant_write(a, static_cast<hipStream_t>(stream)), "quant_kv_write");
+}
+
+size_t specexit_quant_verify_attn_workspace_bytes(const specexit_quant_kv_view* kv, int32_t dtype, int32_t B, int32_t n_q, int32_t n_q_heads) {
+  QuantAttnArgs a;
+  if (fill_quant_attn(a, kv, dtype, B, n_q, n_q_heads)) return 0;
+  return attn_workspace_bytes(a);
+}
+
+int32_t specexit_quant_verify_attn(const specexit_quant_kv_view* kv, int32_t dtype, int32_t B, int32_t n_q, int32_t n_q_heads,
+                                   const void* q, const int32_t* ctx_len, const uint64_t* mask, float scale, void* out,
+                                   void* workspace, size_t workspace_bytes, uint32_t flags, void* stream) {
+  QuantAttnArgs a;
+  int32_t rc = fill_quant_attn(a, kv, dtype, B, n_q, n_q_heads);
+  if (rc) return rc;
+  if (!q || !ctx_len || !out) return fail(SPECEXIT_EINVAL, "quant_verify_attn: a required pointer is null");
+  if (!(scale > 0.f)) return fail(SPECEXIT_EINVAL, "quant_verify_attn: scale must be positive");
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255)) return fail(SPECEXIT_EWORKSPACE, "quant_verify_attn: workspace null or not 256-byte aligned");
+  const size_t need = attn_workspace_bytes(a);
+  if (workspace_bytes < need) return fail(SPECEXIT_EWORKSPACE, "quant_verify_attn: workspace %zu < %zu bytes", workspace_bytes, need);
+  a.q = q;
+  a.ctx_len = ctx_len;
+  a.mask = mask;
+  a.scale = scale;
+  a.out = out;
+  a.status = status_for(flags);
+  attn_carve(a, workspace);
+  return check_hip(launch_quant_attn(a, static_cast<hipStream_t>(stream)), "quant_verify_attn");
+}
+
+int32_t specexit_quant_kv_compact(const specexit_quant_kv_view* kv, int32_t n_layers, int64_t layer_stride_bytes,
+                                  int64_t scale_stride_bytes, int32_t B, int32_t n_q, const int32_t* ctx_len,
+                                  const int32_t* accept_path, const int32_t* accept_len, int32_t dtype,
+                                  const int32_t* last_node, const void* block_hidden, int32_t D, void* hidden_next,
+                                  uint32_t flags, void* stream) {
+  QuantCompactArgs a;
+  memset(&a, 0, sizeof(a));
+  int32_t rc = fill_quant_kv(a.kv, kv, "quant_kv_compact");
+  if (rc) return rc;
+  if (B < 1) return fail(SPECEXIT_EINVAL, "quant_kv_compact: B < 1");
+  if (n_q < 1 || n_q > SPECEXIT_MAX_NQ) return fail(SPECEXIT_EINVAL, "quant_kv_compact: n_q %d outside 1..64", n_q);
+  if (n_layers < 1) return fail(SPECEXIT_EINVAL, "quant_kv_compact: n_layers < 1");
+  if (n_layers > 1 && (layer_stride_bytes <= 0 || layer_stride_bytes % 16 || scale_stride_bytes <= 0 || scale_stride_bytes % 16))
+    return fail(SPECEXIT_EINVAL, "quant_kv_compact: layer strides must be positive multiples of 16 bytes");
+  if (!ctx_len || !accept_path || !accept_len) return fail(SPECEXIT_EINVAL, "quant_kv_compact: a required pointer is null");
+  a.d = kv->head_dim;
+  a.layer_stride = n_layers > 1 ? layer_stride_bytes : 0;
+  a.scale_stride = n_layers > 1 ? scale_stride_bytes : 0;
+  a.n_layers = n_layers; a.B = B; a.n_q = n_q;
+  a.ctx_len = ctx_len; a.accept_path = accept_path; a.accept_len = accept_len; a.last_node = last_node;
+  a.status = status_for(flags);
+  if (block_hidden) {
+    if (!dtype_ok(dtype)) return fail(SPECEXIT_EINVAL, "quant_kv_compact: unknown dtype %d", dtype);
+    if (!last_node || !hidden_next) return fail(SPECEXIT_EINVAL, "quant_kv_compact: block_hidden given without last_node / hidden_next");
+    if (D < 1 || (static_cast<int64_t>(D) * static_cast<int64_t>(esize(dtype))) % 16 || D > (1 << 28)) return fail(SPECEXIT_EINVAL, "quant_kv_compact: D * element size must be a multiple of 16");
+    a.block_hidden = block_hidden; a.hidden_next = hidden_next;
+    a.hidden_row_bytes = static_cast<int>(D * esize(dtype));
+  }
+  if (kv->n_kv_heads > 65535 || B > 65535 || n_layers > 65535) return fail(SPECEXIT_EUNSUPPORTED, "quant_kv_compact: grid too large");
+  return check_hip(launch_quant_compact(a, static_cast<hipStream_t>(stream)), "quant_kv_compact");
+}
+
+size_t specexit_sample_workspace_bytes(int32_t dtype, int32_t M, int32_t V) {
+  SampleArgs a;
+  if (fill_sample(a, dtype, M, V)) return 0;
+  return sample_carve(a, nullptr);
+}
+
+int32_t specexit_sample(int32_t dtype, int32_t M, int32_t V, const void* logits, int64_t ld, int32_t rows_per_seq,
+                        const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                        const float* u, int32_t* token, float* prob, void* workspace, size_t workspace_bytes,
+                        uint32_t flags, void* stream) {
+  SampleArgs a;
+  int32_t rc = fill_sample(a, dtype, M, V);
+  if (rc) return rc;
+  if (!logits || !u || !token) return fail(SPECEXIT_EINVAL, "sample: a required pointer is null");
+  if (ld < V) return fail(SPECEXIT_EINVAL, "sample: row stride %lld is less than V", static_cast<long long>(ld));
+  if (rows_per_seq < 1) return fail(SPECEXIT_EINVAL, "sample: rows_per_seq < 1");
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255)) return fail(SPECEXIT_EWORKSPACE, "sample: workspace null or not 256-byte aligned");
+  const size_t need = sample_carve(a, workspace);
+  if (workspace_bytes < need) return fail(SPECEXIT_EWORKSPACE, "sample: workspace %zu < %zu bytes", workspace_bytes, need);
+  a.logits = logits;
+  a.ld = ld;
+  a.rows_per_seq = rows_per_seq;
+  a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p;
+  a.u = u;
+  a.token = token;
+  a.prob = prob;
+  a.status = status_for(flags);
+  return check_hip(launch_sample(a, static_cast<hipStream_t>(stream)), "sample");
 }
 
 }  // extern "C"

@@ -1,0 +1,755 @@
+// Verification attention over the 8-bit cache (quant_kv.hip), on the matrix cores.
+//
+// The keys of the launch are dealt to the workgroups in equal shares (attn_sched.hpp); a workgroup takes one (sequence, KV head)
+// unit's key range at a time, against all R = G * n_q query rows that share the head, so that the cache is read once.  It has NK
+// rings of S LDS slots; ring kg takes the 32-key tiles kg, kg + NK, .. of the range, brought in by direct global->LDS loads S - 1 tiles ahead.
+// The ring's NR waves own RTW 16-row tiles of the queries each:
+//   S^T = K Q^T : block-scaled matrix instruction, 16 keys x 16 rows x 128 products.  A = the codes as they lie in the cache, with
+//                 the keys' scale bytes as its scales.  B = the queries as a sum of e4m3 parts, each with its own power of two:
+//                 a part takes four bits of what is left, so two parts hold a bf16 value.  The products are exact: nothing of the
+//                 queries is rounded away, and no key is converted.  (The instruction drops what lies 2^-23 below its largest product, some
+//                 1e-5 of a score, which the rounding to bf16 hides and fp32 results do not: there, keys are converted to bf16,
+//                 exactly, and the queries are three bf16 parts.  With six e4m3 parts the tiny fp32 shape was off by 3.4e-5.)
+//   softmax     : online, per wave, in log2 units; lane (row, q) owns 8 keys of its row;
+//   O^T += V^T P^T : A = V codes, transposed on the way out of LDS (eight keys of a column per lane) and converted to bf16,
+//                 which is exact; B = the probabilities times the keys' scales (powers of two: exact) in PP bf16 parts.
+// 64-wide heads need half the products: the instruction's second half then takes the same codes with the next part of the queries.
+#include "attn_sched.hpp"
+#include "common.hpp"
+#include "kernels.hpp"
+#include "quant.hpp"
+#include "stream.hpp"
+
+#include <float.h>
+
+#include <algorithm>
+
+namespace sx {
+
+namespace {
+
+typedef int v2i_t __attribute__((ext_vector_type(2)));
+typedef int v8i_t __attribute__((ext_vector_type(8)));
+typedef float v2f_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+typedef __attribute__((address_space(3))) v2i_t* lds_v2i_t;
+
+constexpr int kMaxPages = 2048;      // page ids of a segment kept in LDS (8 KB)
+constexpr int kTileKeys = 32;
+constexpr size_t kRingLds = 128 * 1024;
+
+__host__ __device__ constexpr int slot_bytes(int hd) { return 2 * kTileKeys * hd; }    // K codes, then V codes
+__host__ __device__ constexpr int ring_slots(int hd, int nk) { return static_cast<int>(kRingLds) / (nk * slot_bytes(hd)) > 16 ? 16 : static_cast<int>(kRingLds) / (nk * slot_bytes(hd)); }
+constexpr int kScaleSlot = 2 * kTileKeys;        // K scale bytes, then V scale bytes
+
+// XOR swizzles of the 16-byte chunks of a tile row, so that the 16 rows (K) or 16 rows x 1 chunk (V) that an instruction reads at once lie on
+// different banks: 128-wide rows are two to the 256 bytes of all banks, 64-wide ones four.
+template <int HD> __device__ __forceinline__ int swz_k(int key) { return HD == 128 ? (key >> 1) & 7 : (key >> 2) & 3; }
+template <int HD> __device__ __forceinline__ int swz_v(int key) {      // (V reads take keys 4 q .. + 3 and 16 + 4 q .. + 3 together)
+  return HD == 128 ? ((key >> 1) & 3) | ((key >> 4) & 1) << 2 : ((key >> 2) & 1) | ((key >> 4) & 1) << 1;
+}
+
+__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }   // (hands a NaN on)
+__device__ __forceinline__ float max3_nan(float a, float b, float c) { return max_nan(max_nan(a, b), c); }
+
+__device__ __forceinline__ uint32_t two_bf16(uint32_t codes, bool hi) {
+  const bf16x2_t v = hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.0f, false);
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// 16 keys x 16 rows: a with the scale bytes of `sa` (byte 0), b with byte OP of `sb`
+template <int OP> __device__ __forceinline__ f32x4_t mfma_scaled(v8i_t a, v8i_t b, f32x4_t c, int sa, int sb) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, sa, OP, sb);
+}
+
+// vmcnt <= n: a load of each of the last n requests may still be on its way
+template <int N> __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(vmcnt_imm(N)); }
+// waits until at most `tiles` tiles of PER requests each are (a uniform number up to MOST)
+template <int PER, int MOST> __device__ __forceinline__ void wait_tiles(int tiles) {
+  if constexpr (MOST <= 0) {
+    wait_loads<0>();
+  } else {
+    if (tiles >= MOST) wait_loads<(PER * MOST > 63 ? 63 : PER * MOST)>();
+    else wait_tiles<PER, MOST - 1>(tiles);
+  }
+}
+
+// four bytes per lane: lane l's land at lds_base + 4 l
+__device__ __forceinline__ void load_to_lds4(const void* src, const void* lds_base) {
+  const uint32_t l = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr_t)lds_base));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(l), "v"(src) : "memory");
+}
+
+// parts of the queries and of the probabilities
+template <typename T> struct Parts { static constexpr int q = 2, p = 2; };        // bf16: two e4m3 ones and two bf16 ones, 16 bits of a probability
+template <> struct Parts<float> { static constexpr int q = 3, p = 3; };           // fp32: three bf16 ones, all 24 bits of both
+
+constexpr int ml_floats(int nk, int rows) { return nk > 1 ? 2 * nk * rows : 0; }
+__host__ __device__ constexpr size_t quant_lds_bytes(int hd, int nk, int rows, int B, bool paged) {
+  const size_t s = static_cast<size_t>(nk) * ring_slots(hd, nk);
+  return s * slot_bytes(hd) + s * kScaleSlot + static_cast<size_t>(nk > 1 ? 2 * nk * rows : 0) * sizeof(float) + static_cast<size_t>(attn_sched_words(B)) * sizeof(int) +
+         (paged ? static_cast<size_t>(kMaxPages + 1) * sizeof(int) : 0);
+}
+
+template <int HD, typename T, int NK, int NR, int RTW>
+__global__ __launch_bounds__(64 * NK * NR, RTW <= 2 ? 2 : (NK * NR + 3) / 4) void k_quant_attn(const QuantAttnArgs a) {
+  constexpr int S = ring_slots(HD, NK);
+  constexpr int RP = 16 * NR * RTW;               // query rows covered (padded)
+  constexpr int kSlot = slot_bytes(HD);
+  constexpr int kChunks = HD / 16;                // 16-byte chunks of a row
+  constexpr int kKeysPP = 1024 / HD;              // keys of a 1 KB piece
+  constexpr int kTileP = kTileKeys / kKeysPP;     // pieces of a K (or V) tile
+  constexpr int kPieces = 2 * kTileP / NR;        // pieces that a wave requests of a tile
+  static_assert(2 * kTileP % NR == 0, "the waves of a ring share a tile evenly");
+  static_assert(NK == 1 || NR * RTW <= S, "a ring's slots hold its sums");
+  constexpr int kReq = kPieces + 1;               // requests of a wave per tile
+  constexpr bool kCodes = sizeof(T) == 2;         // the keys' codes are multiplied as they are
+  constexpr int NP = Parts<T>::q, PP = Parts<T>::p;
+  constexpr int NM = HD == 128 ? NP : 1;          // block-scaled matrix instructions for 16 keys x 16 rows
+  constexpr int kKS = HD / 32;                    // k steps of bf16 ones
+  constexpr int kDT = HD / 16;
+  extern __shared__ uint4 smem4[];
+  char* smem = reinterpret_cast<char*>(smem4);
+  char* scales = smem + NK * S * kSlot;
+  float* ml_lds = reinterpret_cast<float*>(scales + NK * S * kScaleSlot);
+  int* sched_lds = reinterpret_cast<int*>(ml_lds + ml_floats(NK, RP));
+  int* pg_lds = sched_lds + attn_sched_words(a.B);
+  const int lane = threadIdx.x & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kg = wv / NR, rr = wv % NR;
+  const int G = a.G, R = G * a.n_q;
+  const int fr = lane & 15, fq = lane >> 4;
+  const AttnTable table = attn_sched_build(a, sched_lds);
+  const AttnLine line = attn_sched_line(a, table);
+  if (static_cast<int>(blockIdx.x) >= line.W) return;   // the whole workgroup leaves together
+  const int x_hi = attn_sched_lo(line, blockIdx.x + 1);
+  bool again = false;                             // a segment before this one used the rings
+  AttnSeg seg = attn_sched_next(a, table, true, line.pad, attn_sched_lo(line, blockIdx.x), x_hi);
+  if (seg.next < x_hi) attn_sched_keep(a, table);
+  for (; seg.s1 > seg.s0; seg = attn_sched_next(a, table, false, line.pad, seg.next, x_hi)) {
+  attn_sched_publish(a, seg);
+  const int g = seg.g, b = seg.b;
+  const int L = __builtin_amdgcn_readfirstlane(seg.L);
+  const int s0 = seg.s0, s1 = __builtin_amdgcn_readfirstlane(seg.s1);
+  const int ntl = (s1 - s0 + kTileKeys - 1) / kTileKeys;   // tiles of the segment
+  const int nit = (ntl + NK - 1) / NK;            // tile steps (the same for all rings)
+  const int mine = (ntl - kg + NK - 1) / NK;      // tiles of this ring
+  char* ring = smem + kg * (S * kSlot);
+  char* ring_s = scales + kg * (S * kScaleSlot);
+
+  // ---- this wave's query rows (rows past the last one repeat it and are not stored): lane (row, q) holds columns 16 q .. + 15 and, of
+  // 128-wide heads, 64 + 16 q .. + 15; in the converted form 32 s + 8 q .. + 7 of every k step s
+  constexpr int kQ = HD / 4;                      // columns of a lane
+  float x[RTW][kQ];
+  uint64_t rowmask[RTW];
+#pragma unroll
+  for (int t = 0; t < RTW; ++t) {
+    const int r = min(16 * (rr * RTW + t) + fr, R - 1);
+    const int i = (r * a.g_inv) >> 16;            // r / G
+    const T* qp = static_cast<const T*>(a.q) + ((static_cast<size_t>(b) * a.n_q + i) * a.Hq + g * G + (r - i * G)) * HD;
+#pragma unroll
+    for (int c = 0; c < kQ; c += 4) {
+      const T* p = qp + (kCodes ? 16 * fq + (c & 15) + (c >> 4) * 64 : 8 * fq + (c & 7) + (c >> 3) * 32);
+      if constexpr (sizeof(T) == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        x[t][c] = __uint_as_float(v.x << 16); x[t][c + 1] = __uint_as_float(v.x & 0xFFFF0000u);
+        x[t][c + 2] = __uint_as_float(v.y << 16); x[t][c + 3] = __uint_as_float(v.y & 0xFFFF0000u);
+      } else {
+        const float4 v = *reinterpret_cast<const float4*>(p);
+        x[t][c] = v.x; x[t][c + 1] = v.y; x[t][c + 2] = v.z; x[t][c + 3] = v.w;
+      }
+    }
+    rowmask[t] = a.mask ? a.mask[static_cast<size_t>(b) * a.mask_stride + i] : ((2ull << i) - 1ull);
+  }
+
+  // ---- page ids of the segment to LDS: loads from there do not count against the vector-memory counter that paces the tile loads
+  const int ps = a.page_size;
+  auto page_of = [&](int p) { return a.page_shift >= 0 ? p >> a.page_shift : static_cast<int>(static_cast<uint32_t>(p) / static_cast<uint32_t>(ps)); };
+  int pg0 = 0;
+  if (a.paged) {
+    pg0 = page_of(s0);
+    const int npg = page_of(s1 - 1) - pg0 + 1;
+    const int32_t* ptab = a.page_table + static_cast<size_t>(b) * a.max_pages + pg0;
+    for (int i = threadIdx.x; i < npg; i += 64 * NK * NR) pg_lds[i] = checked_page(ptab[i], a.n_pages, a.status);
+  }
+  if (a.paged || again) __syncthreads();          // the page ids are there, and the rings are free of the segment before
+  again = true;
+
+  // ---- tile requests.  A tile is two halves of 16 keys, each within one page; piece j holds kKeysPP keys from kKeysPP (j % kTileP) on, lane l
+  // fetches key l / kChunks of them, chunk (l % kChunks) ^ swizzle(key).
+  const int lkey = lane / kChunks, lpos = lane % kChunks;
+  // (selected as values: left alone the compiler selects the arguments' addresses and loads through them for every tile, which waits for all
+  // requests in flight)
+  uint64_t ks_at = reinterpret_cast<uint64_t>(a.ks), vs_at = reinterpret_cast<uint64_t>(a.vs);
+  asm volatile("" : "+s"(ks_at), "+s"(vs_at));
+  const char* const scale_pool = reinterpret_cast<const char*>(lane < 8 ? ks_at : vs_at) + 4 * (lane & 3);
+  const int64_t seq_row = (static_cast<int64_t>(b) * a.Hkv + g) * a.l_max;
+  auto row_of = [&](int p) -> int64_t {           // entry p of the unit, uniform
+    if (!a.paged) return seq_row + p;
+    const int n = page_of(p);
+    const int page = __builtin_amdgcn_readfirstlane(pg_lds[n - pg0]);
+    return (static_cast<int64_t>(page) * a.Hkv + g) * ps + (p - n * ps);
+  };
+  auto issue = [&](int it) {
+    if (it >= mine) return;                       // uniform per wave
+    const int t0 = s0 + kTileKeys * (it * NK + kg);
+    char* slot = ring + (it % S) * kSlot;
+    const int n = s1 - t0;                        // keys from here to the end of the segment
+    const int64_t r0 = row_of(t0);
+    const int64_t r1 = n > 16 ? row_of(t0 + 16) : r0;
+    if (n >= kTileKeys) {
+#pragma unroll
+      for (int u = 0; u < kPieces; ++u) {
+        const int j = rr * kPieces + u;
+        const int key = kKeysPP * (j & (kTileP - 1));          // the piece's first key
+        const int64_t row = (key & 16 ? r1 : r0) + (key & 15);
+        const bool is_v = j >= kTileP;
+        const int chunk = lpos ^ (is_v ? swz_v<HD>(key + lkey) : swz_k<HD>(key + lkey));
+        load_to_lds16(static_cast<const char*>(is_v ? a.v : a.k) + row * HD, static_cast<uint32_t>(lkey * HD + (chunk << 4)), slot + j * 1024);
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < kPieces; ++u) {
+        const int j = rr * kPieces + u;
+        const int key = kKeysPP * (j & (kTileP - 1)) + lkey;
+        const int at = min(key, n - 1);                        // keys past the range repeat the last one and are masked
+        const int64_t row = (at & 16 ? r1 : r0) + (at & 15);
+        const bool is_v = j >= kTileP;
+        load_to_lds16(static_cast<const char*>(is_v ? a.v : a.k) + row * HD + ((lpos ^ (is_v ? swz_v<HD>(key) : swz_k<HD>(key))) << 4), slot + j * 1024);
+      }
+    }
+    // scale bytes: lanes 0..7 four keys' K scales each, lanes 8..15 V scales (the entries behind the last one are inside the cache: pages and
+    // contiguous caches are multiples of 16 entries)
+    if (lane < 16) {
+      load_to_lds4(scale_pool + (lane & 4 ? r1 : r0), ring_s + (it % S) * kScaleSlot);
+    }
+  };
+
+  f32x4_t oacc[kDT][RTW];
+  float m_run[RTW], l_run[RTW];
+#pragma unroll
+  for (int t = 0; t < RTW; ++t) {
+    m_run[t] = -FLT_MAX;
+    l_run[t] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < kDT; ++dt) oacc[dt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const float sl2 = a.scale * 1.44269504088896340736f;    // scores are kept in log2 units
+
+  // ---- the queries' parts.  Codes: a row's scale as in the cache, then four bits at a time; v8i m of a row is the whole of part m (128-wide
+  // heads), or parts 0 and 1; scale bytes of instruction m: byte m.
+  v8i_t qf[RTW][NM];
+  int qs[RTW];
+  uint4 qb[RTW][NP][kKS];
+#pragma unroll
+  for (int t = 0; t < RTW; ++t) {
+    if constexpr (kCodes) {
+      float big = 0.f;
+#pragma unroll
+      for (int c = 0; c < kQ; ++c) big = fmaxf(big, fabsf(x[t][c]));
+      const int s = min(quant_scale_byte(__float_as_uint(quad_row_max(big))), 254);
+      const float inv = quant_scale_inverse(s);
+#pragma unroll
+      for (int c = 0; c < kQ; ++c) x[t][c] *= inv;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+#pragma unroll
+        for (int c = 0; c < kQ; c += 4) {
+          int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[t][c], x[t][c + 1], 0, false);
+          w = __builtin_amdgcn_cvt_pk_fp8_f32(x[t][c + 2], x[t][c + 3], w, true);
+          if constexpr (HD == 128) qf[t][p][c / 4] = w;
+          else qf[t][0][p * 4 + c / 4] = w;
+          if (p + 1 < NP) {
+            const v2f_t lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+            x[t][c] = (x[t][c] - lo[0]) * 16.f; x[t][c + 1] = (x[t][c + 1] - lo[1]) * 16.f;
+            x[t][c + 2] = (x[t][c + 2] - hi[0]) * 16.f; x[t][c + 3] = (x[t][c + 3] - hi[1]) * 16.f;
+          }
+        }
+      }
+      // (lanes q hold the scales of products 32 q .. + 31)
+      qs[t] = HD == 128 ? s | max(s - 4, 0) << 8 : max(s - 4 * (fq >> 1), 0);
+    } else {
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int s = 0; s < kKS; ++s) {
+          float* y = x[t] + 8 * s;
+          qb[t][p][s] = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+          float hi[8];
+          unpack16(qb[t][p][s], hi);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] -= hi[e];
+        }
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));       // from here on vmcnt counts tile requests only
+#pragma unroll 1
+  for (int it = 0; it < S - 1; ++it) issue(it);
+
+  // a lane's part of the operand addresses
+  const int k_row = fr * HD, k_chunk = fq ^ swz_k<HD>(fr);      // (swz_k(16 + key) == swz_k(key) for 128-wide and 64-wide heads)
+  const int v_key = (fr >> 1) < 4 ? 4 * fq + (fr >> 1) : 16 + 4 * fq + (fr >> 1) - 4;
+  const int v_at = v_key * HD + (fr & 1) * 8, v_swz = swz_v<HD>(v_key);
+
+#pragma unroll 1
+  for (int it = 0; it < nit; ++it) {
+    // this wave's pieces of tile `it` have landed once at most those of the tiles behind it are outstanding (loads return in order)
+    wait_tiles<kReq, S - 2>(min(it + S - 2, mine - 1) - it);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    if constexpr (NR > 1) __builtin_amdgcn_s_barrier();         // tile `it` complete; slot of tile it - 1 free
+    else __builtin_amdgcn_s_waitcnt(0xC07F);                    // lgkmcnt(0): tile it - 1 is read
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    issue(it + S - 1);
+    if (it >= mine) continue;
+    const int t0 = s0 + kTileKeys * (it * NK + kg);
+    const char* k_lds = ring + (it % S) * kSlot;
+    const char* v_lds = k_lds + kSlot / 2;
+    const char* s_lds = ring_s + (it % S) * kScaleSlot;
+
+    // ---- S^T = K Q^T, both halves of 16 keys
+    const uint32_t vs0 = *reinterpret_cast<const uint32_t*>(s_lds + kTileKeys + 4 * fq), vs1 = *reinterpret_cast<const uint32_t*>(s_lds + kTileKeys + 16 + 4 * fq);
+    f32x4_t sacc[2][RTW];
+    if constexpr (kCodes) {
+      v8i_t kf[2];
+      int ksc[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const char* row = k_lds + j * 16 * HD + k_row;
+        const int4 lo = *reinterpret_cast<const int4*>(row + (k_chunk << 4));
+        const int4 hi = HD == 128 ? *reinterpret_cast<const int4*>(row + ((k_chunk ^ 4) << 4)) : lo;
+        kf[j] = v8i_t{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+        ksc[j] = *reinterpret_cast<const uint8_t*>(s_lds + 16 * j + fr);
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int t = 0; t < RTW; ++t) {
+          f32x4_t c = f32x4_t{0.f, 0.f, 0.f, 0.f};
+          if constexpr (NM > 1) c = mfma_scaled<1>(kf[j], qf[t][1], c, ksc[j], qs[t]);     // (the lesser part first)
+          sacc[j][t] = mfma_scaled<0>(kf[j], qf[t][0], c, ksc[j], qs[t]);
+        }
+    } else {
+      const uint32_t ks0 = *reinterpret_cast<const uint32_t*>(s_lds + 4 * fq), ks1 = *reinterpret_cast<const uint32_t*>(s_lds + 16 + 4 * fq);
+      const float ks[2][4] = {{quant_scale<0>(ks0), quant_scale<1>(ks0), quant_scale<2>(ks0), quant_scale<3>(ks0)},
+                              {quant_scale<0>(ks1), quant_scale<1>(ks1), quant_scale<2>(ks1), quant_scale<3>(ks1)}};
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        f32x4_t part[RTW][NP];
+#pragma unroll
+        for (int t = 0; t < RTW; ++t)
+#pragma unroll
+          for (int p = 0; p < NP; ++p) part[t][p] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < kKS; ++s) {
+          const uint2 c = *reinterpret_cast<const uint2*>(k_lds + j * 16 * HD + k_row + (((2 * s + (fq >> 1)) ^ swz_k<HD>(fr)) << 4) + (fq & 1) * 8);
+          const uint4 ka = make_uint4(two_bf16(c.x, false), two_bf16(c.x, true), two_bf16(c.y, false), two_bf16(c.y, true));
+#pragma unroll
+          for (int t = 0; t < RTW; ++t)
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+              part[t][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka), __builtin_bit_cast(bf16x8_t, qb[t][p][s]), part[t][p], 0, 0, 0);
+        }
+#pragma unroll
+        for (int t = 0; t < RTW; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sacc[j][t][e] = ((part[t][2][e] + part[t][1][e]) + part[t][0][e]) * ks[j][e];
+      }
+    }
+
+    // ---- online softmax; lane (row, q) owns keys t0 + 16 j + 4 q + e of its row.  The reference of the exponents moves only when a score
+    // exceeds its row's by more than kSlack.
+    constexpr float kSlack = 8.f;
+    const bool plain = t0 + kTileKeys <= min(L, s1) && sl2 > 0.f;
+    const float vs[8] = {quant_scale<0>(vs0), quant_scale<1>(vs0), quant_scale<2>(vs0), quant_scale<3>(vs0),
+                         quant_scale<0>(vs1), quant_scale<1>(vs1), quant_scale<2>(vs1), quant_scale<3>(vs1)};
+    uint4 pf[RTW][PP];
+#pragma unroll
+    for (int t = 0; t < RTW; ++t) {
+      float z[8];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[4 * j + e] = sacc[j][t][e];
+      float unit = sl2;
+      if (!plain) {
+        unit = 1.f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int p = t0 + 16 * j + 4 * fq + e;
+            bool vis = p < s1;
+            if (vis && p >= L) vis = (rowmask[t] >> (p - L)) & 1ull;
+            z[4 * j + e] = vis ? z[4 * j + e] * sl2 : -INFINITY;
+          }
+      }
+      const float mt = max3_nan(max3_nan(z[0], z[1], z[2]), max3_nan(z[3], z[4], z[5]), max_nan(z[6], z[7])) * unit;
+      if (__builtin_amdgcn_ballot_w64(mt > m_run[t] + kSlack) != 0ull) {
+        const float m_new = fmaxf(m_run[t], quad_row_max(mt));
+        const float al = __builtin_amdgcn_exp2f(m_run[t] - m_new);
+        m_run[t] = m_new;
+        l_run[t] *= al;
+#pragma unroll
+        for (int dt = 0; dt < kDT; ++dt) {
+          oacc[dt][t][0] *= al; oacc[dt][t][1] *= al;
+          oacc[dt][t][2] *= al; oacc[dt][t][3] *= al;
+        }
+      }
+      float pr[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) pr[e] = __builtin_amdgcn_exp2f(fmaf(z[e], unit, -m_run[t]));
+      l_run[t] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) pr[e] *= vs[e];
+#pragma unroll
+      for (int p = 0; p < PP; ++p) {
+        pf[t][p] = make_uint4(pack_bf16x2(pr[0], pr[1]), pack_bf16x2(pr[2], pr[3]), pack_bf16x2(pr[4], pr[5]), pack_bf16x2(pr[6], pr[7]));
+        if (p + 1 < PP) {
+          float hi[8];
+          unpack16(pf[t][p], hi);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) pr[e] -= hi[e];
+        }
+      }
+    }
+
+    // ---- O^T += V^T P^T
+#pragma unroll
+    for (int dt = 0; dt < kDT; ++dt) {
+      const v2i_t c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i_t)(lds_ptr_t)(v_lds + v_at + ((dt ^ v_swz) << 4)));
+      const uint4 va = make_uint4(two_bf16(c[0], false), two_bf16(c[0], true), two_bf16(c[1], false), two_bf16(c[1], true));
+#pragma unroll
+      for (int t = 0; t < RTW; ++t)
+#pragma unroll
+        for (int p = PP - 1; p >= 0; --p)
+          oacc[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, va), __builtin_bit_cast(bf16x8_t, pf[t][p]), oacc[dt][t], 0, 0, 0);
+    }
+  }
+
+  // ---- the segment's partial result.  Several rings: each leaves its sums in its own slots (16-byte pieces of a row swizzled), every wave adds some
+  // rows, in the order of the rings.
+  const size_t unit = static_cast<size_t>(blockIdx.x) + static_cast<size_t>(b) * a.Hkv + g;   // partial slot of segment (w, u)
+#pragma unroll
+  for (int t = 0; t < RTW; ++t) l_run[t] = quad_row_sum(l_run[t]);
+  if constexpr (NK == 1) {
+#pragma unroll
+    for (int t = 0; t < RTW; ++t) {
+      const int r = 16 * (rr * RTW + t) + fr;
+      if (r >= R) continue;
+      if (fq == 0) *reinterpret_cast<float2*>(a.part_ml + (unit * R + r) * 2) = make_float2(m_run[t], l_run[t]);
+      float* dst = a.part_o + (unit * R + r) * HD + 4 * fq;
+#pragma unroll
+      for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<float4*>(dst + 16 * dt) = make_float4(oacc[dt][t][0], oacc[dt][t][1], oacc[dt][t][2], oacc[dt][t][3]);
+    }
+    __syncthreads();                              // (the schedule's table is there for the next segment)
+  } else {
+    if constexpr (NR > 1) __syncthreads();        // the ring's last tile is read by all its waves
+#pragma unroll
+    for (int t = 0; t < RTW; ++t) {
+      const int r = 16 * (rr * RTW + t) + fr;
+      if (fq == 0) *reinterpret_cast<float2*>(ml_lds + 2 * (kg * RP + r)) = make_float2(m_run[t], l_run[t]);
+#pragma unroll
+      for (int dt = 0; dt < kDT; ++dt)
+        *reinterpret_cast<float4*>(ring + r * (4 * HD) + (((4 * dt + fq) ^ fr) << 4)) = make_float4(oacc[dt][t][0], oacc[dt][t][1], oacc[dt][t][2], oacc[dt][t][3]);
+    }
+    __syncthreads();
+    constexpr int C4 = HD / 4, RPW = 64 / C4;     // 16-byte pieces of a row, rows that a wave adds at a time
+    const int c4 = lane % C4;
+#pragma unroll 1
+    for (int r = RPW * wv + lane / C4; r < R; r += RPW * NK * NR) {
+      float2 ml[NK];
+      float4 o[NK];
+#pragma unroll
+      for (int k = 0; k < NK; ++k) {
+        ml[k] = *reinterpret_cast<const float2*>(ml_lds + 2 * (k * RP + r));
+        o[k] = *reinterpret_cast<const float4*>(smem + k * (S * kSlot) + r * (4 * HD) + ((c4 ^ (r & 15)) << 4));
+      }
+      float mm = ml[0].x;
+#pragma unroll
+      for (int k = 1; k < NK; ++k) mm = fmaxf(mm, ml[k].x);
+      float sum = 0.f;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < NK; ++k) {
+        const float f = __builtin_amdgcn_exp2f(ml[k].x - mm);
+        sum = fmaf(f, ml[k].y, sum);
+        v.x = fmaf(f, o[k].x, v.x); v.y = fmaf(f, o[k].y, v.y);
+        v.z = fmaf(f, o[k].z, v.z); v.w = fmaf(f, o[k].w, v.w);
+      }
+      *reinterpret_cast<float4*>(a.part_o + (unit * R + r) * HD + 4 * c4) = v;
+      if (c4 == 0) *reinterpret_cast<float2*>(a.part_ml + (unit * R + r) * 2) = make_float2(mm, sum);
+    }
+  }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------- merging the segments
+
+// Row of entry p of a unit in the pools.
+__device__ __forceinline__ size_t quant_entry(const QuantAttnArgs& a, int b, int g, int p) {
+  if (!a.paged) return (static_cast<size_t>(b) * a.Hkv + g) * a.l_max + p;
+  const int n = static_cast<int>(static_cast<uint32_t>(p) / static_cast<uint32_t>(a.page_size));
+  const int page = checked_page(a.page_table[static_cast<size_t>(b) * a.max_pages + n], a.n_pages, a.status);
+  return (static_cast<size_t>(page) * a.Hkv + g) * a.page_size + (p - n * a.page_size);
+}
+
+__device__ __forceinline__ void two_f32(uint32_t codes, bool hi, float* f) {
+  const v2f_t v = hi ? __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(codes), true) : __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(codes), false);
+  f[0] = v[0];
+  f[1] = v[1];
+}
+
+// One output row again, by one wave, key by key and with hidden keys left out.  The matrix instructions multiply every value of a tile with a
+// probability, hidden ones with 0, so that a NaN among entries that a row does not see (a block's entries that were never written)
+// reaches its sums, and infinite products of queries in parts are NaN: rows whose result is not finite are taken here, and are NaN
+// only where what they see makes them so.
+template <typename T, int D>
+__device__ __forceinline__ void quant_row_again(const QuantAttnArgs& a, int b, int i, int h) {
+  constexpr int LPK = D / 8, KPW = 64 / LPK;      // lanes of a key, keys of a wave
+  const int lane = threadIdx.x & 63;
+  const int kq = lane / LPK, c = lane % LPK;
+  const int g = h / a.G, L = attn_ctx_len(a, b), n = L + a.n_blk;
+  const size_t row = ((static_cast<size_t>(b) * a.n_q + i) * a.Hq + h) * D;
+  const uint64_t seen = a.mask ? a.mask[static_cast<size_t>(b) * a.mask_stride + i] : ((2ull << i) - 1ull);
+  float q[8], acc[8], m = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    q[e] = Elem<T>::load(static_cast<const T*>(a.q) + row + 8 * c + e);
+    acc[e] = 0.f;
+  }
+#pragma unroll 1
+  for (int p0 = 0; p0 < n; p0 += KPW) {
+    const int p = p0 + kq;
+    const bool vis = p < n && (p < L || (seen >> (p - L) & 1ull));
+    const size_t at = quant_entry(a, b, g, min(p, n - 1));
+    const uint2 kr = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.k) + at * D + 8 * c);
+    const uint2 vr = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.v) + at * D + 8 * c);
+    const float ks = quant_scale<0>(static_cast<const uint8_t*>(a.ks)[at]), vs = quant_scale<0>(static_cast<const uint8_t*>(a.vs)[at]);
+    float kf[8], vf[8], x = 0.f;
+    two_f32(kr.x, false, kf); two_f32(kr.x, true, kf + 2); two_f32(kr.y, false, kf + 4); two_f32(kr.y, true, kf + 6);
+    two_f32(vr.x, false, vf); two_f32(vr.x, true, vf + 2); two_f32(vr.y, false, vf + 4); two_f32(vr.y, true, vf + 6);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x = fmaf(q[e], kf[e] * ks, x);
+#pragma unroll
+    for (int o = 1; o < LPK; o <<= 1) x += __shfl_xor(x, o, 64);
+    x = vis ? x * a.scale : -INFINITY;
+    float mt = x;
+#pragma unroll
+    for (int o = LPK; o < 64; o <<= 1) mt = fmaxf(mt, __shfl_xor(mt, o, 64));
+    const float m_new = fmaxf(m, mt);
+    float al = 1.f, pr = 0.f;
+    if (m_new != -INFINITY) {
+      al = m == -INFINITY ? 0.f : expf(m - m_new);
+      pr = expf(x - m_new);
+    }
+    if (x != x) pr = x;
+    m = m_new;
+    sum = fmaf(sum, al, pr);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = fmaf(pr, vis ? vf[e] * vs : 0.f, acc[e] * al);
+  }
+#pragma unroll
+  for (int o = LPK; o < 64; o <<= 1) {
+    sum += __shfl_xor(sum, o, 64);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
+  }
+  if (kq == 0) {
+    T* dst = static_cast<T*>(a.out) + row + 8 * c;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float v = sum == 0.f ? 0.f : acc[e] / sum;
+      if constexpr (sizeof(T) == 2) dst[e] = static_cast<bf16_t>(pack_bf16x2(v, v));
+      else dst[e] = v;
+    }
+  }
+}
+
+// Exact log-sum-exp merge of the segments of one (sequence, query, head), WPR waves per output row.  Latency is all there is: the unit's
+// first and last workgroup, one round to memory for (max, sum) pairs and the first partial outputs, a meeting of the waves.
+// Lane s of every wave holds the weights of segments s, s + 64, ..; half a wave (128-wide heads; a quarter of 64-wide ones) has a segment's row.
+constexpr int kEarly = 6;        // partial outputs requested with the (max, sum) pairs, per group of lanes
+
+template <typename T, int D, int WPR>
+__global__ __launch_bounds__(256) void k_quant_combine(const QuantAttnArgs a) {
+  constexpr int C4 = D / 4, GPW = 64 / C4, NG = WPR * GPW;     // float4 columns; groups of a wave and of a row
+  __shared__ float4 gs[WPR > 1 ? NG : 1][C4];
+  arguments_at_once<sizeof(QuantAttnArgs)>();
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = WPR == 4 ? static_cast<int>(blockIdx.x) : static_cast<int>(blockIdx.x) * 4 + wv;
+  if (row >= a.B * a.n_q * a.Hq) return;          // (one wave per row)
+  const int b = row / (a.n_q * a.Hq), ih = row - b * (a.n_q * a.Hq), i = ih / a.Hq, h = ih - i * a.Hq;
+  const int R = a.G * a.n_q, g = h / a.G, r = i * a.G + h - g * a.G;
+  typedef const __attribute__((address_space(4))) int* words_t;           // (scalar loads: nothing writes these words meanwhile)
+  const int u = b * a.Hkv + g;
+  const words_t ends = (words_t)a.sched + 2 * u;
+  const int w_first = ends[0], n_seg = ends[1] - w_first + 1;
+  const size_t slot = static_cast<size_t>(w_first) + u;
+  const float* ml_p = a.part_ml + (slot * R + r) * 2;
+  const size_t ml_step = 2 * static_cast<size_t>(R), po_step = static_cast<size_t>(R) * D;
+  const int sg = (WPR == 4 ? wv * GPW : 0) + lane / C4, c4 = lane % C4;
+  const float* po = a.part_o + (slot * R + r) * D + c4 * 4;
+  float2 ml = *reinterpret_cast<const float2*>(ml_p + min(lane, n_seg - 1) * ml_step);
+  float4 o[kEarly];
+#pragma unroll
+  for (int k = 0; k < kEarly; ++k) o[k] = *reinterpret_cast<const float4*>(po + min(sg + k * NG, n_seg - 1) * po_step);
+  float mmax = ml.x;
+  for (int s = 64 + lane; s < n_seg; s += 64) mmax = fmaxf(mmax, ml_p[s * ml_step]);
+  mmax = wave_max_dpp(mmax);
+  float den = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s0 = 0; s0 < n_seg; s0 += 64) {
+    if (s0 > 0) ml = *reinterpret_cast<const float2*>(ml_p + min(s0 + lane, n_seg - 1) * ml_step);
+    const float w = s0 + lane < n_seg ? __builtin_amdgcn_exp2f(ml.x - mmax) : 0.f;
+    den += w != 0.f || ml.y != ml.y ? w * ml.y : 0.f;             // (a NaN counts whatever its weight)
+    const int n = min(64, n_seg - s0);
+    for (int sb = 0; sb < n; sb += kEarly * NG) {                 // (uniform)
+      const int s = sb + sg;
+      if (s0 + sb > 0) {
+#pragma unroll
+        for (int k = 0; k < kEarly; ++k) o[k] = *reinterpret_cast<const float4*>(po + (s0 + min(s + k * NG, n - 1)) * po_step);
+      }
+#pragma unroll
+      for (int k = 0; k < kEarly; ++k) {
+        float wk = __shfl(w, min(s + k * NG, n - 1), 64);
+        if (s + k * NG >= n) wk = 0.f;
+        if (wk != 0.f) {
+          acc.x = fmaf(wk, o[k].x, acc.x); acc.y = fmaf(wk, o[k].y, acc.y);
+          acc.z = fmaf(wk, o[k].z, acc.z); acc.w = fmaf(wk, o[k].w, acc.w);
+        }
+      }
+    }
+  }
+  den = wave_sum_dpp(den);
+  if constexpr (WPR > 1) {
+    gs[sg][c4] = acc;
+    __syncthreads();
+    if (wv > 0) return;
+    acc = gs[0][c4];                              // (the first wave's lanes all hold the row then, group 0 stores it)
+#pragma unroll
+    for (int k = 1; k < NG; ++k) { acc.x += gs[k][c4].x; acc.y += gs[k][c4].y; acc.z += gs[k][c4].z; acc.w += gs[k][c4].w; }
+  } else {
+#pragma unroll
+    for (int off = C4; off < 64; off <<= 1) {
+      acc.x += __shfl_xor(acc.x, off, 64); acc.y += __shfl_xor(acc.y, off, 64);
+      acc.z += __shfl_xor(acc.z, off, 64); acc.w += __shfl_xor(acc.w, off, 64);
+    }
+  }
+  // a row that sees nothing has a sum of 0 and is all zeros
+  const float inv = den == 0.f ? 0.f : 1.0f / den;
+  if constexpr (sizeof(T) == 2) {
+    acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
+  } else if (den != 0.f) {
+    acc.x /= den; acc.y /= den; acc.z /= den; acc.w /= den;
+  }
+  const float all = (acc.x + acc.y) + (acc.z + acc.w);
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(fabsf(all) < INFINITY)) != 0ull, 0)) {
+    quant_row_again<T, D>(a, b, i, h);
+    return;
+  }
+  if (lane < C4) {
+    T* dst = static_cast<T*>(a.out) + static_cast<size_t>(row) * D + c4 * 4;
+    // (as bytes: the caller's buffer may begin at any element)
+    if constexpr (sizeof(T) == 2) {
+      const uint2 v = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
+      __builtin_memcpy(dst, &v, sizeof(v));
+    } else {
+      __builtin_memcpy(dst, &acc, sizeof(acc));
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------- launches
+
+// Rings of a workgroup, waves of a ring, row tiles of a wave.
+struct Form { int nk, nr, rtw; };
+Form form_of(bool f32, int d, int tiles) {
+  if (f32) {
+    if (d == 64) return tiles <= 2 ? Form{4, 1, 2} : tiles <= 4 ? Form{2, 2, 2} : Form{2, 4, 2};
+    return tiles <= 1 ? Form{4, 1, 1} : tiles <= 2 ? Form{2, 2, 1} : tiles <= 4 ? Form{2, 4, 1} : Form{1, 8, 1};
+  }
+  switch (tiles) {
+    case 1: return {4, 1, 1};
+    case 2: return {4, 1, 2};
+    case 3: return {4, 1, 3};
+    case 4: return {4, 1, 4};
+    case 5: case 6: return {2, 2, 3};
+    default: return {2, 2, 4};
+  }
+}
+int row_tiles(const QuantAttnArgs& a) { return (a.G * a.n_q + 15) / 16; }
+Form form_of(const QuantAttnArgs& a) { return form_of(a.dtype == 0, a.d, row_tiles(a)); }
+
+template <int HD, typename T, int NK, int NR, int RTW>
+hipError_t launch_one(const QuantAttnArgs& a, hipStream_t s) {
+  static_assert(quant_lds_bytes(HD, NK, 16 * NR * RTW, kAttnMaxSeqs, true) <= 160 * 1024, "the LDS of a compute unit");
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_quant_attn<HD, T, NK, NR, RTW>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+  if (attr != hipSuccess) return attr;
+  hipLaunchKernelGGL((k_quant_attn<HD, T, NK, NR, RTW>), dim3(a.wgrid), dim3(64 * NK * NR), quant_lds_bytes(HD, NK, 16 * NR * RTW, a.B, a.paged != 0), s, a);
+  return hipGetLastError();
+}
+
+template <int HD> hipError_t launch_bf16(const QuantAttnArgs& a, hipStream_t s) {
+  const Form f = form_of(a);
+  if (f.nr == 1) {
+    switch (f.rtw) {
+      case 1: return launch_one<HD, bf16_t, 4, 1, 1>(a, s);
+      case 2: return launch_one<HD, bf16_t, 4, 1, 2>(a, s);
+      case 3: return launch_one<HD, bf16_t, 4, 1, 3>(a, s);
+      default: return launch_one<HD, bf16_t, 4, 1, 4>(a, s);
+    }
+  }
+  return f.rtw == 3 ? launch_one<HD, bf16_t, 2, 2, 3>(a, s) : launch_one<HD, bf16_t, 2, 2, 4>(a, s);
+}
+
+hipError_t launch_f32(const QuantAttnArgs& a, hipStream_t s) {
+  const Form f = form_of(a);
+  if (a.d == 64) return f.nk == 4 ? launch_one<64, float, 4, 1, 2>(a, s) : f.nr == 2 ? launch_one<64, float, 2, 2, 2>(a, s) : launch_one<64, float, 2, 4, 2>(a, s);
+  switch (f.nr) {
+    case 1: return launch_one<128, float, 4, 1, 1>(a, s);
+    case 2: return launch_one<128, float, 2, 2, 1>(a, s);
+    case 4: return launch_one<128, float, 2, 4, 1>(a, s);
+    default: return launch_one<128, float, 1, 8, 1>(a, s);
+  }
+}
+
+template <typename T, int D> hipError_t launch_combine(const QuantAttnArgs& a, hipStream_t s) {
+  const int64_t units = static_cast<int64_t>(a.B) * a.Hkv, rows = static_cast<int64_t>(a.B) * a.n_q * a.Hq;
+  if (rows * units > 256 * static_cast<int64_t>(a.wgrid)) hipLaunchKernelGGL((k_quant_combine<T, D, 1>), dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_quant_combine<T, D, 4>), dim3(static_cast<unsigned>(rows)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+bool quant_attn_plan(QuantAttnArgs& a, int num_cus) {
+  a.use_mfma = kTwoPart;                          // (its maxima are in log2 units)
+  a.G = a.Hq / a.Hkv;
+  a.g_inv = (65536 + a.G - 1) / a.G;
+  a.pad = a.d == 64 ? 6 : 4;
+  a.wide_from = 2400;
+  a.page_shift = (a.page_size & (a.page_size - 1)) == 0 ? 31 - __builtin_clz(static_cast<unsigned>(a.page_size)) : -1;
+  if (a.B > kAttnMaxSeqs || a.l_max < a.n_blk) return false;
+  const int64_t units = static_cast<int64_t>(a.B) * a.Hkv;
+  const int64_t gmax = (a.l_max + kAttnGran - 1) / kAttnGran;      // granules of the longest possible unit
+  if (units * (gmax + a.pad) >= (1ll << 30)) return false;
+  const AttnLine line = attn_sched_line(static_cast<int>(a.B * gmax), a.B, a.Hkv, a.pad, a.wide_from, 0, num_cus);
+  int64_t w = line.W;
+  if (line.T > kAttnSpread && w < kAttnSpread) w = std::min<int64_t>(kAttnSpread, num_cus);   // (fewer granules may take more workgroups)
+  if (a.paged) {                                  // a segment's page ids have to fit LDS
+    const int64_t seg_gran = static_cast<int64_t>(kMaxPages) * a.page_size / kAttnGran;
+    w = std::max(w, (line.T + seg_gran - 1) / seg_gran);
+  }
+  if (w > kAttnMaxGrid) return false;
+  a.wgrid = static_cast<int>(w);
+  return true;
+}
+
+hipError_t launch_quant_attn(const QuantAttnArgs& a, hipStream_t s) {
+  const hipError_t e = a.dtype == 0 ? launch_f32(a, s) : a.d == 128 ? launch_bf16<128>(a, s) : launch_bf16<64>(a, s);
+  if (e != hipSuccess) return e;
+  if (a.dtype == 0) return a.d == 128 ? launch_combine<float, 128>(a, s) : launch_combine<float, 64>(a, s);
+  return a.d == 128 ? launch_combine<bf16_t, 128>(a, s) : launch_combine<bf16_t, 64>(a, s);
+}
+
+}  // namespace sx

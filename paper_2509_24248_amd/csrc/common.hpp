@@ -145,6 +145,7 @@ constexpr int kStatusBadLength = 1;  // ctx_len / pos < 0 or beyond the cache ca
 constexpr int kStatusBadPage = 2;    // page id outside 0 .. n_pages-1
 constexpr int kStatusBadToken = 3;   // token id outside 0 .. V-1
 constexpr int kStatusBadNode = 4;    // node id, path entry or row index outside its block
+constexpr int kStatusBadSetting = 5; // a sampling setting outside its range
 
 __device__ __forceinline__ void report_status(int* status, int code) {
   if (status) atomicCAS(status, 0, code);

@@ -226,6 +226,74 @@ void attn_carve(AttnArgs& a, void* workspace);   // points part_o / part_ml / sc
 typedef void (*KernelHook)(int id, int phase, hipStream_t s);
 hipError_t launch_attn(const AttnArgs& a, hipStream_t s, KernelHook hook = nullptr, int hook_id = 0);
 
+// ---- 8-bit KV cache (quant_kv.hip, attn_quant.hip) --------------------------------------
+// One layer's cache: e4m3 codes as the pools of an ordinary cache, and a scale byte per row.
+struct QuantKv {
+  int paged;
+  void *k, *v, *ks, *vs;
+  const int32_t* page_table;
+  int page_size, max_pages;
+  int64_t l_max, n_pages;
+  int Hkv;
+};
+struct QuantWriteArgs {
+  QuantKv kv;
+  int f32, d;                // source rows fp32, else bf16; head_dim
+  int B, T, groups;          // groups of tokens that a wave takes (quant_write_plan)
+  int64_t tasks;             // waves
+  const void *k, *v;         // [B][T] tokens `token_stride` elements apart, [Hkv][d] of each
+  int64_t token_stride;
+  const int32_t *pos, *count;
+  int* status;
+};
+bool quant_write_plan(QuantWriteArgs& a);
+hipError_t launch_quant_write(const QuantWriteArgs& a, hipStream_t s);
+struct QuantCompactArgs {
+  QuantKv kv;
+  int d;
+  int64_t layer_stride, scale_stride;      // bytes between two layers' codes and scales
+  int n_layers, B, n_q;
+  const int32_t *ctx_len, *accept_path, *accept_len, *last_node;
+  int* status;
+  const void* block_hidden;
+  void* hidden_next;
+  int hidden_row_bytes;
+};
+hipError_t launch_quant_compact(const QuantCompactArgs& a, hipStream_t s);
+// k, v: codes; dtype: of q and out
+struct QuantAttnArgs : AttnArgs {
+  const void *ks, *vs;
+  int page_shift;            // log2 of the page size, -1 where it is no power of two
+};
+bool quant_attn_plan(QuantAttnArgs& a, int num_cus);
+hipError_t launch_quant_attn(const QuantAttnArgs& a, hipStream_t s);   // (workspace as attn_workspace_bytes / attn_carve)
+
+// ---- sampled tokens (sample.hip) -----------------------------------------------------------
+constexpr int kSampleMaxK = 1024, kSampleMaxSegs = 512;      // segments of 512 tokens
+struct SampleRow {
+  int listed, mode, lo, hi;
+  float top;
+};
+struct SampleArgs {
+  int f32, M, V;
+  int64_t ld;
+  const void* logits;
+  int rows_per_seq;
+  const float *temperature, *top_p, *min_p;      // [ceil(M / rows_per_seq)] or nullptr
+  const int32_t* top_k;
+  const float* u;            // [M]
+  int32_t* token;
+  float* prob;               // or nullptr
+  int* status;
+  int segs, chunk_segs, chunks;                  // sample_plan
+  unsigned long long *hist, *chunk_sums, *seg_mass, *list;      // sample_carve
+  float* chunk_top;
+  SampleRow* row_info;
+};
+void sample_plan(SampleArgs& a);
+size_t sample_carve(SampleArgs& a, void* base);
+hipError_t launch_sample(const SampleArgs& a, hipStream_t s);
+
 // ---- draft-step glue kernels -----------------------------------------------------------
 struct DraftDims {
   int dtype, D, Hq, Hkv, d, I, V;

@@ -1,0 +1,204 @@
+// The 8-bit KV cache: rows quantised as they are written, and the compaction that closes a round over them.
+//
+// A row (one token of one KV head, d values) is stored as d e4m3 codes and one scale byte s, and stands for code 2^(s - 127).
+// With amax = m 2^E the row's largest finite magnitude, 1 <= m < 2, s = E + 127 - 8 + (m > 1.75): the least power of two that
+// brings the row within e4m3's 448 = 1.75 2^8.  A power of two because multiplying by it is exact: a code is one rounding of the
+// value (to nearest even, at most 2^-4 of it; what lies more than 2^14 below the row's largest has e4m3's subnormal step, 2^-9), the
+// same whatever order or machine computes it, and because it is the scale that the block-scaled matrix instructions
+// multiply with (attn_quant.hip).  e4m3 is a floating type, so a finer scale would only move values within a binade.
+#include "common.hpp"
+#include "kernels.hpp"
+#include "quant.hpp"
+
+namespace sx {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTok = 16;        // tokens of a wave of the writing kernel
+
+// maximum over the 16 (or 8) lanes that hold a row
+template <int CTRL> __device__ __forceinline__ uint32_t row_umax(uint32_t v) {
+  return max(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, 0xf, 0xf, false)));
+}
+
+// Row of entry p of (sequence b, KV head h) in the pools, or -1: outside the cache, or a page outside the pool.
+__device__ __forceinline__ int64_t quant_row(const QuantKv& kv, int b, int h, int64_t p, int* status) {
+  if (!kv.paged) return (static_cast<int64_t>(b) * kv.Hkv + h) * kv.l_max + p;
+  const uint32_t in_seq = static_cast<uint32_t>(p) / static_cast<uint32_t>(kv.page_size);
+  const int page = kv.page_table[static_cast<size_t>(b) * kv.max_pages + in_seq];
+  if (!page_in_pool(page, kv.n_pages, status)) return -1;
+  return (static_cast<int64_t>(page) * kv.Hkv + h) * kv.page_size + (p - static_cast<int64_t>(in_seq) * kv.page_size);
+}
+
+// A wave takes sixteen tokens of K or V of one head: D / 8 lanes a row, eight values a lane, all loads of the wave requested together.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void k_quant_write(const QuantWriteArgs a) {
+  constexpr int LPR = D / 8, RPI = 64 / LPR, U = kTok / RPI;     // lanes of a row, rows of an instruction, instructions
+  const int lane = threadIdx.x & 63;
+  const int64_t task = static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (task >= a.tasks) return;
+  const int which = static_cast<int>(task & 1);
+  const uint32_t rest = static_cast<uint32_t>(task >> 1);
+  const uint32_t bg = rest / static_cast<uint32_t>(a.kv.Hkv), h = rest - bg * a.kv.Hkv;
+  const uint32_t b = bg / static_cast<uint32_t>(a.groups), t0 = (bg - b * a.groups) * kTok;
+  const int count = a.count ? min(a.count[b], a.T) : a.T;
+  const int pos = a.pos[b];
+  const int sub = lane / LPR, c = lane % LPR;
+  const T* src = static_cast<const T*>(which ? a.v : a.k) + (static_cast<int64_t>(b) * a.T + t0) * a.token_stride + h * D + c * 8;
+  uint4 raw[U][sizeof(T) / 2];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int t = u * RPI + sub;
+    const bool in = static_cast<int>(t0) + t < count;
+    const uint4* p = reinterpret_cast<const uint4*>(src + static_cast<int64_t>(in ? t : 0) * a.token_stride);
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(T) / 2; ++i) raw[u][i] = in ? p[i] : make_uint4(0, 0, 0, 0);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int t = static_cast<int>(t0) + u * RPI + sub;
+    float x[8];
+    if constexpr (sizeof(T) == 2) {
+      unpack16(raw[u][0], x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        x[4 * i] = __uint_as_float(raw[u][i].x); x[4 * i + 1] = __uint_as_float(raw[u][i].y);
+        x[4 * i + 2] = __uint_as_float(raw[u][i].z); x[4 * i + 3] = __uint_as_float(raw[u][i].w);
+      }
+    }
+    uint32_t amax = 0;              // magnitudes compare like their bits
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t bits = __float_as_uint(x[e]) & 0x7FFFFFFFu;
+      amax = max(amax, bits < 0x7F800000u ? bits : 0u);
+    }
+    amax = row_umax<0xB1>(amax);                       // lanes 1, 2, 4 (and 8) apart
+    amax = row_umax<0x4E>(amax);
+    amax = row_umax<0x141>(amax);
+    if constexpr (LPR == 16) amax = row_umax<0x140>(amax);
+    const int s = quant_scale_byte(amax);
+    const float inv = quant_scale_inverse(s);
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      w[i] = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i] * inv, x[4 * i + 1] * inv, static_cast<int>(w[i]), false);
+      w[i] = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2] * inv, x[4 * i + 3] * inv, static_cast<int>(w[i]), true);
+    }
+    // a value that is not finite has the NaN code with its sign
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t bits = __float_as_uint(x[e]);
+      if ((bits & 0x7FFFFFFFu) >= 0x7F800000u) {
+        const int sh = 8 * (e & 3);
+        w[e >> 2] = (w[e >> 2] & ~(0xFFu << sh)) | ((0x7Fu | (bits >> 24 & 0x80u)) << sh);
+      }
+    }
+    if (t >= count) continue;
+    const int64_t p = static_cast<int64_t>(pos) + t;
+    if (p < 0 || p >= a.kv.l_max) {
+      report_status(a.status, kStatusBadLength);
+      continue;
+    }
+    const int64_t row = quant_row(a.kv, b, h, p, a.status);
+    if (row < 0) continue;
+    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(which ? a.kv.v : a.kv.k) + row * D + c * 8) = make_uint2(w[0], w[1]);
+    if (c == 0) static_cast<uint8_t*>(which ? a.kv.vs : a.kv.ks)[row] = static_cast<uint8_t>(s);
+  }
+}
+
+// grid = (KV heads, sequences, layers), as k_kv_compact: every row is read before any is written.  Lane j of every wave holds
+// path entry j, so that what has to move is known after one round to memory.
+constexpr int kItems = 2 * 63 * 8 / kThreads + 1;      // 16-byte pieces of a thread, at most
+
+__global__ __launch_bounds__(kThreads) void k_quant_compact(const QuantCompactArgs a) {
+  const int h = blockIdx.x, b = blockIdx.y, layer = blockIdx.z;
+  const int lane = threadIdx.x & 63;
+  const int L = a.ctx_len[b];
+  const int m = max(0, min(a.accept_len[b], a.n_q - 1));
+  const int my_node = lane < a.n_q ? a.accept_path[static_cast<size_t>(b) * a.n_q + lane] : -1;
+  const bool in_cache = L >= 0 && static_cast<int64_t>(L) + a.n_q <= a.kv.l_max;
+  if (!in_cache) report_status(a.status, kStatusBadLength);
+  if (h == 0 && layer == 0 && a.block_hidden) {
+    int node = a.last_node[b];
+    if (node < 0 || node >= a.n_q) report_status(a.status, kStatusBadNode);
+    node = max(0, min(node, a.n_q - 1));
+    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(a.block_hidden) + (static_cast<size_t>(b) * a.n_q + node) * a.hidden_row_bytes);
+    uint4* dst = reinterpret_cast<uint4*>(static_cast<char*>(a.hidden_next) + static_cast<size_t>(b) * a.hidden_row_bytes);
+    for (int i = threadIdx.x; i < (a.hidden_row_bytes >> 4); i += kThreads) dst[i] = src[i];
+  }
+  if (!in_cache) return;                               // uniform over the workgroup
+  const uint64_t away = __builtin_amdgcn_ballot_w64(lane < m && my_node != lane + 1);
+  if (!away) return;
+  const int first = __ffsll(static_cast<unsigned long long>(away)) - 1;
+  const int lpr = a.d >> 4, rows = m - first;          // 16-byte pieces of a row; rows that may move
+  const int items = 2 * rows * lpr;
+  // item: K rows then V rows; -1 where nothing moves
+  auto node_of = [&](int j) {
+    const int node = __shfl(my_node, j, 64);
+    return node >= 1 && node < a.n_q ? node : -1;
+  };
+  uint4 buf[kItems];
+  int64_t from[kItems];
+#pragma unroll
+  for (int u = 0; u < kItems; ++u) {
+    const int it = threadIdx.x + u * kThreads;
+    const int j = first + min(it, items - 1) % (rows * lpr) / lpr, piece = it % lpr;
+    const int node = node_of(j);
+    from[u] = -1;
+    if (it < items && node < 0) report_status(a.status, kStatusBadNode);
+    if (it < items && node >= 0) from[u] = quant_row(a.kv, b, h, L + node, a.status);
+    if (from[u] >= 0)
+      buf[u] = reinterpret_cast<const uint4*>(static_cast<const char*>(it >= rows * lpr ? a.kv.v : a.kv.k) + layer * a.layer_stride + from[u] * a.d)[piece];
+  }
+  // scale bytes: threads 0 .. 2 rows - 1
+  const int sj = first + min(static_cast<int>(threadIdx.x), 2 * rows - 1) % rows;
+  const int snode = node_of(sj);
+  const bool has_scale = static_cast<int>(threadIdx.x) < 2 * rows && snode >= 0;
+  uint8_t* scales = static_cast<uint8_t*>(static_cast<int>(threadIdx.x) >= rows ? a.kv.vs : a.kv.ks) + layer * a.scale_stride;
+  int64_t sfrom = -1;
+  uint8_t sbyte = 0;
+  if (has_scale) sfrom = quant_row(a.kv, b, h, L + snode, a.status);
+  if (sfrom >= 0) sbyte = scales[sfrom];
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kItems; ++u) {
+    const int it = threadIdx.x + u * kThreads;
+    if (from[u] < 0) continue;
+    const int j = first + it % (rows * lpr) / lpr, piece = it % lpr;
+    const int64_t to = quant_row(a.kv, b, h, L + 1 + j, a.status);
+    if (to >= 0) reinterpret_cast<uint4*>(static_cast<char*>(it >= rows * lpr ? a.kv.v : a.kv.k) + layer * a.layer_stride + to * a.d)[piece] = buf[u];
+  }
+  if (sfrom >= 0) {
+    const int64_t to = quant_row(a.kv, b, h, L + 1 + sj, a.status);
+    if (to >= 0) scales[to] = sbyte;
+  }
+}
+
+template <typename T>
+hipError_t launch_write(const QuantWriteArgs& a, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>((a.tasks + kThreads / 64 - 1) / (kThreads / 64)));
+  if (a.d == 128) hipLaunchKernelGGL((k_quant_write<T, 128>), grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((k_quant_write<T, 64>), grid, dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Sets the launch's task count; false: more than one launch takes.
+bool quant_write_plan(QuantWriteArgs& a) {
+  a.groups = (a.T + kTok - 1) / kTok;
+  const int64_t pairs = static_cast<int64_t>(a.B) * a.groups * a.kv.Hkv;
+  a.tasks = 2 * pairs;
+  return pairs < (1ll << 31) - 1;
+}
+
+hipError_t launch_quant_write(const QuantWriteArgs& a, hipStream_t s) { return a.f32 ? launch_write<float>(a, s) : launch_write<bf16_t>(a, s); }
+
+hipError_t launch_quant_compact(const QuantCompactArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(k_quant_compact, dim3(a.kv.Hkv, a.B, a.n_layers), dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace sx

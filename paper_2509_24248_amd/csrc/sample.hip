@@ -1,0 +1,648 @@
+// A token per row of logits from a given uniform number: temperature, top-k, top-p, min-p, then the inverse of the kept weights'
+// cumulative sum in index order.
+//
+// Weights are w = 2^((l - l_max) log2(e) / T), in 64-bit arithmetic (a polynomial: see weight()) and added up as 45-bit fixed-point
+// numbers, so that a sum is the same whatever its order, and so exact that a draw next to the border of two tokens falls
+// where 64 bits put it.  Tokens below 2^-40 of the best one's weight count as none.
+//
+// What a filter keeps is a prefix of the tokens in the order (logit descending, index ascending).  Three launches find it without
+// sorting a row; a row is cut into chunks, so that few rows fill the chip too:
+//   1 k_sample_bins  one pass over the logits: a histogram of every chunk over bins of 1/16 nat of l / T (count and mass of a
+//                    bin in one 64-bit LDS atomic; the bins lie on one grid for all chunks of a row, counted from the chunk's best).
+//   2 k_sample_mass  adds the row's histograms, takes the bins that the borders of top-k and top-p lie in, reads the logits
+//                    again: masses of what is kept for certain per segment of 512 tokens, and a list of the tokens in doubt.
+//   3 k_sample_pick  a workgroup per row sorts the list (at most 4096), cuts it, finds the draw's segment and in it the token.
+// Bound by memory at many rows: the logits are read twice, the second time mostly from the last-level cache; at few rows
+// by the latencies of three launches.
+#include "common.hpp"
+#include "kernels.hpp"
+
+#include <limits.h>
+
+namespace sx {
+
+namespace {
+
+constexpr int kT = 512;                 // threads of a workgroup
+constexpr int kWaves = kT / 64;
+constexpr int kSeg = 512;               // tokens of a segment (a wave's step; a workgroup's in the last kernel)
+constexpr int kBins = 512;              // bins of a histogram: 32 nats
+constexpr float kPerNat = 16.f;
+constexpr int kChunkSegs = 64;          // segments of a chunk, at most
+constexpr int kList = 4096, kListPart = 2048;      // tokens in doubt of a row, and of one of its chunks
+constexpr int kFar = 1 << 29;           // bins are forced into -kFar .. kFar
+constexpr double kFix = 35184372088832.0;          // 2^45
+constexpr double kFloor = 9.094947017729282e-13;   // 2^-40
+constexpr int kCountBit = 42;
+
+enum { kModeEmpty = 0, kModeAll = 1, kModeTopK = 2, kModeTopP = 3, kModeScan = 4 };
+
+// A row's settings, forced into range.
+struct Setting {
+  int k;             // 0: off
+  float s;           // bins per logit
+  double c;          // log2(e) / T
+  double p, m;       // top-p (1: off), min-p
+};
+__device__ __forceinline__ Setting setting_of(const SampleArgs& a, int row) {
+  const int i = row / a.rows_per_seq;
+  float T = a.temperature ? a.temperature[i] : 1.f;
+  const float p = a.top_p ? a.top_p[i] : 1.f, m = a.min_p ? a.min_p[i] : 0.f;
+  int k = a.top_k ? a.top_k[i] : 0;
+  Setting s;
+  if (k < 0 || k >= a.V) k = 0;
+  if (k > kSampleMaxK) {
+    report_status(a.status, kStatusBadSetting);
+    k = kSampleMaxK;
+  }
+  if (!(T >= 9.765625e-4f)) { k = 1; T = 1.f; }         // greedy
+  T = fminf(T, 7.9228163e28f);
+  s.k = k;
+  s.s = kPerNat / T;
+  s.c = 1.4426950408889634 / static_cast<double>(T);
+  s.p = p < 1.f ? fmaxf(p, 0.f) : 1.0;                   // (NaN: off)
+  s.m = fmax(fmin(static_cast<double>(m), 1.0), kFloor); // (NaN: off)
+  if (m != m) s.m = kFloor;
+  return s;
+}
+
+__device__ __forceinline__ int bin_of(float l, float s) { return static_cast<int>(floorf(fminf(fmaxf(l * s, -static_cast<float>(kFar)), static_cast<float>(kFar)))); }
+
+// order of the logits as unsigned numbers, and a token's place: better tokens have smaller ones
+__device__ __forceinline__ uint32_t key_of(float l) {
+  const uint32_t u = __float_as_uint(l);
+  return u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key ^ ((key >> 31) - 1u | 0x80000000u)); }
+__device__ __forceinline__ uint64_t place_of(float l, int idx) { return static_cast<uint64_t>(~key_of(l)) << 32 | static_cast<uint32_t>(idx); }
+
+// 2^((l - top) c), 0 below 2^-40.  2^f for |f| <= 1/2 as the Taylor sum of e^(f ln 2) to degree 11: what is left out is (ln 2 / 2)^12 / 12! < 7e-15.
+__device__ __forceinline__ double weight(float l, float top, double c) {
+  const double d = l == top ? 0.0 : static_cast<double>(l) - static_cast<double>(top);      // (also where both are infinite)
+  const double t = d * c;
+  if (!(t > -40.5)) return 0.0;
+  const double n = rint(t), f = t - n;
+  double y = 4.44553827187081e-10;
+  y = fma(y, f, 7.054911620801121e-09);
+  y = fma(y, f, 1.0178086009239696e-07);
+  y = fma(y, f, 1.3215486790144305e-06);
+  y = fma(y, f, 1.5252733804059838e-05);
+  y = fma(y, f, 0.00015403530393381606);
+  y = fma(y, f, 0.0013333558146428441);
+  y = fma(y, f, 0.009618129107628477);
+  y = fma(y, f, 0.055504108664821576);
+  y = fma(y, f, 0.2402265069591007);
+  y = fma(y, f, 0.6931471805599453);
+  y = fma(y, f, 1.0);
+  const double w = __longlong_as_double(__double_as_longlong(y) + (static_cast<int64_t>(static_cast<int>(n)) << 52));
+  return w >= kFloor ? w : 0.0;
+}
+// a weight in units of 2^-45 (adding 2^52 leaves the rounded number in the low bits)
+__device__ __forceinline__ uint64_t fixed(double w) { return static_cast<uint64_t>(__double_as_longlong(fma(w, kFix, 4503599627370496.0))) & 0xFFFFFFFFFFFFFull; }
+
+__device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int o) { return static_cast<uint64_t>(__shfl_xor(static_cast<unsigned long long>(v), o, 64)); }
+__device__ __forceinline__ uint64_t wave_sum64(uint64_t v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += shfl_xor64(v, o);
+  return v;
+}
+__device__ __forceinline__ uint64_t wave_scan64(uint64_t v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint64_t up = static_cast<uint64_t>(__shfl_up(static_cast<unsigned long long>(v), o, 64));
+    if (lane >= o) v += up;
+  }
+  return v;
+}
+// inclusive sum over the workgroup; `part` [kWaves] is free again behind the next barrier
+__device__ __forceinline__ uint64_t block_scan64(uint64_t v, uint64_t* part) {
+  const int wv = threadIdx.x >> 6;
+  v = wave_scan64(v);
+  if ((threadIdx.x & 63) == 63) part[wv] = v;
+  __syncthreads();
+  for (int i = 0; i < wv; ++i) v += part[i];
+  return v;
+}
+
+template <typename T> __device__ __forceinline__ float value(T v);
+template <> __device__ __forceinline__ float value<float>(float v) { return v == v ? v + 0.f : -INFINITY; }       // (-0 is 0, NaN is never drawn)
+template <> __device__ __forceinline__ float value<bf16_t>(bf16_t v) { return value<float>(bf16_to_f32(v)); }
+
+// eight tokens of a lane: an instruction of the wave reads consecutive bytes
+template <typename T> __device__ __forceinline__ int token_of(int seg, int lane, int e) {
+  return sizeof(T) == 4 ? seg * kSeg + 256 * (e >> 2) + 4 * lane + (e & 3) : seg * kSeg + 8 * lane + e;
+}
+template <typename T> __device__ __forceinline__ void load_seg(const T* row, int V, int seg, float (&x)[8]) {
+  const int lane = threadIdx.x & 63;
+  T raw[8];
+  if ((seg + 1) * kSeg <= V) {
+    // (as bytes: a row may begin at any element)
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) __builtin_memcpy(raw + i * (16 / sizeof(T)), row + token_of<T>(seg, lane, i * (16 / static_cast<int>(sizeof(T)))), 16);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = value<T>(raw[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int i = token_of<T>(seg, lane, e);
+      x[e] = i < V ? value<T>(row[i]) : -INFINITY;
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------ 1: histograms
+
+template <typename T>
+__global__ __launch_bounds__(kT) void k_sample_bins(const SampleArgs a) {
+  __shared__ unsigned long long hist[kBins];
+  __shared__ float best[kWaves];
+  const int row = blockIdx.y, chunk = blockIdx.x, lane = threadIdx.x & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const T* logits = static_cast<const T*>(a.logits) + static_cast<int64_t>(row) * a.ld;
+  const int seg0 = chunk * a.chunk_segs, seg1 = min(seg0 + a.chunk_segs, a.segs);
+  constexpr int N = kChunkSegs / kWaves;
+  float x[N][8], top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int seg = seg0 + wv + i * kWaves;
+    if (seg < seg1) {
+      load_seg<T>(logits, a.V, seg, x[i]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[i][e] = -INFINITY;
+    }
+  }
+  const Setting st = setting_of(a, row);
+  for (int j = threadIdx.x; j < kBins; j += kT) hist[j] = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, x[i][e]);
+  top = wave_max_dpp(top);
+  if (lane == 0) best[wv] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, best[w]);
+  const int origin = bin_of(top, st.s);
+  if (top > -INFINITY) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (seg0 + wv + i * kWaves >= seg1) break;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float l = x[i][e];
+        const int g = bin_of(l, st.s), j = origin - g;
+        if (l > -INFINITY && j < kBins) {
+          // how far below the bin's upper edge, in bins: the product's rounding error counts as well
+          const float prod = l * st.s;
+          const float below = fminf(fmaxf((static_cast<float>(g) - prod) + 1.f - fmaf(l, st.s, -prod), 0.f), 1.f);
+          const uint32_t part = static_cast<uint32_t>(exp2f(below * (-1.44269504f / kPerNat)) * 16777216.f);
+          atomicAdd(&hist[j], (1ull << kCountBit) + part);
+        }
+      }
+    }
+  }
+  __syncthreads();
+  const size_t at = static_cast<size_t>(row) * a.chunks + chunk;
+  for (int j = threadIdx.x; j < kBins; j += kT) a.hist[at * kBins + j] = hist[j];
+  if (threadIdx.x == 0) {
+    a.chunk_top[at] = top;
+    if (chunk == 0) a.row_info[row].listed = 0;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------ 2: masses and the list
+
+template <typename T>
+__global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
+  __shared__ int cnt_part[kWaves], found[4], n_list, base_list;
+  __shared__ double mass_part[kWaves];
+  __shared__ unsigned long long sums[2];
+  __shared__ uint64_t list[kListPart];
+  const int row = blockIdx.y, chunk = blockIdx.x, lane = threadIdx.x & 63, tid = threadIdx.x;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Setting st = setting_of(a, row);
+  const size_t first = static_cast<size_t>(row) * a.chunks;
+  // ---- the row's best logit and its histogram: thread j has bin j
+  float top = -INFINITY;
+  for (int c = 0; c < a.chunks; ++c) top = fmaxf(top, a.chunk_top[first + c]);
+  const int origin = bin_of(top, st.s);
+  uint64_t h = 0;
+  for (int c = 0; c < a.chunks; ++c) {
+    const float t = a.chunk_top[first + c];
+    const int i = tid - (origin - bin_of(t, st.s));         // (0 .. 2^31 apart)
+    if (t > -INFINITY && i >= 0) h += a.hist[(first + c) * kBins + i];
+  }
+  const int count = static_cast<int>(h >> kCountBit);
+  const double mass = static_cast<double>(h & ((1ull << kCountBit) - 1)) * static_cast<double>(exp2f(static_cast<float>(tid) * (-1.44269504f / kPerNat)));
+  int cum = wave_scan(count);
+  double cmass = mass;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double up = __shfl_up(cmass, o, 64);
+    if (lane >= o) cmass += up;
+  }
+  if (lane == 63) { cnt_part[wv] = cum; mass_part[wv] = cmass; }
+  if (tid < 4) found[tid] = kBins - 1;
+  if (tid == 0) n_list = 0;
+  if (tid < 2) sums[tid] = 0;
+  __syncthreads();
+  double all = 0.0;
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wv) { cum += cnt_part[w]; cmass += mass_part[w]; }
+    all += mass_part[w];
+  }
+  // the bins of the borders: the first whose sum reaches them; of top-p those that 1e-5 more or less could make it (a bin's mass is
+  // known to some 2e-6: T in 32 bits, one rounding of the exponential)
+  const double lo_at = st.p * all * (1.0 - 1e-5), hi_at = st.p * all * (1.0 + 1e-5);
+  if (st.k > 0 && cum >= st.k && cum - count < st.k) found[0] = tid;
+  if (cmass >= lo_at) atomicMin(&found[1], tid);
+  if (cmass >= hi_at) atomicMin(&found[2], tid);
+  __syncthreads();
+  int mode = top == -INFINITY ? kModeEmpty : origin >= kFar || origin <= -kFar ? kModeScan : st.k > 0 ? kModeTopK : st.p < 1.0 ? kModeTopP : kModeAll;
+  const int lo = mode == kModeAll ? kFar : mode == kModeTopP ? found[1] : 0;            // bins in front of it are kept
+  const int hi = mode == kModeTopK ? found[0] : mode == kModeTopP ? max(found[1], found[2]) : -1;     // from lo to it: in doubt
+  if (chunk == 0 && tid == 0) {
+    SampleRow& r = a.row_info[row];
+    r.mode = mode;
+    r.lo = lo;
+    r.hi = hi;
+    r.top = top;
+  }
+  if (mode == kModeEmpty || mode == kModeScan) return;       // uniform
+  // ---- the chunk's tokens
+  const T* logits = static_cast<const T*>(a.logits) + static_cast<int64_t>(row) * a.ld;
+  const int seg0 = chunk * a.chunk_segs, seg1 = min(seg0 + a.chunk_segs, a.segs);
+  uint64_t total = 0, above = 0;
+  for (int seg = seg0 + wv; seg < seg1; seg += kWaves) {
+    float x[8];
+    load_seg<T>(logits, a.V, seg, x);
+    uint64_t kept = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int j = origin - bin_of(x[e], st.s);
+      bool doubt = false;
+      if (mode != kModeTopK || j <= hi) {
+        const double w = weight(x[e], top, st.c);
+        const uint64_t f = fixed(w);
+        total += f;
+        if (j < lo) {
+          above += f;
+          if (w >= st.m) kept += f;
+        }
+        doubt = j >= lo && j <= hi && w > 0.0;
+      }
+      if (__builtin_amdgcn_ballot_w64(doubt) != 0ull) {
+        if (doubt) {
+          const int at = atomicAdd(&n_list, 1);
+          if (at < kListPart) list[at] = place_of(x[e], token_of<T>(seg, lane, e));
+        }
+      }
+    }
+    if (mode != kModeTopK) {
+      kept = wave_sum64(kept);
+      if (lane == 0) a.seg_mass[static_cast<size_t>(row) * a.segs + seg] = kept;
+    }
+  }
+  if (mode == kModeTopP) {
+    total = wave_sum64(total);
+    above = wave_sum64(above);
+    if (lane == 0) {
+      atomicAdd(&sums[0], total);
+      atomicAdd(&sums[1], above);
+    }
+  }
+  __syncthreads();
+  if (tid == 0) {
+    a.chunk_sums[2 * (first + chunk)] = sums[0];
+    a.chunk_sums[2 * (first + chunk) + 1] = sums[1];
+    // (a list that does not fit is counted as too long, and the last kernel does without it)
+    base_list = n_list > 0 ? atomicAdd(&a.row_info[row].listed, n_list <= kListPart ? n_list : kList + 1) : 0;
+  }
+  __syncthreads();
+  if (n_list <= kListPart)
+    for (int i = tid; i < n_list; i += kT)
+      if (base_list + i < kList) a.list[static_cast<size_t>(row) * kList + base_list + i] = list[i];
+}
+
+// ------------------------------------------------------------------------------------------------------------ 3: the draw
+
+struct PickLds {
+  uint64_t list[kList];
+  uint64_t pre[kList];               // the sorted list's weights, then their inclusive sums
+  uint64_t seg[kSampleMaxSegs];
+  uint64_t part[kWaves], part2[kWaves];
+  unsigned long long digit_mass[256], wide;
+  uint32_t digit_count[256];
+  int count[kSampleMaxSegs];
+  int keep, pick, seg_at;
+  uint64_t seg_before;
+  // scan's results
+  uint32_t key;
+  int n_equal;
+  uint32_t before;
+  uint64_t mass_before;
+};
+
+// The token at the end of the best `want` ones (by count), or of those whose better ones sum to less than `target`: its key, how many of its equals belong to them, and
+// their mass.  Radix selection over the whole row, eight bits at a time.  The workgroup's threads all get the results.
+struct Border {
+  uint32_t key;
+  int equal;             // equals that are kept
+  uint64_t mass;         // of everything kept
+};
+template <typename T>
+__device__ Border scan_border(const SampleArgs& a, const T* logits, const Setting& st, float top, PickLds& s, int want, double target) {
+  const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  uint32_t prefix = 0, before = 0;
+  uint64_t mass_before = 0;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    if (tid < 256) { s.digit_mass[tid] = 0; s.digit_count[tid] = 0; }
+    __syncthreads();
+    for (int seg = wv; seg < a.segs; seg += kWaves) {
+      float x[8];
+      load_seg<T>(logits, a.V, seg, x);
+#pragma unroll 1
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t key = key_of(x[e]);
+        if (shift < 24 && key >> (shift + 8) != prefix) continue;
+        const double w = weight(x[e], top, st.c);
+        if (w > 0.0) {
+          const uint32_t d = key >> shift & 255u;
+          atomicAdd(&s.digit_count[d], 1u);
+          atomicAdd(&s.digit_mass[d], static_cast<unsigned long long>(fixed(w)));
+        }
+      }
+    }
+    __syncthreads();
+    if (tid == 0) {
+      int last = -1;                   // the lowest digit there is, if the border is not reached
+      int at = -1;
+      uint32_t n = before;
+      uint64_t m = mass_before;
+      for (int d = 255; d >= 0 && at < 0; --d) {
+        if (s.digit_count[d] == 0) continue;
+        last = d;
+        if (want > 0 ? n + s.digit_count[d] >= static_cast<uint32_t>(want) : static_cast<double>(m + s.digit_mass[d]) >= target) at = d;
+        else { n += s.digit_count[d]; m += s.digit_mass[d]; }
+      }
+      if (at < 0 && last >= 0) { at = last; n -= s.digit_count[last]; m -= s.digit_mass[last]; }
+      at = max(at, 0);
+      s.key = prefix << 8 | static_cast<uint32_t>(at);
+      s.n_equal = static_cast<int>(s.digit_count[at]);
+      s.before = n;
+      s.mass_before = m;
+    }
+    __syncthreads();
+    prefix = s.key;
+    before = s.before;
+    mass_before = s.mass_before;
+  }
+  const uint64_t w = fixed(weight(logit_of(prefix), top, st.c));
+  int c = s.n_equal;
+  if (want > 0) {
+    c = min(c, want - static_cast<int>(before));
+  } else if (w > 0) {
+    // equal j of them is kept where mass_before + j w < target
+    const double room = (target - static_cast<double>(mass_before)) / static_cast<double>(w);
+    int n = room < static_cast<double>(c) ? max(static_cast<int>(ceil(room)), 0) : c;
+    if (n > 0 && !(static_cast<double>(mass_before + static_cast<uint64_t>(n - 1) * w) < target)) --n;
+    else if (n < c && static_cast<double>(mass_before + static_cast<uint64_t>(n) * w) < target) ++n;
+    c = n;
+  }
+  __syncthreads();
+  return {prefix, c, mass_before + static_cast<uint64_t>(c) * w};
+}
+
+template <typename T>
+__global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
+  extern __shared__ uint4 smem4[];
+  PickLds& s = *reinterpret_cast<PickLds*>(smem4);
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const SampleRow info = a.row_info[row];
+  const Setting st = setting_of(a, row);
+  const T* logits = static_cast<const T*>(a.logits) + static_cast<int64_t>(row) * a.ld;
+  const float top = info.top;
+  if (info.mode == kModeEmpty) {                  // uniform
+    if (tid == 0) {
+      a.token[row] = -1;
+      if (a.prob) a.prob[row] = 0.f;
+    }
+    return;
+  }
+  const int origin = bin_of(top, st.s);
+  int lo = info.lo, hi = info.hi;                 // kept: bins in front of lo, and to hi where the place is not behind `cut`
+  uint64_t cut = ~0ull;
+  const bool listed = info.mode == kModeTopK || info.mode == kModeTopP;
+  const int n = listed ? info.listed : 0;
+  if (info.mode == kModeScan || n > kList) {
+    // ---- without histograms and list: a row whose logits are far from anything (2^26 nats), or whose list is too long, as where more than 4096 tokens
+    // of nearly one weight lie at the border
+    lo = 0;
+    hi = INT_MAX;
+    if (st.k > 0 || st.p < 1.0) {
+      Border b = {0, 0, 0};
+      if (st.k > 0) b = scan_border<T>(a, logits, st, top, s, st.k, 0.0);
+      if (st.p < 1.0) {
+        double of = static_cast<double>(b.mass);
+        if (st.k <= 0) {
+          if (tid == 0) s.wide = 0;
+          __syncthreads();
+          uint64_t mine = 0;
+          for (int seg = wv; seg < a.segs; seg += kWaves) {
+            float x[8];
+            load_seg<T>(logits, a.V, seg, x);
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) mine += fixed(weight(x[e], top, st.c));
+          }
+          mine = wave_sum64(mine);
+          if (lane == 0) atomicAdd(&s.wide, static_cast<unsigned long long>(mine));
+          __syncthreads();
+          of = static_cast<double>(s.wide);
+        }
+        const Border q = scan_border<T>(a, logits, st, top, s, 0, st.p * of);
+        const bool equal = st.k > 0 && q.key == b.key;
+        b = {q.key, max(equal ? min(q.equal, b.equal) : q.equal, 1), 0};
+      }
+      // the last of the kept equals, in index order: equals per segment, then in the segment that has it
+      for (int seg = wv; seg < a.segs; seg += kWaves) {
+        float x[8];
+        load_seg<T>(logits, a.V, seg, x);
+        int eq = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) eq += __popcll(__builtin_amdgcn_ballot_w64(x[e] > -INFINITY && key_of(x[e]) == b.key));
+        if (lane == 0) s.count[seg] = eq;
+      }
+      __syncthreads();
+      if (wv == 0) {
+        int left = b.equal, seg = 0;
+        while (seg < a.segs - 1 && left > s.count[seg]) left -= s.count[seg++];          // (uniform)
+        int last = INT_MAX;
+        for (int r = 0; r < kSeg / 64; ++r) {
+          const int i = seg * kSeg + r * 64 + lane;
+          const float l = i < a.V ? value<T>(logits[i]) : -INFINITY;
+          uint64_t eq = __builtin_amdgcn_ballot_w64(l > -INFINITY && key_of(l) == b.key);
+          const int c = __popcll(eq);
+          if (left > 0 && left <= c) {
+            for (int q = 1; q < left; ++q) eq &= eq - 1;
+            last = seg * kSeg + r * 64 + __ffsll(static_cast<unsigned long long>(eq)) - 1;
+          }
+          left -= c;
+        }
+        if (lane == 0) s.pick = last;
+      }
+      __syncthreads();
+      cut = static_cast<uint64_t>(~b.key) << 32 | static_cast<uint32_t>(s.pick);
+    }
+    for (int seg = wv; seg < a.segs; seg += kWaves) {
+      float x[8];
+      load_seg<T>(logits, a.V, seg, x);
+      uint64_t kept = 0;
+#pragma unroll 1
+      for (int e = 0; e < 8; ++e) {
+        const double w = weight(x[e], top, st.c);
+        if (w >= st.m && place_of(x[e], token_of<T>(seg, lane, e)) <= cut) kept += fixed(w);
+      }
+      kept = wave_sum64(kept);
+      if (lane == 0) s.seg[seg] = kept;
+    }
+    for (int i = a.segs + tid; i < kSampleMaxSegs; i += kT) s.seg[i] = 0;
+    __syncthreads();
+  } else {
+    // ---- the list, sorted by place
+    for (int i = tid; i < kSampleMaxSegs; i += kT) s.seg[i] = i < a.segs && info.mode != kModeTopK ? a.seg_mass[static_cast<size_t>(row) * a.segs + i] : 0;
+    if (listed) {
+      uint64_t total = 0, above = 0;
+      if (info.mode == kModeTopP) {
+        for (int c = 0; c < a.chunks; ++c) {
+          total += a.chunk_sums[2 * (static_cast<size_t>(row) * a.chunks + c)];
+          above += a.chunk_sums[2 * (static_cast<size_t>(row) * a.chunks + c) + 1];
+        }
+      }
+      int n2 = 64;
+      while (n2 < n) n2 *= 2;
+      for (int i = tid; i < n2; i += kT) s.list[i] = i < n ? a.list[static_cast<size_t>(row) * kList + i] : ~0ull;
+      if (tid == 0) s.keep = 0;
+      __syncthreads();
+      for (int size = 2; size <= n2; size *= 2)
+        for (int step = size / 2; step > 0; step /= 2) {
+          for (int i = tid; i < n2 / 2; i += kT) {
+            const int at = 2 * i - (i & (step - 1)), to = at + step;
+            const uint64_t x = s.list[at], y = s.list[to];
+            if ((x > y) == ((at & size) == 0)) { s.list[at] = y; s.list[to] = x; }
+          }
+          __syncthreads();
+        }
+      // weights and their inclusive sums: a thread has `per` neighbours
+      const int per = (n2 + kT - 1) / kT;
+      uint64_t own = 0;
+      for (int i = tid * per; i < min((tid + 1) * per, n2); ++i) {
+        own += i < n ? fixed(weight(logit_of(~static_cast<uint32_t>(s.list[i] >> 32)), top, st.c)) : 0;
+        s.pre[i] = own;
+      }
+      const uint64_t upto = block_scan64(own, s.part);
+      for (int i = tid * per; i < min((tid + 1) * per, n2); ++i) s.pre[i] += upto - own;
+      __syncthreads();
+      const int most = info.mode == kModeTopK ? min(st.k, n) : n;
+      const double target = st.p * static_cast<double>(info.mode == kModeTopK ? (most > 0 ? s.pre[most - 1] : 0) : total);
+      for (int i = tid; i < most; i += kT) {
+        const uint64_t better = above + (i > 0 ? s.pre[i - 1] : 0);
+        if (st.p >= 1.0 || static_cast<double>(better) < target || (i == 0 && above == 0)) atomicMax(&s.keep, i + 1);
+      }
+      __syncthreads();
+      const int keep = s.keep;
+      cut = keep > 0 ? s.list[keep - 1] : 0ull;
+      for (int i = tid; i < keep; i += kT) {
+        const double w = weight(logit_of(~static_cast<uint32_t>(s.list[i] >> 32)), top, st.c);
+        if (w >= st.m) atomicAdd(reinterpret_cast<unsigned long long*>(&s.seg[static_cast<uint32_t>(s.list[i]) / kSeg]), static_cast<unsigned long long>(fixed(w)));
+      }
+    }
+    __syncthreads();
+  }
+  // ---- the segment: the first whose sum is above u times all of it
+  static_assert(kSampleMaxSegs == kT && kSeg == kT, "a thread per segment, a thread per token of a segment");
+  if (tid == 0) {
+    s.pick = INT_MAX;
+    s.seg_at = 0;
+    s.seg_before = 0;
+  }
+  const uint64_t mass = s.seg[tid], upto = block_scan64(mass, s.part);
+  uint64_t all = 0;
+  for (int w = 0; w < kWaves; ++w) all += s.part[w];
+  float u = a.u[row];
+  if (!(u >= 0.f)) u = 0.f;
+  u = fminf(u, 0.99999994f);
+  uint64_t x = static_cast<uint64_t>(static_cast<double>(all) * static_cast<double>(u));
+  if (x >= all) x = all > 0 ? all - 1 : 0;
+  if (upto > x && upto - mass <= x) {
+    s.seg_at = tid;
+    s.seg_before = upto - mass;
+  }
+  __syncthreads();
+  const int idx = s.seg_at * kSeg + tid;
+  const float l = idx < a.V ? value<T>(logits[idx]) : -INFINITY;
+  const double w = weight(l, top, st.c);
+  const int j = origin - bin_of(l, st.s);
+  const bool kept = w >= st.m && (j < lo || (j <= hi && place_of(l, idx) <= cut));
+  const uint64_t sum = s.seg_before + block_scan64(kept ? fixed(w) : 0, s.part2);
+  if (kept && sum > x) atomicMin(&s.pick, tid);
+  __syncthreads();
+  if (tid == s.pick || (tid == 0 && s.pick == INT_MAX)) {
+    a.token[row] = s.pick == INT_MAX ? -1 : idx;
+    if (a.prob) a.prob[row] = s.pick == INT_MAX ? 0.f : static_cast<float>(w * kFix / static_cast<double>(all));
+  }
+}
+
+template <typename T> hipError_t launch_as(const SampleArgs& a, hipStream_t s) {
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_sample_pick<T>), hipFuncAttributeMaxDynamicSharedMemorySize, sizeof(PickLds));
+  if (attr != hipSuccess) return attr;
+  hipLaunchKernelGGL((k_sample_bins<T>), dim3(a.chunks, a.M), dim3(kT), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((k_sample_mass<T>), dim3(a.chunks, a.M), dim3(kT), 0, s, a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((k_sample_pick<T>), dim3(a.M), dim3(kT), sizeof(PickLds), s, a);
+  return hipGetLastError();
+}
+
+size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
+
+}  // namespace
+
+void sample_plan(SampleArgs& a) {
+  a.segs = (a.V + kSeg - 1) / kSeg;
+  // two workgroups per compute unit where the rows are few, no more than twenty to a row: each of the second kernel's reads the histograms of all
+  int chunks = (512 + a.M - 1) / a.M;
+  if (chunks > 20) chunks = 20;
+  if (chunks > (a.segs + kWaves - 1) / kWaves) chunks = (a.segs + kWaves - 1) / kWaves;
+  const int least = (a.segs + kChunkSegs - 1) / kChunkSegs;
+  if (chunks < least) chunks = least;
+  a.chunk_segs = (a.segs + chunks - 1) / chunks;
+  a.chunks = (a.segs + a.chunk_segs - 1) / a.chunk_segs;
+}
+
+// Lays the workspace out (base null: only its size).
+size_t sample_carve(SampleArgs& a, void* base) {
+  char* p = static_cast<char*>(base);
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    char* r = p ? p + off : nullptr;
+    off += align256(bytes);
+    return r;
+  };
+  const size_t M = static_cast<size_t>(a.M), C = static_cast<size_t>(a.chunks);
+  a.hist = reinterpret_cast<unsigned long long*>(take(M * C * kBins * 8));
+  a.chunk_sums = reinterpret_cast<unsigned long long*>(take(M * C * 2 * 8));
+  a.seg_mass = reinterpret_cast<unsigned long long*>(take(M * a.segs * 8));
+  a.list = reinterpret_cast<unsigned long long*>(take(M * kList * 8));
+  a.chunk_top = reinterpret_cast<float*>(take(M * C * 4));
+  a.row_info = reinterpret_cast<SampleRow*>(take(M * sizeof(SampleRow)));
+  return off;
+}
+
+hipError_t launch_sample(const SampleArgs& a, hipStream_t s) { return a.f32 ? launch_as<float>(a, s) : launch_as<bf16_t>(a, s); }
+
+}  // namespace sx
