@@ -34,13 +34,14 @@ typedef float v2f_t __attribute__((ext_vector_type(2)));
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
 typedef __attribute__((address_space(3))) v2i_t* lds_v2i_t;
 
-constexpr int kMaxPages = 2048;      // page ids of a segment kept in LDS (8 KB)
+constexpr int kMaxGroups = 2048;     // groups of 16 keys of a paged segment, whose places in the pool are kept in LDS (8 KB)
 constexpr int kTileKeys = 32;
 constexpr size_t kRingLds = 128 * 1024;
 
 __host__ __device__ constexpr int slot_bytes(int hd) { return 2 * kTileKeys * hd; }    // K codes, then V codes
-__host__ __device__ constexpr int ring_slots(int hd, int nk) { return static_cast<int>(kRingLds) / (nk * slot_bytes(hd)) > 16 ? 16 : static_cast<int>(kRingLds) / (nk * slot_bytes(hd)); }
 constexpr int kScaleSlot = 2 * kTileKeys;        // K scale bytes, then V scale bytes
+// Slots of a ring.
+__host__ __device__ constexpr int ring_slots(int hd, int nk) { return static_cast<int>(kRingLds) / (nk * slot_bytes(hd)) > 8 ? 8 : static_cast<int>(kRingLds) / (nk * slot_bytes(hd)); }
 
 // XOR swizzles of the 16-byte chunks of a tile row, so that the 16 rows (K) or 16 rows x 1 chunk (V) that an instruction reads at once lie on
 // different banks: 128-wide rows are two to the 256 bytes of all banks, 64-wide ones four.
@@ -80,31 +81,31 @@ __device__ __forceinline__ void load_to_lds4(const void* src, const void* lds_ba
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(l), "v"(src) : "memory");
 }
 
-// parts of the queries and of the probabilities
-template <typename T> struct Parts { static constexpr int q = 2, p = 2; };        // bf16: two e4m3 ones and two bf16 ones, 16 bits of a probability
-template <> struct Parts<float> { static constexpr int q = 3, p = 3; };           // fp32: three bf16 ones, all 24 bits of both
+// parts of the queries: bf16 ones in two e4m3 parts, fp32 ones in three bf16 parts
+template <typename T> struct Parts { static constexpr int q = sizeof(T) == 2 ? 2 : 3; };
 
 constexpr int ml_floats(int nk, int rows) { return nk > 1 ? 2 * nk * rows : 0; }
 __host__ __device__ constexpr size_t quant_lds_bytes(int hd, int nk, int rows, int B, bool paged) {
   const size_t s = static_cast<size_t>(nk) * ring_slots(hd, nk);
   return s * slot_bytes(hd) + s * kScaleSlot + static_cast<size_t>(nk > 1 ? 2 * nk * rows : 0) * sizeof(float) + static_cast<size_t>(attn_sched_words(B)) * sizeof(int) +
-         (paged ? static_cast<size_t>(kMaxPages + 1) * sizeof(int) : 0);
+         (paged ? static_cast<size_t>(kMaxGroups) * sizeof(int) : 0);
 }
 
-template <int HD, typename T, int NK, int NR, int RTW>
-__global__ __launch_bounds__(64 * NK * NR, RTW <= 2 ? 2 : (NK * NR + 3) / 4) void k_quant_attn(const QuantAttnArgs a) {
+template <int HD, typename T, int NK, int NR, int RTW, int PP, int KT>
+__global__ __launch_bounds__(64 * NK * NR, NK * NR <= 8 ? 2 : (NK * NR + 3) / 4) void k_quant_attn(const QuantAttnArgs a) {
   constexpr int S = ring_slots(HD, NK);
   constexpr int RP = 16 * NR * RTW;               // query rows covered (padded)
   constexpr int kSlot = slot_bytes(HD);
   constexpr int kChunks = HD / 16;                // 16-byte chunks of a row
   constexpr int kKeysPP = 1024 / HD;              // keys of a 1 KB piece
   constexpr int kTileP = kTileKeys / kKeysPP;     // pieces of a K (or V) tile
-  constexpr int kPieces = 2 * kTileP / NR;        // pieces that a wave requests of a tile
-  static_assert(2 * kTileP % NR == 0, "the waves of a ring share a tile evenly");
+  constexpr int kPieces = (2 * kTileP + NR - 1) / NR;      // pieces that a wave requests of a tile, at most
   static_assert(NK == 1 || NR * RTW <= S, "a ring's slots hold its sums");
-  constexpr int kReq = kPieces + 1;               // requests of a wave per tile
+  static_assert(S >= 2 * KT && S % KT == 0, "a step is requested while the one before it is worked on");
+  constexpr int kVAhead = NK * NR <= 8 ? 8 : 3;       // V reads in front of their use, as many as the registers allow
+  constexpr int kReq = 2 * kTileP / NR + 1;       // requests of a wave per tile, at least
   constexpr bool kCodes = sizeof(T) == 2;         // the keys' codes are multiplied as they are
-  constexpr int NP = Parts<T>::q, PP = Parts<T>::p;
+  constexpr int NP = Parts<T>::q;
   constexpr int NM = HD == 128 ? NP : 1;          // block-scaled matrix instructions for 16 keys x 16 rows
   constexpr int kKS = HD / 32;                    // k steps of bf16 ones
   constexpr int kDT = HD / 16;
@@ -113,12 +114,10 @@ __global__ __launch_bounds__(64 * NK * NR, RTW <= 2 ? 2 : (NK * NR + 3) / 4) voi
   char* scales = smem + NK * S * kSlot;
   float* ml_lds = reinterpret_cast<float*>(scales + NK * S * kScaleSlot);
   int* sched_lds = reinterpret_cast<int*>(ml_lds + ml_floats(NK, RP));
-  int* pg_lds = sched_lds + attn_sched_words(a.B);
-  const int lane = threadIdx.x & 63;
+  uint32_t* group_lds = reinterpret_cast<uint32_t*>(sched_lds + attn_sched_words(a.B));
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kg = wv / NR, rr = wv % NR;
   const int G = a.G, R = G * a.n_q;
-  const int fr = lane & 15, fq = lane >> 4;
   const AttnTable table = attn_sched_build(a, sched_lds);
   const AttnLine line = attn_sched_line(a, table);
   if (static_cast<int>(blockIdx.x) >= line.W) return;   // the whole workgroup leaves together
@@ -128,11 +127,15 @@ __global__ __launch_bounds__(64 * NK * NR, RTW <= 2 ? 2 : (NK * NR + 3) / 4) voi
   if (seg.next < x_hi) attn_sched_keep(a, table);
   for (; seg.s1 > seg.s0; seg = attn_sched_next(a, table, false, line.pad, seg.next, x_hi)) {
   attn_sched_publish(a, seg);
+  // (what follows from the lane is worked out anew for every segment, and for its end: held through the tiles it is registers)
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));
+  const int fr = lane & 15, fq = lane >> 4;
   const int g = seg.g, b = seg.b;
   const int L = __builtin_amdgcn_readfirstlane(seg.L);
   const int s0 = seg.s0, s1 = __builtin_amdgcn_readfirstlane(seg.s1);
   const int ntl = (s1 - s0 + kTileKeys - 1) / kTileKeys;   // tiles of the segment
-  const int nit = (ntl + NK - 1) / NK;            // tile steps (the same for all rings)
+  const int nit = (ntl + NK - 1) / NK;            // tiles of every ring, at most
   const int mine = (ntl - kg + NK - 1) / NK;      // tiles of this ring
   char* ring = smem + kg * (S * kSlot);
   char* ring_s = scales + kg * (S * kScaleSlot);
@@ -162,67 +165,73 @@ __global__ __launch_bounds__(64 * NK * NR, RTW <= 2 ? 2 : (NK * NR + 3) / 4) voi
     rowmask[t] = a.mask ? a.mask[static_cast<size_t>(b) * a.mask_stride + i] : ((2ull << i) - 1ull);
   }
 
-  // ---- page ids of the segment to LDS: loads from there do not count against the vector-memory counter that paces the tile loads
-  const int ps = a.page_size;
-  auto page_of = [&](int p) { return a.page_shift >= 0 ? p >> a.page_shift : static_cast<int>(static_cast<uint32_t>(p) / static_cast<uint32_t>(ps)); };
-  int pg0 = 0;
+  // ---- the places of the segment's groups of 16 keys to LDS, in units of 16 rows of the pool (a page is a multiple of 16 entries): loads from there
+  // do not count against the vector-memory counter that paces the tile loads, and a wave needs no multiplication for a request.
+  const uint32_t group0 = static_cast<uint32_t>(s0) >> 4;
   if (a.paged) {
-    pg0 = page_of(s0);
-    const int npg = page_of(s1 - 1) - pg0 + 1;
-    const int32_t* ptab = a.page_table + static_cast<size_t>(b) * a.max_pages + pg0;
-    for (int i = threadIdx.x; i < npg; i += 64 * NK * NR) pg_lds[i] = checked_page(ptab[i], a.n_pages, a.status);
+    const uint32_t per = static_cast<uint32_t>(a.page_size) >> 4;           // groups of a page
+    const int ng = (s1 - s0 + 15) >> 4;
+    const int32_t* ptab = a.page_table + static_cast<size_t>(b) * a.max_pages;
+    for (int i = threadIdx.x; i < ng; i += 64 * NK * NR) {
+      const uint32_t at = group0 + i, n = a.page_shift >= 0 ? at >> (a.page_shift - 4) : at / per;
+      group_lds[i] = (static_cast<uint32_t>(checked_page(ptab[n], a.n_pages, a.status)) * static_cast<uint32_t>(a.Hkv) + g) * per + (at - n * per);
+    }
   }
-  if (a.paged || again) __syncthreads();          // the page ids are there, and the rings are free of the segment before
+  if (a.paged || again) __syncthreads();          // the groups are there, and the rings are free of the segment before
   again = true;
 
-  // ---- tile requests.  A tile is two halves of 16 keys, each within one page; piece j holds kKeysPP keys from kKeysPP (j % kTileP) on, lane l
-  // fetches key l / kChunks of them, chunk (l % kChunks) ^ swizzle(key).
+  // ---- requests of a tile.  Piece j holds kKeysPP keys from kKeysPP (j % kTileP) on (K, then V), lane l fetches key l / kChunks of them, chunk
+  // (l % kChunks) ^ swizzle(key).  A wave has the same pieces of every tile; of an address only the group's place is new.
   const int lkey = lane / kChunks, lpos = lane % kChunks;
+  uint64_t k_pool = reinterpret_cast<uint64_t>(a.k), v_pool = reinterpret_cast<uint64_t>(a.v), ks_pool = reinterpret_cast<uint64_t>(a.ks), vs_pool = reinterpret_cast<uint64_t>(a.vs);
   // (selected as values: left alone the compiler selects the arguments' addresses and loads through them for every tile, which waits for all
   // requests in flight)
-  uint64_t ks_at = reinterpret_cast<uint64_t>(a.ks), vs_at = reinterpret_cast<uint64_t>(a.vs);
-  asm volatile("" : "+s"(ks_at), "+s"(vs_at));
-  const char* const scale_pool = reinterpret_cast<const char*>(lane < 8 ? ks_at : vs_at) + 4 * (lane & 3);
-  const int64_t seq_row = (static_cast<int64_t>(b) * a.Hkv + g) * a.l_max;
-  auto row_of = [&](int p) -> int64_t {           // entry p of the unit, uniform
-    if (!a.paged) return seq_row + p;
-    const int n = page_of(p);
-    const int page = __builtin_amdgcn_readfirstlane(pg_lds[n - pg0]);
-    return (static_cast<int64_t>(page) * a.Hkv + g) * ps + (p - n * ps);
-  };
+  asm volatile("" : "+s"(k_pool), "+s"(v_pool), "+s"(ks_pool), "+s"(vs_pool));
+  uint64_t piece_at[kPieces];
+#pragma unroll
+  for (int u = 0; u < kPieces; ++u) {
+    const int j = rr + u * NR, key = kKeysPP * (j & (kTileP - 1)) + lkey;
+    const bool is_v = j >= kTileP;
+    piece_at[u] = (is_v ? v_pool : k_pool) + ((key & 15) * HD + ((lpos ^ (is_v ? swz_v<HD>(key) : swz_k<HD>(key))) << 4));
+  }
+  // scale bytes: lanes 0..7 four keys' K scales each, lanes 8..15 V scales
+  const uint64_t scale_at = (lane & 8 ? vs_pool : ks_pool) + 4 * (lane & 3);
+  const uint32_t unit_group = static_cast<uint32_t>((static_cast<uint64_t>(b) * a.Hkv + g) * static_cast<uint64_t>(a.l_max) >> 4) + group0;      // (contiguous)
   auto issue = [&](int it) {
     if (it >= mine) return;                       // uniform per wave
-    const int t0 = s0 + kTileKeys * (it * NK + kg);
+    const int first = kTileKeys * (it * NK + kg); // the tile's first key in the segment
+    const int n = s1 - s0 - first;                // keys from there to the end
+    uint32_t g0, g1;                              // places of the tile's two groups
+    if (a.paged) {
+      g0 = group_lds[first >> 4];
+      g1 = group_lds[(first >> 4) + (n > 16 ? 1 : 0)];
+    } else {
+      g0 = unit_group + (first >> 4);
+      g1 = g0 + (n > 16 ? 1 : 0);
+    }
     char* slot = ring + (it % S) * kSlot;
-    const int n = s1 - t0;                        // keys from here to the end of the segment
-    const int64_t r0 = row_of(t0);
-    const int64_t r1 = n > 16 ? row_of(t0 + 16) : r0;
     if (n >= kTileKeys) {
 #pragma unroll
       for (int u = 0; u < kPieces; ++u) {
-        const int j = rr * kPieces + u;
-        const int key = kKeysPP * (j & (kTileP - 1));          // the piece's first key
-        const int64_t row = (key & 16 ? r1 : r0) + (key & 15);
-        const bool is_v = j >= kTileP;
-        const int chunk = lpos ^ (is_v ? swz_v<HD>(key + lkey) : swz_k<HD>(key + lkey));
-        load_to_lds16(static_cast<const char*>(is_v ? a.v : a.k) + row * HD, static_cast<uint32_t>(lkey * HD + (chunk << 4)), slot + j * 1024);
+        const int j = rr + u * NR;
+        if (2 * kTileP % NR != 0 && j >= 2 * kTileP) break;
+        const uint32_t at = kKeysPP * (j & (kTileP - 1)) & 16 ? g1 : g0;
+        load_to_lds16(reinterpret_cast<const void*>(piece_at[u] + static_cast<uint64_t>(at) * (16 * HD)), slot + j * 1024);
       }
     } else {
+      // keys past the range repeat the last one and are masked
 #pragma unroll
       for (int u = 0; u < kPieces; ++u) {
-        const int j = rr * kPieces + u;
-        const int key = kKeysPP * (j & (kTileP - 1)) + lkey;
-        const int at = min(key, n - 1);                        // keys past the range repeat the last one and are masked
-        const int64_t row = (at & 16 ? r1 : r0) + (at & 15);
+        const int j = rr + u * NR;
+        if (2 * kTileP % NR != 0 && j >= 2 * kTileP) break;
+        const int key = kKeysPP * (j & (kTileP - 1)) + lkey, to = min(key, n - 1);
         const bool is_v = j >= kTileP;
-        load_to_lds16(static_cast<const char*>(is_v ? a.v : a.k) + row * HD + ((lpos ^ (is_v ? swz_v<HD>(key) : swz_k<HD>(key))) << 4), slot + j * 1024);
+        const uint64_t at = (is_v ? v_pool : k_pool) + static_cast<uint64_t>(to & 16 ? g1 : g0) * (16 * HD) + (to & 15) * HD + ((lpos ^ (is_v ? swz_v<HD>(key) : swz_k<HD>(key))) << 4);
+        load_to_lds16(reinterpret_cast<const void*>(at), slot + j * 1024);
       }
     }
-    // scale bytes: lanes 0..7 four keys' K scales each, lanes 8..15 V scales (the entries behind the last one are inside the cache: pages and
-    // contiguous caches are multiples of 16 entries)
-    if (lane < 16) {
-      load_to_lds4(scale_pool + (lane & 4 ? r1 : r0), ring_s + (it % S) * kScaleSlot);
-    }
+    // (the bytes behind the last entry are inside the cache: pages and contiguous caches are multiples of 16 entries)
+    if (lane < 16) load_to_lds4(reinterpret_cast<const void*>(scale_at + (static_cast<uint64_t>(lane & 4 ? g1 : g0) << 4)), ring_s + (it % S) * kScaleSlot);
   };
 
   f32x4_t oacc[kDT][RTW];
@@ -284,56 +293,88 @@ __global__ __launch_bounds__(64 * NK * NR, RTW <= 2 ? 2 : (NK * NR + 3) / 4) voi
   }
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));       // from here on vmcnt counts tile requests only
 #pragma unroll 1
-  for (int it = 0; it < S - 1; ++it) issue(it);
+  for (int it = 0; it < S - KT; ++it) issue(it);
 
   // a lane's part of the operand addresses
-  const int k_row = fr * HD, k_chunk = fq ^ swz_k<HD>(fr);      // (swz_k(16 + key) == swz_k(key) for 128-wide and 64-wide heads)
+  // (one for K and one for V, a read is the exclusive or with its number: held in registers they are a dozen)
+  int k_at = fr * HD + (kCodes ? (fq ^ swz_k<HD>(fr)) << 4 : (((fq >> 1) ^ swz_k<HD>(fr)) << 4) + (fq & 1) * 8);
   const int v_key = (fr >> 1) < 4 ? 4 * fq + (fr >> 1) : 16 + 4 * fq + (fr >> 1) - 4;
-  const int v_at = v_key * HD + (fr & 1) * 8, v_swz = swz_v<HD>(v_key);
+  int v_at = v_key * HD + (fr & 1) * 8 + (swz_v<HD>(v_key) << 4);
 
-#pragma unroll 1
-  for (int it = 0; it < nit; ++it) {
-    // this wave's pieces of tile `it` have landed once at most those of the tiles behind it are outstanding (loads return in order)
-    wait_tiles<kReq, S - 2>(min(it + S - 2, mine - 1) - it);
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    if constexpr (NR > 1) __builtin_amdgcn_s_barrier();         // tile `it` complete; slot of tile it - 1 free
-    else __builtin_amdgcn_s_waitcnt(0xC07F);                    // lgkmcnt(0): tile it - 1 is read
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    issue(it + S - 1);
-    if (it >= mine) continue;
-    const int t0 = s0 + kTileKeys * (it * NK + kg);
+  uint4 kreg[2][HD / 64];
+  int ksc[2];
+  v2i_t vreg[kDT];
+  uint32_t ksw[2], vsw[2];
+  auto read_k = [&](int it) {
     const char* k_lds = ring + (it % S) * kSlot;
-    const char* v_lds = k_lds + kSlot / 2;
     const char* s_lds = ring_s + (it % S) * kScaleSlot;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if constexpr (kCodes) {
+        // chunks q and, of 128-wide heads, q + 4 of key 16 j + row   (swz_k(16 + key) == swz_k(key))
+#pragma unroll
+        for (int c = 0; c < HD / 64; ++c) kreg[j][c] = *reinterpret_cast<const uint4*>(k_lds + (k_at ^ (c << 6)) + j * 16 * HD);
+        ksc[j] = *reinterpret_cast<const uint8_t*>(s_lds + 16 * j + fr);
+      } else {
+        // eight codes of every k step
+#pragma unroll
+        for (int s = 0; s < kKS; ++s) {
+          const uint2 c = *reinterpret_cast<const uint2*>(k_lds + (k_at ^ (s << 5)) + j * 16 * HD);
+          if (s & 1) { kreg[j][s >> 1].z = c.x; kreg[j][s >> 1].w = c.y; }
+          else { kreg[j][s >> 1].x = c.x; kreg[j][s >> 1].y = c.y; }
+        }
+        ksw[j] = *reinterpret_cast<const uint32_t*>(s_lds + 16 * j + 4 * fq);
+      }
+    }
+  };
+  auto read_v = [&](int it, int dt) {
+    vreg[dt] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i_t)(lds_ptr_t)(ring + (it % S) * kSlot + kSlot / 2 + (v_at ^ (dt << 4))));
+  };
+  auto read_vs = [&](int it) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) vsw[j] = *reinterpret_cast<const uint32_t*>(ring_s + (it % S) * kScaleSlot + kTileKeys + 16 * j + 4 * fq);
+  };
+#pragma unroll 1
+  for (int it0 = 0; it0 < nit; it0 += KT) {
+    // this wave's pieces of the KT tiles from it0 on have landed once at most those of the tiles requested behind them are outstanding (loads
+    // return in order); behind the barrier everyone's have, and the slots of the KT tiles before are free
+    wait_tiles<kReq, S - 2 * KT>(min(it0 + S - KT, mine) - (it0 + KT));
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    if constexpr (NR > 1) __builtin_amdgcn_s_barrier();
+    else __builtin_amdgcn_s_waitcnt(0xC07F);      // lgkmcnt(0): of one wave, the tiles before are read
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll 1
+    for (int k = 0; k < KT; ++k) issue(it0 + S - KT + k);
+#pragma unroll 1
+    for (int it = it0; it < min(it0 + KT, mine); ++it) {
+    read_k(it);
+    read_vs(it);
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" : "+v"(k_at), "+v"(v_at));
+    const int t0 = s0 + kTileKeys * (it * NK + kg);
 
     // ---- S^T = K Q^T, both halves of 16 keys
-    const uint32_t vs0 = *reinterpret_cast<const uint32_t*>(s_lds + kTileKeys + 4 * fq), vs1 = *reinterpret_cast<const uint32_t*>(s_lds + kTileKeys + 16 + 4 * fq);
     f32x4_t sacc[2][RTW];
     if constexpr (kCodes) {
       v8i_t kf[2];
-      int ksc[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const char* row = k_lds + j * 16 * HD + k_row;
-        const int4 lo = *reinterpret_cast<const int4*>(row + (k_chunk << 4));
-        const int4 hi = HD == 128 ? *reinterpret_cast<const int4*>(row + ((k_chunk ^ 4) << 4)) : lo;
-        kf[j] = v8i_t{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-        ksc[j] = *reinterpret_cast<const uint8_t*>(s_lds + 16 * j + fr);
+        const uint4 lo = kreg[j][0], hi = kreg[j][HD / 64 - 1];          // (64-wide heads: the same codes twice)
+        kf[j] = v8i_t{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
       }
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int p = NM - 1; p >= 0; --p)                // (the lesser part first, and all of it: an accumulator's second product waits for the first)
 #pragma unroll
-        for (int t = 0; t < RTW; ++t) {
-          f32x4_t c = f32x4_t{0.f, 0.f, 0.f, 0.f};
-          if constexpr (NM > 1) c = mfma_scaled<1>(kf[j], qf[t][1], c, ksc[j], qs[t]);     // (the lesser part first)
-          sacc[j][t] = mfma_scaled<0>(kf[j], qf[t][0], c, ksc[j], qs[t]);
-        }
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int t = 0; t < RTW; ++t) {
+            const f32x4_t c = p == NM - 1 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sacc[j][t];
+            sacc[j][t] = p == 1 ? mfma_scaled<1>(kf[j], qf[t][p], c, ksc[j], qs[t]) : mfma_scaled<0>(kf[j], qf[t][p], c, ksc[j], qs[t]);
+          }
     } else {
-      const uint32_t ks0 = *reinterpret_cast<const uint32_t*>(s_lds + 4 * fq), ks1 = *reinterpret_cast<const uint32_t*>(s_lds + 16 + 4 * fq);
-      const float ks[2][4] = {{quant_scale<0>(ks0), quant_scale<1>(ks0), quant_scale<2>(ks0), quant_scale<3>(ks0)},
-                              {quant_scale<0>(ks1), quant_scale<1>(ks1), quant_scale<2>(ks1), quant_scale<3>(ks1)}};
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
+        const float ks[4] = {quant_scale<0>(ksw[j]), quant_scale<1>(ksw[j]), quant_scale<2>(ksw[j]), quant_scale<3>(ksw[j])};
         f32x4_t part[RTW][NP];
 #pragma unroll
         for (int t = 0; t < RTW; ++t)
@@ -341,8 +382,9 @@ __global__ __launch_bounds__(64 * NK * NR, RTW <= 2 ? 2 : (NK * NR + 3) / 4) voi
           for (int p = 0; p < NP; ++p) part[t][p] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < kKS; ++s) {
-          const uint2 c = *reinterpret_cast<const uint2*>(k_lds + j * 16 * HD + k_row + (((2 * s + (fq >> 1)) ^ swz_k<HD>(fr)) << 4) + (fq & 1) * 8);
-          const uint4 ka = make_uint4(two_bf16(c.x, false), two_bf16(c.x, true), two_bf16(c.y, false), two_bf16(c.y, true));
+          const uint4 r = kreg[j][s >> 1];
+          const uint32_t c0 = s & 1 ? r.z : r.x, c1 = s & 1 ? r.w : r.y;
+          const uint4 ka = make_uint4(two_bf16(c0, false), two_bf16(c0, true), two_bf16(c1, false), two_bf16(c1, true));
 #pragma unroll
           for (int t = 0; t < RTW; ++t)
 #pragma unroll
@@ -352,40 +394,50 @@ __global__ __launch_bounds__(64 * NK * NR, RTW <= 2 ? 2 : (NK * NR + 3) / 4) voi
 #pragma unroll
         for (int t = 0; t < RTW; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sacc[j][t][e] = ((part[t][2][e] + part[t][1][e]) + part[t][0][e]) * ks[j][e];
+          for (int e = 0; e < 4; ++e) sacc[j][t][e] = ((part[t][2][e] + part[t][1][e]) + part[t][0][e]) * ks[e];
       }
     }
+    const float vs[8] = {quant_scale<0>(vsw[0]), quant_scale<1>(vsw[0]), quant_scale<2>(vsw[0]), quant_scale<3>(vsw[0]),
+                         quant_scale<0>(vsw[1]), quant_scale<1>(vsw[1]), quant_scale<2>(vsw[1]), quant_scale<3>(vsw[1])};
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int dt = 0; dt < min(kVAhead, kDT); ++dt) read_v(it, dt);
+    __builtin_amdgcn_sched_barrier(0);
 
     // ---- online softmax; lane (row, q) owns keys t0 + 16 j + 4 q + e of its row.  The reference of the exponents moves only when a score
     // exceeds its row's by more than kSlack.
     constexpr float kSlack = 8.f;
     const bool plain = t0 + kTileKeys <= min(L, s1) && sl2 > 0.f;
-    const float vs[8] = {quant_scale<0>(vs0), quant_scale<1>(vs0), quant_scale<2>(vs0), quant_scale<3>(vs0),
-                         quant_scale<0>(vs1), quant_scale<1>(vs1), quant_scale<2>(vs1), quant_scale<3>(vs1)};
-    uint4 pf[RTW][PP];
+    float z[RTW][8], unit = sl2;
 #pragma unroll
-    for (int t = 0; t < RTW; ++t) {
-      float z[8];
+    for (int t = 0; t < RTW; ++t)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) z[4 * j + e] = sacc[j][t][e];
-      float unit = sl2;
-      if (!plain) {
-        unit = 1.f;
+        for (int e = 0; e < 4; ++e) z[t][4 * j + e] = sacc[j][t][e];
+    if (!plain) {
+      unit = 1.f;
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+      for (int t = 0; t < RTW; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int p = t0 + 16 * j + 4 * fq + e;
-            bool vis = p < s1;
-            if (vis && p >= L) vis = (rowmask[t] >> (p - L)) & 1ull;
-            z[4 * j + e] = vis ? z[4 * j + e] * sl2 : -INFINITY;
-          }
-      }
-      const float mt = max3_nan(max3_nan(z[0], z[1], z[2]), max3_nan(z[3], z[4], z[5]), max_nan(z[6], z[7])) * unit;
-      if (__builtin_amdgcn_ballot_w64(mt > m_run[t] + kSlack) != 0ull) {
-        const float m_new = fmaxf(m_run[t], quad_row_max(mt));
+        for (int e = 0; e < 8; ++e) {
+          const int p = t0 + 16 * (e >> 2) + 4 * fq + (e & 3);
+          bool vis = p < s1;
+          if (vis && p >= L) vis = (rowmask[t] >> (p - L)) & 1ull;
+          z[t][e] = vis ? z[t][e] * sl2 : -INFINITY;
+        }
+    }
+    float mt[RTW];
+    bool grown = false;
+#pragma unroll
+    for (int t = 0; t < RTW; ++t) {
+      mt[t] = max3_nan(max3_nan(z[t][0], z[t][1], z[t][2]), max3_nan(z[t][3], z[t][4], z[t][5]), max_nan(z[t][6], z[t][7])) * unit;
+      grown |= mt[t] > m_run[t] + kSlack;
+    }
+    if (__builtin_amdgcn_ballot_w64(grown) != 0ull) {            // (one test for all of a wave's rows, so that what follows is one stretch of code)
+#pragma unroll
+      for (int t = 0; t < RTW; ++t) {
+        const float m_new = fmaxf(m_run[t], quad_row_max(mt[t]));
         const float al = __builtin_amdgcn_exp2f(m_run[t] - m_new);
         m_run[t] = m_new;
         l_run[t] *= al;
@@ -395,9 +447,13 @@ __global__ __launch_bounds__(64 * NK * NR, RTW <= 2 ? 2 : (NK * NR + 3) / 4) voi
           oacc[dt][t][2] *= al; oacc[dt][t][3] *= al;
         }
       }
+    }
+    uint4 pf[RTW][PP];
+#pragma unroll
+    for (int t = 0; t < RTW; ++t) {
       float pr[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) pr[e] = __builtin_amdgcn_exp2f(fmaf(z[e], unit, -m_run[t]));
+      for (int e = 0; e < 8; ++e) pr[e] = __builtin_amdgcn_exp2f(fmaf(z[t][e], unit, -m_run[t]));
       l_run[t] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
 #pragma unroll
       for (int e = 0; e < 8; ++e) pr[e] *= vs[e];
@@ -413,31 +469,40 @@ __global__ __launch_bounds__(64 * NK * NR, RTW <= 2 ? 2 : (NK * NR + 3) / 4) voi
       }
     }
 
-    // ---- O^T += V^T P^T
+    // ---- O^T += V^T P^T: a column tile is converted while the one before it is multiplied, into registers of its own
+    auto convert = [&](int dt) { return make_uint4(two_bf16(vreg[dt][0], false), two_bf16(vreg[dt][0], true), two_bf16(vreg[dt][1], false), two_bf16(vreg[dt][1], true)); };
+    uint4 va = convert(0), vb;
 #pragma unroll
     for (int dt = 0; dt < kDT; ++dt) {
-      const v2i_t c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i_t)(lds_ptr_t)(v_lds + v_at + ((dt ^ v_swz) << 4)));
-      const uint4 va = make_uint4(two_bf16(c[0], false), two_bf16(c[0], true), two_bf16(c[1], false), two_bf16(c[1], true));
+      if (dt + kVAhead < kDT) read_v(it, dt + kVAhead);
+      if (dt + 1 < kDT) vb = convert(dt + 1);
+      __builtin_amdgcn_sched_barrier(0);          // (all conversions first would take four registers for every one of these)
 #pragma unroll
-      for (int t = 0; t < RTW; ++t)
+      for (int p = PP - 1; p >= 0; --p)
 #pragma unroll
-        for (int p = PP - 1; p >= 0; --p)
+        for (int t = 0; t < RTW; ++t)
           oacc[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, va), __builtin_bit_cast(bf16x8_t, pf[t][p]), oacc[dt][t], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      va = vb;
+    }
     }
   }
 
   // ---- the segment's partial result.  Several rings: each leaves its sums in its own slots (16-byte pieces of a row swizzled), every wave adds some
   // rows, in the order of the rings.
+  int lane_e = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane_e));
+  const int fr_e = lane_e & 15, fq_e = lane_e >> 4;
   const size_t unit = static_cast<size_t>(blockIdx.x) + static_cast<size_t>(b) * a.Hkv + g;   // partial slot of segment (w, u)
 #pragma unroll
   for (int t = 0; t < RTW; ++t) l_run[t] = quad_row_sum(l_run[t]);
   if constexpr (NK == 1) {
 #pragma unroll
     for (int t = 0; t < RTW; ++t) {
-      const int r = 16 * (rr * RTW + t) + fr;
+      const int r = 16 * (rr * RTW + t) + fr_e;
       if (r >= R) continue;
-      if (fq == 0) *reinterpret_cast<float2*>(a.part_ml + (unit * R + r) * 2) = make_float2(m_run[t], l_run[t]);
-      float* dst = a.part_o + (unit * R + r) * HD + 4 * fq;
+      if (fq_e == 0) *reinterpret_cast<float2*>(a.part_ml + (unit * R + r) * 2) = make_float2(m_run[t], l_run[t]);
+      float* dst = a.part_o + (unit * R + r) * HD + 4 * fq_e;
 #pragma unroll
       for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<float4*>(dst + 16 * dt) = make_float4(oacc[dt][t][0], oacc[dt][t][1], oacc[dt][t][2], oacc[dt][t][3]);
     }
@@ -446,17 +511,17 @@ __global__ __launch_bounds__(64 * NK * NR, RTW <= 2 ? 2 : (NK * NR + 3) / 4) voi
     if constexpr (NR > 1) __syncthreads();        // the ring's last tile is read by all its waves
 #pragma unroll
     for (int t = 0; t < RTW; ++t) {
-      const int r = 16 * (rr * RTW + t) + fr;
-      if (fq == 0) *reinterpret_cast<float2*>(ml_lds + 2 * (kg * RP + r)) = make_float2(m_run[t], l_run[t]);
+      const int r = 16 * (rr * RTW + t) + fr_e;
+      if (fq_e == 0) *reinterpret_cast<float2*>(ml_lds + 2 * (kg * RP + r)) = make_float2(m_run[t], l_run[t]);
 #pragma unroll
       for (int dt = 0; dt < kDT; ++dt)
-        *reinterpret_cast<float4*>(ring + r * (4 * HD) + (((4 * dt + fq) ^ fr) << 4)) = make_float4(oacc[dt][t][0], oacc[dt][t][1], oacc[dt][t][2], oacc[dt][t][3]);
+        *reinterpret_cast<float4*>(ring + r * (4 * HD) + (((4 * dt + fq_e) ^ fr_e) << 4)) = make_float4(oacc[dt][t][0], oacc[dt][t][1], oacc[dt][t][2], oacc[dt][t][3]);
     }
     __syncthreads();
     constexpr int C4 = HD / 4, RPW = 64 / C4;     // 16-byte pieces of a row, rows that a wave adds at a time
-    const int c4 = lane % C4;
+    const int c4 = lane_e % C4;
 #pragma unroll 1
-    for (int r = RPW * wv + lane / C4; r < R; r += RPW * NK * NR) {
+    for (int r = RPW * wv + lane_e / C4; r < R; r += RPW * NK * NR) {
       float2 ml[NK];
       float4 o[NK];
 #pragma unroll
@@ -661,56 +726,36 @@ __global__ __launch_bounds__(256) void k_quant_combine(const QuantAttnArgs a) {
 
 // ---------------------------------------------------------------------------------------------------- launches
 
-// Rings of a workgroup, waves of a ring, row tiles of a wave.
-struct Form { int nk, nr, rtw; };
-Form form_of(bool f32, int d, int tiles) {
-  if (f32) {
-    if (d == 64) return tiles <= 2 ? Form{4, 1, 2} : tiles <= 4 ? Form{2, 2, 2} : Form{2, 4, 2};
-    return tiles <= 1 ? Form{4, 1, 1} : tiles <= 2 ? Form{2, 2, 1} : tiles <= 4 ? Form{2, 4, 1} : Form{1, 8, 1};
-  }
-  switch (tiles) {
-    case 1: return {4, 1, 1};
-    case 2: return {4, 1, 2};
-    case 3: return {4, 1, 3};
-    case 4: return {4, 1, 4};
-    case 5: case 6: return {2, 2, 3};
-    default: return {2, 2, 4};
-  }
-}
 int row_tiles(const QuantAttnArgs& a) { return (a.G * a.n_q + 15) / 16; }
-Form form_of(const QuantAttnArgs& a) { return form_of(a.dtype == 0, a.d, row_tiles(a)); }
 
-template <int HD, typename T, int NK, int NR, int RTW>
+template <int HD, typename T, int NK, int NR, int RTW, int PP, int KT>
 hipError_t launch_one(const QuantAttnArgs& a, hipStream_t s) {
   static_assert(quant_lds_bytes(HD, NK, 16 * NR * RTW, kAttnMaxSeqs, true) <= 160 * 1024, "the LDS of a compute unit");
-  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_quant_attn<HD, T, NK, NR, RTW>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_quant_attn<HD, T, NK, NR, RTW, PP, KT>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL((k_quant_attn<HD, T, NK, NR, RTW>), dim3(a.wgrid), dim3(64 * NK * NR), quant_lds_bytes(HD, NK, 16 * NR * RTW, a.B, a.paged != 0), s, a);
+  hipLaunchKernelGGL((k_quant_attn<HD, T, NK, NR, RTW, PP, KT>), dim3(a.wgrid), dim3(64 * NK * NR), quant_lds_bytes(HD, NK, 16 * NR * RTW, a.B, a.paged != 0), s, a);
   return hipGetLastError();
 }
 
 template <int HD> hipError_t launch_bf16(const QuantAttnArgs& a, hipStream_t s) {
-  const Form f = form_of(a);
-  if (f.nr == 1) {
-    switch (f.rtw) {
-      case 1: return launch_one<HD, bf16_t, 4, 1, 1>(a, s);
-      case 2: return launch_one<HD, bf16_t, 4, 1, 2>(a, s);
-      case 3: return launch_one<HD, bf16_t, 4, 1, 3>(a, s);
-      default: return launch_one<HD, bf16_t, 4, 1, 4>(a, s);
-    }
+  constexpr int K2 = HD == 64 ? 4 : 2;            // tiles of a step
+  switch (row_tiles(a)) {
+    case 1: return launch_one<HD, bf16_t, 8, 1, 1, 2, 1>(a, s);
+    case 2: return launch_one<HD, bf16_t, 4, 2, 1, 2, 1>(a, s);
+    case 3: return launch_one<HD, bf16_t, 4, 3, 1, 1, 1>(a, s);
+    case 4: return launch_one<HD, bf16_t, 4, 4, 1, 1, 1>(a, s);
+    case 5: return launch_one<HD, bf16_t, 2, 5, 1, 1, HD == 64 ? 4 : 1>(a, s);
+    case 6: return launch_one<HD, bf16_t, 2, 6, 1, 1, K2>(a, s);
+    default: return launch_one<HD, bf16_t, 2, 4, 2, 1, K2>(a, s);
   }
-  return f.rtw == 3 ? launch_one<HD, bf16_t, 2, 2, 3>(a, s) : launch_one<HD, bf16_t, 2, 2, 4>(a, s);
 }
 
 hipError_t launch_f32(const QuantAttnArgs& a, hipStream_t s) {
-  const Form f = form_of(a);
-  if (a.d == 64) return f.nk == 4 ? launch_one<64, float, 4, 1, 2>(a, s) : f.nr == 2 ? launch_one<64, float, 2, 2, 2>(a, s) : launch_one<64, float, 2, 4, 2>(a, s);
-  switch (f.nr) {
-    case 1: return launch_one<128, float, 4, 1, 1>(a, s);
-    case 2: return launch_one<128, float, 2, 2, 1>(a, s);
-    case 4: return launch_one<128, float, 2, 4, 1>(a, s);
-    default: return launch_one<128, float, 1, 8, 1>(a, s);
-  }
+  const int tiles = row_tiles(a);
+  if (a.d == 64) return tiles <= 2 ? launch_one<64, float, 4, 1, 2, 3, 1>(a, s) : tiles <= 4 ? launch_one<64, float, 2, 2, 2, 3, 1>(a, s) : launch_one<64, float, 2, 4, 2, 3, 1>(a, s);
+  if (tiles <= 1) return launch_one<128, float, 4, 1, 1, 3, 1>(a, s);
+  if (tiles <= 2) return launch_one<128, float, 2, 2, 1, 3, 1>(a, s);
+  return tiles <= 4 ? launch_one<128, float, 2, 4, 1, 3, 1>(a, s) : launch_one<128, float, 1, 8, 1, 3, 1>(a, s);
 }
 
 template <typename T, int D> hipError_t launch_combine(const QuantAttnArgs& a, hipStream_t s) {
@@ -736,8 +781,8 @@ bool quant_attn_plan(QuantAttnArgs& a, int num_cus) {
   const AttnLine line = attn_sched_line(static_cast<int>(a.B * gmax), a.B, a.Hkv, a.pad, a.wide_from, 0, num_cus);
   int64_t w = line.W;
   if (line.T > kAttnSpread && w < kAttnSpread) w = std::min<int64_t>(kAttnSpread, num_cus);   // (fewer granules may take more workgroups)
-  if (a.paged) {                                  // a segment's page ids have to fit LDS
-    const int64_t seg_gran = static_cast<int64_t>(kMaxPages) * a.page_size / kAttnGran;
+  if (a.paged) {                                  // a segment's groups have to fit LDS
+    const int64_t seg_gran = kMaxGroups * 16 / kAttnGran;
     w = std::max(w, (line.T + seg_gran - 1) / seg_gran);
   }
   if (w > kAttnMaxGrid) return false;

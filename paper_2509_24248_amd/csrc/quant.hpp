@@ -10,10 +10,15 @@ __device__ __forceinline__ int quant_scale_byte(uint32_t amax) {
   return max(s, 1);
 }
 __device__ __forceinline__ float quant_scale_inverse(int s) { return __uint_as_float(static_cast<uint32_t>(254 - s) << 23); }
-// byte E of a word of four scale bytes, as the factor it stands for
+// byte E of a word of four scale bytes, as the factor it stands for: the byte in the exponent's place
 template <int E> __device__ __forceinline__ float quant_scale(uint32_t w) {
-  const uint32_t at = E == 0 ? w << 23 : E == 1 ? w << 15 : E == 2 ? w << 7 : w >> 1;
-  return __uint_as_float(at & 0x7F800000u);
+  uint32_t x;
+  const uint32_t by = 23;
+  if constexpr (E == 0) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(x) : "v"(by), "v"(w));
+  if constexpr (E == 1) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(x) : "v"(by), "v"(w));
+  if constexpr (E == 2) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(x) : "v"(by), "v"(w));
+  if constexpr (E == 3) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3" : "=v"(x) : "v"(by), "v"(w));
+  return __uint_as_float(x);
 }
 
 }  // namespace sx
