@@ -269,10 +269,10 @@ bool quant_attn_plan(QuantAttnArgs& a, int num_cus);
 hipError_t launch_quant_attn(const QuantAttnArgs& a, hipStream_t s);   // (workspace as attn_workspace_bytes / attn_carve)
 
 // ---- sampled tokens (sample.hip) -----------------------------------------------------------
-constexpr int kSampleMaxK = 1024, kSampleMaxSegs = 512;      // segments of 512 tokens
+constexpr int kSampleMaxK = 1024, kSampleMaxSegs = 512, kSampleMaxChunks = 20;      // segments of 512 tokens
 struct SampleRow {
-  int listed, mode, lo, hi;
-  float top;
+  int listed, mode;
+  float top, sure, doubt;
 };
 struct SampleArgs {
   int f32, M, V;

@@ -11,7 +11,7 @@
 //                    bin in one 64-bit LDS atomic; the bins lie on one grid for all chunks of a row, counted from the chunk's best).
 //   2 k_sample_mass  adds the row's histograms, takes the bins that the borders of top-k and top-p lie in, reads the logits
 //                    again: masses of what is kept for certain per segment of 512 tokens, and a list of the tokens in doubt.
-//   3 k_sample_pick  a workgroup per row sorts the list (at most 4096), cuts it, finds the draw's segment and in it the token.
+//   3 k_sample_pick  a workgroup per row finds the border in the list (at most 4096), the draw's segment and in it the token.
 // Bound by memory at many rows: the logits are read twice, the second time mostly from the last-level cache; at few rows
 // by the latencies of three launches.
 #include "common.hpp"
@@ -76,43 +76,84 @@ __device__ __forceinline__ uint32_t key_of(float l) {
 __device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key ^ ((key >> 31) - 1u | 0x80000000u)); }
 __device__ __forceinline__ uint64_t place_of(float l, int idx) { return static_cast<uint64_t>(~key_of(l)) << 32 | static_cast<uint32_t>(idx); }
 
-// 2^((l - top) c), 0 below 2^-40.  2^f for |f| <= 1/2 as the Taylor sum of e^(f ln 2) to degree 11: what is left out is (ln 2 / 2)^12 / 12! < 7e-15.
+// The least logit whose bin is `bin` or above (bins grow with the logit): by six bits of its key at a time, a lane per candidate.
+__device__ __forceinline__ float least_of(int bin, float s) {
+  uint32_t key = 0;
+#pragma unroll
+  for (int shift = 26; shift >= -4; shift -= 6) {
+    const int by = shift < 0 ? 0 : shift, width = shift < 0 ? 4 : 64;          // (32 bits: five times six, and two)
+    const uint32_t lane = threadIdx.x & 63;
+    const uint32_t mine = key + (lane << by);
+    const float l = logit_of(mine);
+    // (keys of NaN lie below -infinity's and above infinity's)
+    const bool below = static_cast<int>(lane) < width && (mine < 0x007FFFFFu || (mine <= 0xFF800000u && bin_of(l, s) < bin));
+    const int n = __popcll(__builtin_amdgcn_ballot_w64(below));
+    key += shift < 0 ? static_cast<uint32_t>(n) : static_cast<uint32_t>(n > 0 ? n - 1 : 0) << by;
+  }
+  return logit_of(key);
+}
+
+// 2^((l - top) c), 0 below 2^-40.  2^f for |f| <= 1/2 by a polynomial of degree 9 through its values at Chebyshev's points,
+// 3.2e-14 off at most.
 __device__ __forceinline__ double weight(float l, float top, double c) {
   const double d = l == top ? 0.0 : static_cast<double>(l) - static_cast<double>(top);      // (also where both are infinite)
-  const double t = d * c;
-  if (!(t > -40.5)) return 0.0;
+  const double t = fmax(d * c, -64.0);
   const double n = rint(t), f = t - n;
-  double y = 4.44553827187081e-10;
-  y = fma(y, f, 7.054911620801121e-09);
-  y = fma(y, f, 1.0178086009239696e-07);
-  y = fma(y, f, 1.3215486790144305e-06);
-  y = fma(y, f, 1.5252733804059838e-05);
-  y = fma(y, f, 0.00015403530393381606);
-  y = fma(y, f, 0.0013333558146428441);
-  y = fma(y, f, 0.009618129107628477);
-  y = fma(y, f, 0.055504108664821576);
-  y = fma(y, f, 0.2402265069591007);
-  y = fma(y, f, 0.6931471805599453);
-  y = fma(y, f, 1.0);
+  double y = 1.0205905413765595e-07;
+  y = fma(y, f, 1.325964524488711e-06);
+  y = fma(y, f, 1.5252672924850737e-05);
+  y = fma(y, f, 0.0001540343375125101);
+  y = fma(y, f, 0.0013333558200794592);
+  y = fma(y, f, 0.009618129193934313);
+  y = fma(y, f, 0.05550410866465167);
+  y = fma(y, f, 0.2402265069564034);
+  y = fma(y, f, 0.6931471805599462);
+  y = fma(y, f, 1.0);                             // (1.0000000000000135 would be the fit's: the best token weighs 1)
   const double w = __longlong_as_double(__double_as_longlong(y) + (static_cast<int64_t>(static_cast<int>(n)) << 52));
   return w >= kFloor ? w : 0.0;
 }
 // a weight in units of 2^-45 (adding 2^52 leaves the rounded number in the low bits)
 __device__ __forceinline__ uint64_t fixed(double w) { return static_cast<uint64_t>(__double_as_longlong(fma(w, kFix, 4503599627370496.0))) & 0xFFFFFFFFFFFFFull; }
 
-__device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int o) { return static_cast<uint64_t>(__shfl_xor(static_cast<unsigned long long>(v), o, 64)); }
-__device__ __forceinline__ uint64_t wave_sum64(uint64_t v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += shfl_xor64(v, o);
-  return v;
+// Values of other lanes without LDS (as wave_scan): 0 where there is no such lane.
+template <int CTRL, int ROWS> __device__ __forceinline__ uint64_t lane64(uint64_t v) {
+  const uint32_t lo = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(static_cast<uint32_t>(v)), CTRL, ROWS, 0xf, false));
+  const uint32_t hi = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(static_cast<uint32_t>(v >> 32)), CTRL, ROWS, 0xf, false));
+  return static_cast<uint64_t>(hi) << 32 | lo;
 }
 __device__ __forceinline__ uint64_t wave_scan64(uint64_t v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint64_t up = static_cast<uint64_t>(__shfl_up(static_cast<unsigned long long>(v), o, 64));
-    if (lane >= o) v += up;
-  }
+  v += lane64<0x111, 0xf>(v);
+  v += lane64<0x112, 0xf>(v);
+  v += lane64<0x114, 0xf>(v);
+  v += lane64<0x118, 0xf>(v);
+  v += lane64<0x142, 0xa>(v);
+  v += lane64<0x143, 0xc>(v);
+  return v;
+}
+__device__ __forceinline__ double wave_scan64(double v) {
+  auto lanes = [](double x, auto f) { return __longlong_as_double(static_cast<long long>(f(static_cast<uint64_t>(__double_as_longlong(x))))); };
+  v += lanes(v, [](uint64_t x) { return lane64<0x111, 0xf>(x); });
+  v += lanes(v, [](uint64_t x) { return lane64<0x112, 0xf>(x); });
+  v += lanes(v, [](uint64_t x) { return lane64<0x114, 0xf>(x); });
+  v += lanes(v, [](uint64_t x) { return lane64<0x118, 0xf>(x); });
+  v += lanes(v, [](uint64_t x) { return lane64<0x142, 0xa>(x); });
+  v += lanes(v, [](uint64_t x) { return lane64<0x143, 0xc>(x); });
+  return v;
+}
+// (uniform)
+__device__ __forceinline__ uint64_t wave_sum64(uint64_t v) {
+  v = wave_scan64(v);
+  return static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(static_cast<uint32_t>(v >> 32)), 63))) << 32 |
+         static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(static_cast<uint32_t>(v)), 63));
+}
+// (in lane 63)
+__device__ __forceinline__ uint64_t wave_max64(uint64_t v) {
+  v = max(v, lane64<0x111, 0xf>(v));
+  v = max(v, lane64<0x112, 0xf>(v));
+  v = max(v, lane64<0x114, 0xf>(v));
+  v = max(v, lane64<0x118, 0xf>(v));
+  v = max(v, lane64<0x142, 0xa>(v));
+  v = max(v, lane64<0x143, 0xc>(v));
   return v;
 }
 // inclusive sum over the workgroup; `part` [kWaves] is free again behind the next barrier
@@ -121,7 +162,8 @@ __device__ __forceinline__ uint64_t block_scan64(uint64_t v, uint64_t* part) {
   v = wave_scan64(v);
   if ((threadIdx.x & 63) == 63) part[wv] = v;
   __syncthreads();
-  for (int i = 0; i < wv; ++i) v += part[i];
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) v += i < wv ? part[i] : 0;
   return v;
 }
 
@@ -216,39 +258,43 @@ __global__ __launch_bounds__(kT) void k_sample_bins(const SampleArgs a) {
 
 template <typename T>
 __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
-  __shared__ int cnt_part[kWaves], found[4], n_list, base_list;
+  __shared__ int cnt_part[kWaves], found[3], n_list, base_list;
   __shared__ double mass_part[kWaves];
   __shared__ unsigned long long sums[2];
   __shared__ uint64_t list[kListPart];
   const int row = blockIdx.y, chunk = blockIdx.x, lane = threadIdx.x & 63, tid = threadIdx.x;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Setting st = setting_of(a, row);
+  const T* logits = static_cast<const T*>(a.logits) + static_cast<int64_t>(row) * a.ld;
+  const int seg0 = chunk * a.chunk_segs, seg1 = min(seg0 + a.chunk_segs, a.segs);
+  float next[8];                                  // (the first tokens are requested with everything else)
+  if (seg0 + wv < seg1) load_seg<T>(logits, a.V, seg0 + wv, next);
   const size_t first = static_cast<size_t>(row) * a.chunks;
-  // ---- the row's best logit and its histogram: thread j has bin j
-  float top = -INFINITY;
-  for (int c = 0; c < a.chunks; ++c) top = fmaxf(top, a.chunk_top[first + c]);
+  const float chunk_top = lane < a.chunks ? a.chunk_top[first + lane] : -INFINITY;
+  const Setting st = setting_of(a, row);
+  // ---- the row's best logit and its histogram: thread j has bin j, lane c how far chunk c's bins lie behind it
+  const float top = wave_max_dpp(chunk_top);
   const int origin = bin_of(top, st.s);
+  const int behind = chunk_top > -INFINITY ? origin - bin_of(chunk_top, st.s) : kBins;
+  if (tid < 3) found[tid] = kBins - 1;
+  if (tid == 0) n_list = 0;
+  if (tid < 2) sums[tid] = 0;
   uint64_t h = 0;
-  for (int c = 0; c < a.chunks; ++c) {
-    const float t = a.chunk_top[first + c];
-    const int i = tid - (origin - bin_of(t, st.s));         // (0 .. 2^31 apart)
-    if (t > -INFINITY && i >= 0) h += a.hist[(first + c) * kBins + i];
+  for (int c0 = 0; c0 < a.chunks; c0 += kSampleMaxChunks / 2) {      // (half of the loads in flight: the second half is often empty)
+#pragma unroll
+    for (int e = 0; e < kSampleMaxChunks / 2; ++e) {
+      const int c = c0 + e, by = c < a.chunks ? __builtin_amdgcn_readlane(behind, c & 63) : kBins;
+      const uint64_t v = a.hist[(first + min(c, a.chunks - 1)) * kBins + max(tid - by, 0)];
+      h += tid >= by ? v : 0;
+    }
   }
   const int count = static_cast<int>(h >> kCountBit);
   const double mass = static_cast<double>(h & ((1ull << kCountBit) - 1)) * static_cast<double>(exp2f(static_cast<float>(tid) * (-1.44269504f / kPerNat)));
   int cum = wave_scan(count);
-  double cmass = mass;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double up = __shfl_up(cmass, o, 64);
-    if (lane >= o) cmass += up;
-  }
+  double cmass = wave_scan64(mass);
   if (lane == 63) { cnt_part[wv] = cum; mass_part[wv] = cmass; }
-  if (tid < 4) found[tid] = kBins - 1;
-  if (tid == 0) n_list = 0;
-  if (tid < 2) sums[tid] = 0;
   __syncthreads();
   double all = 0.0;
+#pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     if (w < wv) { cum += cnt_part[w]; cmass += mass_part[w]; }
     all += mass_part[w];
@@ -256,53 +302,67 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
   // the bins of the borders: the first whose sum reaches them; of top-p those that 1e-5 more or less could make it (a bin's mass is
   // known to some 2e-6: T in 32 bits, one rounding of the exponential)
   const double lo_at = st.p * all * (1.0 - 1e-5), hi_at = st.p * all * (1.0 + 1e-5);
-  if (st.k > 0 && cum >= st.k && cum - count < st.k) found[0] = tid;
-  if (cmass >= lo_at) atomicMin(&found[1], tid);
-  if (cmass >= hi_at) atomicMin(&found[2], tid);
+  auto first_of = [&](bool reached, int which) {
+    const uint64_t m = __builtin_amdgcn_ballot_w64(reached);
+    if (m && lane == 0) atomicMin(&found[which], 64 * wv + __ffsll(static_cast<unsigned long long>(m)) - 1);
+  };
+  first_of(st.k > 0 && cum >= st.k, 0);
+  first_of(cmass >= lo_at, 1);
+  first_of(cmass >= hi_at, 2);
   __syncthreads();
-  int mode = top == -INFINITY ? kModeEmpty : origin >= kFar || origin <= -kFar ? kModeScan : st.k > 0 ? kModeTopK : st.p < 1.0 ? kModeTopP : kModeAll;
-  const int lo = mode == kModeAll ? kFar : mode == kModeTopP ? found[1] : 0;            // bins in front of it are kept
-  const int hi = mode == kModeTopK ? found[0] : mode == kModeTopP ? max(found[1], found[2]) : -1;     // from lo to it: in doubt
+  const int mode = top == -INFINITY ? kModeEmpty : origin >= kFar || origin <= -kFar ? kModeScan : st.k > 0 ? kModeTopK : st.p < 1.0 ? kModeTopP : kModeAll;
+  // logits from `sure` on are kept for certain, from `doubt` on the list decides
+  float sure = NAN, doubt = NAN;
+  if (mode == kModeTopK) doubt = least_of(origin - found[0], st.s);
+  if (mode == kModeTopP) {
+    sure = found[1] > 0 ? least_of(origin - found[1] + 1, st.s) : NAN;
+    doubt = least_of(origin - max(found[1], found[2]), st.s);
+  }
+  if (mode == kModeAll) sure = -INFINITY;
   if (chunk == 0 && tid == 0) {
     SampleRow& r = a.row_info[row];
     r.mode = mode;
-    r.lo = lo;
-    r.hi = hi;
+    r.sure = sure;
+    r.doubt = doubt;
     r.top = top;
   }
   if (mode == kModeEmpty || mode == kModeScan) return;       // uniform
   // ---- the chunk's tokens
-  const T* logits = static_cast<const T*>(a.logits) + static_cast<int64_t>(row) * a.ld;
-  const int seg0 = chunk * a.chunk_segs, seg1 = min(seg0 + a.chunk_segs, a.segs);
   uint64_t total = 0, above = 0;
   for (int seg = seg0 + wv; seg < seg1; seg += kWaves) {
     float x[8];
-    load_seg<T>(logits, a.V, seg, x);
-    uint64_t kept = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int j = origin - bin_of(x[e], st.s);
-      bool doubt = false;
-      if (mode != kModeTopK || j <= hi) {
+    for (int e = 0; e < 8; ++e) x[e] = next[e];
+    if (seg + kWaves < seg1) load_seg<T>(logits, a.V, seg + kWaves, next);
+    uint32_t in_doubt = 0;                        // bit e: token e
+    if (mode == kModeTopK) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) in_doubt |= x[e] >= doubt ? 1u << e : 0u;
+    } else {
+      uint64_t kept = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
         const double w = weight(x[e], top, st.c);
-        const uint64_t f = fixed(w);
+        const uint64_t f = fixed(w), in = x[e] >= sure ? f : 0;
         total += f;
-        if (j < lo) {
-          above += f;
-          if (w >= st.m) kept += f;
-        }
-        doubt = j >= lo && j <= hi && w > 0.0;
+        above += in;
+        kept += w >= st.m ? in : 0;
+        in_doubt |= x[e] >= doubt && !(x[e] >= sure) ? 1u << e : 0u;
       }
-      if (__builtin_amdgcn_ballot_w64(doubt) != 0ull) {
-        if (doubt) {
-          const int at = atomicAdd(&n_list, 1);
-          if (at < kListPart) list[at] = place_of(x[e], token_of<T>(seg, lane, e));
-        }
-      }
-    }
-    if (mode != kModeTopK) {
       kept = wave_sum64(kept);
       if (lane == 0) a.seg_mass[static_cast<size_t>(row) * a.segs + seg] = kept;
+    }
+    if (__builtin_amdgcn_ballot_w64(in_doubt != 0) != 0ull) {
+      const int mine = __popc(in_doubt), upto = wave_scan(mine);
+      int at = 0;
+      if (lane == 63) at = atomicAdd(&n_list, upto);
+      at = __builtin_amdgcn_readlane(at, 63) + upto - mine;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (in_doubt >> e & 1u) {
+          if (at < kListPart) list[at] = place_of(x[e], token_of<T>(seg, lane, e));
+          ++at;
+        }
     }
   }
   if (mode == kModeTopP) {
@@ -330,15 +390,15 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
 
 struct PickLds {
   uint64_t list[kList];
-  uint64_t pre[kList];               // the sorted list's weights, then their inclusive sums
+  uint64_t w[kList];                 // the list's weights
   uint64_t seg[kSampleMaxSegs];
   uint64_t part[kWaves], part2[kWaves];
   unsigned long long digit_mass[256], wide;
   uint32_t digit_count[256];
   int count[kSampleMaxSegs];
-  int keep, pick, seg_at;
-  uint64_t seg_before;
-  // scan's results
+  int pick, seg_at, digit;
+  uint64_t seg_before, cut;
+  // results of a round of a selection
   uint32_t key;
   int n_equal;
   uint32_t before;
@@ -415,6 +475,90 @@ __device__ Border scan_border(const SampleArgs& a, const T* logits, const Settin
   return {prefix, c, mass_before + static_cast<uint64_t>(c) * w};
 }
 
+// The place of the last kept token of the list: the want-th best (want > 0), or the last whose better ones sum to less than `target` on top of
+// `base`; ~0 where all are kept, 0 where none is.  Radix selection by eight bits of the places at a time, from the highest that differ; it ends
+// with the first digit that holds a single token.  All threads get the result.
+__device__ uint64_t list_border(PickLds& s, int n, int want, uint64_t base, double target) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (n == 0) return 0;
+  if (want <= 0) {
+    target = fmax(target, 1.0);                   // (a weight is 32 units at least: the best token is always kept)
+    if (static_cast<double>(base) >= target) return 0;
+  }
+  uint64_t least = 0, most = 0;                   // (of the complements: 0 is what lanes that are not there give)
+  for (int i = tid; i < n; i += kT) {
+    least = max(least, ~s.list[i]);
+    most = max(most, s.list[i]);
+  }
+  least = wave_max64(least);
+  most = wave_max64(most);
+  if (lane == 63) { s.part[wv] = least; s.part2[wv] = most; }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    least = max(least, s.part[w]);
+    most = max(most, s.part2[w]);
+  }
+  uint64_t lo = ~least;
+  int shift = max(0, 56 - __clzll(static_cast<long long>(most - lo)));
+  uint32_t before = 0;
+  uint64_t mass_before = base;
+  for (;;) {
+    __syncthreads();
+    if (tid < 256) { s.digit_mass[tid] = 0; s.digit_count[tid] = 0; }
+    if (tid == 0) s.digit = 256;
+    __syncthreads();
+    for (int i = tid; i < n; i += kT) {
+      const uint64_t d = (s.list[i] - lo) >> shift;
+      if (s.list[i] >= lo && d < 256) {
+        atomicAdd(&s.digit_count[d], 1u);
+        if (want <= 0) atomicAdd(&s.digit_mass[d], static_cast<unsigned long long>(s.w[i]));
+      }
+    }
+    __syncthreads();
+    // inclusive sums over the digits: waves 0..3
+    int c = 0, cum = 0;
+    uint64_t m = 0, cmass = 0;
+    if (tid < 256) {
+      c = static_cast<int>(s.digit_count[tid]);
+      m = s.digit_mass[tid];
+      cum = wave_scan(c);
+      cmass = wave_scan64(m);
+      if (lane == 63) { s.count[wv] = cum; s.part[wv] = cmass; }
+    }
+    __syncthreads();
+    if (tid < 256) {
+#pragma unroll
+      for (int w = 0; w < 3; ++w)
+        if (w < wv) { cum += s.count[w]; cmass += s.part[w]; }
+      const bool reached = want > 0 ? before + cum >= static_cast<uint32_t>(want) : static_cast<double>(mass_before + cmass) >= target;
+      const uint64_t r = __builtin_amdgcn_ballot_w64(reached);
+      if (r && lane == 0) atomicMin(&s.digit, 64 * wv + __ffsll(static_cast<unsigned long long>(r)) - 1);
+    }
+    __syncthreads();
+    const int d = s.digit;
+    if (d == 256) return ~0ull;                   // (only in the first round: the border is not reached)
+    if (tid == d) {
+      s.n_equal = c;
+      s.before = before + static_cast<uint32_t>(cum - c);
+      s.mass_before = mass_before + (cmass - m);
+    }
+    __syncthreads();
+    lo += static_cast<uint64_t>(d) << shift;
+    if (shift == 0) return lo;
+    if (s.n_equal == 1) {
+      for (int i = tid; i < n; i += kT)
+        if (s.list[i] >= lo && (s.list[i] - lo) >> shift == 0) s.cut = s.list[i];
+      __syncthreads();
+      return s.cut;
+    }
+    before = s.before;
+    mass_before = s.mass_before;
+    shift = max(0, shift - 8);
+  }
+}
+
 template <typename T>
 __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
   extern __shared__ uint4 smem4[];
@@ -432,16 +576,15 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
     }
     return;
   }
-  const int origin = bin_of(top, st.s);
-  int lo = info.lo, hi = info.hi;                 // kept: bins in front of lo, and to hi where the place is not behind `cut`
+  float sure = info.sure, doubt = info.doubt;     // kept: logits from `sure` on, and from `doubt` on where the place is not behind `cut`
   uint64_t cut = ~0ull;
   const bool listed = info.mode == kModeTopK || info.mode == kModeTopP;
   const int n = listed ? info.listed : 0;
   if (info.mode == kModeScan || n > kList) {
     // ---- without histograms and list: a row whose logits are far from anything (2^26 nats), or whose list is too long, as where more than 4096 tokens
     // of nearly one weight lie at the border
-    lo = 0;
-    hi = INT_MAX;
+    sure = NAN;
+    doubt = -INFINITY;
     if (st.k > 0 || st.p < 1.0) {
       Border b = {0, 0, 0};
       if (st.k > 0) b = scan_border<T>(a, logits, st, top, s, st.k, 0.0);
@@ -511,52 +654,44 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
     for (int i = a.segs + tid; i < kSampleMaxSegs; i += kT) s.seg[i] = 0;
     __syncthreads();
   } else {
-    // ---- the list, sorted by place
-    for (int i = tid; i < kSampleMaxSegs; i += kT) s.seg[i] = i < a.segs && info.mode != kModeTopK ? a.seg_mass[static_cast<size_t>(row) * a.segs + i] : 0;
+    // ---- the list
+    s.seg[tid] = tid < a.segs && info.mode != kModeTopK ? a.seg_mass[static_cast<size_t>(row) * a.segs + tid] : 0;
     if (listed) {
+      for (int i = tid; i < n; i += kT) {
+        const uint64_t p = a.list[static_cast<size_t>(row) * kList + i];
+        s.list[i] = p;
+        s.w[i] = fixed(weight(logit_of(~static_cast<uint32_t>(p >> 32)), top, st.c));
+      }
       uint64_t total = 0, above = 0;
       if (info.mode == kModeTopP) {
-        for (int c = 0; c < a.chunks; ++c) {
-          total += a.chunk_sums[2 * (static_cast<size_t>(row) * a.chunks + c)];
-          above += a.chunk_sums[2 * (static_cast<size_t>(row) * a.chunks + c) + 1];
+        if (lane < a.chunks) {
+          total = a.chunk_sums[2 * (static_cast<size_t>(row) * a.chunks + lane)];
+          above = a.chunk_sums[2 * (static_cast<size_t>(row) * a.chunks + lane) + 1];
         }
+        total = wave_sum64(total);
+        above = wave_sum64(above);
       }
-      int n2 = 64;
-      while (n2 < n) n2 *= 2;
-      for (int i = tid; i < n2; i += kT) s.list[i] = i < n ? a.list[static_cast<size_t>(row) * kList + i] : ~0ull;
-      if (tid == 0) s.keep = 0;
       __syncthreads();
-      for (int size = 2; size <= n2; size *= 2)
-        for (int step = size / 2; step > 0; step /= 2) {
-          for (int i = tid; i < n2 / 2; i += kT) {
-            const int at = 2 * i - (i & (step - 1)), to = at + step;
-            const uint64_t x = s.list[at], y = s.list[to];
-            if ((x > y) == ((at & size) == 0)) { s.list[at] = y; s.list[to] = x; }
-          }
+      if (info.mode == kModeTopK) {
+        cut = list_border(s, n, st.k, 0, 0.0);
+        if (st.p < 1.0) {
+          uint64_t mine = 0;
+          for (int i = tid; i < n; i += kT) mine += s.list[i] <= cut ? s.w[i] : 0;
+          mine = wave_sum64(mine);
           __syncthreads();
+          if (lane == 0) s.part[wv] = mine;
+          __syncthreads();
+          for (int w = 0; w < kWaves; ++w) total += s.part[w];
+          __syncthreads();
+          cut = min(cut, list_border(s, n, 0, 0, st.p * static_cast<double>(total)));
         }
-      // weights and their inclusive sums: a thread has `per` neighbours
-      const int per = (n2 + kT - 1) / kT;
-      uint64_t own = 0;
-      for (int i = tid * per; i < min((tid + 1) * per, n2); ++i) {
-        own += i < n ? fixed(weight(logit_of(~static_cast<uint32_t>(s.list[i] >> 32)), top, st.c)) : 0;
-        s.pre[i] = own;
+      } else {
+        cut = list_border(s, n, 0, above, st.p * static_cast<double>(total));
       }
-      const uint64_t upto = block_scan64(own, s.part);
-      for (int i = tid * per; i < min((tid + 1) * per, n2); ++i) s.pre[i] += upto - own;
-      __syncthreads();
-      const int most = info.mode == kModeTopK ? min(st.k, n) : n;
-      const double target = st.p * static_cast<double>(info.mode == kModeTopK ? (most > 0 ? s.pre[most - 1] : 0) : total);
-      for (int i = tid; i < most; i += kT) {
-        const uint64_t better = above + (i > 0 ? s.pre[i - 1] : 0);
-        if (st.p >= 1.0 || static_cast<double>(better) < target || (i == 0 && above == 0)) atomicMax(&s.keep, i + 1);
-      }
-      __syncthreads();
-      const int keep = s.keep;
-      cut = keep > 0 ? s.list[keep - 1] : 0ull;
-      for (int i = tid; i < keep; i += kT) {
-        const double w = weight(logit_of(~static_cast<uint32_t>(s.list[i] >> 32)), top, st.c);
-        if (w >= st.m) atomicAdd(reinterpret_cast<unsigned long long*>(&s.seg[static_cast<uint32_t>(s.list[i]) / kSeg]), static_cast<unsigned long long>(fixed(w)));
+      for (int i = tid; i < n; i += kT) {
+        const uint64_t p = s.list[i];
+        if (p <= cut && s.w[i] > 0 && (st.m <= kFloor || weight(logit_of(~static_cast<uint32_t>(p >> 32)), top, st.c) >= st.m))
+          atomicAdd(reinterpret_cast<unsigned long long*>(&s.seg[static_cast<uint32_t>(p) / kSeg]), static_cast<unsigned long long>(s.w[i]));
       }
     }
     __syncthreads();
@@ -584,8 +719,7 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
   const int idx = s.seg_at * kSeg + tid;
   const float l = idx < a.V ? value<T>(logits[idx]) : -INFINITY;
   const double w = weight(l, top, st.c);
-  const int j = origin - bin_of(l, st.s);
-  const bool kept = w >= st.m && (j < lo || (j <= hi && place_of(l, idx) <= cut));
+  const bool kept = w >= st.m && (l >= sure || (l >= doubt && place_of(l, idx) <= cut));
   const uint64_t sum = s.seg_before + block_scan64(kept ? fixed(w) : 0, s.part2);
   if (kept && sum > x) atomicMin(&s.pick, tid);
   __syncthreads();
@@ -616,7 +750,7 @@ void sample_plan(SampleArgs& a) {
   a.segs = (a.V + kSeg - 1) / kSeg;
   // two workgroups per compute unit where the rows are few, no more than twenty to a row: each of the second kernel's reads the histograms of all
   int chunks = (512 + a.M - 1) / a.M;
-  if (chunks > 20) chunks = 20;
+  if (chunks > kSampleMaxChunks) chunks = kSampleMaxChunks;
   if (chunks > (a.segs + kWaves - 1) / kWaves) chunks = (a.segs + kWaves - 1) / kWaves;
   const int least = (a.segs + kChunkSegs - 1) / kChunkSegs;
   if (chunks < least) chunks = least;
