@@ -272,7 +272,7 @@ hipError_t launch_quant_attn(const QuantAttnArgs& a, hipStream_t s);   // (works
 constexpr int kSampleMaxK = 1024, kSampleMaxSegs = 512, kSampleMaxChunks = 20;      // segments of 512 tokens
 struct SampleRow {
   int listed, mode;
-  float top, sure, doubt;
+  float top, sure, doubt, least, min_p;      // logits: the best one, and the borders
 };
 struct SampleArgs {
   int f32, M, V;
@@ -286,7 +286,8 @@ struct SampleArgs {
   float* prob;               // or nullptr
   int* status;
   int segs, chunk_segs, chunks;                  // sample_plan
-  unsigned long long *hist, *chunk_sums, *seg_mass, *list;      // sample_carve
+  uint32_t* hist;                                // sample_carve
+  unsigned long long *chunk_sums, *seg_mass, *list;
   float* chunk_top;
   SampleRow* row_info;
 };

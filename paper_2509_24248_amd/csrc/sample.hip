@@ -18,6 +18,7 @@
 #include "kernels.hpp"
 
 #include <limits.h>
+#include <type_traits>
 
 namespace sx {
 
@@ -33,7 +34,6 @@ constexpr int kList = 4096, kListPart = 2048;      // tokens in doubt of a row, 
 constexpr int kFar = 1 << 29;           // bins are forced into -kFar .. kFar
 constexpr double kFix = 35184372088832.0;          // 2^45
 constexpr double kFloor = 9.094947017729282e-13;   // 2^-40
-constexpr int kCountBit = 42;
 
 enum { kModeEmpty = 0, kModeAll = 1, kModeTopK = 2, kModeTopP = 3, kModeScan = 4 };
 
@@ -76,28 +76,24 @@ __device__ __forceinline__ uint32_t key_of(float l) {
 __device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key ^ ((key >> 31) - 1u | 0x80000000u)); }
 __device__ __forceinline__ uint64_t place_of(float l, int idx) { return static_cast<uint64_t>(~key_of(l)) << 32 | static_cast<uint32_t>(idx); }
 
-// The least logit whose bin is `bin` or above (bins grow with the logit): by six bits of its key at a time, a lane per candidate.
-__device__ __forceinline__ float least_of(int bin, float s) {
+// The least logit that `reached` holds for (it has to hold from some logit on): by six bits of its key at a time, a lane per candidate.
+template <typename F> __device__ __forceinline__ float least_of(F reached) {
   uint32_t key = 0;
-#pragma unroll
+#pragma unroll 1
   for (int shift = 26; shift >= -4; shift -= 6) {
     const int by = shift < 0 ? 0 : shift, width = shift < 0 ? 4 : 64;          // (32 bits: five times six, and two)
     const uint32_t lane = threadIdx.x & 63;
     const uint32_t mine = key + (lane << by);
-    const float l = logit_of(mine);
     // (keys of NaN lie below -infinity's and above infinity's)
-    const bool below = static_cast<int>(lane) < width && (mine < 0x007FFFFFu || (mine <= 0xFF800000u && bin_of(l, s) < bin));
+    const bool below = static_cast<int>(lane) < width && (mine < 0x007FFFFFu || (mine <= 0xFF800000u && !reached(logit_of(mine))));
     const int n = __popcll(__builtin_amdgcn_ballot_w64(below));
     key += shift < 0 ? static_cast<uint32_t>(n) : static_cast<uint32_t>(n > 0 ? n - 1 : 0) << by;
   }
   return logit_of(key);
 }
 
-// 2^((l - top) c), 0 below 2^-40.  2^f for |f| <= 1/2 by a polynomial of degree 9 through its values at Chebyshev's points,
-// 3.2e-14 off at most.
-__device__ __forceinline__ double weight(float l, float top, double c) {
-  const double d = l == top ? 0.0 : static_cast<double>(l) - static_cast<double>(top);      // (also where both are infinite)
-  const double t = fmax(d * c, -64.0);
+// 2^t, |t| < 1000: 2^f for |f| <= 1/2 by a polynomial of degree 9 through its values at Chebyshev's points, 3.2e-14 off at most.
+__device__ __forceinline__ double exp2_of(double t) {
   const double n = rint(t), f = t - n;
   double y = 1.0205905413765595e-07;
   y = fma(y, f, 1.325964524488711e-06);
@@ -108,12 +104,25 @@ __device__ __forceinline__ double weight(float l, float top, double c) {
   y = fma(y, f, 0.05550410866465167);
   y = fma(y, f, 0.2402265069564034);
   y = fma(y, f, 0.6931471805599462);
-  y = fma(y, f, 1.0);                             // (1.0000000000000135 would be the fit's: the best token weighs 1)
-  const double w = __longlong_as_double(__double_as_longlong(y) + (static_cast<int64_t>(static_cast<int>(n)) << 52));
+  y = fma(y, f, 1.0);
+  return __longlong_as_double(__double_as_longlong(y) + (static_cast<int64_t>(static_cast<int>(n)) << 52));
+}
+// a weight in units of 2^-45, rounded, on top of the bits of 2^52
+constexpr uint64_t kBias = 0x4330000000000000ull;
+__device__ __forceinline__ uint64_t biased(double w) { return static_cast<uint64_t>(__double_as_longlong(fma(w, kFix, 4503599627370496.0))); }
+// The weights of a row whose best logit is finite: 2^(l c - top c) with one rounding of the exponent (that of top c is the same for every token);
+// l from top - 1600 / s on, whose weight of 2^-144 is no unit.
+struct Scale {
+  double c, k;
+};
+__device__ __forceinline__ double weight(float l, const Scale& z) { return exp2_of(fma(static_cast<double>(l), z.c, -z.k)); }
+__device__ __forceinline__ uint64_t fixed(double w) { return biased(w) - kBias; }
+// The same for any row, as it is needed where infinities may meet: 0 below 2^-40.
+__device__ __forceinline__ double weight_far(float l, float top, double c) {
+  const double d = l == top ? 0.0 : static_cast<double>(l) - static_cast<double>(top);
+  const double w = exp2_of(fmax(d * c, -64.0));
   return w >= kFloor ? w : 0.0;
 }
-// a weight in units of 2^-45 (adding 2^52 leaves the rounded number in the low bits)
-__device__ __forceinline__ uint64_t fixed(double w) { return static_cast<uint64_t>(__double_as_longlong(fma(w, kFix, 4503599627370496.0))) & 0xFFFFFFFFFFFFFull; }
 
 // Values of other lanes without LDS (as wave_scan): 0 where there is no such lane.
 template <int CTRL, int ROWS> __device__ __forceinline__ uint64_t lane64(uint64_t v) {
@@ -139,6 +148,9 @@ __device__ __forceinline__ double wave_scan64(double v) {
   v += lanes(v, [](uint64_t x) { return lane64<0x142, 0xa>(x); });
   v += lanes(v, [](uint64_t x) { return lane64<0x143, 0xc>(x); });
   return v;
+}
+__device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int m) {
+  return static_cast<uint64_t>(static_cast<uint32_t>(__shfl_xor(static_cast<int>(static_cast<uint32_t>(v >> 32)), m))) << 32 | static_cast<uint32_t>(__shfl_xor(static_cast<int>(static_cast<uint32_t>(v)), m));
 }
 // (uniform)
 __device__ __forceinline__ uint64_t wave_sum64(uint64_t v) {
@@ -167,11 +179,11 @@ __device__ __forceinline__ uint64_t block_scan64(uint64_t v, uint64_t* part) {
   return v;
 }
 
-template <typename T> __device__ __forceinline__ float value(T v);
-template <> __device__ __forceinline__ float value<float>(float v) { return v == v ? v + 0.f : -INFINITY; }       // (-0 is 0, NaN is never drawn)
-template <> __device__ __forceinline__ float value<bf16_t>(bf16_t v) { return value<float>(bf16_to_f32(v)); }
+__device__ __forceinline__ float as_f32(float v) { return v; }
+__device__ __forceinline__ float as_f32(bf16_t v) { return bf16_to_f32(v); }
+__device__ __forceinline__ float value(float v) { return v == v ? v + 0.f : -INFINITY; }       // (-0 is 0, NaN is never drawn)
 
-// eight tokens of a lane: an instruction of the wave reads consecutive bytes
+// eight tokens of a lane as they are (NaN too, which no comparison holds for): an instruction of the wave reads consecutive bytes
 template <typename T> __device__ __forceinline__ int token_of(int seg, int lane, int e) {
   return sizeof(T) == 4 ? seg * kSeg + 256 * (e >> 2) + 4 * lane + (e & 3) : seg * kSeg + 8 * lane + e;
 }
@@ -183,12 +195,12 @@ template <typename T> __device__ __forceinline__ void load_seg(const T* row, int
 #pragma unroll
     for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) __builtin_memcpy(raw + i * (16 / sizeof(T)), row + token_of<T>(seg, lane, i * (16 / static_cast<int>(sizeof(T)))), 16);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = value<T>(raw[e]);
+    for (int e = 0; e < 8; ++e) x[e] = as_f32(raw[e]);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int i = token_of<T>(seg, lane, e);
-      x[e] = i < V ? value<T>(row[i]) : -INFINITY;
+      x[e] = i < V ? as_f32(row[i]) : -INFINITY;
     }
   }
 }
@@ -197,7 +209,7 @@ template <typename T> __device__ __forceinline__ void load_seg(const T* row, int
 
 template <typename T>
 __global__ __launch_bounds__(kT) void k_sample_bins(const SampleArgs a) {
-  __shared__ unsigned long long hist[kBins];
+  __shared__ uint4 hist[kBins];        // four copies of a bin: the lanes of a wave that meet in a bin add one after the other
   __shared__ float best[kWaves];
   const int row = blockIdx.y, chunk = blockIdx.x, lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -216,7 +228,7 @@ __global__ __launch_bounds__(kT) void k_sample_bins(const SampleArgs a) {
     }
   }
   const Setting st = setting_of(a, row);
-  for (int j = threadIdx.x; j < kBins; j += kT) hist[j] = 0;
+  for (int j = threadIdx.x; j < kBins; j += kT) hist[j] = make_uint4(0, 0, 0, 0);
 #pragma unroll
   for (int i = 0; i < N; ++i)
 #pragma unroll
@@ -226,28 +238,40 @@ __global__ __launch_bounds__(kT) void k_sample_bins(const SampleArgs a) {
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) top = fmaxf(top, best[w]);
-  const int origin = bin_of(top, st.s);
-  if (top > -INFINITY) {
+  const bool counts = st.k > 0, masses = !counts && st.p < 1.0;        // what the borders need
+  if (!counts && !masses) {
+    if (threadIdx.x == 0) {
+      a.chunk_top[static_cast<size_t>(row) * a.chunks + chunk] = top;
+      if (chunk == 0) a.row_info[row].listed = 0;
+    }
+    return;                            // uniform
+  }
+  // (whole numbers below 2^29, or the row goes another way: their differences are exact)
+  const float origin = floorf(top * st.s);
+  uint32_t* const mine = reinterpret_cast<uint32_t*>(hist) + (lane & 3);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if (seg0 + wv + i * kWaves >= seg1) break;
+  for (int i = 0; i < N; ++i) {
+    if (seg0 + wv + i * kWaves >= seg1) break;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float l = x[i][e];
-        const int g = bin_of(l, st.s), j = origin - g;
-        if (l > -INFINITY && j < kBins) {
+    for (int e = 0; e < 8; ++e) {
+      const float l = x[i][e], prod = l * st.s, g = floorf(prod), j = origin - g;
+      if (j < static_cast<float>(kBins)) {
+        uint32_t add = 1;
+        if (masses) {                  // uniform
           // how far below the bin's upper edge, in bins: the product's rounding error counts as well
-          const float prod = l * st.s;
-          const float below = fminf(fmaxf((static_cast<float>(g) - prod) + 1.f - fmaf(l, st.s, -prod), 0.f), 1.f);
-          const uint32_t part = static_cast<uint32_t>(exp2f(below * (-1.44269504f / kPerNat)) * 16777216.f);
-          atomicAdd(&hist[j], (1ull << kCountBit) + part);
+          const float below = fminf(fmaxf((g - prod) + 1.f - fmaf(l, st.s, -prod), 0.f), 1.f);
+          add = static_cast<uint32_t>(fmaf(__builtin_amdgcn_exp2f(below * (-1.44269504f / kPerNat)), 65536.f, 0.5f));
         }
+        atomicAdd(&mine[4 * static_cast<int>(j)], add);
       }
     }
   }
   __syncthreads();
   const size_t at = static_cast<size_t>(row) * a.chunks + chunk;
-  for (int j = threadIdx.x; j < kBins; j += kT) a.hist[at * kBins + j] = hist[j];
+  for (int j = threadIdx.x; j < kBins; j += kT) {
+    const uint4 h = hist[j];
+    a.hist[at * kBins + j] = h.x + h.y + h.z + h.w;
+  }
   if (threadIdx.x == 0) {
     a.chunk_top[at] = top;
     if (chunk == 0) a.row_info[row].listed = 0;
@@ -260,6 +284,7 @@ template <typename T>
 __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
   __shared__ int cnt_part[kWaves], found[3], n_list, base_list;
   __shared__ double mass_part[kWaves];
+  __shared__ float borders[4];
   __shared__ unsigned long long sums[2];
   __shared__ uint64_t list[kListPart];
   const int row = blockIdx.y, chunk = blockIdx.x, lane = threadIdx.x & 63, tid = threadIdx.x;
@@ -278,93 +303,125 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
   if (tid < 3) found[tid] = kBins - 1;
   if (tid == 0) n_list = 0;
   if (tid < 2) sums[tid] = 0;
-  uint64_t h = 0;
-  for (int c0 = 0; c0 < a.chunks; c0 += kSampleMaxChunks / 2) {      // (half of the loads in flight: the second half is often empty)
+  const int mode = top == -INFINITY ? kModeEmpty : origin >= kFar || origin <= kBins - kFar ? kModeScan : st.k > 0 ? kModeTopK : st.p < 1.0 ? kModeTopP : kModeAll;
+  const float bottom = top - 100.f * kPerNat / st.s;
+  const Scale z = {st.c, static_cast<double>(top) * st.c};
+  if (mode == kModeTopK || mode == kModeTopP) {
+    uint32_t h = 0;
+    for (int c0 = 0; c0 < a.chunks; c0 += kSampleMaxChunks / 2) {      // (half of the loads in flight: the second half is often empty)
 #pragma unroll
-    for (int e = 0; e < kSampleMaxChunks / 2; ++e) {
-      const int c = c0 + e, by = c < a.chunks ? __builtin_amdgcn_readlane(behind, c & 63) : kBins;
-      const uint64_t v = a.hist[(first + min(c, a.chunks - 1)) * kBins + max(tid - by, 0)];
-      h += tid >= by ? v : 0;
+      for (int e = 0; e < kSampleMaxChunks / 2; ++e) {
+        const int c = c0 + e, by = c < a.chunks ? __builtin_amdgcn_readlane(behind, c & 63) : kBins;
+        const uint32_t v = a.hist[(first + min(c, a.chunks - 1)) * kBins + max(tid - by, 0)];
+        h += tid >= by ? v : 0;
+      }
+    }
+    auto first_of = [&](bool reached, int which) {
+      const uint64_t m = __builtin_amdgcn_ballot_w64(reached);
+      if (m && lane == 0) atomicMin(&found[which], 64 * wv + __ffsll(static_cast<unsigned long long>(m)) - 1);
+    };
+    // the bins of the borders: the first whose sum reaches them; of top-p those that 2e-5 more or less could make it (a bin's mass is
+    // known to some 1e-5: half a unit of 2^-16, T in 32 bits, roundings of the exponentials)
+    if (mode == kModeTopK) {
+      int cum = wave_scan(static_cast<int>(h));
+      if (lane == 63) cnt_part[wv] = cum;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) cum += w < wv ? cnt_part[w] : 0;
+      first_of(cum >= st.k, 0);
+    } else {
+      double cum = wave_scan64(static_cast<double>(h) * static_cast<double>(exp2f(static_cast<float>(tid) * (-1.44269504f / kPerNat)))), all = 0.0;
+      if (lane == 63) mass_part[wv] = cum;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        cum += w < wv ? mass_part[w] : 0.0;
+        all += mass_part[w];
+      }
+      first_of(cum >= st.p * all * (1.0 - 2e-5), 1);
+      first_of(cum >= st.p * all * (1.0 + 2e-5), 2);
+    }
+    __syncthreads();
+  }
+  // logits from `sure` on are kept for certain, from `doubt` on the list decides; those below `least` count as none, those below `min_p` are not kept
+  if (mode != kModeEmpty && mode != kModeScan) {
+    if (wv == 0) {
+      const int bin = origin - (mode == kModeTopK ? found[0] : max(found[1], found[2]));
+      const float v = mode == kModeAll ? NAN : least_of([&](float l) { return bin_of(l, st.s) >= bin; });
+      if (lane == 0) borders[0] = v;
+    } else if (wv == 1) {
+      const int bin = origin - found[1] + 1;
+      const float v = mode == kModeAll ? -INFINITY : mode == kModeTopK || found[1] == 0 ? NAN : least_of([&](float l) { return bin_of(l, st.s) >= bin; });
+      if (lane == 0) borders[1] = v;
+    } else if (wv == 2) {
+      const float v = least_of([&](float l) { return l >= top || weight(fmaxf(l, bottom), z) >= kFloor; });
+      if (lane == 0) borders[2] = v;
+    } else if (wv == 3) {
+      const float v = least_of([&](float l) { return l >= top || weight(fmaxf(l, bottom), z) >= st.m; });
+      if (lane == 0) borders[3] = v;
     }
   }
-  const int count = static_cast<int>(h >> kCountBit);
-  const double mass = static_cast<double>(h & ((1ull << kCountBit) - 1)) * static_cast<double>(exp2f(static_cast<float>(tid) * (-1.44269504f / kPerNat)));
-  int cum = wave_scan(count);
-  double cmass = wave_scan64(mass);
-  if (lane == 63) { cnt_part[wv] = cum; mass_part[wv] = cmass; }
   __syncthreads();
-  double all = 0.0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wv) { cum += cnt_part[w]; cmass += mass_part[w]; }
-    all += mass_part[w];
-  }
-  // the bins of the borders: the first whose sum reaches them; of top-p those that 1e-5 more or less could make it (a bin's mass is
-  // known to some 2e-6: T in 32 bits, one rounding of the exponential)
-  const double lo_at = st.p * all * (1.0 - 1e-5), hi_at = st.p * all * (1.0 + 1e-5);
-  auto first_of = [&](bool reached, int which) {
-    const uint64_t m = __builtin_amdgcn_ballot_w64(reached);
-    if (m && lane == 0) atomicMin(&found[which], 64 * wv + __ffsll(static_cast<unsigned long long>(m)) - 1);
-  };
-  first_of(st.k > 0 && cum >= st.k, 0);
-  first_of(cmass >= lo_at, 1);
-  first_of(cmass >= hi_at, 2);
-  __syncthreads();
-  const int mode = top == -INFINITY ? kModeEmpty : origin >= kFar || origin <= -kFar ? kModeScan : st.k > 0 ? kModeTopK : st.p < 1.0 ? kModeTopP : kModeAll;
-  // logits from `sure` on are kept for certain, from `doubt` on the list decides
-  float sure = NAN, doubt = NAN;
-  if (mode == kModeTopK) doubt = least_of(origin - found[0], st.s);
-  if (mode == kModeTopP) {
-    sure = found[1] > 0 ? least_of(origin - found[1] + 1, st.s) : NAN;
-    doubt = least_of(origin - max(found[1], found[2]), st.s);
-  }
-  if (mode == kModeAll) sure = -INFINITY;
+  const float doubt = borders[0], sure = borders[1], least = borders[2], min_p = borders[3];
   if (chunk == 0 && tid == 0) {
     SampleRow& r = a.row_info[row];
     r.mode = mode;
+    r.top = top;
     r.sure = sure;
     r.doubt = doubt;
-    r.top = top;
+    r.least = least;
+    r.min_p = min_p;
   }
   if (mode == kModeEmpty || mode == kModeScan) return;       // uniform
   // ---- the chunk's tokens
   uint64_t total = 0, above = 0;
-  for (int seg = seg0 + wv; seg < seg1; seg += kWaves) {
-    float x[8];
+  auto tokens = [&](auto weighed, auto apart) {    // are weights needed, and those above `sure` apart from those that are kept
+    const float keep = min_p > sure ? min_p : sure;          // (NaN: none)
+    for (int seg = seg0 + wv; seg < seg1; seg += kWaves) {
+      float x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = next[e];
-    if (seg + kWaves < seg1) load_seg<T>(logits, a.V, seg + kWaves, next);
-    uint32_t in_doubt = 0;                        // bit e: token e
-    if (mode == kModeTopK) {
+      for (int e = 0; e < 8; ++e) x[e] = next[e];
+      if (seg + kWaves < seg1) load_seg<T>(logits, a.V, seg + kWaves, next);
+      if (weighed) {
+        uint64_t kept = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) in_doubt |= x[e] >= doubt ? 1u << e : 0u;
-    } else {
-      uint64_t kept = 0;
+        for (int e = 0; e < 8; ++e) {
+          const uint64_t f = biased(weight(x[e] >= least ? x[e] : bottom, z));
+          total += f;
+          if (apart) above += x[e] >= sure ? f : kBias;
+          kept += x[e] >= keep ? f : kBias;
+        }
+        kept -= 8 * kBias;
+        if (!apart) above += kept;
+        kept = wave_sum64(kept);
+        if (lane == 0) a.seg_mass[static_cast<size_t>(row) * a.segs + seg] = kept;
+        total -= 8 * kBias;
+        if (apart) above -= 8 * kBias;
+      }
+      uint64_t in_doubt[8];
+      int found_here = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const double w = weight(x[e], top, st.c);
-        const uint64_t f = fixed(w), in = x[e] >= sure ? f : 0;
-        total += f;
-        above += in;
-        kept += w >= st.m ? in : 0;
-        in_doubt |= x[e] >= doubt && !(x[e] >= sure) ? 1u << e : 0u;
+        in_doubt[e] = __builtin_amdgcn_ballot_w64(x[e] >= doubt) & ~__builtin_amdgcn_ballot_w64(x[e] >= sure);
+        found_here += __popcll(in_doubt[e]);
       }
-      kept = wave_sum64(kept);
-      if (lane == 0) a.seg_mass[static_cast<size_t>(row) * a.segs + seg] = kept;
-    }
-    if (__builtin_amdgcn_ballot_w64(in_doubt != 0) != 0ull) {
-      const int mine = __popc(in_doubt), upto = wave_scan(mine);
-      int at = 0;
-      if (lane == 63) at = atomicAdd(&n_list, upto);
-      at = __builtin_amdgcn_readlane(at, 63) + upto - mine;
+      if (found_here) {                            // uniform
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&n_list, found_here);
+        at = __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (in_doubt >> e & 1u) {
-          if (at < kListPart) list[at] = place_of(x[e], token_of<T>(seg, lane, e));
-          ++at;
-        }
+        for (int e = 0; e < 8; ++e)
+          if (in_doubt[e]) {                       // uniform
+            const int mine = at + static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(in_doubt[e] >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(in_doubt[e]), 0u)));
+            if ((in_doubt[e] >> lane & 1u) && mine < kListPart) list[mine] = place_of(value(x[e]), token_of<T>(seg, lane, e));
+            at += __popcll(in_doubt[e]);
+          }
+      }
     }
-  }
+  };
+  if (mode == kModeTopK) tokens(std::false_type{}, std::false_type{});
+  else if (mode == kModeAll || !(min_p > sure)) tokens(std::true_type{}, std::false_type{});
+  else tokens(std::true_type{}, std::true_type{});
   if (mode == kModeTopP) {
     total = wave_sum64(total);
     above = wave_sum64(above);
@@ -388,6 +445,7 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
 
 // ------------------------------------------------------------------------------------------------------------ 3: the draw
 
+constexpr int kPairs = kT / 4;          // a list that is compared pair by pair
 struct PickLds {
   uint64_t list[kList];
   uint64_t w[kList];                 // the list's weights
@@ -425,9 +483,9 @@ __device__ Border scan_border(const SampleArgs& a, const T* logits, const Settin
       load_seg<T>(logits, a.V, seg, x);
 #pragma unroll 1
       for (int e = 0; e < 8; ++e) {
-        const uint32_t key = key_of(x[e]);
+        const uint32_t key = key_of(value(x[e]));
         if (shift < 24 && key >> (shift + 8) != prefix) continue;
-        const double w = weight(x[e], top, st.c);
+        const double w = weight_far(value(x[e]), top, st.c);
         if (w > 0.0) {
           const uint32_t d = key >> shift & 255u;
           atomicAdd(&s.digit_count[d], 1u);
@@ -459,7 +517,7 @@ __device__ Border scan_border(const SampleArgs& a, const T* logits, const Settin
     before = s.before;
     mass_before = s.mass_before;
   }
-  const uint64_t w = fixed(weight(logit_of(prefix), top, st.c));
+  const uint64_t w = fixed(weight_far(logit_of(prefix), top, st.c));
   int c = s.n_equal;
   if (want > 0) {
     c = min(c, want - static_cast<int>(before));
@@ -559,13 +617,62 @@ __device__ uint64_t list_border(PickLds& s, int n, int want, uint64_t base, doub
   }
 }
 
+// The same for a short list, of both borders at once (k > 0: `total` is of no account): every place against every other, four threads to one.
+__device__ uint64_t pairs_border(PickLds& s, int n, int k, double p, uint64_t base, uint64_t total) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int i = tid >> 2;
+  const uint64_t mine = i < n ? s.list[i] : 0, w = i < n ? s.w[i] : 0;
+  int rank = 0;
+  uint64_t better = 0;
+  for (int j = tid & 3; j < n; j += 4) {
+    const bool b = s.list[j] < mine;
+    rank += b ? 1 : 0;
+    better += b ? s.w[j] : 0;
+  }
+  rank += __shfl_xor(rank, 1);
+  rank += __shfl_xor(rank, 2);
+  better += shfl_xor64(better, 1);
+  better += shfl_xor64(better, 2);
+  bool kept = i < n;
+  if (k > 0) {
+    kept = kept && rank < k;
+    if (p < 1.0) {
+      const uint64_t sum = wave_sum64(kept && (tid & 3) == 0 ? w : 0);
+      if (lane == 0) s.part[wv] = sum;
+      __syncthreads();
+      total = 0;
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) total += s.part[v];
+    }
+  }
+  if (p < 1.0) kept = kept && static_cast<double>(base + better) < fmax(p * static_cast<double>(total), 1.0);
+  const uint64_t last = wave_max64(kept ? mine : 0);
+  if (lane == 63) s.part2[wv] = last;
+  __syncthreads();
+  uint64_t cut = 0;
+#pragma unroll
+  for (int v = 0; v < kWaves; ++v) cut = max(cut, s.part2[v]);
+  return cut;
+}
+
 template <typename T>
 __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
   extern __shared__ uint4 smem4[];
   PickLds& s = *reinterpret_cast<PickLds*>(smem4);
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // (what is needed in any case is requested at once)
+  uint64_t early[2], seg_mass = 0, total = 0, above = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) early[i] = a.list[static_cast<size_t>(row) * kList + i * kT + tid];
+  if (tid < a.segs) seg_mass = a.seg_mass[static_cast<size_t>(row) * a.segs + tid];
+  if (lane < a.chunks) {
+    total = a.chunk_sums[2 * (static_cast<size_t>(row) * a.chunks + lane)];
+    above = a.chunk_sums[2 * (static_cast<size_t>(row) * a.chunks + lane) + 1];
+  }
   const SampleRow info = a.row_info[row];
+  float u = a.u[row];
   const Setting st = setting_of(a, row);
   const T* logits = static_cast<const T*>(a.logits) + static_cast<int64_t>(row) * a.ld;
   const float top = info.top;
@@ -580,7 +687,9 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
   uint64_t cut = ~0ull;
   const bool listed = info.mode == kModeTopK || info.mode == kModeTopP;
   const int n = listed ? info.listed : 0;
-  if (info.mode == kModeScan || n > kList) {
+  const bool scanned = info.mode == kModeScan || n > kList;
+  const Scale z = {st.c, static_cast<double>(top) * st.c};
+  if (scanned) {
     // ---- without histograms and list: a row whose logits are far from anything (2^26 nats), or whose list is too long, as where more than 4096 tokens
     // of nearly one weight lie at the border
     sure = NAN;
@@ -598,7 +707,7 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
             float x[8];
             load_seg<T>(logits, a.V, seg, x);
 #pragma unroll 1
-            for (int e = 0; e < 8; ++e) mine += fixed(weight(x[e], top, st.c));
+            for (int e = 0; e < 8; ++e) mine += fixed(weight_far(value(x[e]), top, st.c));
           }
           mine = wave_sum64(mine);
           if (lane == 0) atomicAdd(&s.wide, static_cast<unsigned long long>(mine));
@@ -615,7 +724,7 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
         load_seg<T>(logits, a.V, seg, x);
         int eq = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) eq += __popcll(__builtin_amdgcn_ballot_w64(x[e] > -INFINITY && key_of(x[e]) == b.key));
+        for (int e = 0; e < 8; ++e) eq += __popcll(__builtin_amdgcn_ballot_w64(x[e] > -INFINITY && key_of(value(x[e])) == b.key));
         if (lane == 0) s.count[seg] = eq;
       }
       __syncthreads();
@@ -625,7 +734,7 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
         int last = INT_MAX;
         for (int r = 0; r < kSeg / 64; ++r) {
           const int i = seg * kSeg + r * 64 + lane;
-          const float l = i < a.V ? value<T>(logits[i]) : -INFINITY;
+          const float l = i < a.V ? value(as_f32(logits[i])) : -INFINITY;
           uint64_t eq = __builtin_amdgcn_ballot_w64(l > -INFINITY && key_of(l) == b.key);
           const int c = __popcll(eq);
           if (left > 0 && left <= c) {
@@ -645,8 +754,8 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
       uint64_t kept = 0;
 #pragma unroll 1
       for (int e = 0; e < 8; ++e) {
-        const double w = weight(x[e], top, st.c);
-        if (w >= st.m && place_of(x[e], token_of<T>(seg, lane, e)) <= cut) kept += fixed(w);
+        const double w = weight_far(value(x[e]), top, st.c);
+        if (w >= st.m && place_of(value(x[e]), token_of<T>(seg, lane, e)) <= cut) kept += fixed(w);
       }
       kept = wave_sum64(kept);
       if (lane == 0) s.seg[seg] = kept;
@@ -655,24 +764,20 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
     __syncthreads();
   } else {
     // ---- the list
-    s.seg[tid] = tid < a.segs && info.mode != kModeTopK ? a.seg_mass[static_cast<size_t>(row) * a.segs + tid] : 0;
+    s.seg[tid] = info.mode != kModeTopK ? seg_mass : 0;
     if (listed) {
       for (int i = tid; i < n; i += kT) {
-        const uint64_t p = a.list[static_cast<size_t>(row) * kList + i];
+        const uint64_t p = i < kT ? early[0] : i < 2 * kT ? early[1] : a.list[static_cast<size_t>(row) * kList + i];
         s.list[i] = p;
-        s.w[i] = fixed(weight(logit_of(~static_cast<uint32_t>(p >> 32)), top, st.c));
+        const float l = logit_of(~static_cast<uint32_t>(p >> 32));
+        s.w[i] = l >= info.least ? fixed(weight(l, z)) : 0;
       }
-      uint64_t total = 0, above = 0;
-      if (info.mode == kModeTopP) {
-        if (lane < a.chunks) {
-          total = a.chunk_sums[2 * (static_cast<size_t>(row) * a.chunks + lane)];
-          above = a.chunk_sums[2 * (static_cast<size_t>(row) * a.chunks + lane) + 1];
-        }
-        total = wave_sum64(total);
-        above = wave_sum64(above);
-      }
+      total = info.mode == kModeTopP ? wave_sum64(total) : 0;
+      above = info.mode == kModeTopP ? wave_sum64(above) : 0;
       __syncthreads();
-      if (info.mode == kModeTopK) {
+      if (n <= kPairs) {
+        cut = pairs_border(s, n, st.k, st.p, above, total);
+      } else if (info.mode == kModeTopK) {
         cut = list_border(s, n, st.k, 0, 0.0);
         if (st.p < 1.0) {
           uint64_t mine = 0;
@@ -690,7 +795,7 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
       }
       for (int i = tid; i < n; i += kT) {
         const uint64_t p = s.list[i];
-        if (p <= cut && s.w[i] > 0 && (st.m <= kFloor || weight(logit_of(~static_cast<uint32_t>(p >> 32)), top, st.c) >= st.m))
+        if (p <= cut && logit_of(~static_cast<uint32_t>(p >> 32)) >= info.min_p)
           atomicAdd(reinterpret_cast<unsigned long long*>(&s.seg[static_cast<uint32_t>(p) / kSeg]), static_cast<unsigned long long>(s.w[i]));
       }
     }
@@ -706,7 +811,6 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
   const uint64_t mass = s.seg[tid], upto = block_scan64(mass, s.part);
   uint64_t all = 0;
   for (int w = 0; w < kWaves; ++w) all += s.part[w];
-  float u = a.u[row];
   if (!(u >= 0.f)) u = 0.f;
   u = fminf(u, 0.99999994f);
   uint64_t x = static_cast<uint64_t>(static_cast<double>(all) * static_cast<double>(u));
@@ -717,9 +821,9 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
   }
   __syncthreads();
   const int idx = s.seg_at * kSeg + tid;
-  const float l = idx < a.V ? value<T>(logits[idx]) : -INFINITY;
-  const double w = weight(l, top, st.c);
-  const bool kept = w >= st.m && (l >= sure || (l >= doubt && place_of(l, idx) <= cut));
+  const float l = idx < a.V ? value(as_f32(logits[idx])) : -INFINITY;
+  const double w = scanned ? weight_far(l, top, st.c) : weight(l >= info.min_p ? l : top, z);
+  const bool kept = (scanned ? w >= st.m : l >= info.min_p) && (l >= sure || (l >= doubt && place_of(l, idx) <= cut));
   const uint64_t sum = s.seg_before + block_scan64(kept ? fixed(w) : 0, s.part2);
   if (kept && sum > x) atomicMin(&s.pick, tid);
   __syncthreads();
@@ -768,7 +872,7 @@ size_t sample_carve(SampleArgs& a, void* base) {
     return r;
   };
   const size_t M = static_cast<size_t>(a.M), C = static_cast<size_t>(a.chunks);
-  a.hist = reinterpret_cast<unsigned long long*>(take(M * C * kBins * 8));
+  a.hist = reinterpret_cast<uint32_t*>(take(M * C * kBins * 4));
   a.chunk_sums = reinterpret_cast<unsigned long long*>(take(M * C * 2 * 8));
   a.seg_mass = reinterpret_cast<unsigned long long*>(take(M * a.segs * 8));
   a.list = reinterpret_cast<unsigned long long*>(take(M * kList * 8));
