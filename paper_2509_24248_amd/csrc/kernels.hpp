@@ -258,6 +258,7 @@ struct QuantCompactArgs {
   const void* block_hidden;
   void* hidden_next;
   int hidden_row_bytes;
+  int moves, tasks;                        // waves that move rows, and all (set by the launch)
 };
 hipError_t launch_quant_compact(const QuantCompactArgs& a, hipStream_t s);
 // k, v: codes; dtype: of q and out

@@ -108,72 +108,80 @@ __global__ __launch_bounds__(kThreads) void k_quant_write(const QuantWriteArgs a
   }
 }
 
-// grid = (KV heads, sequences, layers), as k_kv_compact: every row is read before any is written.  Lane j of every wave holds
-// path entry j, so that what has to move is known after one round to memory.
-constexpr int kItems = 2 * 63 * 8 / kThreads + 1;      // 16-byte pieces of a thread, at most
-
+// A wave per layer, sequence and KV head, and one per sequence that copies its hidden row.  Lane j holds path entry j and where its row
+// comes from and goes to; the rows are then moved by all lanes, D / 16 of them to one, and all are read before any is written.  U: sixteen-byte
+// pieces of a lane.
+template <int D, int U>
 __global__ __launch_bounds__(kThreads) void k_quant_compact(const QuantCompactArgs a) {
-  const int h = blockIdx.x, b = blockIdx.y, layer = blockIdx.z;
   const int lane = threadIdx.x & 63;
-  const int L = a.ctx_len[b];
-  const int m = max(0, min(a.accept_len[b], a.n_q - 1));
-  const int my_node = lane < a.n_q ? a.accept_path[static_cast<size_t>(b) * a.n_q + lane] : -1;
-  const bool in_cache = L >= 0 && static_cast<int64_t>(L) + a.n_q <= a.kv.l_max;
-  if (!in_cache) report_status(a.status, kStatusBadLength);
-  if (h == 0 && layer == 0 && a.block_hidden) {
+  int task = static_cast<int>(blockIdx.x) * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (task >= a.tasks) return;
+  if (task >= a.moves) {
+    const int b = task - a.moves;
     int node = a.last_node[b];
     if (node < 0 || node >= a.n_q) report_status(a.status, kStatusBadNode);
     node = max(0, min(node, a.n_q - 1));
     const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(a.block_hidden) + (static_cast<size_t>(b) * a.n_q + node) * a.hidden_row_bytes);
     uint4* dst = reinterpret_cast<uint4*>(static_cast<char*>(a.hidden_next) + static_cast<size_t>(b) * a.hidden_row_bytes);
-    for (int i = threadIdx.x; i < (a.hidden_row_bytes >> 4); i += kThreads) dst[i] = src[i];
+#pragma unroll 8
+    for (int i = lane; i < (a.hidden_row_bytes >> 4); i += 64) dst[i] = src[i];
+    return;
   }
-  if (!in_cache) return;                               // uniform over the workgroup
-  const uint64_t away = __builtin_amdgcn_ballot_w64(lane < m && my_node != lane + 1);
+  const int layer = task / (a.B * a.kv.Hkv);
+  task -= layer * a.B * a.kv.Hkv;
+  const int b = task / a.kv.Hkv, h = task - b * a.kv.Hkv;
+  const int L = a.ctx_len[b];
+  const int m = max(0, min(a.accept_len[b], a.n_q - 1));
+  const int node = lane < a.n_q ? a.accept_path[static_cast<size_t>(b) * a.n_q + lane] : -1;
+  if (L < 0 || static_cast<int64_t>(L) + a.n_q > a.kv.l_max) {
+    report_status(a.status, kStatusBadLength);
+    return;
+  }
+  const uint64_t away = __builtin_amdgcn_ballot_w64(lane < m && node != lane + 1);
   if (!away) return;
-  const int first = __ffsll(static_cast<unsigned long long>(away)) - 1;
-  const int lpr = a.d >> 4, rows = m - first;          // 16-byte pieces of a row; rows that may move
-  const int items = 2 * rows * lpr;
-  // item: K rows then V rows; -1 where nothing moves
-  auto node_of = [&](int j) {
-    const int node = __shfl(my_node, j, 64);
-    return node >= 1 && node < a.n_q ? node : -1;
+  const int first = __ffsll(static_cast<unsigned long long>(away)) - 1, rows = m - first;      // rows that may move
+  // rows of path entry `lane`; -1 where nothing moves
+  int64_t from = -1, to = -1;
+  if (lane >= first && lane < m) {
+    if (node >= 1 && node < a.n_q) {
+      from = quant_row(a.kv, b, h, L + node, a.status);
+      to = quant_row(a.kv, b, h, L + 1 + lane, a.status);
+      if (from < 0) to = -1;
+    } else {
+      report_status(a.status, kStatusBadNode);
+    }
+  }
+  char* const pool[2] = {static_cast<char*>(a.kv.k) + layer * a.layer_stride, static_cast<char*>(a.kv.v) + layer * a.layer_stride};
+  uint8_t* const ks = static_cast<uint8_t*>(a.kv.ks) + layer * a.scale_stride;
+  uint8_t* const vs = static_cast<uint8_t*>(a.kv.vs) + layer * a.scale_stride;
+  uint8_t k_scale = 0, v_scale = 0;
+  if (to >= 0) { k_scale = ks[from]; v_scale = vs[from]; }
+  constexpr int LPR = D / 16;
+  const int items = 2 * rows * LPR;                    // K rows, then V rows
+  auto row_of = [](int64_t row, int j) {
+    return static_cast<int64_t>(static_cast<uint64_t>(static_cast<uint32_t>(__shfl(static_cast<int>(row >> 32), j))) << 32 | static_cast<uint32_t>(__shfl(static_cast<int>(row), j)));
   };
-  uint4 buf[kItems];
-  int64_t from[kItems];
+  uint4 buf[U];
 #pragma unroll
-  for (int u = 0; u < kItems; ++u) {
-    const int it = threadIdx.x + u * kThreads;
-    const int j = first + min(it, items - 1) % (rows * lpr) / lpr, piece = it % lpr;
-    const int node = node_of(j);
-    from[u] = -1;
-    if (it < items && node < 0) report_status(a.status, kStatusBadNode);
-    if (it < items && node >= 0) from[u] = quant_row(a.kv, b, h, L + node, a.status);
-    if (from[u] >= 0)
-      buf[u] = reinterpret_cast<const uint4*>(static_cast<const char*>(it >= rows * lpr ? a.kv.v : a.kv.k) + layer * a.layer_stride + from[u] * a.d)[piece];
+  for (int u = 0; u < U; ++u) {
+    buf[u] = make_uint4(0, 0, 0, 0);
+    if (64 * u < items) {                              // uniform
+      const int r = (64 * u + lane) / LPR, v = r >= rows;
+      const int j = min(first + r - (v ? rows : 0), 63);
+      const int64_t dst = row_of(to, j), src = row_of(from, j);
+      if (64 * u + lane < items && dst >= 0) buf[u] = *reinterpret_cast<const uint4*>(pool[v] + src * D + (lane % LPR) * 16);
+    }
   }
-  // scale bytes: threads 0 .. 2 rows - 1
-  const int sj = first + min(static_cast<int>(threadIdx.x), 2 * rows - 1) % rows;
-  const int snode = node_of(sj);
-  const bool has_scale = static_cast<int>(threadIdx.x) < 2 * rows && snode >= 0;
-  uint8_t* scales = static_cast<uint8_t*>(static_cast<int>(threadIdx.x) >= rows ? a.kv.vs : a.kv.ks) + layer * a.scale_stride;
-  int64_t sfrom = -1;
-  uint8_t sbyte = 0;
-  if (has_scale) sfrom = quant_row(a.kv, b, h, L + snode, a.status);
-  if (sfrom >= 0) sbyte = scales[sfrom];
-  __syncthreads();
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // (nothing is written before everything has arrived)
 #pragma unroll
-  for (int u = 0; u < kItems; ++u) {
-    const int it = threadIdx.x + u * kThreads;
-    if (from[u] < 0) continue;
-    const int j = first + it % (rows * lpr) / lpr, piece = it % lpr;
-    const int64_t to = quant_row(a.kv, b, h, L + 1 + j, a.status);
-    if (to >= 0) reinterpret_cast<uint4*>(static_cast<char*>(it >= rows * lpr ? a.kv.v : a.kv.k) + layer * a.layer_stride + to * a.d)[piece] = buf[u];
+  for (int u = 0; u < U; ++u) {
+    if (64 * u < items) {
+      const int r = (64 * u + lane) / LPR, v = r >= rows;
+      const int64_t dst = row_of(to, min(first + r - (v ? rows : 0), 63));
+      if (64 * u + lane < items && dst >= 0) *reinterpret_cast<uint4*>(pool[v] + dst * D + (lane % LPR) * 16) = buf[u];
+    }
   }
-  if (sfrom >= 0) {
-    const int64_t to = quant_row(a.kv, b, h, L + 1 + sj, a.status);
-    if (to >= 0) scales[to] = sbyte;
-  }
+  if (to >= 0) { ks[to] = k_scale; vs[to] = v_scale; }
 }
 
 template <typename T>
@@ -196,8 +204,20 @@ bool quant_write_plan(QuantWriteArgs& a) {
 
 hipError_t launch_quant_write(const QuantWriteArgs& a, hipStream_t s) { return a.f32 ? launch_write<float>(a, s) : launch_write<bf16_t>(a, s); }
 
-hipError_t launch_quant_compact(const QuantCompactArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(k_quant_compact, dim3(a.kv.Hkv, a.B, a.n_layers), dim3(kThreads), 0, s, a);
+hipError_t launch_quant_compact(const QuantCompactArgs& args, hipStream_t s) {
+  QuantCompactArgs a = args;
+  a.moves = a.n_layers * a.B * a.kv.Hkv;
+  a.tasks = a.moves + (a.block_hidden ? a.B : 0);
+  const dim3 grid((a.tasks + kThreads / 64 - 1) / (kThreads / 64));
+  // pieces of a lane: 2 (n_q - 1) rows of d bytes over 64 lanes at most; four (a block of 17 at d = 128) hold the registers of sixteen free
+  const bool few = 2 * (a.n_q - 1) * (a.d / 16) <= 4 * 64;
+  if (a.d == 128) {
+    if (few) hipLaunchKernelGGL((k_quant_compact<128, 4>), grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((k_quant_compact<128, 16>), grid, dim3(kThreads), 0, s, a);
+  } else {
+    if (few) hipLaunchKernelGGL((k_quant_compact<64, 4>), grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((k_quant_compact<64, 16>), grid, dim3(kThreads), 0, s, a);
+  }
   return hipGetLastError();
 }
 
