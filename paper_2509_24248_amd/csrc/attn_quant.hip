@@ -81,8 +81,8 @@ __device__ __forceinline__ void load_to_lds4(const void* src, const void* lds_ba
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(l), "v"(src) : "memory");
 }
 
-// parts of the queries: bf16 ones in two e4m3 parts, fp32 ones in three bf16 parts
-template <typename T> struct Parts { static constexpr int q = sizeof(T) == 2 ? 2 : 3; };
+// parts of the queries: bf16 ones in two e4m3 parts, fp32 ones in three bf16 parts; and bf16 parts of the probabilities
+template <typename T> struct Parts { static constexpr int q = sizeof(T) == 2 ? 2 : 3, p = sizeof(T) == 2 ? 1 : 3; };
 
 constexpr int ml_floats(int nk, int rows) { return nk > 1 ? 2 * nk * rows : 0; }
 __host__ __device__ constexpr size_t quant_lds_bytes(int hd, int nk, int rows, int B, bool paged) {
@@ -91,7 +91,7 @@ __host__ __device__ constexpr size_t quant_lds_bytes(int hd, int nk, int rows, i
          (paged ? static_cast<size_t>(kMaxGroups) * sizeof(int) : 0);
 }
 
-template <int HD, typename T, int NK, int NR, int RTW, int PP, int KT>
+template <int HD, typename T, int NK, int NR, int RTW, int KT>
 __global__ __launch_bounds__(64 * NK * NR, NK * NR <= 8 ? 2 : (NK * NR + 3) / 4) void k_quant_attn(const QuantAttnArgs a) {
   constexpr int S = ring_slots(HD, NK);
   constexpr int RP = 16 * NR * RTW;               // query rows covered (padded)
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(64 * NK * NR, NK * NR <= 8 ? 2 : (NK * NR + 3) / 4)
   constexpr int kVAhead = NK * NR <= 8 ? 8 : 3;       // V reads in front of their use, as many as the registers allow
   constexpr int kReq = 2 * kTileP / NR + 1;       // requests of a wave per tile, at least
   constexpr bool kCodes = sizeof(T) == 2;         // the keys' codes are multiplied as they are
-  constexpr int NP = Parts<T>::q;
+  constexpr int NP = Parts<T>::q, PP = Parts<T>::p;
   constexpr int NM = HD == 128 ? NP : 1;          // block-scaled matrix instructions for 16 keys x 16 rows
   constexpr int kKS = HD / 32;                    // k steps of bf16 ones
   constexpr int kDT = HD / 16;
@@ -728,36 +728,49 @@ __global__ __launch_bounds__(256) void k_quant_combine(const QuantAttnArgs a) {
 
 int row_tiles(const QuantAttnArgs& a) { return (a.G * a.n_q + 15) / 16; }
 
-template <int HD, typename T, int NK, int NR, int RTW, int PP, int KT>
+template <int HD, typename T, int NK, int NR, int RTW, int KT>
 hipError_t launch_one(const QuantAttnArgs& a, hipStream_t s) {
   static_assert(quant_lds_bytes(HD, NK, 16 * NR * RTW, kAttnMaxSeqs, true) <= 160 * 1024, "the LDS of a compute unit");
-  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_quant_attn<HD, T, NK, NR, RTW, PP, KT>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_quant_attn<HD, T, NK, NR, RTW, KT>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL((k_quant_attn<HD, T, NK, NR, RTW, PP, KT>), dim3(a.wgrid), dim3(64 * NK * NR), quant_lds_bytes(HD, NK, 16 * NR * RTW, a.B, a.paged != 0), s, a);
+  hipLaunchKernelGGL((k_quant_attn<HD, T, NK, NR, RTW, KT>), dim3(a.wgrid), dim3(64 * NK * NR), quant_lds_bytes(HD, NK, 16 * NR * RTW, a.B, a.paged != 0), s, a);
   return hipGetLastError();
 }
 
+// The form by the number of 16-row tiles: the fewest waves that hold all rows as one ring's, and as many rings as sixteen waves and the LDS of
+// a compute unit take.  One wave of a SIMD alone issues every 5.3 cycles, four together every 2.6 to 4.4, so twelve to sixteen waves are
+// wanted; a wave of two tiles (from seven on) shares the conversion of V.  Microseconds of a call over 8 sequences of 2048 .. 16384 tokens,
+// 8 KV heads, 128-wide (64-wide), against the next form's at the same rows:
+//   rows 16: 31.6, not 35.8 (21.1, 28.2)   28: 34.4, 42.9 (26.3, 33.3)   48: 41.3, 45.9 (31.6, 35.2)   64: 46.4, 60.2 (35.8, 45.5)
+//        72: 59.3, 63.9 (44.4, 45.2)   96: 62.1, 70.8 (46.2, 51.3)   128: 72.5, 76.8 with eight waves of one tile (52.6, 55.7)
+// Probabilities are one bf16 part, off by half a step (2^-8) at most, as the results are rounded anyway; two parts
+// took 34.4 -> 36.4 at 28 rows, 59.3 -> 67.9 at 72.  A step of two tiles (four of 64-wide heads) halves the barriers where the ring's slots
+// allow it: 96 rows 64.6 -> 62.1 (48.8 -> 46.2), 112 rows 71.6 -> 68.9; below it gains nothing or costs (48 rows 40.8 -> 43.0).
 template <int HD> hipError_t launch_bf16(const QuantAttnArgs& a, hipStream_t s) {
   constexpr int K2 = HD == 64 ? 4 : 2;            // tiles of a step
   switch (row_tiles(a)) {
-    case 1: return launch_one<HD, bf16_t, 8, 1, 1, 2, 1>(a, s);
-    case 2: return launch_one<HD, bf16_t, 4, 2, 1, 2, 1>(a, s);
-    case 3: return launch_one<HD, bf16_t, 4, 3, 1, 1, 1>(a, s);
-    case 4: return launch_one<HD, bf16_t, 4, 4, 1, 1, 1>(a, s);
-    case 5: return launch_one<HD, bf16_t, 2, 5, 1, 1, HD == 64 ? 4 : 1>(a, s);
-    case 6: return launch_one<HD, bf16_t, 2, 6, 1, 1, K2>(a, s);
-    default: return launch_one<HD, bf16_t, 2, 4, 2, 1, K2>(a, s);
+    case 1: return launch_one<HD, bf16_t, 8, 1, 1, 1>(a, s);
+    case 2: return launch_one<HD, bf16_t, 4, 2, 1, 1>(a, s);
+    case 3: return launch_one<HD, bf16_t, 4, 3, 1, 1>(a, s);
+    case 4: return launch_one<HD, bf16_t, 4, 4, 1, 1>(a, s);
+    case 5: return launch_one<HD, bf16_t, 2, 5, 1, HD == 64 ? 4 : 1>(a, s);
+    case 6: return launch_one<HD, bf16_t, 2, 6, 1, K2>(a, s);
+    default: return launch_one<HD, bf16_t, 2, 4, 2, K2>(a, s);
   }
 }
 
+// fp32: three parts of queries and probabilities take the registers of sixteen waves.  8 sequences of 500 .. 4000 tokens, 128-wide, against the
+// form of twice the rows: 16 rows 18.1 us, not 24.6; 28 rows 25.3, 31.5; 64 rows 35.6, 49.9.  64-wide: 28 rows 18.9, 24.7; 64 rows 27.1, 34.8.
 hipError_t launch_f32(const QuantAttnArgs& a, hipStream_t s) {
   const int tiles = row_tiles(a);
-  if (a.d == 64) return tiles <= 2 ? launch_one<64, float, 4, 1, 2, 3, 1>(a, s) : tiles <= 4 ? launch_one<64, float, 2, 2, 2, 3, 1>(a, s) : launch_one<64, float, 2, 4, 2, 3, 1>(a, s);
-  if (tiles <= 1) return launch_one<128, float, 4, 1, 1, 3, 1>(a, s);
-  if (tiles <= 2) return launch_one<128, float, 2, 2, 1, 3, 1>(a, s);
-  return tiles <= 4 ? launch_one<128, float, 2, 4, 1, 3, 1>(a, s) : launch_one<128, float, 1, 8, 1, 3, 1>(a, s);
+  if (a.d == 64) return tiles <= 2 ? launch_one<64, float, 4, 1, 2, 1>(a, s) : tiles <= 4 ? launch_one<64, float, 2, 2, 2, 1>(a, s) : launch_one<64, float, 2, 4, 2, 1>(a, s);
+  if (tiles <= 1) return launch_one<128, float, 4, 1, 1, 1>(a, s);
+  if (tiles <= 2) return launch_one<128, float, 2, 2, 1, 1>(a, s);
+  return tiles <= 4 ? launch_one<128, float, 2, 4, 1, 1>(a, s) : launch_one<128, float, 1, 8, 1, 1>(a, s);
 }
 
+// Four waves to an output row while the rows are few: latency is what counts then (one sequence, 28 rows a head: 12.0 us a call, not 13.0);
+// one wave where there are enough rows to fill the chip (8 sequences of 28 rows a head: 36.3 us, not 38.2; of 96 rows: 62.1, 69.6).
 template <typename T, int D> hipError_t launch_combine(const QuantAttnArgs& a, hipStream_t s) {
   const int64_t units = static_cast<int64_t>(a.B) * a.Hkv, rows = static_cast<int64_t>(a.B) * a.n_q * a.Hq;
   if (rows * units > 256 * static_cast<int64_t>(a.wgrid)) hipLaunchKernelGGL((k_quant_combine<T, D, 1>), dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, s, a);
@@ -771,8 +784,9 @@ bool quant_attn_plan(QuantAttnArgs& a, int num_cus) {
   a.use_mfma = kTwoPart;                          // (its maxima are in log2 units)
   a.G = a.Hq / a.Hkv;
   a.g_inv = (65536 + a.G - 1) / a.G;
-  a.pad = a.d == 64 ? 6 : 4;
-  a.wide_from = 2400;
+  // a workgroup's start at a unit costs some eight granules: with 4, 8, 14 the 8 sequences of 28 rows took 36.9, 34.7, 34.8 us
+  a.pad = 8;
+  a.wide_from = 2400;                             // (1000 .. 5000 are alike)
   a.page_shift = (a.page_size & (a.page_size - 1)) == 0 ? 31 - __builtin_clz(static_cast<unsigned>(a.page_size)) : -1;
   if (a.B > kAttnMaxSeqs || a.l_max < a.n_blk) return false;
   const int64_t units = static_cast<int64_t>(a.B) * a.Hkv;
