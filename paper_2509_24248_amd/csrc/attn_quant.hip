@@ -739,12 +739,12 @@ hipError_t launch_one(const QuantAttnArgs& a, hipStream_t s) {
 
 // The form by the number of 16-row tiles: the fewest waves that hold all rows as one ring's, and as many rings as sixteen waves and the LDS of
 // a compute unit take.  One wave of a SIMD alone issues every 5.3 cycles, four together every 2.6 to 4.4, so twelve to sixteen waves are
-// wanted; a wave of two tiles (from seven on) shares the conversion of V.  Microseconds of a call over 8 sequences of 2048 .. 16384 tokens,
+// wanted, evenly over the four SIMDs (five tiles on two rings, three waves to some SIMDs and two to others: 61.5 us, not 57.3); a wave of two tiles (from seven on) shares the conversion of V.  Microseconds of a call over 8 sequences of 2048 .. 16384 tokens,
 // 8 KV heads, 128-wide (64-wide), against the next form's at the same rows:
 //   rows 16: 31.6, not 35.8 (21.1, 28.2)   28: 34.4, 42.9 (26.3, 33.3)   48: 41.3, 45.9 (31.6, 35.2)   64: 46.4, 60.2 (35.8, 45.5)
-//        72: 59.3, 63.9 (44.4, 45.2)   96: 62.1, 70.8 (46.2, 51.3)   128: 72.5, 76.8 with eight waves of one tile (52.6, 55.7)
+//        72: 57.3, 63.9 (40.1, 45.2)   96: 62.1, 70.8 (46.2, 51.3)   128: 72.5, 76.8 with eight waves of one tile (52.6, 55.7)
 // Probabilities are one bf16 part, off by half a step (2^-8) at most, as the results are rounded anyway; two parts
-// took 34.4 -> 36.4 at 28 rows, 59.3 -> 67.9 at 72.  A step of two tiles (four of 64-wide heads) halves the barriers where the ring's slots
+// took 34.4 -> 36.4 at 28 rows, 59.3 -> 67.9 at 72 (on two rings).  A step of two tiles (four of 64-wide heads) halves the barriers where the ring's slots
 // allow it: 96 rows 64.6 -> 62.1 (48.8 -> 46.2), 112 rows 71.6 -> 68.9; below it gains nothing or costs (48 rows 40.8 -> 43.0).
 template <int HD> hipError_t launch_bf16(const QuantAttnArgs& a, hipStream_t s) {
   constexpr int K2 = HD == 64 ? 4 : 2;            // tiles of a step
@@ -753,7 +753,7 @@ template <int HD> hipError_t launch_bf16(const QuantAttnArgs& a, hipStream_t s) 
     case 2: return launch_one<HD, bf16_t, 4, 2, 1, 1>(a, s);
     case 3: return launch_one<HD, bf16_t, 4, 3, 1, 1>(a, s);
     case 4: return launch_one<HD, bf16_t, 4, 4, 1, 1>(a, s);
-    case 5: return launch_one<HD, bf16_t, 2, 5, 1, HD == 64 ? 4 : 1>(a, s);
+    case 5: return launch_one<HD, bf16_t, 3, 5, 1, HD == 64 ? 4 : 1>(a, s);
     case 6: return launch_one<HD, bf16_t, 2, 6, 1, K2>(a, s);
     default: return launch_one<HD, bf16_t, 2, 4, 2, K2>(a, s);
   }
