@@ -286,7 +286,7 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
   __shared__ double mass_part[kWaves];
   __shared__ float borders[4];
   __shared__ unsigned long long sums[2];
-  __shared__ uint64_t list[kListPart];
+  __shared__ uint2 list[kListPart];
   const int row = blockIdx.y, chunk = blockIdx.x, lane = threadIdx.x & 63, tid = threadIdx.x;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const T* logits = static_cast<const T*>(a.logits) + static_cast<int64_t>(row) * a.ld;
@@ -351,7 +351,7 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
       if (lane == 0) borders[0] = v;
     } else if (wv == 1) {
       const int bin = origin - found[1] + 1;
-      const float v = mode == kModeAll ? -INFINITY : mode == kModeTopK || found[1] == 0 ? NAN : least_of([&](float l) { return bin_of(l, st.s) >= bin; });
+      const float v = mode != kModeTopP || found[1] == 0 ? NAN : least_of([&](float l) { return bin_of(l, st.s) >= bin; });
       if (lane == 0) borders[1] = v;
     } else if (wv == 2) {
       const float v = least_of([&](float l) { return l >= top || weight(fmaxf(l, bottom), z) >= kFloor; });
@@ -362,7 +362,7 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
     }
   }
   __syncthreads();
-  const float doubt = borders[0], sure = borders[1], least = borders[2], min_p = borders[3];
+  const float doubt = borders[0], least = borders[2], min_p = borders[3], sure = mode == kModeAll ? min_p : borders[1];
   if (chunk == 0 && tid == 0) {
     SampleRow& r = a.row_info[row];
     r.mode = mode;
@@ -376,7 +376,7 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
   // ---- the chunk's tokens
   uint64_t total = 0, above = 0;
   auto tokens = [&](auto weighed, auto apart) {    // are weights needed, and those above `sure` apart from those that are kept
-    const float keep = min_p > sure ? min_p : sure;          // (NaN: none)
+    const float keep = apart ? min_p : sure;
     for (int seg = seg0 + wv; seg < seg1; seg += kWaves) {
       float x[8];
 #pragma unroll
@@ -409,18 +409,20 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
         int at = 0;
         if (lane == 0) at = atomicAdd(&n_list, found_here);
         at = __builtin_amdgcn_readfirstlane(at);
+        if (at + found_here <= kListPart) {        // (as they are: their places follow when the list is written)
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (in_doubt[e]) {                       // uniform
-            const int mine = at + static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(in_doubt[e] >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(in_doubt[e]), 0u)));
-            if ((in_doubt[e] >> lane & 1u) && mine < kListPart) list[mine] = place_of(value(x[e]), token_of<T>(seg, lane, e));
-            at += __popcll(in_doubt[e]);
-          }
+          for (int e = 0; e < 8; ++e)
+            if (in_doubt[e]) {                     // uniform
+              const uint32_t mine = __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(in_doubt[e] >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(in_doubt[e]), static_cast<uint32_t>(at)));
+              if (__builtin_amdgcn_inverse_ballot_w64(in_doubt[e])) list[mine] = make_uint2(__float_as_uint(x[e]), static_cast<uint32_t>(token_of<T>(seg, lane, e)));
+              at += __popcll(in_doubt[e]);
+            }
+        }
       }
     }
   };
   if (mode == kModeTopK) tokens(std::false_type{}, std::false_type{});
-  else if (mode == kModeAll || !(min_p > sure)) tokens(std::true_type{}, std::false_type{});
+  else if (!(min_p > sure)) tokens(std::true_type{}, std::false_type{});
   else tokens(std::true_type{}, std::true_type{});
   if (mode == kModeTopP) {
     total = wave_sum64(total);
@@ -440,7 +442,7 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
   __syncthreads();
   if (n_list <= kListPart)
     for (int i = tid; i < n_list; i += kT)
-      if (base_list + i < kList) a.list[static_cast<size_t>(row) * kList + base_list + i] = list[i];
+      if (base_list + i < kList) a.list[static_cast<size_t>(row) * kList + base_list + i] = place_of(value(__uint_as_float(list[i].x)), static_cast<int>(list[i].y));
 }
 
 // ------------------------------------------------------------------------------------------------------------ 3: the draw
