@@ -279,7 +279,7 @@ size_t specexit_verify_attn_workspace_bytes(const specexit_kv_view *kv, int32_t 
  * z = hidden . w^T with w [V + n_extra, D]; argmax[r] = lowest index of the maximum of
  * z[r, 0:V].  Rows V.. of w (the widened head's signal rows, Eq. 1) never enter the
  * argmax; their products go to extra_out [M, n_extra].  max_logit, extra_out and
- * logits_dbg ([M, V] fp32, every logit; for tests) may be NULL.  1 <= M <= 144. */
+ * logits_dbg ([M, V] fp32, every logit; what specexit_sample draws from) may be NULL.  1 <= M <= 144. */
 int32_t specexit_lmhead_argmax(int32_t dtype, int32_t M, int32_t D, int32_t V, int32_t n_extra,
                                const void *hidden /*[M,D]*/, const void *w /*[V+n_extra,D]*/,
                                int32_t *argmax /*[M]*/, float *max_logit /*[M]*/,
@@ -379,7 +379,7 @@ int32_t specexit_quant_kv_write(const specexit_quant_kv_view *kv, int32_t dtype,
 /* ---- stage 2 over the 8-bit cache: specexit_verify_attn with such a view (Alg. 1) ----
  * Arguments, masks and limits as there; dtype is that of q and out.  The queries and the
  * cache's numbers are multiplied as they are: nothing is rounded but sums (fp32), probabilities
- * (16 bits; fp32: 24) and the output.  Entries that a row does not see may hold anything, NaN
+ * (to bf16; fp32 results: to 24 bits) and the output.  Entries that a row does not see may hold anything, NaN
  * included; a row that sees nothing (an empty context and an empty mask word) is all zeros. */
 int32_t specexit_quant_verify_attn(const specexit_quant_kv_view *kv, int32_t dtype, int32_t B, int32_t n_q,
                                    int32_t n_q_heads, const void *q, const int32_t *ctx_len /*[B]*/,

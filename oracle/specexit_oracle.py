@@ -22,6 +22,11 @@ What is computed (SpecExit, arXiv 2509.24248):
                     path's K/V entries moved next to the context and the
                     hidden state of the last accepted node: the cache and
                     hidden-state update that closes a round of Alg. 1.
+* quant_rows, dequant_rows
+                  - rows of an 8-bit cache (e4m3 codes, a power of two per row):
+                    verify_attn and kv_compact over them are those above.
+* sample          - a token from logits and a uniform number: temperature,
+                    top-k, top-p, min-p (Alg. 1 samples the target's token).
 * accept_exit     - accepted tokens / accept length / recover token (Alg. 1),
                     EWMA smoothing (Sec. 3.3 "Signal Smoothing", Appendix
                     "Signal Smoothing" EWMA equation, alpha = 0.1; the sliding

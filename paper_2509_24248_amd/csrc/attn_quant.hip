@@ -14,6 +14,13 @@
 //   O^T += V^T P^T : A = V codes, transposed on the way out of LDS (eight keys of a column per lane) and converted to bf16,
 //                 which is exact; B = the probabilities times the keys' scales (powers of two: exact) in PP bf16 parts.
 // 64-wide heads need half the products: the instruction's second half then takes the same codes with the next part of the queries.
+//
+// What bounds it.  Few rows: memory (8 sequences of 2k to 16k tokens, 28 rows a head, 153 MB: 30.5 us = 5.0 TB/s, and 4.6 for the merge).  Many:
+// instructions.  16 rows x 32 keys take a wave some 122 vector instructions of 4.4 cycles - 32 convert V, 8 exponentials of 8.4 - and 256 cycles of
+// matrix instructions on a unit that issues one or the other: 16 sequences of 8k to 32k, 72 rows: 180 to 197 us for 681 MB, 129 at a copy's rate.
+// Short: the split from the lengths, its first loads and the merge (one sequence of 4096: 8.8 and 3.6 us).
+// Tried: both operands of the next tile in registers across the barrier (no gain); two workgroups of five waves per compute unit (slower); three or
+// four row tiles to a wave, one wave a SIMD (slower: 5.3 cycles an instruction); tiles unrolled over the ring's slots (spills).
 #include "attn_sched.hpp"
 #include "common.hpp"
 #include "kernels.hpp"

@@ -7,13 +7,15 @@
 //
 // What a filter keeps is a prefix of the tokens in the order (logit descending, index ascending).  Three launches find it without
 // sorting a row; a row is cut into chunks, so that few rows fill the chip too:
-//   1 k_sample_bins  one pass over the logits: a histogram of every chunk over bins of 1/16 nat of l / T (count and mass of a
-//                    bin in one 64-bit LDS atomic; the bins lie on one grid for all chunks of a row, counted from the chunk's best).
-//   2 k_sample_mass  adds the row's histograms, takes the bins that the borders of top-k and top-p lie in, reads the logits
+//   1 k_sample_bins  one pass over the logits: a histogram of every chunk over bins of 1/16 nat of l / T (counts for top-k, else
+//                    masses for top-p, else none; the bins lie on one grid for all chunks of a row, counted from the chunk's best).
+//   2 k_sample_mass  adds the row's histograms, takes the bins that the borders of top-k and top-p lie in, finds the least logits of
+//                    those (a search over the keys of all floats: what follows compares logits, not weights or bins), reads the logits
 //                    again: masses of what is kept for certain per segment of 512 tokens, and a list of the tokens in doubt.
 //   3 k_sample_pick  a workgroup per row finds the border in the list (at most 4096), the draw's segment and in it the token.
-// Bound by memory at many rows: the logits are read twice, the second time mostly from the last-level cache; at few rows
-// by the latencies of three launches.
+// What bounds it: 144 rows of 151936 fp32 logits (87.5 MB, 16.6 us at a copy's rate) take 20.5 us in the first kernel (4.3 TB/s), 34 in the
+// second (vector instructions, 84 % of its time: fifteen in 64 bits and as many others for a token's weight) and 12 in the third; 7 rows with
+// top-k 4.3, 7.7 and 6.4 us: chains of dependent loads, five in the last.  One pass that kept every weight would write as much as it reads.
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -29,6 +31,7 @@ constexpr int kWaves = kT / 64;
 constexpr int kSeg = 512;               // tokens of a segment (a wave's step; a workgroup's in the last kernel)
 constexpr int kBins = 512;              // bins of a histogram: 32 nats
 constexpr float kPerNat = 16.f;
+static_assert(kBins == kT, "a thread per bin");
 constexpr int kChunkSegs = 64;          // segments of a chunk, at most
 constexpr int kList = 4096, kListPart = 2048;      // tokens in doubt of a row, and of one of its chunks
 constexpr int kFar = 1 << 29;           // bins are forced into -kFar .. kFar
@@ -209,7 +212,8 @@ template <typename T> __device__ __forceinline__ void load_seg(const T* row, int
 
 template <typename T>
 __global__ __launch_bounds__(kT) void k_sample_bins(const SampleArgs a) {
-  __shared__ uint4 hist[kBins];        // four copies of a bin: the lanes of a wave that meet in a bin add one after the other
+  __shared__ uint4 hist[kBins];        // four copies of a bin: the lanes of a wave that meet in a bin add one after the other (64-bit sums in
+                                       // one copy, counts and masses together, took 28.7 us for the 144 rows)
   __shared__ float best[kWaves];
   const int row = blockIdx.y, chunk = blockIdx.x, lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -447,7 +451,8 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
 
 // ------------------------------------------------------------------------------------------------------------ 3: the draw
 
-constexpr int kPairs = kT / 4;          // a list that is compared pair by pair
+constexpr int kPairs = kT / 4;          // tokens of a list that is compared pair by pair: both borders at once, in place of two selections of two or
+                                        // three rounds with six meetings of the workgroup each (7 rows with top-k 20 to 50: 9.8 -> 6.4 us)
 struct PickLds {
   uint64_t list[kList];
   uint64_t w[kList];                 // the list's weights
@@ -854,7 +859,8 @@ size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 void sample_plan(SampleArgs& a) {
   a.segs = (a.V + kSeg - 1) / kSeg;
-  // two workgroups per compute unit where the rows are few, no more than twenty to a row: each of the second kernel's reads the histograms of all
+  // two workgroups per compute unit where the rows are few, no more than twenty to a row: each of the second kernel's reads the histograms of all.
+  // (7 rows: 12 chunks 19.1 us, 20 18.4, 32 19.4; 48 rows: 6 chunks 33.0, 11 32.3, 20 38.5; 144 rows, 5 chunks 64.5, 10 68.0)
   int chunks = (512 + a.M - 1) / a.M;
   if (chunks > kSampleMaxChunks) chunks = kSampleMaxChunks;
   if (chunks > (a.segs + kWaves - 1) / kWaves) chunks = (a.segs + kWaves - 1) / kWaves;

@@ -66,10 +66,11 @@ def attn(cache, q, L, mask=None, scale=None, dtype="bf16", flags=0, view=None):
     return out.float().cpu().numpy()
 
 
-def attn_bound(ref, q, k, v, n, scale, dtype):
+def attn_bound(ref, weighed, q, k, v, n, scale, dtype):
     """How far the result may be off, element by element.
 
-    bf16: the output's rounding (half a step, 2^-8 of the value); probabilities in two bf16 parts, 2^-16 of each; a score's sum drops from
+    bf16: the output's rounding (half a step, 2^-8 of the value); the probabilities' roundings, half a step each: the scale of a V row is a power of
+    two, so sum p |v| of the row's own probabilities (`weighed`) times 2^-8 at most; a score's sum drops from
     each of the d products of a part what lies 2^-23 below the largest one, d 2^-23 scale max|q| max|k| for the first part and a sixteenth of it for
     the second, which moves a probability by that and the normaliser by as much again; sums over n keys in fp32, 2^-23 n.
     fp32: products are exact, sums of d and of n numbers in fp32: 2^-23 (d + n) of the absolute ones."""
@@ -77,7 +78,7 @@ def attn_bound(ref, q, k, v, n, scale, dtype):
     top = scale * np.nanmax(np.abs(q)) * np.nanmax(np.abs(k))
     vmax = np.nanmax(np.abs(v))
     if dtype == "bf16":
-        return 2.0 ** -8 * np.abs(ref) + vmax * (2.0 ** -15 + 2.2 * d * 2.0 ** -23 * top + n * 2.0 ** -23)
+        return 2.0 ** -8 * (np.abs(ref) + weighed) + vmax * (2.0 ** -15 + 2.2 * d * 2.0 ** -23 * top + n * 2.0 ** -23)
     return 2.0 ** -23 * np.abs(ref) + vmax * (2.0 ** -22 + 2 * d * 2.0 ** -23 * top + n * 2.0 ** -23)
 
 
@@ -88,11 +89,12 @@ def check_attn(cache, q, L, mask=None, scale=None, dtype="bf16", got=None, only=
     if got is None:
         got = attn(cache, q, L, mask, scale, dtype)
     ref = O.verify_attn(q, k, v, L, mask, scale, cache.table, cache.page or 16, only)
+    weighed = O.verify_attn(q, k, np.abs(v), L, mask, scale, cache.table, cache.page or 16, only)
     if only is not None:
         sel = tuple(np.array(only).T)
-        got, ref = got[sel], ref[sel]
+        got, ref, weighed = got[sel], ref[sel], weighed[sel]
     assert np.isfinite(got).all()
-    bound = attn_bound(ref, q, k, v, int(max(L)) + q.shape[1], scale, dtype)
+    bound = attn_bound(ref, weighed, q, k, v, int(max(L)) + q.shape[1], scale, dtype)
     over = np.abs(got - ref) / bound
     assert over.max() <= 1.0, (float(over.max()), float(np.abs(got - ref).max()))
     return float(over.max())

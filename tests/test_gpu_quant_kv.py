@@ -210,3 +210,9 @@ def test_bad_nodes_lengths_and_pages_move_nothing_and_are_reported():
         lib.specexit_set_dev_status(None)
     for a, w in zip(t, want):
         np.testing.assert_array_equal(a.cpu().numpy(), w)
+
+
+@pytest.mark.parametrize("d,page,n_q", [(128, 16, 17), (128, None, 18), (128, 16, 33), (64, None, 33), (64, 16, 34), (64, 16, 64)])
+def test_rows_of_a_wave(d, page, n_q):
+    """Blocks on both sides of the size up to which a lane moves four pieces."""
+    test_accepted_path_moves("bf16", d, page, 2, n_q)

@@ -127,7 +127,8 @@ def test_rounds(dtype, page, tree):
                         codes[at], sc[at] = cq[b, i], sq[b, i]
             k, v = cache.values()
             ref = O.verify_attn(x["q"], k, v, L, mask, scale, cache.table, page or 16)
-            err = np.abs(out.float().cpu().numpy() - ref) / attn_bound(ref, x["q"], k, v, int(L.max()) + n_q, scale, dtype)
+            weighed = O.verify_attn(x["q"], k, np.abs(v), L, mask, scale, cache.table, page or 16)
+            err = np.abs(out.float().cpu().numpy() - ref) / attn_bound(ref, weighed, x["q"], k, v, int(L.max()) + n_q, scale, dtype)
             assert err.max() <= 1.0, float(err.max())
             # ---- head, draws, acceptance
             np.testing.assert_array_equal(logits.cpu().numpy(), z)

@@ -229,3 +229,36 @@ def test_replays_on_a_stream_of_its_own():
                 assert torch.equal(out[0], got), rep
         finally:
             lib.specexit_graph_destroy(graph)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_lists_of_every_length(dtype):
+    """The tokens that a border lies among: fewer than the threads that compare them pair by pair, as many, more; with ties in bf16."""
+    rng = np.random.default_rng(31)
+    ks = [1, 2, 31, 63, 64, 65, 120, 126, 127, 128, 129, 130, 255, 256, 257, 511, 512, 513, 1000, 1024]
+    ps = [1.0, 0.9, 0.3, 0.0]
+    kw = dict(top_k=np.repeat(ks, len(ps)), top_p=np.tile(ps, len(ks)))
+    M = len(kw["top_k"])
+    x = (rng.standard_normal((M, 3001)) * 2).astype(np.float32)
+    check(x, rng.random(M).astype(np.float32), dtype, **kw)
+
+
+def test_min_p_inside_and_outside_the_nucleus():
+    rng = np.random.default_rng(32)
+    M = 16
+    x = head_like(rng, M, 32003)
+    check(x, rng.random(M).astype(np.float32), temperature=[0.6, 1.3] * 8, top_p=[0.9999, 0.9999, 0.5, 0.5] * 4,
+          min_p=[0.3, 1e-6, 0.9, 1e-3, 1.0, 1e-9, 0.01, 0.0] * 2)
+
+
+def test_logits_far_from_zero():
+    """Around 2^25 temperatures the bins end: rows on both sides, of both signs, with and without borders."""
+    rng = np.random.default_rng(33)
+    V = 700
+    tops = [3.2e7, 3.3554e7, 3.36e7, 1e9, -3.2e7, -3.35539e7, -3.3556e7, -3.4e7, -1e9]
+    x = np.stack([t - 4.0 * rng.integers(0, 10, V) for t in tops] * 4).astype(np.float32)
+    n = len(tops)
+    kw = dict(top_k=[0] * n + [20] * n + [0] * n + [300] * n, top_p=[1.0] * n + [1.0] * n + [0.9] * n + [0.8] * n)
+    check(x, rng.random(len(x)).astype(np.float32), **kw)
+    kw["temperature"] = [0.5] * n + [2.0] * n + [8.0] * n + [20.0] * n
+    check(x, rng.random(len(x)).astype(np.float32), **kw)

@@ -148,3 +148,11 @@ def test_page_tables_of_any_length_are_split(page_size):
     for pages in (1, 64, 8192, 1 << 15):
         kv = paged(page_size=page_size, max_pages_per_seq=pages, n_pages=1 << 20)
         assert sx.specexit_quant_verify_attn_workspace_bytes(kv, sx.BF16, 16, 7, 32) > 0, (pages, sx.last_error())
+
+
+def test_calls_of_more_than_a_launch_are_refused():
+    from paper_2509_24248_amd import binding as sx
+    kv = view()
+    for B, T in ((1, 2 ** 31 - 1), (2 ** 31 - 1, 1), (2 ** 31 - 1, 2 ** 31 - 1)):
+        refused(sx, write(sx, kv, B=B, T=T), sx.EUNSUPPORTED, "more than one call takes")
+    refused(sx, compact(sx, kv, B=65535, layers=65535), sx.EUNSUPPORTED, "grid")
