@@ -289,7 +289,7 @@ struct SampleArgs {
   int segs, chunk_segs, chunks;                  // sample_plan
   uint32_t* hist;                                // sample_carve
   unsigned long long *chunk_sums, *seg_mass, *list;
-  float* chunk_top;
+  float4* chunk_top;         // of a chunk: the best logit, the least that weighs beside it, by what power of two its bins are finer
   SampleRow* row_info;
 };
 void sample_plan(SampleArgs& a);

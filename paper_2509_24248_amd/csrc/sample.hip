@@ -32,6 +32,8 @@ constexpr int kSeg = 512;               // tokens of a segment (a wave's step; a
 constexpr int kBins = 512;              // bins of a histogram: 32 nats
 constexpr float kPerNat = 16.f;
 static_assert(kBins == kT, "a thread per bin");
+constexpr int kFinest = 12;             // bins are 1/16 nat to 2^-16 nat
+constexpr float kWide = 128.f;          // a row whose logits span that many bins has no finer ones
 constexpr int kChunkSegs = 64;          // segments of a chunk, at most
 constexpr int kList = 4096, kListPart = 2048;      // tokens in doubt of a row, and of one of its chunks
 constexpr int kFar = 1 << 29;           // bins are forced into -kFar .. kFar
@@ -208,13 +210,20 @@ template <typename T> __device__ __forceinline__ void load_seg(const T* row, int
   }
 }
 
+// Halvings of the bins, up to kFinest, that leave the logits low .. top within kBins of them, and their numbers below 2^28.
+__device__ __forceinline__ int finer_of(float top, float low, float s) {
+  const float span = top > -INFINITY ? (top - low) * s : static_cast<float>(kBins);            // (NaN where they are infinite: no halving either way)
+  return max(0, min(min(ilogbf(510.f / fmaxf(span, 0.0625f)), ilogbf(268435456.f / fmaxf(fabsf(top * s), 1.f))), kFinest));
+}
+
 // ------------------------------------------------------------------------------------------------------------ 1: histograms
 
 template <typename T>
 __global__ __launch_bounds__(kT) void k_sample_bins(const SampleArgs a) {
   __shared__ uint4 hist[kBins];        // four copies of a bin: the lanes of a wave that meet in a bin add one after the other (64-bit sums in
                                        // one copy, counts and masses together, took 28.7 us for the 144 rows)
-  __shared__ float best[kWaves];
+  __shared__ float best[kWaves], lowest[kWaves];
+  __shared__ int wide;
   const int row = blockIdx.y, chunk = blockIdx.x, lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const T* logits = static_cast<const T*>(a.logits) + static_cast<int64_t>(row) * a.ld;
@@ -239,32 +248,60 @@ __global__ __launch_bounds__(kT) void k_sample_bins(const SampleArgs a) {
     for (int e = 0; e < 8; ++e) top = fmaxf(top, x[i][e]);
   top = wave_max_dpp(top);
   if (lane == 0) best[wv] = top;
+  if (threadIdx.x == 0) wide = 0;
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) top = fmaxf(top, best[w]);
   const bool counts = st.k > 0, masses = !counts && st.p < 1.0;        // what the borders need
   if (!counts && !masses) {
     if (threadIdx.x == 0) {
-      a.chunk_top[static_cast<size_t>(row) * a.chunks + chunk] = top;
+      a.chunk_top[static_cast<size_t>(row) * a.chunks + chunk] = make_float4(top, top, 0.f, 0.f);
       if (chunk == 0) a.row_info[row].listed = 0;
     }
     return;                            // uniform
   }
+  // Rows whose logits lie close together get finer bins, 2^finer of them in 1/16 nat: as fine as the span of what weighs anything allows
+  // (with bins of 1/16 nat only, top-p of 151936 logits of spread 0.3 left 7600 tokens in doubt).
+  // (an eighth of the tokens is enough to tell that a row is wide; 4096 nats away are masked ones)
+  bool far = false;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float d = (top - x[i][0]) * st.s;
+    far |= d >= kWide && d < 4096.f * kPerNat;
+  }
+  if (__builtin_amdgcn_ballot_w64(far) != 0ull && lane == 0) wide = 1;
+  __syncthreads();
+  int finer = 0;
+  float low = -INFINITY;
+  if (!wide && top > -INFINITY) {      // uniform
+    low = top;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) low = (top - x[i][e]) * st.s < static_cast<float>(kBins) ? fminf(low, x[i][e]) : low;
+    low = -wave_max_dpp(-low);
+    if (lane == 0) lowest[wv] = low;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) low = fminf(low, lowest[w]);
+    finer = finer_of(top, low, st.s);
+  }
+  const float s = ldexpf(st.s, finer), step = ldexpf(-1.44269504f / kPerNat, -finer);
   // (whole numbers below 2^29, or the row goes another way: their differences are exact)
-  const float origin = floorf(top * st.s);
+  const float origin = floorf(top * s);
   uint32_t* const mine = reinterpret_cast<uint32_t*>(hist) + (lane & 3);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     if (seg0 + wv + i * kWaves >= seg1) break;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float l = x[i][e], prod = l * st.s, g = floorf(prod), j = origin - g;
+      const float l = x[i][e], prod = l * s, g = floorf(prod), j = origin - g;
       if (j < static_cast<float>(kBins)) {
         uint32_t add = 1;
         if (masses) {                  // uniform
           // how far below the bin's upper edge, in bins: the product's rounding error counts as well
-          const float below = fminf(fmaxf((g - prod) + 1.f - fmaf(l, st.s, -prod), 0.f), 1.f);
-          add = static_cast<uint32_t>(fmaf(__builtin_amdgcn_exp2f(below * (-1.44269504f / kPerNat)), 65536.f, 0.5f));
+          const float below = fminf(fmaxf((g - prod) + 1.f - fmaf(l, s, -prod), 0.f), 1.f);
+          add = static_cast<uint32_t>(fmaf(__builtin_amdgcn_exp2f(below * step), 65536.f, 0.5f));
         }
         atomicAdd(&mine[4 * static_cast<int>(j)], add);
       }
@@ -277,7 +314,7 @@ __global__ __launch_bounds__(kT) void k_sample_bins(const SampleArgs a) {
     a.hist[at * kBins + j] = h.x + h.y + h.z + h.w;
   }
   if (threadIdx.x == 0) {
-    a.chunk_top[at] = top;
+    a.chunk_top[at] = make_float4(top, low, static_cast<float>(finer), 0.f);
     if (chunk == 0) a.row_info[row].listed = 0;
   }
 }
@@ -289,7 +326,7 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
   __shared__ int cnt_part[kWaves], found[3], n_list, base_list;
   __shared__ double mass_part[kWaves];
   __shared__ float borders[4];
-  __shared__ unsigned long long sums[2];
+  __shared__ unsigned long long sums[2], merged[kBins];
   __shared__ uint2 list[kListPart];
   const int row = blockIdx.y, chunk = blockIdx.x, lane = threadIdx.x & 63, tid = threadIdx.x;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -298,12 +335,25 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
   float next[8];                                  // (the first tokens are requested with everything else)
   if (seg0 + wv < seg1) load_seg<T>(logits, a.V, seg0 + wv, next);
   const size_t first = static_cast<size_t>(row) * a.chunks;
-  const float chunk_top = lane < a.chunks ? a.chunk_top[first + lane] : -INFINITY;
+  const float4 chunk_at = lane < a.chunks ? a.chunk_top[first + lane] : make_float4(-INFINITY, -INFINITY, 0.f, 0.f);
+  const float chunk_top = chunk_at.x;
   const Setting st = setting_of(a, row);
   // ---- the row's best logit and its histogram: thread j has bin j, lane c how far chunk c's bins lie behind it
   const float top = wave_max_dpp(chunk_top);
-  const int origin = bin_of(top, st.s);
-  const int behind = chunk_top > -INFINITY ? origin - bin_of(chunk_top, st.s) : kBins;
+  // (bins as wide as the chunk with the widest ones has them, and as the span of the whole row wants them: those of the others are halves,
+  // quarters, .. of them.  Chunks without a token within 32 nats do not count.)
+  const bool counts = chunk_top > -INFINITY && (top - chunk_top) * st.s < static_cast<float>(kBins);
+  int finer = 0;
+  if (__builtin_amdgcn_ballot_w64(counts && chunk_at.z == 0.f) == 0ull) {
+    const float low = -wave_max_dpp(counts ? -chunk_at.y : -INFINITY);
+    finer = min(finer_of(top, low, st.s), static_cast<int>(-wave_max_dpp(counts ? -chunk_at.z : -static_cast<float>(kFinest))));
+  }
+  const float s = ldexpf(st.s, finer);
+  const int origin = bin_of(top, s);
+  const int split = counts ? static_cast<int>(chunk_at.z) - finer : 0;
+  const int chunk_origin = bin_of(chunk_top, ldexpf(s, split));
+  const int behind = counts ? origin - chunk_origin : kBins;      // (where the grids are the same)
+  const bool same = __builtin_amdgcn_ballot_w64(split != 0) == 0ull;
   if (tid < 3) found[tid] = kBins - 1;
   if (tid == 0) n_list = 0;
   if (tid < 2) sums[tid] = 0;
@@ -311,8 +361,29 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
   const float bottom = top - 100.f * kPerNat / st.s;
   const Scale z = {st.c, static_cast<double>(top) * st.c};
   if (mode == kModeTopK || mode == kModeTopP) {
-    uint32_t h = 0;
-    for (int c0 = 0; c0 < a.chunks; c0 += kSampleMaxChunks / 2) {      // (half of the loads in flight: the second half is often empty)
+    uint64_t h = 0;                               // (sums of 2^18 tokens' 2^16)
+    double unit = 1.0;
+    if (!same) {
+      // bins of finer grids, thread j the j-th of every chunk: their counts, or masses below the upper edge of the bin they lie in, are added there
+      merged[tid] = 0;
+      __syncthreads();
+      for (int c = 0; c < a.chunks; ++c) {
+        const int by = __builtin_amdgcn_readlane(split, c);
+        const int fine = __builtin_amdgcn_readlane(chunk_origin, c) - tid, at = origin - (fine >> by);
+        const uint32_t v = __builtin_amdgcn_readlane(static_cast<int>(counts), c) != 0 ? a.hist[(first + c) * kBins + tid] : 0;
+        if (v == 0 || at >= kBins) continue;
+        uint64_t add = v;
+        if (mode == kModeTopP) {
+          const int under = (1 << by) - 1 - (fine & ((1 << by) - 1));
+          add = static_cast<uint64_t>(static_cast<double>(v) * static_cast<double>(exp2f(static_cast<float>(under) * ldexpf(-1.44269504f / kPerNat, -finer - by))) * 1024.0);
+        }
+        atomicAdd(&merged[at], static_cast<unsigned long long>(add));
+      }
+      __syncthreads();
+      h = merged[tid];
+      if (mode == kModeTopP) unit = 1.0 / 1024.0;
+    }
+    for (int c0 = 0; same && c0 < a.chunks; c0 += kSampleMaxChunks / 2) {      // (half of the loads in flight: the second half is often empty)
 #pragma unroll
       for (int e = 0; e < kSampleMaxChunks / 2; ++e) {
         const int c = c0 + e, by = c < a.chunks ? __builtin_amdgcn_readlane(behind, c & 63) : kBins;
@@ -334,7 +405,7 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
       for (int w = 0; w < kWaves; ++w) cum += w < wv ? cnt_part[w] : 0;
       first_of(cum >= st.k, 0);
     } else {
-      double cum = wave_scan64(static_cast<double>(h) * static_cast<double>(exp2f(static_cast<float>(tid) * (-1.44269504f / kPerNat)))), all = 0.0;
+      double cum = wave_scan64(unit * static_cast<double>(h) * static_cast<double>(exp2f(static_cast<float>(tid) * ldexpf(-1.44269504f / kPerNat, -finer)))), all = 0.0;
       if (lane == 63) mass_part[wv] = cum;
       __syncthreads();
 #pragma unroll
@@ -351,11 +422,11 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
   if (mode != kModeEmpty && mode != kModeScan) {
     if (wv == 0) {
       const int bin = origin - (mode == kModeTopK ? found[0] : max(found[1], found[2]));
-      const float v = mode == kModeAll ? NAN : least_of([&](float l) { return bin_of(l, st.s) >= bin; });
+      const float v = mode == kModeAll ? NAN : least_of([&](float l) { return bin_of(l, s) >= bin; });
       if (lane == 0) borders[0] = v;
     } else if (wv == 1) {
       const int bin = origin - found[1] + 1;
-      const float v = mode != kModeTopP || found[1] == 0 ? NAN : least_of([&](float l) { return bin_of(l, st.s) >= bin; });
+      const float v = mode != kModeTopP || found[1] == 0 ? NAN : least_of([&](float l) { return bin_of(l, s) >= bin; });
       if (lane == 0) borders[1] = v;
     } else if (wv == 2) {
       const float v = least_of([&](float l) { return l >= top || weight(fmaxf(l, bottom), z) >= kFloor; });
@@ -884,7 +955,7 @@ size_t sample_carve(SampleArgs& a, void* base) {
   a.chunk_sums = reinterpret_cast<unsigned long long*>(take(M * C * 2 * 8));
   a.seg_mass = reinterpret_cast<unsigned long long*>(take(M * a.segs * 8));
   a.list = reinterpret_cast<unsigned long long*>(take(M * kList * 8));
-  a.chunk_top = reinterpret_cast<float*>(take(M * C * 4));
+  a.chunk_top = reinterpret_cast<float4*>(take(M * C * 16));
   a.row_info = reinterpret_cast<SampleRow*>(take(M * sizeof(SampleRow)));
   return off;
 }

@@ -262,3 +262,21 @@ def test_logits_far_from_zero():
     check(x, rng.random(len(x)).astype(np.float32), **kw)
     kw["temperature"] = [0.5] * n + [2.0] * n + [8.0] * n + [20.0] * n
     check(x, rng.random(len(x)).astype(np.float32), **kw)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sd", [1e-4, 0.01, 0.1, 0.4])
+def test_flat_rows_of_a_long_vocabulary(dtype, sd):
+    """More tokens than 2^16 close together: sums of a bin, bins of their width, borders among thousands; with an offset, and with one stretch
+    of the row lower, higher, or closer together than the rest."""
+    rng = np.random.default_rng(34)
+    V = 200003
+    x = (rng.standard_normal((6, V)) * sd).astype(np.float32)
+    x[1] += 300.0
+    x[2, 60000:90000] -= 5.0
+    x[3, 150000:] += 7.0
+    x[4, :33000] *= 0.001
+    x[5, 70000:140000] = -1e30
+    x[5, 3] = 4.0
+    for kw in (dict(top_p=[0.9]), dict(top_k=[1000], top_p=[0.8]), dict(top_p=[0.3], min_p=[0.9])):
+        check(x, rng.random(6).astype(np.float32), dtype, per=6, **kw)
