@@ -8,14 +8,16 @@
 // What a filter keeps is a prefix of the tokens in the order (logit descending, index ascending).  Three launches find it without
 // sorting a row; a row is cut into chunks, so that few rows fill the chip too:
 //   1 k_sample_bins  one pass over the logits: a histogram of every chunk over bins of 1/16 nat of l / T (counts for top-k, else
-//                    masses for top-p, else none; the bins lie on one grid for all chunks of a row, counted from the chunk's best).
-//   2 k_sample_mass  adds the row's histograms, takes the bins that the borders of top-k and top-p lie in, finds the least logits of
+//                    masses for top-p, else none; counted from the chunk's best, and halved as often as the span of its logits allows).
+//   2 k_sample_mass  adds the row's histograms (the grids of two chunks differ by powers of two), takes the bins that the borders of top-k and top-p lie in, finds the least logits of
 //                    those (a search over the keys of all floats: what follows compares logits, not weights or bins), reads the logits
 //                    again: masses of what is kept for certain per segment of 512 tokens, and a list of the tokens in doubt.
 //   3 k_sample_pick  a workgroup per row finds the border in the list (at most 4096), the draw's segment and in it the token.
-// What bounds it: 144 rows of 151936 fp32 logits (87.5 MB, 16.6 us at a copy's rate) take 20.5 us in the first kernel (4.3 TB/s), 34 in the
+// Rows without any difference need no border but a number.  What is left without a list (more than 4096 tokens within 2^-16 nat of a border, and
+// logits beyond 2^25 temperatures) is a selection over the row by the third kernel, 0.4 to 0.8 ms whatever the number of rows.
+// What bounds it: 144 rows of 151936 fp32 logits (87.5 MB, 16.6 us at a copy's rate) take 21 us in the first kernel (4.2 TB/s), 34 in the
 // second (vector instructions, 84 % of its time: fifteen in 64 bits and as many others for a token's weight) and 12 in the third; 7 rows with
-// top-k 4.3, 7.7 and 6.4 us: chains of dependent loads, five in the last.  One pass that kept every weight would write as much as it reads.
+// top-k 4.5, 8 and 6.4 us: chains of dependent loads, five in the last.  One pass that kept every weight would write as much as it reads.
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -40,7 +42,7 @@ constexpr int kFar = 1 << 29;           // bins are forced into -kFar .. kFar
 constexpr double kFix = 35184372088832.0;          // 2^45
 constexpr double kFloor = 9.094947017729282e-13;   // 2^-40
 
-enum { kModeEmpty = 0, kModeAll = 1, kModeTopK = 2, kModeTopP = 3, kModeScan = 4 };
+enum { kModeEmpty = 0, kModeAll = 1, kModeTopK = 2, kModeTopP = 3, kModeScan = 4, kModeEqual = 5 };
 
 // A row's settings, forced into range.
 struct Setting {
@@ -261,7 +263,7 @@ __global__ __launch_bounds__(kT) void k_sample_bins(const SampleArgs a) {
     return;                            // uniform
   }
   // Rows whose logits lie close together get finer bins, 2^finer of them in 1/16 nat: as fine as the span of what weighs anything allows
-  // (with bins of 1/16 nat only, top-p of 151936 logits of spread 0.3 left 7600 tokens in doubt).
+  // (with bins of 1/16 nat only, top-p of 151936 logits of spread 0.3 left 7600 tokens in doubt: 518 us a row in place of 27).
   // (an eighth of the tokens is enough to tell that a row is wide; 4096 nats away are masked ones)
   bool far = false;
 #pragma unroll
@@ -344,9 +346,11 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
   // quarters, .. of them.  Chunks without a token within 32 nats do not count.)
   const bool counts = chunk_top > -INFINITY && (top - chunk_top) * st.s < static_cast<float>(kBins);
   int finer = 0;
+  bool equal = false;                             // all tokens that weigh anything are equal (a row of zeros)
   if (__builtin_amdgcn_ballot_w64(counts && chunk_at.z == 0.f) == 0ull) {
     const float low = -wave_max_dpp(counts ? -chunk_at.y : -INFINITY);
     finer = min(finer_of(top, low, st.s), static_cast<int>(-wave_max_dpp(counts ? -chunk_at.z : -static_cast<float>(kFinest))));
+    equal = low == top;
   }
   const float s = ldexpf(st.s, finer);
   const int origin = bin_of(top, s);
@@ -357,7 +361,7 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
   if (tid < 3) found[tid] = kBins - 1;
   if (tid == 0) n_list = 0;
   if (tid < 2) sums[tid] = 0;
-  const int mode = top == -INFINITY ? kModeEmpty : origin >= kFar || origin <= kBins - kFar ? kModeScan : st.k > 0 ? kModeTopK : st.p < 1.0 ? kModeTopP : kModeAll;
+  const int mode = top == -INFINITY ? kModeEmpty : origin >= kFar || origin <= kBins - kFar ? kModeScan : equal ? kModeEqual : st.k > 0 ? kModeTopK : st.p < 1.0 ? kModeTopP : kModeAll;
   const float bottom = top - 100.f * kPerNat / st.s;
   const Scale z = {st.c, static_cast<double>(top) * st.c};
   if (mode == kModeTopK || mode == kModeTopP) {
@@ -422,7 +426,7 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
   if (mode != kModeEmpty && mode != kModeScan) {
     if (wv == 0) {
       const int bin = origin - (mode == kModeTopK ? found[0] : max(found[1], found[2]));
-      const float v = mode == kModeAll ? NAN : least_of([&](float l) { return bin_of(l, s) >= bin; });
+      const float v = mode != kModeTopK && mode != kModeTopP ? NAN : least_of([&](float l) { return bin_of(l, s) >= bin; });
       if (lane == 0) borders[0] = v;
     } else if (wv == 1) {
       const int bin = origin - found[1] + 1;
@@ -437,7 +441,7 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
     }
   }
   __syncthreads();
-  const float doubt = borders[0], least = borders[2], min_p = borders[3], sure = mode == kModeAll ? min_p : borders[1];
+  const float doubt = borders[0], least = borders[2], min_p = borders[3], sure = mode == kModeAll || mode == kModeEqual ? min_p : borders[1];
   if (chunk == 0 && tid == 0) {
     SampleRow& r = a.row_info[row];
     r.mode = mode;
@@ -532,7 +536,7 @@ struct PickLds {
   unsigned long long digit_mass[256], wide;
   uint32_t digit_count[256];
   int count[kSampleMaxSegs];
-  int pick, seg_at, digit;
+  int pick, seg_at, digit, last;
   uint64_t seg_before, cut;
   // results of a round of a selection
   uint32_t key;
@@ -540,6 +544,21 @@ struct PickLds {
   uint32_t before;
   uint64_t mass_before;
 };
+
+// All segments of a row, four of a wave requested together: f(segment, its tokens of the lane).
+template <typename T, typename F> __device__ __forceinline__ void each_seg(const SampleArgs& a, const T* logits, F f) {
+  constexpr int kAhead = 4;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int seg = wv; seg < a.segs; seg += kAhead * kWaves) {
+    float x[kAhead][8];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (seg + i * kWaves < a.segs) load_seg<T>(logits, a.V, seg + i * kWaves, x[i]);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (seg + i * kWaves < a.segs) f(seg + i * kWaves, x[i]);
+  }
+}
 
 // The token at the end of the best `want` ones (by count), or of those whose better ones sum to less than `target`: its key, how many of its equals belong to them, and
 // their mass.  Radix selection over the whole row, eight bits at a time.  The workgroup's threads all get the results.
@@ -550,45 +569,62 @@ struct Border {
 };
 template <typename T>
 __device__ Border scan_border(const SampleArgs& a, const T* logits, const Setting& st, float top, PickLds& s, int want, double target) {
-  const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   uint32_t prefix = 0, before = 0;
   uint64_t mass_before = 0;
   for (int shift = 24; shift >= 0; shift -= 8) {
     if (tid < 256) { s.digit_mass[tid] = 0; s.digit_count[tid] = 0; }
     __syncthreads();
-    for (int seg = wv; seg < a.segs; seg += kWaves) {
-      float x[8];
-      load_seg<T>(logits, a.V, seg, x);
+    each_seg<T>(a, logits, [&](int, const float (&x)[8]) {
 #pragma unroll 1
       for (int e = 0; e < 8; ++e) {
-        const uint32_t key = key_of(value(x[e]));
-        if (shift < 24 && key >> (shift + 8) != prefix) continue;
+        const uint32_t key = key_of(value(x[e])), d = key >> shift & 255u;
         const double w = weight_far(value(x[e]), top, st.c);
-        if (w > 0.0) {
-          const uint32_t d = key >> shift & 255u;
+        const bool in = w > 0.0 && !(shift < 24 && key >> (shift + 8) != prefix);
+        const uint64_t m = __builtin_amdgcn_ballot_w64(in);
+        if (m == 0ull) continue;                  // uniform
+        const uint32_t d0 = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(d), __ffsll(static_cast<unsigned long long>(m)) - 1));
+        if (__builtin_amdgcn_ballot_w64(in && d != d0) == 0ull) {      // (equal tokens by the thousand are what leads here)
+          const uint64_t sum = wave_sum64(in ? fixed(w) : 0);
+          if (lane == 0) {
+            atomicAdd(&s.digit_count[d0], static_cast<uint32_t>(__popcll(m)));
+            atomicAdd(&s.digit_mass[d0], static_cast<unsigned long long>(sum));
+          }
+        } else if (in) {
           atomicAdd(&s.digit_count[d], 1u);
           atomicAdd(&s.digit_mass[d], static_cast<unsigned long long>(fixed(w)));
         }
       }
+    });
+    __syncthreads();
+    // sums from the highest digit on: waves 0..3
+    int c = 0, cum = 0;
+    uint64_t m = 0, cmass = 0;
+    if (tid < 256) {
+      c = static_cast<int>(s.digit_count[255 - tid]);
+      m = s.digit_mass[255 - tid];
+      cum = wave_scan(c);
+      cmass = wave_scan64(m);
+      if (lane == 63) { s.count[wv] = cum; s.part[wv] = cmass; }
+    }
+    if (tid == 0) { s.digit = 256; s.last = 0; }
+    __syncthreads();
+    if (tid < 256) {
+#pragma unroll
+      for (int w = 0; w < 3; ++w)
+        if (w < wv) { cum += s.count[w]; cmass += s.part[w]; }
+      const bool reached = c > 0 && (want > 0 ? before + cum >= static_cast<uint32_t>(want) : static_cast<double>(mass_before + cmass) >= target);
+      const uint64_t r = __builtin_amdgcn_ballot_w64(reached), any = __builtin_amdgcn_ballot_w64(c > 0);
+      if (r && lane == 0) atomicMin(&s.digit, 64 * wv + __ffsll(static_cast<unsigned long long>(r)) - 1);
+      if (any && lane == 0) atomicMax(&s.last, 64 * wv + 63 - __clzll(static_cast<long long>(any)));
     }
     __syncthreads();
-    if (tid == 0) {
-      int last = -1;                   // the lowest digit there is, if the border is not reached
-      int at = -1;
-      uint32_t n = before;
-      uint64_t m = mass_before;
-      for (int d = 255; d >= 0 && at < 0; --d) {
-        if (s.digit_count[d] == 0) continue;
-        last = d;
-        if (want > 0 ? n + s.digit_count[d] >= static_cast<uint32_t>(want) : static_cast<double>(m + s.digit_mass[d]) >= target) at = d;
-        else { n += s.digit_count[d]; m += s.digit_mass[d]; }
-      }
-      if (at < 0 && last >= 0) { at = last; n -= s.digit_count[last]; m -= s.digit_mass[last]; }
-      at = max(at, 0);
-      s.key = prefix << 8 | static_cast<uint32_t>(at);
-      s.n_equal = static_cast<int>(s.digit_count[at]);
-      s.before = n;
-      s.mass_before = m;
+    if (tid == (s.digit < 256 ? s.digit : s.last)) {           // (the lowest digit there is, if the border is not reached)
+      s.key = prefix << 8 | static_cast<uint32_t>(255 - tid);
+      s.n_equal = c;
+      s.before = before + static_cast<uint32_t>(cum - c);
+      s.mass_before = mass_before + (cmass - m);
     }
     __syncthreads();
     prefix = s.key;
@@ -777,16 +813,16 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
       if (st.k > 0) b = scan_border<T>(a, logits, st, top, s, st.k, 0.0);
       if (st.p < 1.0) {
         double of = static_cast<double>(b.mass);
-        if (st.k <= 0) {
+        if (info.mode == kModeTopP) {
+          of = static_cast<double>(wave_sum64(total));
+        } else if (st.k <= 0) {
           if (tid == 0) s.wide = 0;
           __syncthreads();
           uint64_t mine = 0;
-          for (int seg = wv; seg < a.segs; seg += kWaves) {
-            float x[8];
-            load_seg<T>(logits, a.V, seg, x);
+          each_seg<T>(a, logits, [&](int, const float (&x)[8]) {
 #pragma unroll 1
             for (int e = 0; e < 8; ++e) mine += fixed(weight_far(value(x[e]), top, st.c));
-          }
+          });
           mine = wave_sum64(mine);
           if (lane == 0) atomicAdd(&s.wide, static_cast<unsigned long long>(mine));
           __syncthreads();
@@ -797,19 +833,23 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
         b = {q.key, max(equal ? min(q.equal, b.equal) : q.equal, 1), 0};
       }
       // the last of the kept equals, in index order: equals per segment, then in the segment that has it
-      for (int seg = wv; seg < a.segs; seg += kWaves) {
-        float x[8];
-        load_seg<T>(logits, a.V, seg, x);
+      each_seg<T>(a, logits, [&](int seg, const float (&x)[8]) {
         int eq = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) eq += __popcll(__builtin_amdgcn_ballot_w64(x[e] > -INFINITY && key_of(value(x[e])) == b.key));
         if (lane == 0) s.count[seg] = eq;
-      }
+      });
       __syncthreads();
+      {
+        const int c = tid < a.segs ? s.count[tid] : 0, upto = static_cast<int>(block_scan64(static_cast<uint64_t>(c), s.part));
+        if (tid == 0) { s.digit = 0; s.n_equal = INT_MAX; }
+        __syncthreads();
+        if (upto >= b.equal && upto - c < b.equal) { s.digit = tid; s.n_equal = b.equal - (upto - c); }
+        __syncthreads();
+      }
       if (wv == 0) {
-        int left = b.equal, seg = 0;
-        while (seg < a.segs - 1 && left > s.count[seg]) left -= s.count[seg++];          // (uniform)
-        int last = INT_MAX;
+        int left = s.n_equal, last = INT_MAX;
+        const int seg = s.digit;
         for (int r = 0; r < kSeg / 64; ++r) {
           const int i = seg * kSeg + r * 64 + lane;
           const float l = i < a.V ? value(as_f32(logits[i])) : -INFINITY;
@@ -826,9 +866,7 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
       __syncthreads();
       cut = static_cast<uint64_t>(~b.key) << 32 | static_cast<uint32_t>(s.pick);
     }
-    for (int seg = wv; seg < a.segs; seg += kWaves) {
-      float x[8];
-      load_seg<T>(logits, a.V, seg, x);
+    each_seg<T>(a, logits, [&](int seg, const float (&x)[8]) {
       uint64_t kept = 0;
 #pragma unroll 1
       for (int e = 0; e < 8; ++e) {
@@ -837,7 +875,7 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
       }
       kept = wave_sum64(kept);
       if (lane == 0) s.seg[seg] = kept;
-    }
+    });
     for (int i = a.segs + tid; i < kSampleMaxSegs; i += kT) s.seg[i] = 0;
     __syncthreads();
   } else {
@@ -889,6 +927,13 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
   const uint64_t mass = s.seg[tid], upto = block_scan64(mass, s.part);
   uint64_t all = 0;
   for (int w = 0; w < kWaves; ++w) all += s.part[w];
+  if (info.mode == kModeEqual) {                  // the first ones by index are kept
+    const uint64_t one = fixed(weight(top, z));
+    uint64_t n_kept = all / one;
+    if (st.k > 0) n_kept = min(n_kept, static_cast<uint64_t>(st.k));
+    if (st.p < 1.0) n_kept = max(static_cast<uint64_t>(ceil(st.p * static_cast<double>(n_kept))), static_cast<uint64_t>(1));
+    all = n_kept * one;
+  }
   if (!(u >= 0.f)) u = 0.f;
   u = fminf(u, 0.99999994f);
   uint64_t x = static_cast<uint64_t>(static_cast<double>(all) * static_cast<double>(u));

@@ -280,3 +280,22 @@ def test_flat_rows_of_a_long_vocabulary(dtype, sd):
     x[5, 3] = 4.0
     for kw in (dict(top_p=[0.9]), dict(top_k=[1000], top_p=[0.8]), dict(top_p=[0.3], min_p=[0.9])):
         check(x, rng.random(6).astype(np.float32), dtype, per=6, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_of_equal_logits(dtype):
+    """Rows of zeros (a padded batch), of another number, with tokens ruled out, or with one other token: the borders go by index."""
+    rng = np.random.default_rng(35)
+    V = 70001
+    x = np.zeros((7, V), np.float32)
+    x[1] = -417.25
+    x[2, ::3] = -np.inf
+    x[3, 20000:60000] = -1e9
+    x[4, 33333] = 1.0
+    x[5] = 2.0 ** 20
+    x[6, 5:] = np.nan
+    for kw in (dict(), dict(top_p=[0.9]), dict(top_p=[0.0]), dict(top_k=[1000]), dict(top_k=[77], top_p=[0.5]), dict(min_p=[1.0]),
+               dict(temperature=[0.0]), dict(temperature=[3.0], top_p=[0.25], min_p=[0.5])):
+        u = rng.random(7).astype(np.float32)
+        u[:2] = 0.0, np.float32(1) - np.float32(2.0 ** -24)
+        check(x, u, dtype, per=7, **kw)
