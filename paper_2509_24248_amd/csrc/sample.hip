@@ -16,7 +16,7 @@
 // Rows without any difference need no border but a number.  What is left without a list (more than 4096 tokens within 2^-16 nat of a border, and
 // logits beyond 2^25 temperatures) is a selection over the row by the third kernel, 0.4 to 0.8 ms whatever the number of rows.
 // What bounds it: 144 rows of 151936 fp32 logits (87.5 MB, 16.6 us at a copy's rate) take 21 us in the first kernel (4.2 TB/s), 34 in the
-// second (vector instructions, 84 % of its time: fifteen in 64 bits and as many others for a token's weight) and 12 in the third; 7 rows with
+// second (vector instructions, 86 % of its time: fifteen in 64 bits and as many others for a token's weight) and 12 in the third; 7 rows with
 // top-k 4.5, 8 and 6.4 us: chains of dependent loads, five in the last.  One pass that kept every weight would write as much as it reads.
 #include "common.hpp"
 #include "kernels.hpp"
