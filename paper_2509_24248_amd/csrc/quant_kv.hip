@@ -14,6 +14,8 @@ namespace sx {
 
 namespace {
 
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+
 constexpr int kThreads = 256;
 constexpr int kTok = 16;        // tokens of a wave of the writing kernel
 
@@ -32,8 +34,9 @@ __device__ __forceinline__ int64_t quant_row(const QuantKv& kv, int b, int h, in
 }
 
 // A wave takes sixteen tokens of K or V of one head: D / 8 lanes a row, eight values a lane, all loads of the wave requested together.
-// Bound by memory: 4 prompts of 4111 tokens, 8 heads, bf16 (76 MB): 16.6 us = 4.6 TB/s, a copy's rate 5.3; a block of 56 tokens: 3.6 us, a launch
-// and two dependent loads.
+// Bound by memory: 4 prompts of 4111 tokens, 8 heads, bf16 (76 MB): 13.8 us = 5.5 TB/s, a copy's rate 5.3 (with every value looked at for being
+// finite, not only the wave's largest, 16.6: the vector unit was busy for 89 % of them); a block of 56 tokens: 3.6 us, a launch and two
+// dependent loads.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void k_quant_write(const QuantWriteArgs a) {
   constexpr int LPR = D / 8, RPI = 64 / LPR, U = kTok / RPI;     // lanes of a row, rows of an instruction, instructions
@@ -71,10 +74,23 @@ __global__ __launch_bounds__(kThreads) void k_quant_write(const QuantWriteArgs a
       }
     }
     uint32_t amax = 0;              // magnitudes compare like their bits
+    if constexpr (sizeof(T) == 2) {
+      auto larger = [](uint32_t p, uint32_t q) { return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, p), __builtin_bit_cast(u16x2_t, q))); };
+      constexpr uint32_t kMag = 0x7FFF7FFFu;
+      const uint32_t two = larger(larger(raw[u][0].x & kMag, raw[u][0].y & kMag), larger(raw[u][0].z & kMag, raw[u][0].w & kMag));
+      amax = max(two << 16, two & 0xFFFF0000u);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t bits = __float_as_uint(x[e]) & 0x7FFFFFFFu;
-      amax = max(amax, bits < 0x7F800000u ? bits : 0u);
+      for (int e = 0; e < 8; ++e) amax = max(amax, __float_as_uint(x[e]) & 0x7FFFFFFFu);
+    }
+    const bool odd = __builtin_amdgcn_ballot_w64(amax >= 0x7F800000u) != 0ull;          // (uniform) some value of the wave is not finite
+    if (odd) {
+      amax = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t bits = __float_as_uint(x[e]) & 0x7FFFFFFFu;
+        amax = max(amax, bits < 0x7F800000u ? bits : 0u);
+      }
     }
     amax = row_umax<0xB1>(amax);                       // lanes 1, 2, 4 (and 8) apart
     amax = row_umax<0x4E>(amax);
@@ -89,12 +105,14 @@ __global__ __launch_bounds__(kThreads) void k_quant_write(const QuantWriteArgs a
       w[i] = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2] * inv, x[4 * i + 3] * inv, static_cast<int>(w[i]), true);
     }
     // a value that is not finite has the NaN code with its sign
+    if (odd) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t bits = __float_as_uint(x[e]);
-      if ((bits & 0x7FFFFFFFu) >= 0x7F800000u) {
-        const int sh = 8 * (e & 3);
-        w[e >> 2] = (w[e >> 2] & ~(0xFFu << sh)) | ((0x7Fu | (bits >> 24 & 0x80u)) << sh);
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t bits = __float_as_uint(x[e]);
+        if ((bits & 0x7FFFFFFFu) >= 0x7F800000u) {
+          const int sh = 8 * (e & 3);
+          w[e >> 2] = (w[e >> 2] & ~(0xFFu << sh)) | ((0x7Fu | (bits >> 24 & 0x80u)) << sh);
+        }
       }
     }
     if (t >= count) continue;

@@ -146,3 +146,48 @@ def test_rounds(dtype, page, tree):
             for a, w in zip(t[:4], (cache.k, cache.v, cache.ks, cache.vs)):
                 np.testing.assert_array_equal(a.cpu().numpy(), w)
             L = new_ctx.cpu().numpy().astype(np.int64)
+
+
+def test_two_streams_at_once():
+    """Writes, attention and draws of two inputs on two streams, each with a cache and workspaces of its own, against the same calls one by one."""
+    lib, rng = H.sx(), np.random.default_rng(41)
+    B, n_q, Hq, Hkv, d, V = 3, 5, 8, 2, 128, 20000
+    sets = []
+    for i in range(2):
+        L = np.array([700 + 900 * i, 33, 2000 - 1000 * i])
+        cache = Cache(rng, B, Hkv, d, L + n_q, 16)
+        view, t = cache.gpu()
+        s = dict(view=view, keep=t, L=torch.from_numpy(L.astype(np.int32)).cuda())
+        for n in ("k", "v"):
+            s[n] = torch.from_numpy(rng.standard_normal((B, n_q, Hkv, d)).astype(np.float32)).cuda().bfloat16()
+        s["q"] = torch.from_numpy(rng.standard_normal((B, n_q, Hq, d)).astype(np.float32)).cuda().bfloat16()
+        s["logits"] = torch.from_numpy((rng.standard_normal((B * n_q, V)) * 2).astype(np.float32)).cuda()
+        s["u"] = torch.from_numpy(rng.random(B * n_q).astype(np.float32)).cuda()
+        s["p"] = torch.full((B,), 0.9, device="cuda")
+        s["ws"] = H.workspace(lib.specexit_quant_verify_attn_workspace_bytes(view, lib.BF16, B, n_q, Hq))
+        s["ws2"] = H.workspace(lib.specexit_sample_workspace_bytes(lib.F32, B * n_q, V))
+        sets.append(s)
+
+    def outputs():
+        return [(torch.empty((B, n_q, Hq, d), dtype=torch.bfloat16, device="cuda"), torch.empty(B * n_q, dtype=torch.int32, device="cuda"),
+                 torch.empty(B * n_q, device="cuda")) for _ in range(2)]
+
+    def calls(s, o, stream):
+        lib.specexit_quant_kv_write(s["view"], lib.BF16, B, n_q, s["k"], s["v"], s["L"], stream=stream)
+        lib.specexit_quant_verify_attn(s["view"], lib.BF16, B, n_q, Hq, s["q"], s["L"], None, d ** -0.5, o[0], s["ws"], stream=stream)
+        lib.specexit_sample(lib.F32, B * n_q, V, s["logits"], s["u"], o[1], o[2], top_p=s["p"], rows_per_seq=n_q, workspace=s["ws2"], stream=stream)
+
+    alone = outputs()
+    for s, o in zip(sets, alone):
+        calls(s, o, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for rep in range(10):
+        both = outputs()
+        torch.cuda.synchronize()
+        for s, o, st in zip(sets, both, streams):
+            calls(s, o, st)
+        torch.cuda.synchronize()
+        for a, b in zip(alone, both):
+            for x, y in zip(a, b):
+                assert torch.equal(x, y), rep
