@@ -388,12 +388,18 @@ __global__ __launch_bounds__(kT) void k_sample_mass(const SampleArgs a) {
       if (mode == kModeTopP) unit = 1.0 / 1024.0;
     }
     for (int c0 = 0; same && c0 < a.chunks; c0 += kSampleMaxChunks / 2) {      // (half of the loads in flight: the second half is often empty)
+      uint32_t v[kSampleMaxChunks / 2];
+      const uint32_t* const hist = a.hist + (first + c0) * kBins;
 #pragma unroll
       for (int e = 0; e < kSampleMaxChunks / 2; ++e) {
-        const int c = c0 + e, by = c < a.chunks ? __builtin_amdgcn_readlane(behind, c & 63) : kBins;
-        const uint32_t v = a.hist[(first + min(c, a.chunks - 1)) * kBins + max(tid - by, 0)];
-        h += tid >= by ? v : 0;
+        v[e] = 0;
+        if (c0 + e < a.chunks) {                  // uniform
+          const int at = tid - __builtin_amdgcn_readlane(behind, c0 + e);
+          if (at >= 0) v[e] = hist[e * kBins + at];
+        }
       }
+#pragma unroll
+      for (int e = 0; e < kSampleMaxChunks / 2; ++e) h += v[e];
     }
     auto first_of = [&](bool reached, int which) {
       const uint64_t m = __builtin_amdgcn_ballot_w64(reached);
