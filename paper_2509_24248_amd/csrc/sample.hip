@@ -14,7 +14,7 @@
 //                    again: masses of what is kept for certain per segment of 512 tokens, and a list of the tokens in doubt.
 //   3 k_sample_pick  a workgroup per row finds the border in the list (at most 4096), the draw's segment and in it the token.
 // Rows without any difference need no border but a number.  What is left without a list (more than 4096 tokens within 2^-16 nat of a border, and
-// logits beyond 2^25 temperatures) is a selection over the row by the third kernel, 0.4 to 0.8 ms whatever the number of rows.
+// logits beyond 2^20 temperatures) is a selection over the row by the third kernel, 0.4 to 0.8 ms whatever the number of rows.
 // What bounds it: 144 rows of 151936 fp32 logits (87.5 MB, 16.6 us at a copy's rate) take 21 us in the first kernel (4.2 TB/s), 34 in the
 // second (vector instructions, 86 % of its time: fifteen in 64 bits and as many others for a token's weight) and 12 in the third; 7 rows with
 // top-k 4.5, 8 and 6.4 us: chains of dependent loads, five in the last.  One pass that kept every weight would write as much as it reads.
@@ -38,7 +38,7 @@ constexpr int kFinest = 12;             // bins are 1/16 nat to 2^-16 nat
 constexpr float kWide = 128.f;          // a row whose logits span that many bins has no finer ones
 constexpr int kChunkSegs = 64;          // segments of a chunk, at most
 constexpr int kList = 4096, kListPart = 2048;      // tokens in doubt of a row, and of one of its chunks
-constexpr int kFar = 1 << 29;           // bins are forced into -kFar .. kFar
+constexpr int kFar = 1 << 24;           // bins are forced into -kFar .. kFar: a product within them is off by half a bin at most
 constexpr double kFix = 35184372088832.0;          // 2^45
 constexpr double kFloor = 9.094947017729282e-13;   // 2^-40
 
@@ -212,10 +212,10 @@ template <typename T> __device__ __forceinline__ void load_seg(const T* row, int
   }
 }
 
-// Halvings of the bins, up to kFinest, that leave the logits low .. top within kBins of them, and their numbers below 2^28.
+// Halvings of the bins, up to kFinest, that leave the logits low .. top within kBins of them (their products rounded), and their numbers below kFar.
 __device__ __forceinline__ int finer_of(float top, float low, float s) {
   const float span = top > -INFINITY ? (top - low) * s : static_cast<float>(kBins);            // (NaN where they are infinite: no halving either way)
-  return max(0, min(min(ilogbf(510.f / fmaxf(span, 0.0625f)), ilogbf(268435456.f / fmaxf(fabsf(top * s), 1.f))), kFinest));
+  return max(0, min(min(ilogbf(508.f / fmaxf(span, 0.0625f)), ilogbf(static_cast<float>(kFar) / fmaxf(fabsf(top * s), 1.f))), kFinest));
 }
 
 // ------------------------------------------------------------------------------------------------------------ 1: histograms
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(kT) void k_sample_bins(const SampleArgs a) {
     finer = finer_of(top, low, st.s);
   }
   const float s = ldexpf(st.s, finer), step = ldexpf(-1.44269504f / kPerNat, -finer);
-  // (whole numbers below 2^29, or the row goes another way: their differences are exact)
+  // (whole numbers below kFar, or the row goes another way: their differences are exact)
   const float origin = floorf(top * s);
   uint32_t* const mine = reinterpret_cast<uint32_t*>(hist) + (lane & 3);
 #pragma unroll
@@ -301,8 +301,8 @@ __global__ __launch_bounds__(kT) void k_sample_bins(const SampleArgs a) {
       if (j < static_cast<float>(kBins)) {
         uint32_t add = 1;
         if (masses) {                  // uniform
-          // how far below the bin's upper edge, in bins: the product's rounding error counts as well
-          const float below = fminf(fmaxf((g - prod) + 1.f - fmaf(l, s, -prod), 0.f), 1.f);
+          // how far below the bin's upper edge, in bins: the product's rounding error counts as well, and may be half a bin either way
+          const float below = fminf(fmaxf((g - prod) + 1.f - fmaf(l, s, -prod), -1.f), 2.f);
           add = static_cast<uint32_t>(fmaf(__builtin_amdgcn_exp2f(below * step), 65536.f, 0.5f));
         }
         atomicAdd(&mine[4 * static_cast<int>(j)], add);

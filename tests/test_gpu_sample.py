@@ -252,7 +252,7 @@ def test_min_p_inside_and_outside_the_nucleus():
 
 
 def test_logits_far_from_zero():
-    """Around 2^25 temperatures the bins end: rows on both sides, of both signs, with and without borders."""
+    """Large logits of both signs, up to where their own spacing is several nats, with and without borders."""
     rng = np.random.default_rng(33)
     V = 700
     tops = [3.2e7, 3.3554e7, 3.36e7, 1e9, -3.2e7, -3.35539e7, -3.3556e7, -3.4e7, -1e9]
@@ -299,3 +299,17 @@ def test_rows_of_equal_logits(dtype):
         u = rng.random(7).astype(np.float32)
         u[:2] = 0.0, np.float32(1) - np.float32(2.0 ** -24)
         check(x, u, dtype, per=7, **kw)
+
+
+@pytest.mark.parametrize("sd", [0.003, 0.3, 3.0])
+def test_offsets_and_odd_temperatures(sd):
+    """Around 2^20 temperatures the bins end; in front of that a logit times the bins per logit is rounded to whole bins."""
+    rng = np.random.default_rng(36)
+    V = 30011
+    tops = [0.0, 999.0, -1000.0, 7e4, 6.6e5, 7.3e5, 7.4e5, -6.9e5, -7.4e5, 3e6]
+    x = (np.array(tops)[:, None] + rng.standard_normal((len(tops), V)) * sd).astype(np.float32)
+    n = len(tops)
+    for T in (0.7, 1.1):
+        u = rng.random(n).astype(np.float32)
+        check(x, u, temperature=[T] * n, top_p=[0.9, 0.5] * (n // 2))
+        check(x, u, temperature=[T] * n, top_k=[100] * n, top_p=[0.95] * n)
