@@ -10,7 +10,7 @@ import harness as H
 
 pytestmark = pytest.mark.gpu
 
-# the weights' polynomial 7e-15, a weight's and the sum's fixed-point steps, 2^-46 of the best weight per token (V 2^-46 of the sum at most), and the
+# the weights' polynomial 3.2e-14, a weight's and the sum's fixed-point steps, 2^-46 of the best weight per token (V 2^-46 of the sum at most), and the
 # rounding of the share to fp32
 def prob_bound(V):
     return 2.0 ** -24 + V * 2.0 ** -46 + 1e-12
