@@ -1,0 +1,83 @@
+"""GPU: attention over the 8-bit cache, every key and tile of keys of it: values that tell them apart (quant_bound.py), the bound of the row itself."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import specexit_oracle as O
+from workloads import gen
+
+from quant_bound import TILE, signed_values, worst_share
+from quant_harness import Cache, attn, queries, tree_masks
+
+pytestmark = pytest.mark.gpu
+
+
+def check(cache, q, L, mask=None, scale=None, dtype="bf16", sequences=None):
+    got = attn(cache, q, L, mask, scale, dtype)
+    worst, size = worst_share(cache, q, L, got, mask, scale, dtype, sequences)
+    print("worst share of the bound %.3f, largest bound %.1e of the outputs" % (worst, size), flush=True)
+    assert worst <= 1.0
+    return got
+
+
+# every count of 16-row tiles, both widths and types; flat scores, so that every key has a share that shows
+@pytest.mark.parametrize("per", [TILE, 1])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,n_q", [(1, 1), (4, 7), (8, 5), (8, 8), (8, 9), (6, 16), (7, 15), (2, 64)])
+def test_every_key_counts(dtype, d, G, n_q, per):
+    rng = np.random.default_rng(G * 100 + n_q + per)
+    L = np.array([d + 77, 700, 31])
+    cache = Cache(rng, 3, 2, d, L + n_q, 16 if per == TILE else None, spread=0.0)
+    signed_values(cache, rng, per)
+    check(cache, queries(rng, 3, n_q, 2 * G, d, dtype), L, None, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [None, 16, 48, 112])
+def test_lengths_and_trees(dtype, page):
+    rng = np.random.default_rng(52)
+    L = np.array([0, 1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 121, 500])
+    n_q = 7
+    cache = Cache(rng, len(L), 2, 128, L + n_q, page, spread=0.0)
+    signed_values(cache, rng, 1)
+    check(cache, queries(rng, len(L), n_q, 8, 128, dtype), L, tree_masks(rng, len(L), n_q), dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,top,page", [(1, 9000, 16), (1, 9000, None), (5, 3000, 48), (70, 400, 16), (130, 60, 16)])
+def test_every_tile_of_every_share(dtype, d, B, top, page):
+    """One long unit over all compute units, shares with the end of one unit and the start of the next, more sequences than a wave has lanes."""
+    rng = np.random.default_rng(B + d)
+    L = rng.integers(max(0, top - 700), top, B)
+    n_q = 3
+    cache = Cache(rng, B, 2, d, L + n_q, page, spread=0.0)
+    signed_values(cache, rng, TILE)
+    check(cache, queries(rng, B, n_q, 8, d, dtype), L, dtype=dtype, sequences=None if B < 10 else sorted(rng.choice(B, 24, replace=False).tolist()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_ordinary_rows_within_their_own_bound(dtype, d):
+    """Rows of magnitudes of their own, as keys and values have them, peaked and flat."""
+    rng = np.random.default_rng(53)
+    L = np.array([300, 37, 1100])
+    n_q = 5
+    cache = Cache(rng, 3, 2, d, L + n_q, 16)
+    q = queries(rng, 3, n_q, 8, d, dtype)
+    for e in (-3, 0, 2):
+        check(cache, np.ldexp(q, e).astype(np.float32), L, dtype=dtype)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_lesser_part_of_bf16_queries(d):
+    """Lesser parts that all point one way: 6 % of every score."""
+    rng = np.random.default_rng(54)
+    n_q, n = 3, 64
+    cache = Cache(rng, 1, 1, d, [n], None)
+    codes, s = O.quant_rows(np.repeat(np.linspace(-2.0, 2.0, n)[:, None], d, 1))
+    cache.k[0, 0, :n], cache.ks[0, 0, :n] = codes, s
+    signed_values(cache, rng, 1)
+    q = np.full((1, n_q, 4, d), 1.0625, np.float32) * np.array([1.0, -1.0, 0.5], np.float32)[None, :, None, None]
+    check(cache, q, np.array([n - n_q]), scale=2.0 / d)
