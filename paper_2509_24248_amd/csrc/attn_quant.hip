@@ -263,7 +263,8 @@ __global__ __launch_bounds__(64 * NK * NR, NK * NR <= 8 ? 2 : (NK * NR + 3) / 4)
       float big = 0.f;
 #pragma unroll
       for (int c = 0; c < kQ; ++c) big = fmaxf(big, fabsf(x[t][c]));
-      const int s = min(quant_scale_byte(__float_as_uint(quad_row_max(big))), 254);
+      // (from 5 on, so that the lesser part, four powers of two below, has a scale byte too: of rows below 2^-114 both are exact to 2^-136)
+      const int s = min(max(quant_scale_byte(__float_as_uint(quad_row_max(big))), 5), 254);
       const float inv = quant_scale_inverse(s);
 #pragma unroll
       for (int c = 0; c < kQ; ++c) x[t][c] *= inv;
@@ -283,7 +284,7 @@ __global__ __launch_bounds__(64 * NK * NR, NK * NR <= 8 ? 2 : (NK * NR + 3) / 4)
         }
       }
       // (lanes q hold the scales of products 32 q .. + 31)
-      qs[t] = HD == 128 ? s | max(s - 4, 0) << 8 : max(s - 4 * (fq >> 1), 0);
+      qs[t] = HD == 128 ? s | (s - 4) << 8 : s - 4 * (fq >> 1);
     } else {
 #pragma unroll
       for (int p = 0; p < NP; ++p)

@@ -81,3 +81,20 @@ def test_the_lesser_part_of_bf16_queries(d):
     signed_values(cache, rng, 1)
     q = np.full((1, n_q, 4, d), 1.0625, np.float32) * np.array([1.0, -1.0, 0.5], np.float32)[None, :, None, None]
     check(cache, q, np.array([n - n_q]), scale=2.0 / d)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("e", [-115, -117, -118, -120])
+def test_the_smallest_queries(d, e):
+    """Rows whose scale byte leaves none for the lesser part, with a scale that makes their scores count."""
+    rng = np.random.default_rng(55)
+    L = np.array([90])
+    cache = Cache(rng, 1, 2, d, L + 4, None, spread=0.0)
+    signed_values(cache, rng, 1)
+    q = gen.round_to_bf16(np.ldexp(queries(rng, 1, 4, 8, d, "bf16"), e).astype(np.float32))
+    check(cache, q, L, scale=np.ldexp(d ** -0.5, -e))
+    # and lesser parts that all point one way
+    q = np.full((1, 4, 8, d), np.ldexp(1.0625, e), np.float32) * np.where(np.arange(8) % 2, 1.0, -1.0).astype(np.float32)[None, None, :, None]
+    codes, s = O.quant_rows(np.repeat(np.linspace(-2.0, 2.0, 94)[:, None], d, 1))
+    cache.k[0, :, :94], cache.ks[0, :, :94] = codes, s
+    check(cache, q, L, scale=np.ldexp(2.0 / d, -e))
