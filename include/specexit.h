@@ -377,10 +377,14 @@ int32_t specexit_quant_kv_write(const specexit_quant_kv_view *kv, int32_t dtype,
                                 uint32_t flags, void *stream);
 
 /* ---- stage 2 over the 8-bit cache: specexit_verify_attn with such a view (Alg. 1) ----
- * Arguments, masks and limits as there; dtype is that of q and out.  The queries and the
- * cache's numbers are multiplied as they are: nothing is rounded but sums (fp32), probabilities
- * (to bf16; fp32 results: to 24 bits) and the output.  Entries that a row does not see may hold anything, NaN
- * included; a row that sees nothing (an empty context and an empty mask word) is all zeros. */
+ * Arguments, masks and limits as there; dtype is that of q and out.  The cache's numbers are multiplied
+ * as they are, fp32 queries to 24 bits.  bf16 queries are held in two parts of four bits with one power of two
+ * a row (one query of one head): with m the row's largest magnitude, elements from 2^-13 m on are exact, smaller ones
+ * are off by at most 2^-21 m, and a score's sum drops what lies 2^-23 below its largest product.  (So a
+ * query channel 2^13 times the others costs them bits, whether or not the keys have that channel; the
+ * plain cache's attention has no such limit.)  Probabilities are rounded to bf16 (fp32 results: 24 bits), sums are fp32.
+ * Entries that a row does not see may hold anything, NaN included; a row that sees nothing (an empty
+ * context and an empty mask word) is all zeros. */
 int32_t specexit_quant_verify_attn(const specexit_quant_kv_view *kv, int32_t dtype, int32_t B, int32_t n_q,
                                    int32_t n_q_heads, const void *q, const int32_t *ctx_len /*[B]*/,
                                    const uint64_t *mask /*[B,n_q] or NULL*/, float scale, void *out,

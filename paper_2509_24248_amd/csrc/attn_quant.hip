@@ -6,10 +6,13 @@
 // The ring's NR waves own RTW 16-row tiles of the queries each:
 //   S^T = K Q^T : block-scaled matrix instruction, 16 keys x 16 rows x 128 products.  A = the codes as they lie in the cache, with
 //                 the keys' scale bytes as its scales.  B = the queries as a sum of e4m3 parts, each with its own power of two:
-//                 a part takes four bits of what is left, so two parts hold a bf16 value.  The products are exact: nothing of the
-//                 queries is rounded away, and no key is converted.  (The instruction drops what lies 2^-23 below its largest product, some
-//                 1e-5 of a score, which the rounding to bf16 hides and fp32 results do not: there, keys are converted to bf16,
-//                 exactly, and the queries are three bf16 parts.  With six e4m3 parts the tiny fp32 shape was off by 3.4e-5.)
+//                 a part takes four bits of what is left, so two parts hold a bf16 value that is a normal number of the first: from 2^-14 of
+//                 the row's power of two on, 2^-13 of its largest value.  What lies below has the lesser part's least step, and is off by half of it,
+//                 2^-21.8 of the largest value, at most.  The products are exact and no key is converted.  (The instruction drops what lies 2^-23
+//                 below its largest product, some 1e-5 of a score, which the rounding to bf16 hides and fp32 results do not: there, keys are
+//                 converted to bf16, exactly, and the queries are three bf16 parts.  With six e4m3 parts the tiny fp32 shape was off by 3.4e-5.
+//                 One bf16 part of the queries and converted keys would hold any bf16 value too: 8 sequences of 2048 .. 16384 tokens 34.0 -> 36.4 us
+//                 at 28 rows, 57.1 -> 65.6 at 72, 16 of 8192 .. 32768 195 -> 226.)
 //   softmax     : online, per wave, in log2 units; lane (row, q) owns 8 keys of its row;
 //   O^T += V^T P^T : A = V codes, transposed on the way out of LDS (eight keys of a column per lane) and converted to bf16,
 //                 which is exact; B = the probabilities times the keys' scales (powers of two: exact) in PP bf16 parts.
@@ -111,7 +114,7 @@ __global__ __launch_bounds__(64 * NK * NR, NK * NR <= 8 ? 2 : (NK * NR + 3) / 4)
   static_assert(S >= 2 * KT && S % KT == 0, "a step is requested while the one before it is worked on");
   constexpr int kVAhead = NK * NR <= 8 ? 8 : 3;       // V reads in front of their use, as many as the registers allow
   constexpr int kReq = 2 * kTileP / NR + 1;       // requests of a wave per tile, at least
-  constexpr bool kCodes = sizeof(T) == 2;         // the keys' codes are multiplied as they are
+  constexpr bool kCodes = sizeof(T) == 2;         // keys are multiplied as codes
   constexpr int NP = Parts<T>::q, PP = Parts<T>::p;
   constexpr int NM = HD == 128 ? NP : 1;          // block-scaled matrix instructions for 16 keys x 16 rows
   constexpr int kKS = HD / 32;                    // k steps of bf16 ones

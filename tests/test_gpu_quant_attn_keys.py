@@ -98,3 +98,18 @@ def test_the_smallest_queries(d, e):
     codes, s = O.quant_rows(np.repeat(np.linspace(-2.0, 2.0, 94)[:, None], d, 1))
     cache.k[0, :, :94], cache.ks[0, :, :94] = codes, s
     check(cache, q, L, scale=np.ldexp(2.0 / d, -e))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("r", [6, 12, 14, 15, 17])
+def test_a_large_query_channel_that_no_key_has(d, r):
+    """Keys with a zero where the query's largest value is, 2^r times the others: the scores are what the others make them.  Up to 2^12 nothing is
+    lost, beyond it 2^-21 of the large value at most for each of the others."""
+    rng = np.random.default_rng(56)
+    L = np.array([130])
+    cache = Cache(rng, 1, 2, d, L + 3, None, spread=0.0)
+    cache.k[..., 5] = 0
+    signed_values(cache, rng, 1)
+    q = rng.uniform(1.0, 2.0, (1, 3, 8, d)) * rng.choice([-1.0, 1.0], (1, 3, 8, d))
+    q[..., 5] = np.ldexp(1.0, r)
+    check(cache, gen.round_to_bf16(q.astype(np.float32)), L, scale=0.5 * d ** -0.5)

@@ -127,3 +127,17 @@ def test_the_reference_is_the_oracles():
             k, v = cache.values()
             ref = O.verify_attn(q, k, v, L, mask, None, cache.table, page or 16)
             assert worst_share(cache, q, L, ref, mask, None, "f32")[0] < 1e-6
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_what_the_two_parts_of_a_query_hold(d):
+    """Exact from 2^-13 of the row's largest magnitude on; below, off by 2^-21 of it at most, and that is met."""
+    rng = np.random.default_rng(8)
+    q = rng.uniform(1.0, 2.0, (400, d)) * np.exp2(-rng.integers(0, 30, (400, d)))
+    q[:, 3] = rng.uniform(1.0, 2.0, 400)
+    q = gen.round_to_bf16(q.astype(np.float32)).astype(np.float64)
+    m = q.max(1, keepdims=True)
+    off = np.abs(sum(two_parts(q)) - q)
+    assert (off[q >= m * 2.0 ** -13] == 0).all()
+    assert (off <= m / 224 * 2.0 ** -14).all() and (off <= m * 2.0 ** -21).all()
+    assert (off > m * 2.0 ** -23).any()
