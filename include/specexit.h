@@ -427,6 +427,7 @@ int32_t specexit_sample(int32_t dtype, int32_t M, int32_t V, const void *logits 
                         int32_t rows_per_seq, const float *temperature, const int32_t *top_k, const float *top_p,
                         const float *min_p, const float *u /*[M]*/, int32_t *token /*[M]*/, float *prob /*[M] or NULL*/,
                         void *workspace, size_t workspace_bytes, uint32_t flags, void *stream);
+/* never less for more rows or a larger V: one of the largest batch's size serves every smaller one */
 size_t specexit_sample_workspace_bytes(int32_t dtype, int32_t M, int32_t V);
 
 /* ---- measurement aid -------------------------------------------------------------------

@@ -287,6 +287,7 @@ struct SampleArgs {
   float* prob;               // or nullptr
   int* status;
   int segs, chunk_segs, chunks;                  // sample_plan
+  int64_t row_chunks;                            // chunks of all rows, at most, of a launch of as many rows or fewer
   uint32_t* hist;                                // sample_carve
   unsigned long long *chunk_sums, *seg_mass, *list;
   float4* chunk_top;         // of a chunk: the best logit, the least that weighs beside it, by what power of two its bins are finer

@@ -22,6 +22,7 @@
 #include "kernels.hpp"
 
 #include <limits.h>
+#include <algorithm>
 #include <type_traits>
 
 namespace sx {
@@ -975,6 +976,8 @@ template <typename T> hipError_t launch_as(const SampleArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+constexpr int kRowChunks = 512;         // chunks of a launch of few rows
+
 size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 }  // namespace
@@ -983,13 +986,13 @@ void sample_plan(SampleArgs& a) {
   a.segs = (a.V + kSeg - 1) / kSeg;
   // two workgroups per compute unit where the rows are few, no more than twenty to a row: each of the second kernel's reads the histograms of all.
   // (7 rows: 12 chunks 19.1 us, 20 18.4, 32 19.4; 48 rows: 6 chunks 33.0, 11 32.3, 20 38.5; 144 rows, 5 chunks 64.5, 10 68.0)
-  int chunks = (512 + a.M - 1) / a.M;
-  if (chunks > kSampleMaxChunks) chunks = kSampleMaxChunks;
-  if (chunks > (a.segs + kWaves - 1) / kWaves) chunks = (a.segs + kWaves - 1) / kWaves;
   const int least = (a.segs + kChunkSegs - 1) / kChunkSegs;
-  if (chunks < least) chunks = least;
+  const int most = std::max(std::min(kSampleMaxChunks, (a.segs + kWaves - 1) / kWaves), least);
+  const int chunks = std::max(std::min((kRowChunks + a.M - 1) / a.M, most), least);
   a.chunk_segs = (a.segs + chunks - 1) / chunks;
   a.chunks = (a.segs + a.chunk_segs - 1) / a.chunk_segs;
+  // (the workspace has room for the chunks of any number of rows up to M: ceil(512 / m) m is less than 512 + m)
+  a.row_chunks = std::min(static_cast<int64_t>(a.M) * most, std::max(static_cast<int64_t>(a.M) * least, static_cast<int64_t>(kRowChunks) - 1 + a.M));
 }
 
 // Lays the workspace out (base null: only its size).
@@ -1001,12 +1004,12 @@ size_t sample_carve(SampleArgs& a, void* base) {
     off += align256(bytes);
     return r;
   };
-  const size_t M = static_cast<size_t>(a.M), C = static_cast<size_t>(a.chunks);
-  a.hist = reinterpret_cast<uint32_t*>(take(M * C * kBins * 4));
-  a.chunk_sums = reinterpret_cast<unsigned long long*>(take(M * C * 2 * 8));
+  const size_t M = static_cast<size_t>(a.M), MC = static_cast<size_t>(a.row_chunks);
+  a.hist = reinterpret_cast<uint32_t*>(take(MC * kBins * 4));
+  a.chunk_sums = reinterpret_cast<unsigned long long*>(take(MC * 2 * 8));
   a.seg_mass = reinterpret_cast<unsigned long long*>(take(M * a.segs * 8));
   a.list = reinterpret_cast<unsigned long long*>(take(M * kList * 8));
-  a.chunk_top = reinterpret_cast<float4*>(take(M * C * 16));
+  a.chunk_top = reinterpret_cast<float4*>(take(MC * 16));
   a.row_info = reinterpret_cast<SampleRow*>(take(M * sizeof(SampleRow)));
   return off;
 }
