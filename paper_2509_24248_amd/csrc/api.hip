@@ -1236,7 +1236,7 @@ int32_t specexit_quant_kv_compact(const specexit_quant_kv_view* kv, int32_t n_la
     a.block_hidden = block_hidden; a.hidden_next = hidden_next;
     a.hidden_row_bytes = static_cast<int>(D * esize(dtype));
   }
-  if (kv->n_kv_heads > 65535 || B > 65535 || n_layers > 65535 || static_cast<int64_t>(kv->n_kv_heads) * B * n_layers + B >= (1 << 26))
+  if (kv->n_kv_heads > 65535 || B > 65535 || n_layers > 65535 || static_cast<int64_t>(kv->n_kv_heads) * B * n_layers + B > kLaunchWaves)
     return fail(SPECEXIT_EUNSUPPORTED, "quant_kv_compact: grid too large");
   return check_hip(launch_quant_compact(a, static_cast<hipStream_t>(stream)), "quant_kv_compact");
 }

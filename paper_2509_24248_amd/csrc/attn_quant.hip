@@ -801,6 +801,7 @@ bool quant_attn_plan(QuantAttnArgs& a, int num_cus) {
   a.page_shift = (a.page_size & (a.page_size - 1)) == 0 ? 31 - __builtin_clz(static_cast<unsigned>(a.page_size)) : -1;
   if (a.B > kAttnMaxSeqs || a.l_max < a.n_blk) return false;
   const int64_t units = static_cast<int64_t>(a.B) * a.Hkv;
+  if (units * a.G * a.n_q > kLaunchWaves) return false;            // (the merge: a wave per row, of as many as that)
   const int64_t gmax = (a.l_max + kAttnGran - 1) / kAttnGran;      // granules of the longest possible unit
   if (units * (gmax + a.pad) >= (1ll << 30)) return false;
   const AttnLine line = attn_sched_line(static_cast<int>(a.B * gmax), a.B, a.Hkv, a.pad, a.wide_from, 0, num_cus);

@@ -248,6 +248,7 @@ struct QuantWriteArgs {
 };
 bool quant_write_plan(QuantWriteArgs& a);
 hipError_t launch_quant_write(const QuantWriteArgs& a, hipStream_t s);
+constexpr int64_t kLaunchWaves = (1ll << 26) - 4;      // waves of a launch of workgroups of four: fewer than 2^32 threads, so 2^24 - 1 workgroups
 struct QuantCompactArgs {
   QuantKv kv;
   int d;

@@ -219,8 +219,7 @@ hipError_t launch_write(const QuantWriteArgs& a, hipStream_t s) {
 bool quant_write_plan(QuantWriteArgs& a) {
   a.groups = (a.T - 1) / kTok + 1;
   const int64_t all = static_cast<int64_t>(a.B) * a.groups;
-  constexpr int64_t kMost = 1ll << 25;            // (a launch has fewer than 2^32 threads)
-  if (all >= kMost || all * a.kv.Hkv >= kMost) return false;
+  if (all > kLaunchWaves || all * a.kv.Hkv > kLaunchWaves / 2) return false;
   a.tasks = 2 * all * a.kv.Hkv;
   return true;
 }

@@ -28,3 +28,18 @@ def test_a_sampling_workspace_serves_every_smaller_vocabulary():
             need = sx.specexit_sample_workspace_bytes(0, M, V)
             assert need >= last, (M, V, need, last)
             last = need
+
+
+def test_calls_at_the_edge_of_a_launch_are_refused():
+    """2^24 workgroups of 256 threads are 2^32 threads, one more than a launch takes."""
+    import test_quant_abi_cpu as abi
+    from paper_2509_24248_amd import binding as sx
+    one = abi.view(n_kv_heads=1)
+    for T in (16 * ((1 << 25) - 1), 16 * (1 << 25)):                    # 2^26 - 2 and 2^26 waves
+        abi.refused(sx, abi.write(sx, one, B=1, T=T, stride=128), sx.EUNSUPPORTED, "more than one call takes")
+    for B, heads, layers in ((2731, 6143, 4), (1, 32768, 2048)):       # 2^26 - 1 and 2^26 + 1 waves
+        abi.refused(sx, abi.compact(sx, abi.view(n_kv_heads=heads), layers=layers, B=B), sx.EUNSUPPORTED, "grid")
+    # the kernel that merges has a wave per row
+    wide = abi.view(n_kv_heads=512, l_max=64)
+    assert sx.specexit_quant_verify_attn_workspace_bytes(wide, sx.BF16, 1024, 64, 1024) == 0 and "can split" in sx.last_error()
+    assert sx.specexit_quant_verify_attn_workspace_bytes(wide, sx.BF16, 1023, 64, 1024) > 0
