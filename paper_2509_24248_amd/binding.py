@@ -466,6 +466,19 @@ def specexit_set_dev_status(word: Optional[torch.Tensor]) -> None:
     _check(LIB.specexit_set_dev_status(None if word is None else C.c_void_p(word.data_ptr())))
 
 
+_STORAGE = {F32: torch.float32, BF16: torch.bfloat16}
+
+
+def _arg(t: Optional[torch.Tensor], dtype: Optional[torch.dtype], n: int, name: str):
+    """Address of a tensor of `n` values at least: the library takes it at its word for type and length (dtype None: of no known type, refused there)."""
+    if t is None:
+        return None
+    assert dtype is None or t.dtype == dtype, f"{name} must be {dtype}, not {t.dtype}"
+    assert t.numel() >= n, f"{name} has {t.numel()} values, {n} are read"
+    assert t.is_cuda and t.is_contiguous(), f"{name}: device-resident contiguous tensors only"
+    return t.data_ptr()
+
+
 def _token_stride(rows: torch.Tensor, B: int, T: int, kv: QuantKVView) -> int:
     """rows: [B, T, Hkv, d], heads and values consecutive, tokens evenly apart (a slice of a fused projection's output will do)."""
     assert rows.is_cuda and tuple(rows.shape) == (B, T, kv.n_kv_heads, kv.head_dim)
@@ -477,10 +490,12 @@ def _token_stride(rows: torch.Tensor, B: int, T: int, kv: QuantKVView) -> int:
 
 def specexit_quant_kv_write(kv: QuantKVView, dtype: int, B: int, T: int, k_rows, v_rows, pos, count=None, flags: int = 0,
                             stream=None) -> None:
+    want = _STORAGE.get(dtype)
+    assert want is None or k_rows.dtype == v_rows.dtype == want, f"k_rows and v_rows must be {want}"
+    pos, count = _arg(pos, torch.int32, B, "pos"), _arg(count, torch.int32, B, "count")
     step = _token_stride(k_rows, B, T, kv)
     assert _token_stride(v_rows, B, T, kv) == step
-    _check(LIB.specexit_quant_kv_write(C.byref(kv), dtype, B, T, C.c_void_p(k_rows.data_ptr()), C.c_void_p(v_rows.data_ptr()), step,
-                                       _ptr(pos), _ptr(count), flags, _stream(stream)))
+    _check(LIB.specexit_quant_kv_write(C.byref(kv), dtype, B, T, k_rows.data_ptr(), v_rows.data_ptr(), step, pos, count, flags, _stream(stream)))
 
 
 def specexit_quant_verify_attn_workspace_bytes(kv: QuantKVView, dtype: int, B: int, n_q: int, n_q_heads: int) -> int:
@@ -489,17 +504,24 @@ def specexit_quant_verify_attn_workspace_bytes(kv: QuantKVView, dtype: int, B: i
 
 def specexit_quant_verify_attn(kv: QuantKVView, dtype: int, B: int, n_q: int, n_q_heads: int, q, ctx_len, mask, scale: float,
                                out, workspace, flags: int = 0, stream=None) -> None:
+    want, n = _STORAGE.get(dtype), B * n_q * n_q_heads * kv.head_dim
+    q, out = _arg(q, want, n, "q"), _arg(out, want, n, "out")
+    ctx_len = _arg(ctx_len, torch.int32, B, "ctx_len")
+    mask = _arg(mask, torch.int64 if mask is None or mask.dtype != torch.uint64 else torch.uint64, B * n_q, "mask")
     wp, wb = _ws_args(workspace)
-    _check(LIB.specexit_quant_verify_attn(C.byref(kv), dtype, B, n_q, n_q_heads, _ptr(q), _ptr(ctx_len), _ptr(mask),
-                                          C.c_float(scale), _ptr(out), wp, wb, flags, _stream(stream)))
+    _check(LIB.specexit_quant_verify_attn(C.byref(kv), dtype, B, n_q, n_q_heads, q, ctx_len, mask, C.c_float(scale), out, wp, wb, flags,
+                                          _stream(stream)))
 
 
 def specexit_quant_kv_compact(kv: QuantKVView, n_layers: int, layer_stride_bytes: int, scale_stride_bytes: int, B: int, n_q: int,
                               ctx_len, accept_path, accept_len, dtype: int = BF16, last_node=None, block_hidden=None, D: int = 0,
                               hidden_next=None, flags: int = 0, stream=None) -> None:
-    _check(LIB.specexit_quant_kv_compact(C.byref(kv), n_layers, layer_stride_bytes, scale_stride_bytes, B, n_q, _ptr(ctx_len),
-                                         _ptr(accept_path), _ptr(accept_len), dtype, _ptr(last_node), _ptr(block_hidden), D,
-                                         _ptr(hidden_next), flags, _stream(stream)))
+    i32, want = torch.int32, _STORAGE.get(dtype)
+    ctx_len, accept_path = _arg(ctx_len, i32, B, "ctx_len"), _arg(accept_path, i32, B * n_q, "accept_path")
+    accept_len, last_node = _arg(accept_len, i32, B, "accept_len"), _arg(last_node, i32, B, "last_node")
+    block_hidden, hidden_next = _arg(block_hidden, want, B * n_q * D, "block_hidden"), _arg(hidden_next, want, B * D, "hidden_next")
+    _check(LIB.specexit_quant_kv_compact(C.byref(kv), n_layers, layer_stride_bytes, scale_stride_bytes, B, n_q, ctx_len, accept_path,
+                                         accept_len, dtype, last_node, block_hidden, D, hidden_next, flags, _stream(stream)))
 
 
 def specexit_sample_workspace_bytes(dtype: int, M: int, V: int) -> int:
@@ -508,12 +530,17 @@ def specexit_sample_workspace_bytes(dtype: int, M: int, V: int) -> int:
 
 def specexit_sample(dtype: int, M: int, V: int, logits, u, token, prob=None, temperature=None, top_k=None, top_p=None, min_p=None,
                     rows_per_seq: int = 1, workspace=None, flags: int = 0, stream=None) -> None:
-    """logits: [M, >= V], rows evenly apart (a slice of wider rows will do)."""
+    """logits: [M, >= V], rows evenly apart (a slice of wider rows will do); settings: one for each rows_per_seq rows, fp32 (top_k int32)."""
+    want, f32, n = _STORAGE.get(dtype), torch.float32, -(-M // max(rows_per_seq, 1))
+    assert want is None or logits.dtype == want, f"logits must be {want}"
+    temperature, top_k = _arg(temperature, f32, n, "temperature"), _arg(top_k, torch.int32, n, "top_k")
+    top_p, min_p = _arg(top_p, f32, n, "top_p"), _arg(min_p, f32, n, "min_p")
+    u, token, prob = _arg(u, f32, M, "u"), _arg(token, torch.int32, M, "token"), _arg(prob, f32, M, "prob")
     assert logits.is_cuda and logits.dim() == 2 and logits.shape[0] == M and logits.shape[1] >= V and logits.stride(1) == 1
     ld = logits.stride(0) if M > 1 else logits.shape[1]
     wp, wb = _ws_args(workspace)
-    _check(LIB.specexit_sample(dtype, M, V, C.c_void_p(logits.data_ptr()), ld, rows_per_seq, _ptr(temperature), _ptr(top_k),
-                               _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(token), _ptr(prob), wp, wb, flags, _stream(stream)))
+    _check(LIB.specexit_sample(dtype, M, V, logits.data_ptr(), ld, rows_per_seq, temperature, top_k, top_p, min_p, u, token, prob, wp, wb,
+                               flags, _stream(stream)))
 
 
 def quant_attn_query(kv: QuantKVView, dtype: int, n_q_heads: int) -> QuantAttnQuery:
