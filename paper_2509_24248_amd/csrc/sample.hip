@@ -13,8 +13,14 @@
 //                    those (a search over the keys of all floats: what follows compares logits, not weights or bins), reads the logits
 //                    again: masses of what is kept for certain per segment of 512 tokens, and a list of the tokens in doubt.
 //   3 k_sample_pick  a workgroup per row finds the border in the list (at most 4096), the draw's segment and in it the token.
-// Rows without any difference need no border but a number.  What is left without a list (more than 4096 tokens within 2^-16 nat of a border, and
-// logits beyond 2^20 temperatures) is a selection over the row by the third kernel, 0.4 to 0.8 ms whatever the number of rows.
+// Rows without any difference need no border but a number.
+// The slow way.  A list holds 4096 tokens, 2048 of a chunk.  What is in doubt is every token of the bins of a row's borders, and those are 1/16 nat wide as soon
+// as one of the row's chunks has a token more than 8 nats (and less than 4096) below its best one; only where all chunks span less are they halved,
+// up to twelve times.  The border of top-p is known to 2e-5 of the sum, so from top-p 0.99998 on everything below it is in doubt.  Rows with more tokens in
+// doubt than that, and logits beyond 2^20 temperatures, are selected from whole by the third kernel, with equal results: 0.42 to 0.49 ms for 151936
+// fp32 logits, 0.71 to 0.82 for 262144, whether of one row or 144.  That happens in earnest (top-p alone, microseconds of 1 row and of 144, not 25 to 75):
+//   151936 logits, a head's rows, top-p 0.9999: 30 and 488; from 0.99997 on 430 and 488    a flat body (deviation 0.3 or 0.5) and one token 10 above: 430, 480
+//   262144 logits of deviation 1 and more, top-p 0.9: 710, 800 (deviation 0.9: 42, and 777 where one of the 144 rows is taken so)
 // What bounds it: 144 rows of 151936 fp32 logits (87.5 MB, 16.6 us at a copy's rate) take 21 us in the first kernel (4.2 TB/s), 34 in the
 // second (vector instructions, 86 % of its time: fifteen in 64 bits and as many others for a token's weight) and 12 in the third; 7 rows with
 // top-k 4.5, 8 and 6.4 us: chains of dependent loads, five in the last.  One pass that kept every weight would write as much as it reads.
@@ -811,7 +817,7 @@ __global__ __launch_bounds__(kT) void k_sample_pick(const SampleArgs a) {
   const bool scanned = info.mode == kModeScan || n > kList;
   const Scale z = {st.c, static_cast<double>(top) * st.c};
   if (scanned) {
-    // ---- without histograms and list: a row whose logits are far from anything (2^26 nats), or whose list is too long, as where more than 4096 tokens
+    // ---- without histograms and list: a row whose logits are far from anything (2^20 temperatures), or whose list is too long, as where more than 4096 tokens
     // of nearly one weight lie at the border
     sure = NAN;
     doubt = -INFINITY;
