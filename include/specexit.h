@@ -417,7 +417,8 @@ int32_t specexit_quant_kv_compact(const specexit_quant_kv_view *kv, int32_t n_la
  * the kept weights' sum (u in [0, 1), forced into it); prob[r] (may be NULL) its share of that sum.  NaN logits are never
  * drawn; if one is +infinity, only such ones are; a row without any logit above -infinity gives token -1 and
  * prob 0.  Weights are 64-bit numbers and their sums fixed-point ones, so that a draw is the same
- * whatever the launch shape, and a border between two tokens, or of a filter, is met to 1e-12 of the sum.
+ * whatever the launch shape.  A weight is rounded to 2^-45 of the best one's, so a border between two tokens, or of a
+ * filter, is met to V 2^-46 + 2^-52 max |l / temperature| of the sum (2.2e-9 at V = 151936, 4e-9 at the most).
  * The drafts of specexit_draft_step and _tree_level are not drawn, so handing
  * these tokens to specexit_accept_exit as target_argmax accepts a draft with the target's own
  * probability of it and leaves the output distributed as without drafts. */
