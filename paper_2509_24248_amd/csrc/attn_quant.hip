@@ -416,8 +416,13 @@ __global__ __launch_bounds__(64 * NK * NR, NK * NR <= 8 ? 2 : (NK * NR + 3) / 4)
     __builtin_amdgcn_sched_barrier(0);
 
     // ---- online softmax; lane (row, q) owns keys t0 + 16 j + 4 q + e of its row.  The reference of the exponents moves only when a score
-    // exceeds its row's by more than kSlack.
-    constexpr float kSlack = 8.f;
+    // exceeds its row's by more than kSlack.  Probabilities of one bf16 part have none: the largest is then 1, which bf16 holds, and its rounding
+    // is what a peaked row's error would be made of: a result whose value is all in that key's is off by half a step, with a slack by up to 2.5.
+    // (Root mean square error against 64 bits, beyond that of fp32 arithmetic rounded to bf16, with a slack of 8 / none: 8 sequences of 300 .. 900, 72
+    // rows 3.5 / 0.5 %; 8 of 2048 .. 16384, 28 rows 2.7 / 0.25 %, 16 rows 1.1 / 0.3 %; 64-wide, 8 of 1000 .. 8000, 64 rows 1.4 / 0.3 %; with two parts
+    // 0.1 % everywhere.  What it costs, 8 sequences of 2048 .. 16384: up to 16 rows nothing, 28 rows 34.2 -> 34.7 us, 48 rows 40.6 -> 41.8, 72 rows 57.2 ->
+    // 59.8, 128 rows 71.2 -> 76.2; 16 of 8192 .. 32768, 72 rows 188 -> 194.  Two parts: 35.8, 44.5, 63.8, 83.6; 223.)
+    constexpr float kSlack = PP == 1 ? 0.f : 8.f;
     const bool plain = t0 + kTileKeys <= min(L, s1) && sl2 > 0.f;
     float z[RTW][8], unit = sl2;
 #pragma unroll

@@ -6,7 +6,7 @@ import torch
 from oracle import specexit_oracle as O
 from workloads import gen
 
-from quant_bound import TILE, signed_values, worst_share
+from quant_bound import TILE, attend, signed_values, unit_rows, visible, worst_share
 from quant_harness import Cache, attn, queries, tree_masks
 
 pytestmark = pytest.mark.gpu
@@ -113,3 +113,33 @@ def test_a_large_query_channel_that_no_key_has(d, r):
     q = rng.uniform(1.0, 2.0, (1, 3, 8, d)) * rng.choice([-1.0, 1.0], (1, 3, 8, d))
     q[..., 5] = np.ldexp(1.0, r)
     check(cache, gen.round_to_bf16(q.astype(np.float32)), L, scale=0.5 * d ** -0.5)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,n_q", [(4, 1), (4, 7), (8, 8), (8, 9), (8, 16)])
+def test_a_rows_largest_probability_is_not_rounded(d, G, n_q):
+    """One key with a value, a few nats above those before it in its ring: its probability is the reference, 1 in bf16, and the result off by the
+    rounding of the output alone, half a step, and by what a score and the sums are off (2^-14 of the result at most: scores of 4 and less, d 2^-23 of
+    their largest product for each of two parts, 4000 numbers added in fp32)."""
+    rng = np.random.default_rng(57)
+    B, Hkv = 8, 4
+    L = np.full(B, 4000)
+    cache = Cache(rng, B, Hkv, d, L + n_q, None, spread=0.0)
+    u = rng.choice([-1.0, 1.0], d)
+    q = gen.round_to_bf16((u * rng.uniform(1.0, 1.5, (B, n_q, Hkv * G, 1))).astype(np.float32))
+    cache.ks -= 2                                              # scores of the other keys: a quarter of a nat
+    cache.v[:] = 0
+    for b in range(B):
+        p = int(rng.integers(200, 3900))
+        codes, s = O.quant_rows(u * rng.uniform(2.0, 3.0, (Hkv, 1)) * d ** -0.5)
+        cache.k[b, :, p], cache.ks[b, :, p] = codes, s
+        cache.v[b, :, p], cache.vs[b, :, p] = rng.integers(0x38, 0x40, (Hkv, d)), 139
+    got = attn(cache, q, L)
+    for b in range(B):
+        see = visible(int(L[b]), n_q, None).repeat(G, 0)
+        for g in range(Hkv):
+            k, v = unit_rows(cache, b, g, int(L[b]) + n_q)
+            ref = attend(q[b, :, g * G:(g + 1) * G].reshape(n_q * G, d), k, v, see, d ** -0.5)[0]
+            half = np.exp2(np.floor(np.log2(ref)) - 8)
+            err = np.abs(got[b, :, g * G:(g + 1) * G].reshape(n_q * G, d) - ref)
+            assert (err <= half + 2.0 ** -14 * ref).all(), (b, g, float((err / half).max()))
