@@ -18,9 +18,9 @@
 //                 which is exact; B = the probabilities times the keys' scales (powers of two: exact) in PP bf16 parts.
 // 64-wide heads need half the products: the instruction's second half then takes the same codes with the next part of the queries.
 //
-// What bounds it.  Few rows: memory (8 sequences of 2k to 16k tokens, 28 rows a head, 153 MB: 30.5 us = 5.0 TB/s, and 4.6 for the merge).  Many:
-// instructions.  16 rows x 32 keys take a wave some 122 vector instructions of 4.4 cycles - 32 convert V, 8 exponentials of 8.4 - and 256 cycles of
-// matrix instructions on a unit that issues one or the other: 16 sequences of 8k to 32k, 72 rows: 180 to 197 us for 681 MB, 129 at a copy's rate.
+// What bounds it.  Few rows: memory (8 sequences of 2k to 16k tokens, 28 rows a head, 153 MB: 31 us = 4.9 TB/s, and 4.7 for the merge).  Many:
+// instructions.  16 rows x 32 keys take a wave some 129 vector instructions of 4.4 cycles - 32 convert V, 8 exponentials of 8.4 - and 256 cycles of
+// matrix instructions on a unit that issues one or the other: 16 sequences of 8k to 32k, 72 rows: 193 to 199 us for 681 MB, 129 at a copy's rate.
 // Short: the split from the lengths, its first loads and the merge (one sequence of 4096: 8.8 and 3.6 us).
 // Tried: both operands of the next tile in registers across the barrier (no gain); two workgroups of five waves per compute unit (slower); three or
 // four row tiles to a wave, one wave a SIMD (slower: 5.3 cycles an instruction); tiles unrolled over the ring's slots (spills).
@@ -757,10 +757,11 @@ hipError_t launch_one(const QuantAttnArgs& a, hipStream_t s) {
 // a compute unit take.  One wave of a SIMD alone issues every 5.3 cycles, four together every 2.6 to 4.4, so twelve to sixteen waves are
 // wanted, evenly over the four SIMDs (five tiles on two rings, three waves to some SIMDs and two to others: 61.5 us, not 57.3); a wave of two tiles (from seven on) shares the conversion of V.  Microseconds of a call over 8 sequences of 2048 .. 16384 tokens,
 // 8 KV heads, 128-wide (64-wide), against the next form's at the same rows:
-//   rows 16: 31.6, not 35.8 (21.1, 28.2)   28: 34.4, 42.9 (26.3, 33.3)   48: 41.3, 45.9 (31.6, 35.2)   64: 46.4, 60.2 (35.8, 45.5)
-//        72: 57.3, 63.9 (40.1, 45.2)   96: 62.1, 70.8 (46.2, 51.3)   128: 72.5, 76.8 with eight waves of one tile (52.6, 55.7)
-// Probabilities are one bf16 part, off by half a step (2^-8) at most, as the results are rounded anyway; two parts
-// took 34.4 -> 36.4 at 28 rows, 59.3 -> 67.9 at 72 (on two rings).  A step of two tiles (four of 64-wide heads) halves the barriers where the ring's slots
+//   rows 16: 31.7, not 34.0 (20.5, 26.5)   28: 34.7, 39.7 (27.0, 31.6)   48: 42.1, 47.4 (32.7, 35.6)   64: 48.6, 58.6 (36.7, 41.2)
+//        72: 59.3, 66.3 (42.4, 46.1)   96: 66.9, 74.6 (47.2, 52.5)   128: 76.8, 78.2 with eight waves of one tile (54.3, 55.6)
+// Probabilities are one bf16 part, off by half a step (2^-8) at most, as the results are rounded anyway: with the largest of a row exact (kSlack) the
+// error against 64 bits is 0.1 to 0.5 % above that of fp32 arithmetic rounded to bf16 (3 to 4 % where a row sees some fifty keys), with two parts
+// 0.1 %, at 35.8 us for 28 rows and 63.8 for 72.  With a slack of 8: a step of two tiles (four of 64-wide heads) halves the barriers where the ring's slots
 // allow it: 96 rows 64.6 -> 62.1 (48.8 -> 46.2), 112 rows 71.6 -> 68.9; below it gains nothing or costs (48 rows 40.8 -> 43.0).
 template <int HD> hipError_t launch_bf16(const QuantAttnArgs& a, hipStream_t s) {
   constexpr int K2 = HD == 64 ? 4 : 2;            // tiles of a step
@@ -775,7 +776,8 @@ template <int HD> hipError_t launch_bf16(const QuantAttnArgs& a, hipStream_t s) 
   }
 }
 
-// fp32: three parts of queries and probabilities take the registers of sixteen waves.  8 sequences of 500 .. 4000 tokens, 128-wide, against the
+// fp32: three parts of queries and probabilities take 172 to 187 registers of a lane, more than twelve or sixteen waves have; four to eight waves (eight
+// for one or two row tiles, which would fit, were not measured).  8 sequences of 500 .. 4000 tokens, 128-wide, against the
 // form of twice the rows: 16 rows 18.1 us, not 24.6; 28 rows 25.3, 31.5; 64 rows 35.6, 49.9.  64-wide: 28 rows 18.9, 24.7; 64 rows 27.1, 34.8.
 hipError_t launch_f32(const QuantAttnArgs& a, hipStream_t s) {
   const int tiles = row_tiles(a);
@@ -797,7 +799,9 @@ template <typename T, int D> hipError_t launch_combine(const QuantAttnArgs& a, h
 }  // namespace
 
 bool quant_attn_plan(QuantAttnArgs& a, int num_cus) {
-  a.use_mfma = kTwoPart;                          // (its maxima are in log2 units)
+  // Not kOnePart, whose launches of middling size spread over 256 workgroups because shorter segments are nearer: with the largest probability of a row
+  // exact it makes no difference (4 sequences of 600 .. 6 of 1500: errors of 1.528e-3 / 1.528e-3 to 1.493e-3 / 1.493e-3, times within 1.5 %).
+  a.use_mfma = kTwoPart;
   a.G = a.Hq / a.Hkv;
   a.g_inv = (65536 + a.G - 1) / a.G;
   // a workgroup's start at a unit costs some eight granules: with 4, 8, 14 the 8 sequences of 28 rows took 36.9, 34.7, 34.8 us

@@ -262,7 +262,7 @@ struct QuantCompactArgs {
   int moves, tasks;                        // waves that move rows, and all (set by the launch)
 };
 hipError_t launch_quant_compact(const QuantCompactArgs& a, hipStream_t s);
-// k, v: codes; dtype: of q and out
+// k, v: codes; dtype: of q and out; use_mfma: only what attn_sched_line makes of it
 struct QuantAttnArgs : AttnArgs {
   const void *ks, *vs;
   int page_shift;            // log2 of the page size, -1 where it is no power of two

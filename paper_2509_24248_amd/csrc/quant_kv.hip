@@ -34,9 +34,9 @@ __device__ __forceinline__ int64_t quant_row(const QuantKv& kv, int b, int h, in
 }
 
 // A wave takes sixteen tokens of K or V of one head: D / 8 lanes a row, eight values a lane, all loads of the wave requested together.
-// Bound by memory: 4 prompts of 4111 tokens, 8 heads, bf16 (76 MB): 13.8 us = 5.5 TB/s, a copy's rate 5.3 (with every value looked at for being
-// finite, not only the wave's largest, 16.6: the vector unit was busy for 89 % of them); a block of 56 tokens: 3.6 us, a launch and two
-// dependent loads.
+// Bound by memory: 4 prompts of 4111 tokens, 8 heads, bf16 (76 MB): 13.8 to 14.4 us = 5.3 to 5.5 TB/s, a copy's rate 5.3 (with every value looked at
+// for being finite, not only the wave's largest, 16.6: the vector unit was busy for 89 % of them); of fp32 ones (126 MB) 19.7 us = 6.4 TB/s; 64-wide
+// heads 9.1 us (38 MB) and 11.0 (63 MB); a block of 56 tokens: 3.6 us, a launch and two dependent loads.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void k_quant_write(const QuantWriteArgs a) {
   constexpr int LPR = D / 8, RPI = 64 / LPR, U = kTok / RPI;     // lanes of a row, rows of an instruction, instructions

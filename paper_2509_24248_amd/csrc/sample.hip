@@ -20,7 +20,7 @@
 // doubt than that, and logits beyond 2^20 temperatures, are selected from whole by the third kernel, with equal results: 0.42 to 0.49 ms for 151936
 // fp32 logits, 0.71 to 0.82 for 262144, whether of one row or 144.  That happens in earnest (top-p alone, microseconds of 1 row and of 144, not 25 to 75):
 //   151936 logits, a head's rows, top-p 0.9999: 30 and 488; from 0.99997 on 430 and 488    a flat body (deviation 0.3 or 0.5) and one token 10 above: 430, 480
-//   262144 logits of deviation 1 and more, top-p 0.9: 710, 800 (deviation 0.9: 42, and 777 where one of the 144 rows is taken so)
+//   262144 logits of deviation 1 and more, top-p 0.9: 710, 800 (deviation 0.9: 42, and 777 where one of the 144 rows is taken so); 144 rows of 151936 of deviation 1.4, top-p 0.95: 460
 // What bounds it: 144 rows of 151936 fp32 logits (87.5 MB, 16.6 us at a copy's rate) take 21 us in the first kernel (4.2 TB/s), 34 in the
 // second (vector instructions, 86 % of its time: fifteen in 64 bits and as many others for a token's weight) and 12 in the third; 7 rows with
 // top-k 4.5, 8 and 6.4 us: chains of dependent loads, five in the last.  One pass that kept every weight would write as much as it reads.

@@ -143,3 +143,20 @@ def test_a_rows_largest_probability_is_not_rounded(d, G, n_q):
             half = np.exp2(np.floor(np.log2(ref)) - 8)
             err = np.abs(got[b, :, g * G:(g + 1) * G].reshape(n_q * G, d) - ref)
             assert (err <= half + 2.0 ** -14 * ref).all(), (b, g, float((err / half).max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_queries_that_are_not_finite(dtype, d):
+    """A query with an infinity or a NaN has scores that are none: its row is NaN, and no other is touched."""
+    rng = np.random.default_rng(58)
+    L = np.array([300, 20])
+    cache = Cache(rng, 2, 2, d, L + 4, 16)
+    q = queries(rng, 2, 4, 8, d, dtype)
+    clean = attn(cache, q, L, dtype=dtype)
+    q[0, 0, 0, 3], q[0, 1, 1, 5], q[1, 2, 2, 7] = np.inf, -np.inf, np.nan
+    q[1, 3, 3] = np.inf
+    bad = ~np.isfinite(q).all(-1)
+    got = attn(cache, q, L, dtype=dtype)
+    assert np.isnan(got[bad]).all()
+    np.testing.assert_array_equal(got[~bad], clean[~bad])
