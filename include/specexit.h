@@ -385,7 +385,7 @@ int32_t specexit_quant_kv_write(const specexit_quant_kv_view *kv, int32_t dtype,
  * query channel 2^13 times the others costs them bits, whether or not the keys have that channel; the
  * plain cache's attention has no such limit.)  Probabilities are rounded to bf16 (fp32 results: 24 bits), sums are fp32.
  * Entries that a row does not see may hold anything, NaN included (a NaN among them makes the call slow: rows of its
- * sequence are computed again key by key, 0.2 us per entry of the context); a row that sees nothing (an empty
+ * sequence are computed again key by key, some 0.2 us per entry of the context); a row that sees nothing (an empty
  * context and an empty mask word) is all zeros. */
 int32_t specexit_quant_verify_attn(const specexit_quant_kv_view *kv, int32_t dtype, int32_t B, int32_t n_q,
                                    int32_t n_q_heads, const void *q, const int32_t *ctx_len /*[B]*/,
