@@ -143,6 +143,46 @@ typedef struct {
   int64_t l_max, n_pages;
 } specexit_quant_kv_view;
 
+/* One layer's latent cache: an entry is one vector of latent_dim + rope_dim values for all query heads - the
+ * key whole, the value with its first latent_dim.
+ *   CONTIG: c is [B, l_max, latent_dim + rope_dim].
+ *   PAGED : c is [n_pages, page_size, latent_dim + rope_dim]; page_table as in specexit_kv_view, page_size any
+ *           multiple of 16, n_pages * page_size < 2^35.
+ * latent_dim in {128, 256, 512}, rope_dim 64; c is 16-byte aligned. */
+typedef struct {
+  uint32_t struct_size;
+  int32_t layout;        /* specexit_kv_layout */
+  int32_t dtype;
+  int32_t latent_dim, rope_dim;
+  void *c;
+  const int32_t *page_table;
+  int32_t page_size, max_pages_per_seq;
+  int64_t l_max, n_pages;
+} specexit_latent_kv_view;
+
+/* A rotation by position: pair c of a head's first rot_dim values, (x_c, x_{c + rot_dim/2}) or, interleaved, (x_2c, x_2c+1),
+ * becomes amplitude (x cos t - y sin t, x sin t + y cos t) with t = position * f_c; values from rot_dim on stay.
+ *   SPECEXIT_ROPE_PLAIN   f_c = theta^(-2c / rot_dim)
+ *   SPECEXIT_ROPE_LINEAR  f_c / factor
+ *   SPECEXIT_ROPE_BANDS   with n = orig_len f_c / 2 pi (turns over the original length) and k = (n - low) / (high - low), forced
+ *                         into 0 .. 1:  f_c (k + (1 - k) / factor)
+ *   SPECEXIT_ROPE_RAMP    with a = floor(at(high)), at least 0, z = ceil(at(low)), at most rot_dim - 1, at(n) = rot_dim ln(orig_len / 2 pi n) / (2 ln theta)
+ *                         and k = (c - a) / max(z - a, 0.001), forced into 0 .. 1:  f_c ((1 - k) + k / factor)
+ * rot_dim even, 2 .. 256; theta > 1; factor >= 1 (unused by PLAIN); 0 < low < high and orig_len >= 1 (BANDS, RAMP); amplitude > 0. */
+#define SPECEXIT_ROPE_PLAIN  0
+#define SPECEXIT_ROPE_LINEAR 1
+#define SPECEXIT_ROPE_BANDS  2
+#define SPECEXIT_ROPE_RAMP   3
+typedef struct {
+  uint32_t struct_size;
+  int32_t rot_dim;
+  int32_t interleaved;
+  int32_t scaling;       /* SPECEXIT_ROPE_* */
+  float theta, factor, low, high;
+  int32_t orig_len;
+  float amplitude;
+} specexit_rope_desc;
+
 /* Exit controller settings.  Defaults of the paper: alpha 0.1 (Appendix, EWMA);
  * confidence > 0.8, progress > 0.3, remaining < 200 for the combined rule, or
  * 0.9 / 0.8 / 100 with a single bit of signal_mask (Appendix, "Stop Threshold"). */
@@ -433,6 +473,77 @@ int32_t specexit_sample(int32_t dtype, int32_t M, int32_t V, const void *logits 
 /* never less for more rows or a larger V: one of the largest batch's size serves every smaller one */
 size_t specexit_sample_workspace_bytes(int32_t dtype, int32_t M, int32_t V);
 
+/* ---- rotary positions (the target's queries and keys in front of its verification attention) ----
+ * specexit_rope_table writes the frequencies of a rotation, f_c / 2 pi as fractions of 2^64, to turns [rot_dim / 2] on the device: once per
+ * model; the calls below read it and take rot_dim, interleaved and amplitude from the same descriptor.  An angle at position p
+ * is off by p (2^-64 turns + 2^-48 f_c) at most. */
+int32_t specexit_rope_table(const specexit_rope_desc *rope, uint64_t *turns /*[rot_dim/2]*/, void *stream);
+
+/* Rotates the heads of rows.  Head h of token t of sequence b lies (b * T + t) * token_stride + h * head_dim elements behind rows, its result at
+ * (b * T + t) * out_stride + h * head_dim of out, for t < count[b] (count NULL: T; at most T of them; other rows of out are left as they are).  Its position is
+ * pos[b] + offset[b, t], or pos[b] + t without offset (a tree's block: the nodes' depths), forced into 0 .. 2^31 - 1.  out may be rows, with the same
+ * stride, and must not overlap it otherwise.  head_dim a multiple of 16 up to 512, at least rot_dim; pointers and strides are multiples of 16 bytes. */
+int32_t specexit_rope(int32_t dtype, const specexit_rope_desc *rope, const uint64_t *turns, int32_t B, int32_t T, int32_t n_heads,
+                      int32_t head_dim, const void *rows, int64_t token_stride, void *out, int64_t out_stride,
+                      const int32_t *pos /*[B]*/, const int32_t *offset /*[B,T] or NULL*/, const int32_t *count /*[B] or NULL*/,
+                      uint32_t flags, void *stream);
+
+/* The block (or prompt) of one layer in one call: queries rotated to q_out [B, T, n_q_heads, head_dim] (n_q_heads 0: none; q_rows and q_out are then
+ * unused), keys rotated and stored, with the values, at cache entries pos[b] + t, t < count[b]; type and head width are the view's.  Rows, positions and counts as in
+ * specexit_rope; keys and values share kv_stride.  Entries outside the cache, or of a page outside the pool, are not written (reported).  No two sequences of a
+ * call may share entries that it writes.  (For the 8-bit cache: specexit_rope on the keys of the fused rows, then specexit_quant_kv_write.) */
+int32_t specexit_rope_kv_write(const specexit_kv_view *kv, const specexit_rope_desc *rope, const uint64_t *turns, int32_t B, int32_t T,
+                               int32_t n_q_heads, const void *q_rows, int64_t q_stride, const void *k_rows, const void *v_rows,
+                               int64_t kv_stride, void *q_out, const int32_t *pos /*[B]*/, const int32_t *offset /*[B,T] or NULL*/,
+                               const int32_t *count /*[B] or NULL*/, uint32_t flags, void *stream);
+
+/* ---- latent cache: entries written ----
+ * rows (token t of sequence b: (b * T + t) * row_stride elements behind, latent_dim + 64 values in the view's dtype) go to entries pos[b] + t, t < count[b]: the latent x as
+ * x / sqrt(mean x^2 + eps) * gain (gain NULL: as it is), the other 64 values rotated (rope->rot_dim must be 64).  With n_q_heads > 0 the queries' rotated part is
+ * written too: 64 values of head h at (b * T + t) * q_stride + h * head_stride behind q_rows become the last 64 of q_out [B, T, n_q_heads, latent_dim + 64], whose first
+ * latent_dim (the query times the key half of the latent's up-projection) are the caller's and stay.  Positions, counts and what is not written as in specexit_rope_kv_write;
+ * pointers and strides are multiples of 16 bytes. */
+int32_t specexit_latent_kv_write(const specexit_latent_kv_view *kv, const specexit_rope_desc *rope, const uint64_t *turns, int32_t B,
+                                 int32_t T, int32_t n_q_heads, const void *rows, int64_t row_stride, const void *gain /*[latent_dim] or NULL*/,
+                                 float eps, const void *q_rows, int64_t q_stride, int64_t head_stride, void *q_out,
+                                 const int32_t *pos /*[B]*/, const int32_t *offset /*[B,T] or NULL*/, const int32_t *count /*[B] or NULL*/,
+                                 uint32_t flags, void *stream);
+
+/* ---- stage 2 over a latent cache: specexit_verify_attn where one vector a token is key and value of every head (Alg. 1) ----
+ * out[b,i,h,:] = sum_j softmax_j(scale * q[b,i,h,:] . c[j]) c[j][0:latent_dim]; q is [B, n_q, n_q_heads, latent_dim + 64], out [B, n_q, n_q_heads, latent_dim] (to be multiplied with the
+ * value half of the up-projection), in the view's dtype and 16-byte aligned (out: 8 suffice).  Context, block entries and masks as in specexit_verify_attn; n_q_heads 1 .. 256, scale > 0.  bf16
+ * probabilities are multiplied in two bf16 parts (16 bits); fp32 products and sums are fp32.
+ * Entries that a row does not see may hold anything, NaN included (values that are not finite among them make the call slow: rows of its sequence are computed
+ * again key by key); a row that sees nothing (an empty context and an empty mask word) is all zeros. */
+int32_t specexit_latent_verify_attn(const specexit_latent_kv_view *kv, int32_t B, int32_t n_q, int32_t n_q_heads, const void *q,
+                                    const int32_t *ctx_len /*[B]*/, const uint64_t *mask /*[B,n_q] or NULL*/, float scale, void *out,
+                                    void *workspace, size_t workspace_bytes, uint32_t flags, void *stream);
+size_t specexit_latent_verify_attn_workspace_bytes(const specexit_latent_kv_view *kv, int32_t B, int32_t n_q, int32_t n_q_heads);
+
+/* ---- after the round, latent cache: specexit_kv_compact for such a view ---- */
+int32_t specexit_latent_kv_compact(const specexit_latent_kv_view *kv, int32_t n_layers, int64_t layer_stride_bytes, int32_t B,
+                                   int32_t n_q, const int32_t *ctx_len /*[B]*/, const int32_t *accept_path /*[B,n_q]*/,
+                                   const int32_t *accept_len /*[B]*/, const int32_t *last_node /*[B]*/,
+                                   const void *block_hidden /*[B,n_q,D] or NULL*/, int32_t D, void *hidden_next /*[B,D]*/,
+                                   uint32_t flags, void *stream);
+
+/* ---- stage 3: what the target thinks of given tokens ----
+ * logits [M, ld] as in specexit_sample; row r takes temperature[r / rows_per_seq] (NULL: 1; forced into 2^-10 .. 2^96).  With p the softmax of a row's logits over its temperature:
+ *   logprob[r, k] = ln p[token[r, k]], k < n_tok (a token of -1 gives NaN; so does any other one outside the vocabulary, reported);
+ *   entropy[r] = - sum p ln p (may be NULL);
+ *   top_token[r, k], top_logprob[r, k] (may be NULL): the n_top best by (logit descending, index ascending); -1 and -infinity behind the last above -infinity.
+ * NaN logits count as -infinity.  If some are +infinity, those share the probability; a row without any logit above -infinity has log probabilities of -infinity and entropy 0.
+ * At least one of entropy, n_tok and n_top is asked for.  The same row gives the same bits whatever else is in the call only where M * V lies on the same side of 4 million logits. */
+#define SPECEXIT_LOGPROB_MAX_TOK 64
+#define SPECEXIT_LOGPROB_MAX_TOP 32
+int32_t specexit_token_logprobs(int32_t dtype, int32_t M, int32_t V, const void *logits /*[M,ld]*/, int64_t ld, int32_t rows_per_seq,
+                                const float *temperature, int32_t n_tok, const int32_t *token /*[M,n_tok]*/, float *logprob /*[M,n_tok]*/,
+                                float *entropy /*[M] or NULL*/, int32_t n_top, int32_t *top_token /*[M,n_top]*/,
+                                float *top_logprob /*[M,n_top] or NULL*/, void *workspace, size_t workspace_bytes, uint32_t flags,
+                                void *stream);
+/* never less for more rows, a larger V or a larger n_top */
+size_t specexit_token_logprobs_workspace_bytes(int32_t dtype, int32_t M, int32_t V, int32_t n_top);
+
 /* ---- measurement aid -------------------------------------------------------------------
  * Hands the library n pairs of caller-owned hipEvent_t ([host] arrays of handles).  From then
  * on, each launch of the named kernel records the next unused pair around that one kernel (for
@@ -459,7 +570,7 @@ int32_t specexit_copy_probe(const void *src, void *dst, size_t bytes, int32_t no
 
 /* ---- scratch sizes, one query for every call ------------------------------------------------
  * Bytes of workspace that call `op` needs for B sequences and n_q block entries (draft tree level:
- * n_q = W rows per sequence; LM head and sampling: M = B * n_q rows).  `desc` is a [host] struct of the op's
+ * n_q = W rows per sequence; LM head, sampling and log probabilities: M = B * n_q rows).  `desc` is a [host] struct of the op's
  * query type below (first field struct_size); 0 is returned for shapes the call would reject and
  * for ops that use no scratch.  The per-call *_workspace_bytes functions give the same numbers. */
 #define SPECEXIT_OP_DRAFT_STEP       0 /* desc: specexit_draft_query                        */
@@ -472,6 +583,10 @@ int32_t specexit_copy_probe(const void *src, void *dst, size_t bytes, int32_t no
 #define SPECEXIT_OP_SAMPLE           7 /* desc: specexit_sample_query                       */
 #define SPECEXIT_OP_QUANT_KV_WRITE   8 /* no scratch: 0                                     */
 #define SPECEXIT_OP_QUANT_KV_COMPACT 9 /* no scratch: 0                                     */
+#define SPECEXIT_OP_ROPE            10 /* specexit_rope, _rope_kv_write, _latent_kv_write: no scratch, 0 */
+#define SPECEXIT_OP_LATENT_VERIFY_ATTN 11 /* desc: specexit_latent_attn_query              */
+#define SPECEXIT_OP_LATENT_KV_COMPACT 12 /* no scratch: 0                                  */
+#define SPECEXIT_OP_TOKEN_LOGPROBS  13 /* desc: specexit_logprobs_query                     */
 typedef struct {
   uint32_t struct_size;
   const specexit_model_desc *desc;
@@ -496,6 +611,15 @@ typedef struct {
   uint32_t struct_size;
   int32_t dtype, vocab;
 } specexit_sample_query;
+typedef struct {
+  uint32_t struct_size;
+  const specexit_latent_kv_view *kv;
+  int32_t n_q_heads;
+} specexit_latent_attn_query;
+typedef struct {
+  uint32_t struct_size;
+  int32_t dtype, vocab, n_top;
+} specexit_logprobs_query;
 size_t specexit_workspace_bytes(int32_t op, const void *desc, int32_t B, int32_t n_q);
 
 const char *specexit_last_error(void); /* [host] thread-local, never NULL */

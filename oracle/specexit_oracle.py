@@ -27,6 +27,10 @@ What is computed (SpecExit, arXiv 2509.24248):
                     verify_attn and kv_compact over them are those above.
 * sample          - a token from logits and a uniform number: temperature,
                     top-k, top-p, min-p (Alg. 1 samples the target's token).
+* rope_frequencies, rope_heads, latent_rows, latent_attn
+                  - a target's queries and keys rotated by position, a latent
+                    cache's entries and the verification attention over them.
+* token_logprobs  - log probabilities of given tokens, entropy, best tokens.
 * accept_exit     - accepted tokens / accept length / recover token (Alg. 1),
                     EWMA smoothing (Sec. 3.3 "Signal Smoothing", Appendix
                     "Signal Smoothing" EWMA equation, alpha = 0.1; the sliding
@@ -653,3 +657,95 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     run = np.cumsum(w[keep])
     j = min(int(np.searchsorted(run, float(u) * run[-1], side="right")), keep.size - 1)
     return int(keep[j]), float(w[keep[j]] / run[-1]), keep
+
+
+# ---------------------------------------------------------------------------
+# rotary positions, the latent cache, log probabilities
+# ---------------------------------------------------------------------------
+
+PLAIN, LINEAR, BANDS, RAMP = 0, 1, 2, 3
+LONG = np.longdouble            # angles of far positions need more than 53 bits to be called exact
+
+
+def rope_frequencies(rot, theta, scaling=PLAIN, factor=1.0, low=1.0, high=32.0, orig_len=4096):
+    """Angle per position of every pair [rot / 2]."""
+    two_pi = 2 * LONG(np.pi) + LONG(2.4492935982947064e-16)            # (what pi loses in 64 bits, twice)
+    c = np.arange(rot // 2).astype(LONG)
+    f = np.exp(-2 * c / rot * np.log(LONG(theta)))
+    if scaling == LINEAR:
+        return f / LONG(factor)
+    if scaling == BANDS:
+        k = np.clip((orig_len * f / two_pi - LONG(low)) / (LONG(high) - LONG(low)), 0, 1)
+        return f * (k + (1 - k) / LONG(factor))
+    if scaling == RAMP:
+        at = lambda n: rot * np.log(orig_len / (two_pi * LONG(n))) / (2 * np.log(LONG(theta)))
+        a, z = max(np.floor(at(high)), LONG(0)), min(np.ceil(at(low)), LONG(rot - 1))
+        k = np.clip((c - a) / max(z - a, LONG(0.001)), 0, 1)
+        return f * ((1 - k) + k / LONG(factor))
+    return f
+
+
+def rope_heads(x, position, frequencies, interleaved=False, amplitude=1.0):
+    """x [T, heads, d] rotated, token t at position[t]: float64 [T, heads, d]."""
+    x = np.asarray(x, dtype=F64)
+    rot = 2 * len(frequencies)
+    first, second = (slice(0, rot, 2), slice(1, rot, 2)) if interleaved else (slice(0, rot // 2), slice(rot // 2, rot))
+    out = x.copy()
+    for t in range(x.shape[0]):
+        angle = LONG(int(position[t])) * frequencies
+        cs, sn = (amplitude * np.cos(angle)).astype(F64), (amplitude * np.sin(angle)).astype(F64)
+        a, b = x[t, :, first], x[t, :, second]
+        out[t, :, first], out[t, :, second] = a * cs - b * sn, a * sn + b * cs
+    return out
+
+
+def latent_rows(rows, gain, eps, position, frequencies, interleaved=False, amplitude=1.0):
+    """Entries of a latent cache from projected rows [T, r + rot]: the latent normalised (gain None: as it is), the rest rotated."""
+    rows = np.asarray(rows, dtype=F64)
+    r = rows.shape[1] - 2 * len(frequencies)
+    lat = rows[:, :r]
+    if gain is not None:
+        lat = lat / np.sqrt((lat ** 2).mean(axis=1, keepdims=True) + eps) * np.asarray(gain, dtype=F64)
+    return np.concatenate([lat, rope_heads(rows[:, None, r:], position, frequencies, interleaved, amplitude)[:, 0]], axis=1)
+
+
+def latent_attn(q, c, r, ctx_len, mask=None, scale=1.0, page_table=None, page_size=16, absolute=False):
+    """verify_attn where entry j of a sequence, c[j] [r + rot], is the key of every head and c[j][:r] its value; rows that see nothing are
+    zero.  q [B, n_q, H, r + rot] -> [B, n_q, H, r].  absolute: with |values|."""
+    B, n_q, H, _ = q.shape
+    out = np.zeros((B, n_q, H, r), dtype=F64)
+    for b in range(B):
+        for i in range(n_q):
+            row = int(mask[b, i]) if mask is not None else (1 << (i + 1)) - 1
+            vis = visible_positions(int(ctx_len[b]), row, n_q)
+            if len(vis) == 0:
+                continue
+            rows = c[b, vis] if page_table is None else c[page_table[b, vis // page_size], vis % page_size]
+            rows = np.asarray(rows, dtype=F64)
+            for h in range(H):
+                p = softmax_two_pass(scale * (rows @ np.asarray(q[b, i, h], dtype=F64)))
+                out[b, i, h] = p @ (np.abs(rows[:, :r]) if absolute else rows[:, :r])
+    return out
+
+
+def token_logprobs(logits, tokens, n_top=0, temperature=1.0):
+    """One row: (log probabilities of `tokens`, entropy, the n_top best token ids, theirs).  NaN counts as -infinity; infinite ones share the
+    probability; a row without any above -infinity: -infinity, entropy 0.  -1 and -infinity behind the last token above -infinity."""
+    l = np.asarray(logits, dtype=F64)
+    l = np.where(np.isnan(l), -np.inf, l)
+    best = l.max()
+    if best == -np.inf:
+        return np.full(len(tokens), -np.inf), 0.0, np.full(n_top, -1), np.full(n_top, -np.inf)
+    with np.errstate(invalid="ignore"):
+        y = np.where(l == best, 0.0, (l - best) / min(max(float(temperature), 2.0 ** -10), 2.0 ** 96))
+    w = np.exp(y)
+    n = int((l == best).sum())
+    rest = w[l != best].sum()
+    logp = y - np.log(n) - np.log1p(rest / n)
+    entropy = np.log(n) + np.log1p(rest / n) - (w * np.where(w > 0, y, 0.0)).sum() / (n + rest)
+    order = [int(i) for i in np.lexsort((np.arange(l.size), -l))[:n_top] if l[i] > -np.inf]
+    top = np.full(n_top, -1)
+    top[:len(order)] = order
+    top_logp = np.full(n_top, -np.inf)
+    top_logp[:len(order)] = logp[order]
+    return logp[np.asarray(tokens, dtype=np.int64)], float(entropy), top, top_logp

@@ -30,6 +30,9 @@ EXPORTS = [
     "specexit_workspace_bytes", "specexit_set_dev_status", "specexit_lmhead_argmax_noalloc",
     "specexit_quant_kv_write", "specexit_quant_verify_attn", "specexit_quant_verify_attn_workspace_bytes",
     "specexit_quant_kv_compact", "specexit_sample", "specexit_sample_workspace_bytes",
+    "specexit_rope_table", "specexit_rope", "specexit_rope_kv_write", "specexit_latent_kv_write",
+    "specexit_latent_verify_attn", "specexit_latent_verify_attn_workspace_bytes", "specexit_latent_kv_compact",
+    "specexit_token_logprobs", "specexit_token_logprobs_workspace_bytes",
 ]
 PROF_DRAFT_HEAD_GEMM, PROF_LMHEAD_GEMM, PROF_VERIFY_ATTN, PROF_DRAFT_ATTN = 0, 1, 2, 3
 PROF_DRAFT_PROJ_IN, PROF_DRAFT_PROJ_OUT = 4, 5
@@ -41,7 +44,10 @@ STATUS_OK, STATUS_BAD_LENGTH, STATUS_BAD_PAGE, STATUS_BAD_TOKEN, STATUS_BAD_NODE
 STATUS_BAD_SETTING = 5
 OP_DRAFT_STEP, OP_VERIFY_ATTN, OP_LMHEAD_ARGMAX, OP_ACCEPT_EXIT, OP_DRAFT_TREE_LEVEL, OP_KV_COMPACT = 0, 1, 2, 3, 4, 5
 OP_QUANT_VERIFY_ATTN, OP_SAMPLE, OP_QUANT_KV_WRITE, OP_QUANT_KV_COMPACT = 6, 7, 8, 9
+OP_ROPE, OP_LATENT_VERIFY_ATTN, OP_LATENT_KV_COMPACT, OP_TOKEN_LOGPROBS = 10, 11, 12, 13
 SAMPLE_MAX_K, SAMPLE_MAX_V = 1024, 262144
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BANDS, ROPE_RAMP = 0, 1, 2, 3
+LOGPROB_MAX_TOK, LOGPROB_MAX_TOP = 64, 32
 
 
 class SpecExitError(RuntimeError):
@@ -79,6 +85,17 @@ class QuantKVView(C.Structure):
                 ("l_max", C.c_int64), ("n_pages", C.c_int64)]
 
 
+class LatentKVView(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("layout", C.c_int32), ("dtype", C.c_int32), ("latent_dim", C.c_int32), ("rope_dim", C.c_int32),
+                ("c", C.c_void_p), ("page_table", C.c_void_p), ("page_size", C.c_int32), ("max_pages_per_seq", C.c_int32),
+                ("l_max", C.c_int64), ("n_pages", C.c_int64)]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("scaling", C.c_int32), ("theta", C.c_float),
+                ("factor", C.c_float), ("low", C.c_float), ("high", C.c_float), ("orig_len", C.c_int32), ("amplitude", C.c_float)]
+
+
 class ExitCfg(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("alpha", C.c_float), ("thr_conf", C.c_float),
                 ("thr_prog", C.c_float), ("thr_rem", C.c_float), ("signal_mask", C.c_uint32),
@@ -106,6 +123,14 @@ class QuantAttnQuery(C.Structure):
 
 class SampleQuery(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("vocab", C.c_int32)]
+
+
+class LatentAttnQuery(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("kv", C.POINTER(LatentKVView)), ("n_q_heads", C.c_int32)]
+
+
+class LogprobsQuery(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("vocab", C.c_int32), ("n_top", C.c_int32)]
 
 
 def _load() -> C.CDLL:
@@ -174,6 +199,26 @@ def _load() -> C.CDLL:
     lib.specexit_sample_workspace_bytes.argtypes = [i32, i32, i32]
     lib.specexit_sample.restype = i32
     lib.specexit_sample.argtypes = [i32, i32, i32, vp, C.c_int64, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, u32, vp]
+    i64 = C.c_int64
+    lib.specexit_rope_table.restype = i32
+    lib.specexit_rope_table.argtypes = [C.POINTER(RopeDesc), vp, vp]
+    lib.specexit_rope.restype = i32
+    lib.specexit_rope.argtypes = [i32, C.POINTER(RopeDesc), vp, i32, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp, u32, vp]
+    lib.specexit_rope_kv_write.restype = i32
+    lib.specexit_rope_kv_write.argtypes = [C.POINTER(KVView), C.POINTER(RopeDesc), vp, i32, i32, i32, vp, i64, vp, vp, i64, vp, vp, vp, vp, u32, vp]
+    lib.specexit_latent_kv_write.restype = i32
+    lib.specexit_latent_kv_write.argtypes = [C.POINTER(LatentKVView), C.POINTER(RopeDesc), vp, i32, i32, i32, vp, i64, vp, f32, vp, i64, i64, vp,
+                                             vp, vp, vp, u32, vp]
+    lib.specexit_latent_verify_attn_workspace_bytes.restype = sz
+    lib.specexit_latent_verify_attn_workspace_bytes.argtypes = [C.POINTER(LatentKVView), i32, i32, i32]
+    lib.specexit_latent_verify_attn.restype = i32
+    lib.specexit_latent_verify_attn.argtypes = [C.POINTER(LatentKVView), i32, i32, i32, vp, vp, vp, f32, vp, vp, sz, u32, vp]
+    lib.specexit_latent_kv_compact.restype = i32
+    lib.specexit_latent_kv_compact.argtypes = [C.POINTER(LatentKVView), i32, i64, i32, i32, vp, vp, vp, vp, vp, i32, vp, u32, vp]
+    lib.specexit_token_logprobs_workspace_bytes.restype = sz
+    lib.specexit_token_logprobs_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.specexit_token_logprobs.restype = i32
+    lib.specexit_token_logprobs.argtypes = [i32, i32, i32, vp, i64, i32, vp, i32, vp, vp, vp, i32, vp, vp, vp, sz, u32, vp]
     lib.specexit_set_dev_status.restype = i32
     lib.specexit_set_dev_status.argtypes = [vp]
     return lib
@@ -551,3 +596,150 @@ def quant_attn_query(kv: QuantKVView, dtype: int, n_q_heads: int) -> QuantAttnQu
 
 def sample_query(dtype: int, vocab: int) -> SampleQuery:
     return SampleQuery(C.sizeof(SampleQuery), dtype, vocab)
+
+
+def latent_kv_view(c: torch.Tensor, rope_dim: int = 64, page_table: Optional[torch.Tensor] = None) -> LatentKVView:
+    """Latent cache; contiguous: c [B, l_max, latent_dim + rope_dim]; paged: c [n_pages, page_size, latent_dim + rope_dim] plus
+    page_table [B, max_pages] int32."""
+    assert c.is_cuda and c.is_contiguous() and c.dim() == 3
+    kv = LatentKVView()
+    kv.struct_size = C.sizeof(LatentKVView)
+    kv.dtype = dtype_code(c.dtype)
+    kv.latent_dim, kv.rope_dim = c.shape[2] - rope_dim, rope_dim
+    kv.c = c.data_ptr()
+    if page_table is None:
+        kv.layout = KV_CONTIG
+        kv.page_table = None
+        kv.page_size, kv.max_pages_per_seq = 16, 0
+        kv.l_max, kv.n_pages = c.shape[1], 0
+    else:
+        assert page_table.dtype == torch.int32 and page_table.is_cuda and page_table.is_contiguous()
+        kv.layout = KV_PAGED
+        kv.page_table = page_table.data_ptr()
+        kv.page_size, kv.max_pages_per_seq = c.shape[1], page_table.shape[1]
+        kv.l_max, kv.n_pages = page_table.shape[1] * c.shape[1], c.shape[0]
+    kv._keep = (c, page_table)
+    return kv
+
+
+def rope_desc(rot_dim: int, theta: float = 1e6, interleaved: bool = False, scaling: int = ROPE_PLAIN, factor: float = 1.0, low: float = 1.0,
+              high: float = 32.0, orig_len: int = 4096, amplitude: float = 1.0) -> RopeDesc:
+    return RopeDesc(C.sizeof(RopeDesc), rot_dim, 1 if interleaved else 0, scaling, theta, factor, low, high, orig_len, amplitude)
+
+
+def specexit_rope_table(rope: RopeDesc, turns, stream=None) -> None:
+    """turns: int64 (or uint64), rot_dim / 2 of them; the calls below read it with the same descriptor."""
+    _check(LIB.specexit_rope_table(C.byref(rope), _turns(rope, turns), _stream(stream)))
+
+
+def _turns(rope: RopeDesc, turns):
+    assert turns.dtype in (torch.int64, torch.uint64), f"turns must hold 64-bit integers, not {turns.dtype}"
+    return _arg(turns, turns.dtype, rope.rot_dim // 2, "turns")
+
+
+def _head_rows(rows: torch.Tensor, B: int, T: int, heads: int, d: int, want, name: str) -> int:
+    """rows: [B, T, heads, d], heads and values consecutive, tokens evenly apart; the elements between two tokens."""
+    assert want is None or rows.dtype == want, f"{name} must be {want}, not {rows.dtype}"
+    assert rows.is_cuda and tuple(rows.shape) == (B, T, heads, d), f"{name}: {tuple(rows.shape)} is not {(B, T, heads, d)}"
+    sb, st, sh, sd = rows.stride()
+    step = st if T > 1 else sb if B > 1 else heads * d
+    assert sd == 1 and (sh == d or heads == 1) and (sb == T * step or B == 1), f"{name}: tokens must lie evenly apart, heads and values consecutive"
+    return step
+
+
+def specexit_rope(dtype: int, rope: RopeDesc, turns, B: int, T: int, n_heads: int, head_dim: int, rows, out, pos, offset=None, count=None,
+                  flags: int = 0, stream=None) -> None:
+    """rows, out: [B, T, n_heads, head_dim], tokens evenly apart (slices of a fused projection's output will do); out may be rows."""
+    want, i32 = _STORAGE.get(dtype), torch.int32
+    step, out_step = _head_rows(rows, B, T, n_heads, head_dim, want, "rows"), _head_rows(out, B, T, n_heads, head_dim, want, "out")
+    pos, offset, count = _arg(pos, i32, B, "pos"), _arg(offset, i32, B * T, "offset"), _arg(count, i32, B, "count")
+    _check(LIB.specexit_rope(dtype, C.byref(rope), _turns(rope, turns), B, T, n_heads, head_dim, rows.data_ptr(), step, out.data_ptr(), out_step,
+                             pos, offset, count, flags, _stream(stream)))
+
+
+def specexit_rope_kv_write(kv: KVView, rope: RopeDesc, turns, B: int, T: int, n_q_heads: int, q_rows, k_rows, v_rows, q_out, pos, offset=None,
+                           count=None, flags: int = 0, stream=None) -> None:
+    """q_rows [B, T, n_q_heads, d], k_rows, v_rows [B, T, n_kv_heads, d]: tokens evenly apart; q_out contiguous."""
+    want, i32, d = _STORAGE.get(kv.dtype), torch.int32, kv.head_dim
+    step = _head_rows(k_rows, B, T, kv.n_kv_heads, d, want, "k_rows")
+    assert _head_rows(v_rows, B, T, kv.n_kv_heads, d, want, "v_rows") == step, "k_rows and v_rows must lie alike"
+    q_step, q_at = (_head_rows(q_rows, B, T, n_q_heads, d, want, "q_rows"), q_rows.data_ptr()) if n_q_heads else (0, None)
+    q_out = _arg(q_out, want, B * T * n_q_heads * d, "q_out") if n_q_heads else None
+    pos, offset, count = _arg(pos, i32, B, "pos"), _arg(offset, i32, B * T, "offset"), _arg(count, i32, B, "count")
+    _check(LIB.specexit_rope_kv_write(C.byref(kv), C.byref(rope), _turns(rope, turns), B, T, n_q_heads, q_at, q_step, k_rows.data_ptr(),
+                                      v_rows.data_ptr(), step, q_out, pos, offset, count, flags, _stream(stream)))
+
+
+def specexit_latent_kv_write(kv: LatentKVView, rope: RopeDesc, turns, B: int, T: int, n_q_heads: int, rows, gain, eps: float, q_rows, q_out, pos,
+                             offset=None, count=None, flags: int = 0, stream=None) -> None:
+    """rows [B, T, latent_dim + 64], tokens evenly apart; q_rows [B, T, n_q_heads, 64], tokens and heads evenly apart; q_out [B, T, n_q_heads,
+    latent_dim + 64] contiguous, its last 64 values are written."""
+    want, i32, w = _STORAGE.get(kv.dtype), torch.int32, kv.latent_dim + kv.rope_dim
+    step = _head_rows(rows.unsqueeze(2), B, T, 1, w, want, "rows")
+    gain = _arg(gain, want, kv.latent_dim, "gain")
+    q_at, q_step, head_step = None, 0, 0
+    if n_q_heads:
+        assert q_rows.is_cuda and q_rows.dtype == want and tuple(q_rows.shape) == (B, T, n_q_heads, kv.rope_dim), "q_rows: wrong type or shape"
+        sb, st, head_step, sd = q_rows.stride()
+        head_step = head_step if n_q_heads > 1 else kv.rope_dim
+        q_step = st if T > 1 else sb if B > 1 else n_q_heads * head_step
+        assert sd == 1 and (sb == T * q_step or B == 1), "q_rows: tokens must lie evenly apart, values consecutive"
+        q_at = q_rows.data_ptr()
+    q_out = _arg(q_out, want, B * T * n_q_heads * w, "q_out") if n_q_heads else None
+    pos, offset, count = _arg(pos, i32, B, "pos"), _arg(offset, i32, B * T, "offset"), _arg(count, i32, B, "count")
+    _check(LIB.specexit_latent_kv_write(C.byref(kv), C.byref(rope), _turns(rope, turns), B, T, n_q_heads, rows.data_ptr(), step, gain, eps, q_at,
+                                        q_step, head_step, q_out, pos, offset, count, flags, _stream(stream)))
+
+
+def specexit_latent_verify_attn_workspace_bytes(kv: LatentKVView, B: int, n_q: int, n_q_heads: int) -> int:
+    return int(LIB.specexit_latent_verify_attn_workspace_bytes(C.byref(kv), B, n_q, n_q_heads))
+
+
+def specexit_latent_verify_attn(kv: LatentKVView, B: int, n_q: int, n_q_heads: int, q, ctx_len, mask, scale: float, out, workspace,
+                                flags: int = 0, stream=None) -> None:
+    want, n = _STORAGE.get(kv.dtype), B * n_q * n_q_heads
+    q, out = _arg(q, want, n * (kv.latent_dim + kv.rope_dim), "q"), _arg(out, want, n * kv.latent_dim, "out")
+    ctx_len = _arg(ctx_len, torch.int32, B, "ctx_len")
+    mask = _arg(mask, torch.int64 if mask is None or mask.dtype != torch.uint64 else torch.uint64, B * n_q, "mask")
+    wp, wb = _ws_args(workspace)
+    _check(LIB.specexit_latent_verify_attn(C.byref(kv), B, n_q, n_q_heads, q, ctx_len, mask, C.c_float(scale), out, wp, wb, flags, _stream(stream)))
+
+
+def specexit_latent_kv_compact(kv: LatentKVView, n_layers: int, layer_stride_bytes: int, B: int, n_q: int, ctx_len, accept_path, accept_len,
+                               last_node=None, block_hidden=None, D: int = 0, hidden_next=None, flags: int = 0, stream=None) -> None:
+    i32, want = torch.int32, _STORAGE.get(kv.dtype)
+    ctx_len, accept_path = _arg(ctx_len, i32, B, "ctx_len"), _arg(accept_path, i32, B * n_q, "accept_path")
+    accept_len, last_node = _arg(accept_len, i32, B, "accept_len"), _arg(last_node, i32, B, "last_node")
+    block_hidden, hidden_next = _arg(block_hidden, want, B * n_q * D, "block_hidden"), _arg(hidden_next, want, B * D, "hidden_next")
+    _check(LIB.specexit_latent_kv_compact(C.byref(kv), n_layers, layer_stride_bytes, B, n_q, ctx_len, accept_path, accept_len, last_node,
+                                          block_hidden, D, hidden_next, flags, _stream(stream)))
+
+
+def specexit_token_logprobs_workspace_bytes(dtype: int, M: int, V: int, n_top: int = 0) -> int:
+    return int(LIB.specexit_token_logprobs_workspace_bytes(dtype, M, V, n_top))
+
+
+def specexit_token_logprobs(dtype: int, M: int, V: int, logits, entropy=None, token=None, logprob=None, top_token=None, top_logprob=None,
+                            temperature=None, rows_per_seq: int = 1, workspace=None, flags: int = 0, stream=None) -> None:
+    """logits: [M, >= V], rows evenly apart; token (int32), logprob: [M, n_tok]; top_token (int32), top_logprob: [M, n_top]."""
+    want, f32, i32 = _STORAGE.get(dtype), torch.float32, torch.int32
+    assert want is None or logits.dtype == want, f"logits must be {want}"
+    assert logits.is_cuda and logits.dim() == 2 and logits.shape[0] == M and logits.shape[1] >= V and logits.stride(1) == 1
+    ld = logits.stride(0) if M > 1 else logits.shape[1]
+    n_tok, n_top = (0 if t is None else t.shape[1] if t.dim() == 2 else 1 for t in (token, top_token))
+    token, logprob = _arg(token, i32, M * n_tok, "token"), _arg(logprob, f32, M * n_tok, "logprob")
+    entropy, temperature = _arg(entropy, f32, M, "entropy"), _arg(temperature, f32, -(-M // max(rows_per_seq, 1)), "temperature")
+    top_token, top_logprob = _arg(top_token, i32, M * n_top, "top_token"), _arg(top_logprob, f32, M * n_top, "top_logprob")
+    wp, wb = _ws_args(workspace)
+    _check(LIB.specexit_token_logprobs(dtype, M, V, logits.data_ptr(), ld, rows_per_seq, temperature, n_tok, token, logprob, entropy, n_top,
+                                       top_token, top_logprob, wp, wb, flags, _stream(stream)))
+
+
+def latent_attn_query(kv: LatentKVView, n_q_heads: int) -> LatentAttnQuery:
+    q = LatentAttnQuery(C.sizeof(LatentAttnQuery), C.pointer(kv), n_q_heads)
+    q._keep = kv
+    return q
+
+
+def logprobs_query(dtype: int, vocab: int, n_top: int = 0) -> LogprobsQuery:
+    return LogprobsQuery(C.sizeof(LogprobsQuery), dtype, vocab, n_top)

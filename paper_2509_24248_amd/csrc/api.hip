@@ -6,6 +6,7 @@
 #include "kernels.hpp"
 
 #include <dlfcn.h>
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
@@ -232,6 +233,95 @@ int32_t fill_sample(SampleArgs& a, int32_t dtype, int32_t M, int32_t V) {
   a.M = M;
   a.V = V;
   sample_plan(a);
+  return SPECEXIT_OK;
+}
+
+// --------------------------------------------------------------------------- rotary positions, latent cache, log probabilities
+int32_t check_rope(const specexit_rope_desc* rope, const char* who) {
+  if (!rope || rope->struct_size != sizeof(specexit_rope_desc)) return fail(SPECEXIT_EINVAL, "%s: rope descriptor missing or of another ABI size", who);
+  if (rope->rot_dim < 2 || rope->rot_dim > 256 || rope->rot_dim % 2) return fail(SPECEXIT_EUNSUPPORTED, "%s: rot_dim %d is not even or outside 2..256", who, rope->rot_dim);
+  if (rope->scaling < SPECEXIT_ROPE_PLAIN || rope->scaling > SPECEXIT_ROPE_RAMP) return fail(SPECEXIT_EINVAL, "%s: unknown scaling %d", who, rope->scaling);
+  if (!(rope->theta > 1.f) || !(rope->theta < INFINITY)) return fail(SPECEXIT_EINVAL, "%s: theta must be above 1", who);
+  if (!(rope->amplitude > 0.f) || !(rope->amplitude < INFINITY)) return fail(SPECEXIT_EINVAL, "%s: amplitude must be positive", who);
+  if (rope->scaling != SPECEXIT_ROPE_PLAIN && (!(rope->factor >= 1.f) || !(rope->factor < INFINITY))) return fail(SPECEXIT_EINVAL, "%s: factor must be at least 1", who);
+  if ((rope->scaling == SPECEXIT_ROPE_BANDS || rope->scaling == SPECEXIT_ROPE_RAMP) &&
+      (!(rope->low > 0.f) || !(rope->high > rope->low) || !(rope->high < INFINITY) || rope->orig_len < 1))
+    return fail(SPECEXIT_EINVAL, "%s: low, high or orig_len out of range", who);
+  static_assert(SPECEXIT_ROPE_LINEAR == kRopeLinear && SPECEXIT_ROPE_BANDS == kRopeBands && SPECEXIT_ROPE_RAMP == kRopeRamp, "scalings of the ABI and of the kernels differ");
+  return SPECEXIT_OK;
+}
+
+// layout, page table and capacity, alike in both views
+template <typename V>
+int32_t fill_place(CachePlace& p, const V* kv, const char* who) {
+  memset(&p, 0, sizeof(p));
+  p.paged = kv->layout == SPECEXIT_KV_PAGED;
+  p.page_table = kv->page_table;
+  p.page_size = p.paged ? kv->page_size : 16;
+  p.max_pages = kv->max_pages_per_seq;
+  p.l_max = p.paged ? static_cast<int64_t>(kv->max_pages_per_seq) * kv->page_size : kv->l_max;
+  p.n_pages = p.paged ? kv->n_pages : 0;
+  if (p.l_max > 0x7fffffff) return fail(SPECEXIT_EUNSUPPORTED, "%s: more than 2^31 - 1 entries per sequence", who);
+  return SPECEXIT_OK;
+}
+
+int32_t check_latent(const specexit_latent_kv_view* kv, const char* who) {
+  if (!kv || kv->struct_size != sizeof(specexit_latent_kv_view)) return fail(SPECEXIT_EINVAL, "%s: latent kv view missing or of another ABI size", who);
+  if (!dtype_ok(kv->dtype)) return fail(SPECEXIT_EINVAL, "%s: unknown kv dtype %d", who, kv->dtype);
+  if (!kv->c) return fail(SPECEXIT_EINVAL, "%s: cache pointer is null", who);
+  if (!aligned16(kv->c)) return fail(SPECEXIT_EINVAL, "%s: the cache must be 16-byte aligned", who);
+  if (kv->latent_dim != 128 && kv->latent_dim != 256 && kv->latent_dim != 512) return fail(SPECEXIT_EUNSUPPORTED, "%s: latent_dim %d not in {128,256,512}", who, kv->latent_dim);
+  if (kv->rope_dim != kLatentRope) return fail(SPECEXIT_EUNSUPPORTED, "%s: rope_dim %d is not %d", who, kv->rope_dim, kLatentRope);
+  if (kv->layout == SPECEXIT_KV_PAGED) {
+    if (!kv->page_table) return fail(SPECEXIT_EINVAL, "%s: paged layout without page_table", who);
+    if (kv->page_size < 16 || kv->page_size % 16) return fail(SPECEXIT_EUNSUPPORTED, "%s: page_size %d is not a multiple of 16", who, kv->page_size);
+    if (kv->max_pages_per_seq < 1 || kv->n_pages < 1) return fail(SPECEXIT_EINVAL, "%s: empty page pool", who);
+    if (kv->n_pages >= (1ll << 35) / kv->page_size) return fail(SPECEXIT_EUNSUPPORTED, "%s: a pool of 2^35 entries or more", who);
+  } else if (kv->layout == SPECEXIT_KV_CONTIG) {
+    if (kv->l_max < 1) return fail(SPECEXIT_EINVAL, "%s: l_max < 1", who);
+  } else {
+    return fail(SPECEXIT_EINVAL, "%s: unknown kv layout %d", who, kv->layout);
+  }
+  return SPECEXIT_OK;
+}
+
+int32_t fill_latent_attn(LatentAttnArgs& a, const specexit_latent_kv_view* kv, int32_t B, int32_t n_q, int32_t n_q_heads) {
+  const char* who = "latent_verify_attn";
+  int32_t rc = check_latent(kv, who);
+  if (rc) return rc;
+  CachePlace p;
+  rc = fill_place(p, kv, who);
+  if (rc) return rc;
+  if (B < 1) return fail(SPECEXIT_EINVAL, "%s: B < 1", who);
+  if (n_q < 1 || n_q > SPECEXIT_MAX_NQ) return fail(SPECEXIT_EINVAL, "%s: n_q %d outside 1..64", who, n_q);
+  if (n_q_heads < 1 || n_q_heads > 256) return fail(SPECEXIT_EUNSUPPORTED, "%s: n_q_heads %d outside 1..256", who, n_q_heads);
+  if (B > 1024) return fail(SPECEXIT_EUNSUPPORTED, "%s: more than 1024 sequences in one call", who);
+  memset(&a, 0, sizeof(a));
+  a.dtype = kv->dtype;
+  a.k = kv->c;
+  a.d = kv->latent_dim;
+  a.paged = p.paged; a.page_table = p.page_table; a.page_size = p.page_size; a.max_pages = p.max_pages;
+  a.l_max = p.l_max; a.n_pages = p.n_pages;
+  a.B = B;
+  a.n_q = a.n_blk = a.mask_stride = n_q;
+  a.Hq = n_q_heads;
+  if (a.l_max < n_q) return fail(SPECEXIT_EINVAL, "%s: the cache holds %lld entries per sequence, fewer than the block's %d", who, static_cast<long long>(a.l_max), n_q);
+  if (!latent_attn_plan(a, num_cus())) return fail(SPECEXIT_EUNSUPPORTED, "%s: %d sequences x %d rows x %lld cache entries is more than one call can split", who, B, n_q * n_q_heads, static_cast<long long>(a.l_max));
+  return SPECEXIT_OK;
+}
+
+int32_t fill_logprob(LogprobArgs& a, int32_t dtype, int32_t M, int32_t V, int32_t n_top) {
+  const char* who = "token_logprobs";
+  if (!dtype_ok(dtype)) return fail(SPECEXIT_EINVAL, "%s: unknown dtype %d", who, dtype);
+  if (M < 1 || M > 65535) return fail(SPECEXIT_EINVAL, "%s: M %d outside 1..65535", who, M);
+  if (V < 1) return fail(SPECEXIT_EINVAL, "%s: V < 1", who);
+  if (V > SPECEXIT_SAMPLE_MAX_V) return fail(SPECEXIT_EUNSUPPORTED, "%s: V %d above %d", who, V, SPECEXIT_SAMPLE_MAX_V);
+  if (n_top < 0 || n_top > SPECEXIT_LOGPROB_MAX_TOP) return fail(SPECEXIT_EUNSUPPORTED, "%s: n_top %d outside 0..%d", who, n_top, SPECEXIT_LOGPROB_MAX_TOP);
+  static_assert(kLogprobMaxTop == SPECEXIT_LOGPROB_MAX_TOP && kLogprobMaxTok == SPECEXIT_LOGPROB_MAX_TOK, "limits of the ABI and of the kernels differ");
+  memset(&a, 0, sizeof(a));
+  a.f32 = dtype == SPECEXIT_F32;
+  a.M = M; a.V = V; a.n_top = n_top;
+  logprob_plan(a);
   return SPECEXIT_OK;
 }
 
@@ -714,10 +804,22 @@ size_t specexit_workspace_bytes(int32_t op, const void* desc, int32_t B, int32_t
       if (!q || q->struct_size != sizeof(*q) || B < 1 || n_q < 1 || static_cast<int64_t>(B) * n_q > 65535) return 0;
       return specexit_sample_workspace_bytes(q->dtype, B * n_q, q->vocab);
     }
+    case SPECEXIT_OP_LATENT_VERIFY_ATTN: {
+      const specexit_latent_attn_query* q = static_cast<const specexit_latent_attn_query*>(desc);
+      if (!q || q->struct_size != sizeof(*q)) return 0;
+      return specexit_latent_verify_attn_workspace_bytes(q->kv, B, n_q, q->n_q_heads);
+    }
+    case SPECEXIT_OP_TOKEN_LOGPROBS: {
+      const specexit_logprobs_query* q = static_cast<const specexit_logprobs_query*>(desc);
+      if (!q || q->struct_size != sizeof(*q) || B < 1 || n_q < 1 || static_cast<int64_t>(B) * n_q > 65535) return 0;
+      return specexit_token_logprobs_workspace_bytes(q->dtype, B * n_q, q->vocab, q->n_top);
+    }
     case SPECEXIT_OP_ACCEPT_EXIT:
     case SPECEXIT_OP_KV_COMPACT:
     case SPECEXIT_OP_QUANT_KV_WRITE:
     case SPECEXIT_OP_QUANT_KV_COMPACT:
+    case SPECEXIT_OP_ROPE:
+    case SPECEXIT_OP_LATENT_KV_COMPACT:
       return 0;   // these calls use no scratch memory
     default:
       fail(SPECEXIT_EINVAL, "workspace_bytes: unknown op %d", op);
@@ -1269,6 +1371,205 @@ int32_t specexit_sample(int32_t dtype, int32_t M, int32_t V, const void* logits,
   a.prob = prob;
   a.status = status_for(flags);
   return check_hip(launch_sample(a, static_cast<hipStream_t>(stream)), "sample");
+}
+
+int32_t specexit_rope_table(const specexit_rope_desc* rope, uint64_t* turns, void* stream) {
+  int32_t rc = check_rope(rope, "rope_table");
+  if (rc) return rc;
+  if (!turns) return fail(SPECEXIT_EINVAL, "rope_table: turns is null");
+  const RopeTableArgs a = {rope->rot_dim, rope->scaling, rope->theta, rope->factor, rope->low, rope->high, rope->orig_len, turns};
+  return check_hip(launch_rope_table(a, static_cast<hipStream_t>(stream)), "rope_table");
+}
+
+int32_t specexit_rope(int32_t dtype, const specexit_rope_desc* rope, const uint64_t* turns, int32_t B, int32_t T, int32_t n_heads,
+                      int32_t head_dim, const void* rows, int64_t token_stride, void* out, int64_t out_stride, const int32_t* pos,
+                      const int32_t* offset, const int32_t* count, uint32_t flags, void* stream) {
+  int32_t rc = check_rope(rope, "rope");
+  if (rc) return rc;
+  if (!dtype_ok(dtype)) return fail(SPECEXIT_EINVAL, "rope: unknown dtype %d", dtype);
+  if (B < 1 || T < 1) return fail(SPECEXIT_EINVAL, "rope: B or T < 1");
+  if (n_heads < 1 || n_heads > 65535) return fail(SPECEXIT_EINVAL, "rope: n_heads %d outside 1..65535", n_heads);
+  if (head_dim < 16 || head_dim > 512 || head_dim % 16) return fail(SPECEXIT_EUNSUPPORTED, "rope: head_dim %d is not a multiple of 16 up to 512", head_dim);
+  if (rope->rot_dim > head_dim) return fail(SPECEXIT_EINVAL, "rope: rot_dim %d is more than head_dim %d", rope->rot_dim, head_dim);
+  if (!turns || !rows || !out || !pos) return fail(SPECEXIT_EINVAL, "rope: a required pointer is null");
+  const int64_t width = static_cast<int64_t>(n_heads) * head_dim;
+  if (token_stride < width || out_stride < width) return fail(SPECEXIT_EINVAL, "rope: a token stride is less than a token's heads");
+  if (!aligned16(rows) || !aligned16(out) || token_stride * esize(dtype) % 16 || out_stride * esize(dtype) % 16)
+    return fail(SPECEXIT_EINVAL, "rope: rows must be 16-byte aligned");
+  if (rows == out && token_stride != out_stride) return fail(SPECEXIT_EINVAL, "rope: in place with two strides");
+  RopeRowsArgs a;
+  memset(&a, 0, sizeof(a));
+  a.f32 = dtype == SPECEXIT_F32;
+  a.d = head_dim; a.Hq = n_heads; a.B = B; a.T = T;
+  a.rot = rope->rot_dim; a.neighbours = rope->interleaved != 0; a.amplitude = rope->amplitude; a.turns = turns;
+  a.q = rows; a.q_stride = token_stride; a.q_out = out; a.out_stride = out_stride;
+  a.pos = pos; a.offset = offset; a.count = count;
+  a.status = status_for(flags);
+  if (!rope_rows_plan(a)) return fail(SPECEXIT_EUNSUPPORTED, "rope: %d sequences x %d tokens x %d heads is more than one call takes", B, T, n_heads);
+  return check_hip(launch_rope_rows(a, static_cast<hipStream_t>(stream)), "rope");
+}
+
+int32_t specexit_rope_kv_write(const specexit_kv_view* kv, const specexit_rope_desc* rope, const uint64_t* turns, int32_t B, int32_t T,
+                               int32_t n_q_heads, const void* q_rows, int64_t q_stride, const void* k_rows, const void* v_rows,
+                               int64_t kv_stride, void* q_out, const int32_t* pos, const int32_t* offset, const int32_t* count,
+                               uint32_t flags, void* stream) {
+  const char* who = "rope_kv_write";
+  RopeRowsArgs a;
+  memset(&a, 0, sizeof(a));
+  int32_t rc = check_kv(kv, who);
+  if (!rc) rc = fill_place(a.kv, kv, who);
+  if (!rc) rc = check_rope(rope, who);
+  if (rc) return rc;
+  if (B < 1 || T < 1) return fail(SPECEXIT_EINVAL, "%s: B or T < 1", who);
+  if (n_q_heads < 0 || n_q_heads > 65535 || kv->n_kv_heads > 65535) return fail(SPECEXIT_EINVAL, "%s: more than 65535 heads", who);
+  if (rope->rot_dim > kv->head_dim) return fail(SPECEXIT_EINVAL, "%s: rot_dim %d is more than head_dim %d", who, rope->rot_dim, kv->head_dim);
+  if (!turns || !k_rows || !v_rows || !pos || (n_q_heads && (!q_rows || !q_out))) return fail(SPECEXIT_EINVAL, "%s: a required pointer is null", who);
+  if (kv_stride < static_cast<int64_t>(kv->n_kv_heads) * kv->head_dim || (n_q_heads && q_stride < static_cast<int64_t>(n_q_heads) * kv->head_dim))
+    return fail(SPECEXIT_EINVAL, "%s: a token stride is less than a token's heads", who);
+  if (!aligned16(k_rows) || !aligned16(v_rows) || kv_stride * esize(kv->dtype) % 16 || !aligned16(kv->k) || !aligned16(kv->v) ||
+      (n_q_heads && (!aligned16(q_rows) || !aligned16(q_out) || q_stride * esize(kv->dtype) % 16)))
+    return fail(SPECEXIT_EINVAL, "%s: rows and caches must be 16-byte aligned", who);
+  if (n_q_heads && q_rows == q_out && q_stride != static_cast<int64_t>(n_q_heads) * kv->head_dim) return fail(SPECEXIT_EINVAL, "%s: in place with two strides", who);
+  a.kc = kv->k; a.vc = kv->v;
+  a.f32 = kv->dtype == SPECEXIT_F32;
+  a.d = kv->head_dim; a.Hq = n_q_heads; a.Hkv = kv->n_kv_heads; a.B = B; a.T = T;
+  a.rot = rope->rot_dim; a.neighbours = rope->interleaved != 0; a.amplitude = rope->amplitude; a.turns = turns;
+  a.q = q_rows; a.q_stride = q_stride; a.q_out = q_out; a.out_stride = static_cast<int64_t>(n_q_heads) * kv->head_dim;
+  a.k = k_rows; a.v = v_rows; a.kv_stride = kv_stride;
+  a.pos = pos; a.offset = offset; a.count = count;
+  a.status = status_for(flags);
+  if (!rope_rows_plan(a)) return fail(SPECEXIT_EUNSUPPORTED, "%s: %d sequences x %d tokens x %d heads is more than one call takes", who, B, T, n_q_heads + 2 * kv->n_kv_heads);
+  return check_hip(launch_rope_rows(a, static_cast<hipStream_t>(stream)), who);
+}
+
+int32_t specexit_latent_kv_write(const specexit_latent_kv_view* kv, const specexit_rope_desc* rope, const uint64_t* turns, int32_t B,
+                                 int32_t T, int32_t n_q_heads, const void* rows, int64_t row_stride, const void* gain, float eps,
+                                 const void* q_rows, int64_t q_stride, int64_t head_stride, void* q_out, const int32_t* pos,
+                                 const int32_t* offset, const int32_t* count, uint32_t flags, void* stream) {
+  const char* who = "latent_kv_write";
+  LatentWriteArgs a;
+  memset(&a, 0, sizeof(a));
+  int32_t rc = check_latent(kv, who);
+  if (!rc) rc = fill_place(a.kv, kv, who);
+  if (!rc) rc = check_rope(rope, who);
+  if (rc) return rc;
+  const size_t e = esize(kv->dtype);
+  if (rope->rot_dim != kLatentRope) return fail(SPECEXIT_EINVAL, "%s: rot_dim %d is not the cache's %d", who, rope->rot_dim, kLatentRope);
+  if (B < 1 || T < 1) return fail(SPECEXIT_EINVAL, "%s: B or T < 1", who);
+  if (n_q_heads < 0 || n_q_heads > 65535) return fail(SPECEXIT_EINVAL, "%s: n_q_heads %d outside 0..65535", who, n_q_heads);
+  if (!turns || !rows || !pos || (n_q_heads && (!q_rows || !q_out))) return fail(SPECEXIT_EINVAL, "%s: a required pointer is null", who);
+  if (!(eps >= 0.f)) return fail(SPECEXIT_EINVAL, "%s: eps is negative", who);
+  if (row_stride < kv->latent_dim + kLatentRope) return fail(SPECEXIT_EINVAL, "%s: row stride %lld is less than an entry", who, static_cast<long long>(row_stride));
+  if (!aligned16(rows) || row_stride * e % 16 || (gain && !aligned16(gain))) return fail(SPECEXIT_EINVAL, "%s: rows and gain must be 16-byte aligned", who);
+  if (n_q_heads) {
+    if (head_stride < kLatentRope || q_stride < (n_q_heads - 1) * head_stride + kLatentRope) return fail(SPECEXIT_EINVAL, "%s: a query stride is less than what it spans", who);
+    if (!aligned16(q_rows) || !aligned16(q_out) || q_stride * e % 16 || head_stride * e % 16) return fail(SPECEXIT_EINVAL, "%s: queries must be 16-byte aligned", who);
+  }
+  a.c = kv->c;
+  a.f32 = kv->dtype == SPECEXIT_F32;
+  a.r = kv->latent_dim; a.B = B; a.T = T; a.H = n_q_heads;
+  a.rows = rows; a.row_stride = row_stride; a.gain = gain; a.eps = eps;
+  a.q_rows = q_rows; a.q_stride = q_stride; a.head_stride = head_stride; a.q_out = q_out;
+  a.neighbours = rope->interleaved != 0; a.amplitude = rope->amplitude; a.turns = turns;
+  a.pos = pos; a.offset = offset; a.count = count;
+  a.status = status_for(flags);
+  if (!latent_write_plan(a)) return fail(SPECEXIT_EUNSUPPORTED, "%s: %d sequences x %d tokens x %d heads is more than one call takes", who, B, T, n_q_heads);
+  return check_hip(launch_latent_write(a, static_cast<hipStream_t>(stream)), who);
+}
+
+size_t specexit_latent_verify_attn_workspace_bytes(const specexit_latent_kv_view* kv, int32_t B, int32_t n_q, int32_t n_q_heads) {
+  LatentAttnArgs a;
+  if (fill_latent_attn(a, kv, B, n_q, n_q_heads)) return 0;
+  return latent_attn_workspace_bytes(a);
+}
+
+int32_t specexit_latent_verify_attn(const specexit_latent_kv_view* kv, int32_t B, int32_t n_q, int32_t n_q_heads, const void* q,
+                                    const int32_t* ctx_len, const uint64_t* mask, float scale, void* out, void* workspace,
+                                    size_t workspace_bytes, uint32_t flags, void* stream) {
+  LatentAttnArgs a;
+  int32_t rc = fill_latent_attn(a, kv, B, n_q, n_q_heads);
+  if (rc) return rc;
+  if (!q || !ctx_len || !out) return fail(SPECEXIT_EINVAL, "latent_verify_attn: a required pointer is null");
+  if (!aligned16(q) || (reinterpret_cast<uintptr_t>(out) & 7)) return fail(SPECEXIT_EINVAL, "latent_verify_attn: q must be 16-byte and out 8-byte aligned");
+  if (!(scale > 0.f)) return fail(SPECEXIT_EINVAL, "latent_verify_attn: scale must be positive");
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255)) return fail(SPECEXIT_EWORKSPACE, "latent_verify_attn: workspace null or not 256-byte aligned");
+  const size_t need = latent_attn_workspace_bytes(a);
+  if (workspace_bytes < need) return fail(SPECEXIT_EWORKSPACE, "latent_verify_attn: workspace %zu < %zu bytes", workspace_bytes, need);
+  a.q = q;
+  a.ctx_len = ctx_len;
+  a.mask = mask;
+  a.scale = scale;
+  a.out = out;
+  a.status = status_for(flags);
+  latent_attn_carve(a, workspace);
+  return check_hip(launch_latent_attn(a, static_cast<hipStream_t>(stream)), "latent_verify_attn");
+}
+
+int32_t specexit_latent_kv_compact(const specexit_latent_kv_view* kv, int32_t n_layers, int64_t layer_stride_bytes, int32_t B,
+                                   int32_t n_q, const int32_t* ctx_len, const int32_t* accept_path, const int32_t* accept_len,
+                                   const int32_t* last_node, const void* block_hidden, int32_t D, void* hidden_next, uint32_t flags,
+                                   void* stream) {
+  const char* who = "latent_kv_compact";
+  int32_t rc = check_latent(kv, who);
+  if (rc) return rc;
+  CachePlace p;
+  rc = fill_place(p, kv, who);
+  if (rc) return rc;
+  if (B < 1) return fail(SPECEXIT_EINVAL, "%s: B < 1", who);
+  if (n_q < 1 || n_q > SPECEXIT_MAX_NQ) return fail(SPECEXIT_EINVAL, "%s: n_q %d outside 1..64", who, n_q);
+  if (n_layers < 1) return fail(SPECEXIT_EINVAL, "%s: n_layers < 1", who);
+  if (n_layers > 1 && (layer_stride_bytes <= 0 || layer_stride_bytes % 16))
+    return fail(SPECEXIT_EINVAL, "%s: layer stride must be a positive multiple of 16 bytes", who);
+  if (!ctx_len || !accept_path || !accept_len) return fail(SPECEXIT_EINVAL, "%s: a required pointer is null", who);
+  CompactArgs a;
+  memset(&a, 0, sizeof(a));
+  a.k = kv->c;
+  a.paged = p.paged; a.page_table = p.page_table; a.page_size = p.page_size; a.max_pages = p.max_pages;
+  a.l_max = p.l_max; a.n_pages = p.n_pages;
+  a.status = status_for(flags);
+  a.layer_stride_bytes = n_layers > 1 ? layer_stride_bytes : 0;
+  a.n_layers = n_layers; a.B = B; a.n_q = n_q; a.Hkv = 1;
+  a.row_bytes = static_cast<int>((kv->latent_dim + kLatentRope) * esize(kv->dtype));
+  a.ctx_len = ctx_len; a.accept_path = accept_path; a.accept_len = accept_len; a.last_node = last_node;
+  if (block_hidden) {
+    if (!last_node || !hidden_next) return fail(SPECEXIT_EINVAL, "%s: block_hidden given without last_node / hidden_next", who);
+    if (D < 1 || D > (1 << 28) || (D * esize(kv->dtype)) % 16) return fail(SPECEXIT_EINVAL, "%s: D * element size must be a multiple of 16", who);
+    a.block_hidden = block_hidden; a.hidden_next = hidden_next;
+    a.hidden_row_bytes = static_cast<int>(D * esize(kv->dtype));
+  }
+  if (B > 65535 || n_layers > 65535) return fail(SPECEXIT_EUNSUPPORTED, "%s: grid too large", who);
+  return check_hip(launch_latent_compact(a, static_cast<hipStream_t>(stream)), who);
+}
+
+size_t specexit_token_logprobs_workspace_bytes(int32_t dtype, int32_t M, int32_t V, int32_t n_top) {
+  LogprobArgs a;
+  if (fill_logprob(a, dtype, M, V, n_top)) return 0;
+  return logprob_carve(a, nullptr);
+}
+
+int32_t specexit_token_logprobs(int32_t dtype, int32_t M, int32_t V, const void* logits, int64_t ld, int32_t rows_per_seq,
+                                const float* temperature, int32_t n_tok, const int32_t* token, float* logprob, float* entropy,
+                                int32_t n_top, int32_t* top_token, float* top_logprob, void* workspace, size_t workspace_bytes,
+                                uint32_t flags, void* stream) {
+  const char* who = "token_logprobs";
+  LogprobArgs a;
+  int32_t rc = fill_logprob(a, dtype, M, V, n_top);
+  if (rc) return rc;
+  if (n_tok < 0 || n_tok > SPECEXIT_LOGPROB_MAX_TOK) return fail(SPECEXIT_EUNSUPPORTED, "%s: n_tok %d outside 0..%d", who, n_tok, SPECEXIT_LOGPROB_MAX_TOK);
+  if (!logits || (n_tok && (!token || !logprob)) || (n_top && !top_token)) return fail(SPECEXIT_EINVAL, "%s: a required pointer is null", who);
+  if (!n_tok && !n_top && !entropy) return fail(SPECEXIT_EINVAL, "%s: nothing is asked for", who);
+  if (reinterpret_cast<uintptr_t>(logits) % esize(dtype)) return fail(SPECEXIT_EINVAL, "%s: logits are not aligned to their type", who);
+  if (ld < V) return fail(SPECEXIT_EINVAL, "%s: row stride %lld is less than V", who, static_cast<long long>(ld));
+  if (rows_per_seq < 1) return fail(SPECEXIT_EINVAL, "%s: rows_per_seq < 1", who);
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255)) return fail(SPECEXIT_EWORKSPACE, "%s: workspace null or not 256-byte aligned", who);
+  const size_t need = logprob_carve(a, workspace);
+  if (workspace_bytes < need) return fail(SPECEXIT_EWORKSPACE, "%s: workspace %zu < %zu bytes", who, workspace_bytes, need);
+  a.logits = logits; a.ld = ld;
+  a.rows_per_seq = rows_per_seq; a.temperature = temperature;
+  a.n_tok = n_tok; a.token = token; a.logprob = logprob;
+  a.entropy = entropy; a.top_token = top_token; a.top_logprob = top_logprob;
+  a.status = status_for(flags);
+  return check_hip(launch_logprob(a, static_cast<hipStream_t>(stream)), who);
 }
 
 }  // extern "C"

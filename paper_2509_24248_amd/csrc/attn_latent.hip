@@ -1,0 +1,657 @@
+// Verification attention over a latent cache: an entry is one vector of LD + 64 values, the key of every query head whole and the value with its
+// first LD, so all R = n_q_heads n_q query rows of a sequence share it.
+//
+//   s_j = scale q . (c_j | k_j),  o = sum_j softmax_j(s) c_j          2 (2 LD + 64) operations a row and entry of (LD + 64) e bytes
+//
+// The rows of a sequence are cut into blocks of up to 128 (fp32: 64); a workgroup takes an equal share of all keys of all (sequence, block) units
+// (attn_sched.hpp, the blocks in the place of KV heads).  Inside it the tiles of 32 keys (fp32: 16) lie in LDS once, as they lie in memory, and are read
+// twice from there:
+//   S^T = C Q^T    : A operand = entries (row = key), B operand = the rows' queries, held in registers;
+//   softmax        : online, per wave, in log2 units;
+//   O^T += C^T P^T : A operand = the same tile by columns (ds_read_b64_tr_b16; fp32: plain reads, a key's sixteen columns to sixteen lanes), B operand = P^T
+//                    straight from the softmax registers.
+// fp32 uses the fp32 matrix instructions: neither entries nor probabilities lose a digit.
+//
+// A workgroup has four waves, one per SIMD with all of its registers (128 rows of 512 columns: 256 of accumulators and 144 of queries): NR waves of RTW
+// 16-row tiles share a ring of tiles, NK rings have keys of their own and are added at the end, in their order.  S slots a ring.
+// Tiles are brought in by direct global -> LDS loads, a ring's waves a quarter or half each.
+#include "attn_sched.hpp"
+#include "common.hpp"
+#include "kernels.hpp"
+#include "stream.hpp"
+
+#include <float.h>
+#include <limits.h>
+
+namespace sx {
+
+namespace {
+
+constexpr int kLds = 160 * 1024;
+constexpr int kPe = kLatentRope;
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+template <typename T> struct Tile;
+// XOR swizzle of a row's 16-byte chunks.  A bf16 row is an odd number of 128 bytes, so a key's parity already picks one half of the banks; the
+// permuted bits of the rest keep apart the sixteen keys of a K read (one chunk each) as well as the eight keys of a transpose read (an even chunk and
+// the next).  An fp32 row is a whole number of 256 bytes: the key itself.
+template <> struct Tile<bf16_t> {
+  static constexpr int kKeys = 32;
+  __host__ __device__ static constexpr int swz(int key) { return ((key >> 1 & 3) << 1) | (key >> 3 & 1); }
+  __host__ __device__ static constexpr int flip(int group) { return (group & 1) << 4; }       // of a piece's source, from group to group of 8 keys
+};
+template <> struct Tile<float> {
+  static constexpr int kKeys = 16;
+  __host__ __device__ static constexpr int swz(int key) { return key & 15; }
+  __host__ __device__ static constexpr int flip(int group) { return group << 6; }             // groups of 4 keys
+};
+
+constexpr int slot_bytes(int ld, int e) { return (e == 2 ? 32 : 16) * (ld + kPe) * e; }
+// Slots of a ring: what the LDS of a compute unit holds beside the schedule's table and the merge's pairs.
+constexpr int kTableBytes = attn_sched_words(kAttnMaxSeqs) * 4 + 1024;
+constexpr int stages_of(int ld, int e, int nk) {
+  const int most = (kLds - kTableBytes) / (nk * slot_bytes(ld, e));
+  return most < 1 ? 1 : most > 4 ? 4 : most;
+}
+
+// Registers of a lane for accumulators and queries.  Up to 190 everything is done in 256 ordinary ones; beyond that the accumulators are in the other 256, which
+// only matrix instructions work on: see the rescaling.
+constexpr int held_registers(int ld, int e, int rtw) { return rtw * (ld / 4 + (ld + kPe) * e / 16); }
+constexpr bool in_agprs(int ld, int e, int rtw) { return held_registers(ld, e, rtw) > 190; }
+
+template <typename T, int LD, int RTW, int NR, int NK, bool PAGED>
+__global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_latent_ring(const LatentAttnArgs a) {
+  static_assert(NR * NK == 4, "four waves");
+  constexpr bool kF32 = sizeof(T) == 4;
+  constexpr int S = stages_of(LD, sizeof(T), NK);
+  constexpr int kKeys = Tile<T>::kKeys, kGroup = kKeys / 4;
+  constexpr int kRowB = (LD + kPe) * static_cast<int>(sizeof(T)), kCPR = kRowB / 16;
+  constexpr int kSlot = slot_bytes(LD, sizeof(T));
+  constexpr int kPP = kGroup * kRowB / 1024;        // 1 KB pieces of a group of keys
+  constexpr int kGroups = 4 / NR;                   // groups of a tile that a wave brings in
+  constexpr int kPieces = kGroups * kPP;
+  constexpr int kKS = kCPR / 4, kDT = LD / 16, kHalves = kKeys / 16;
+  static_assert(kPP * 1024 == kGroup * kRowB && kCPR % 8 == 0, "whole pieces");
+  // Probabilities of bf16 calls: two bf16 parts (16 bits) where the matrix instructions have the time, up to 64 rows; with 128 rows one, normalised with its own sum.
+  constexpr bool kSplitP = !kF32 && RTW == 1;
+  constexpr float kSlack = kF32 || kSplitP ? 8.f : 0.f;      // of the softmax reference, log2 units: see attn_mfma.hip
+  extern __shared__ uint4 smem4[];
+  char* smem = reinterpret_cast<char*>(smem4);
+  float* ml_lds = reinterpret_cast<float*>(smem + NK * S * kSlot);
+  int* sched_lds = reinterpret_cast<int*>(ml_lds + (NK > 1 ? NK * NR * 16 * 2 : 0));
+  const int lane = threadIdx.x & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kg = wv / NR, rr = wv % NR;
+  const int fr = lane & 15, fq = lane >> 4;
+  const AttnTable table = attn_sched_build(a, sched_lds);
+  const AttnLine line = attn_sched_line(a, table);
+  if (static_cast<int>(blockIdx.x) >= line.W) return;         // the whole workgroup leaves together
+  const int x_hi = attn_sched_lo(line, blockIdx.x + 1);
+  // where a lane of a piece fetches from, behind the first key of its group
+  uint32_t lane_off[kPP];
+#pragma unroll
+  for (int p = 0; p < kPP; ++p) {
+    const int n = 64 * p + lane, row = n / kCPR, at = n % kCPR;
+    lane_off[p] = static_cast<uint32_t>(row * kRowB + ((at ^ Tile<T>::swz(row)) << 4));
+  }
+  const float sl2 = a.scale * 1.44269504088896340736f;
+  bool again = false;
+  AttnSeg seg = attn_sched_next(a, table, true, line.pad, attn_sched_lo(line, blockIdx.x), x_hi);
+  if (seg.next < x_hi) attn_sched_keep(a, table);
+  for (; seg.s1 > seg.s0; seg = attn_sched_next(a, table, false, line.pad, seg.next, x_hi)) {
+    attn_sched_publish(a, seg);
+    const int b = seg.b, row0 = seg.g * a.block_rows;
+    const int R = min(a.block_rows, a.rows - row0);
+    const int L = __builtin_amdgcn_readfirstlane(seg.L);
+    const int s0 = seg.s0, s1 = __builtin_amdgcn_readfirstlane(seg.s1);
+    const int ntl = (s1 - s0 + kKeys - 1) / kKeys;
+    const int nit = (ntl + NK - 1) / NK;
+    char* ring = smem + kg * (S * kSlot);
+
+    // ---- the rows' queries and mask words (rows past the last repeat it and are not stored)
+    uint4 qf[kKS][RTW];
+    uint64_t rowmask[RTW];
+    int rho[RTW];
+#pragma unroll
+    for (int t = 0; t < RTW; ++t) {
+      rho[t] = 16 * (rr * RTW + t) + fr;
+      const int row = row0 + min(rho[t], R - 1);
+      const uint4* qp = reinterpret_cast<const uint4*>(static_cast<const char*>(a.q) + (static_cast<int64_t>(b) * a.rows + row) * kRowB) + fq;
+#pragma unroll
+      for (int ks = 0; ks < kKS; ++ks) qf[ks][t] = qp[4 * ks];
+      const int i = row / a.Hq;
+      rowmask[t] = a.mask ? a.mask[static_cast<int64_t>(b) * a.mask_stride + i] : ((2ull << i) - 1ull);
+    }
+    if (again) __syncthreads();                     // the rings are free of the segment before
+    again = true;
+
+    // ---- tiles.  Paged: a lane holds where 16 keys lie in the pool (in units of 16 entries), for 64 of them; the next 64 are on their way.
+    int ids = 0, ids_next = 0, chunk = 0;
+    auto fetch_ids = [&](int c) {
+      const int p = min(s0 + 16 * (64 * c + lane), s1 - 1) & ~15;
+      const int in_seq = static_cast<int>(static_cast<uint32_t>(p) / static_cast<uint32_t>(a.page_size));
+      const int page = checked_page(a.page_table[static_cast<int64_t>(b) * a.max_pages + in_seq], a.n_pages, a.status);
+      return page * (a.page_size >> 4) + ((p - in_seq * a.page_size) >> 4);
+    };
+    if (PAGED) {
+      ids = fetch_ids(0);
+      if (s1 - s0 > 1024) ids_next = fetch_ids(1);
+    }
+    const char* seq = static_cast<const char*>(a.k) + static_cast<int64_t>(b) * a.l_max * kRowB;
+    int id0 = 0, id1 = 0;                           // of a tile's first and second 16 keys
+    auto locate = [&](int it) {
+      const int t0 = kKeys * (it * NK + kg);
+      if (!PAGED || s0 + t0 >= s1) return;
+      const int blk = t0 >> 4;
+      if (blk >> 6 != chunk) {
+        chunk = blk >> 6;
+        ids = ids_next;
+        if (s0 + 1024 * (chunk + 1) < s1) ids_next = fetch_ids(chunk + 1);
+      }
+      id0 = __builtin_amdgcn_readlane(ids, blk & 63);
+      if (kHalves == 2) id1 = __builtin_amdgcn_readlane(ids, (blk & 63) + 1);
+    };
+    auto entry = [&](int t0, int key) -> const char* {        // of the tile from key t0 on
+      if (!PAGED) return seq + static_cast<int64_t>(t0 + key) * kRowB;
+      return static_cast<const char*>(a.k) + (static_cast<int64_t>(key < 16 ? id0 : id1) * 16 + (key & 15)) * kRowB;
+    };
+    auto issue = [&](int it) {                      // (after locate of the same tile)
+      const int t0 = s0 + kKeys * (it * NK + kg);
+      if (t0 >= s1) return;
+      char* slot = ring + (it % S) * kSlot;
+#pragma unroll
+      for (int u = 0; u < kGroups; ++u) {
+        const int gr = rr * kGroups + u;
+        char* to = slot + gr * (kPP * 1024);
+        if (t0 + kKeys <= s1) {
+          const char* base = entry(t0, gr * kGroup);
+#pragma unroll
+          for (int p = 0; p < kPP; ++p) {
+            uint32_t off = lane_off[p];
+            asm volatile("" : "+v"(off));           // (an instruction here, not a register for every group and piece)
+            load_to_lds16(base, off ^ Tile<T>::flip(gr), to + p * 1024);
+          }
+        } else {
+          int ln = lane;                            // (worked out here, once per segment at most)
+          asm volatile("" : "+v"(ln));
+#pragma unroll 1
+          for (int p = 0; p < kPP; ++p) {
+            const int n = 64 * p + ln, row = n / kCPR, key = gr * kGroup + row;
+            load_to_lds16(entry(t0, min(key, s1 - 1 - t0)) + (((n - row * kCPR) ^ Tile<T>::swz(key)) << 4), to + p * 1024);     // keys past the range are masked below
+          }
+        }
+      }
+    };
+
+    f32x4_t oacc[kDT][RTW], lacc[RTW];
+    float m_run[RTW], l_run[RTW];
+#pragma unroll
+    for (int t = 0; t < RTW; ++t) {
+      m_run[t] = -FLT_MAX;
+      l_run[t] = 0.f;
+      lacc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int dt = 0; dt < kDT; ++dt) oacc[dt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    // A short segment has all its tiles in flight at once, behind the queries; of a longer one the first, so that the wait for the queries is not one for a
+    // whole ring.
+    const int together = S <= 2 || nit < S ? S : 1;
+#pragma unroll 1
+    for (int it = 0; it < together; ++it) {
+      locate(it);
+      issue(it);
+    }
+    // operand addresses: a K read is chunk 4 ks + fq of key fr, a column read the chunks 2 dt, 2 dt + 1 of key 4 fq + fr / 4 (fp32: column 16 dt + fr of key 4 fq + e)
+    int k_at = fr * kRowB + ((fq ^ Tile<T>::swz(fr)) << 4);
+    const int vkey = kF32 ? 4 * fq : 4 * fq + (fr >> 2);
+    int v_at = kF32 ? vkey * kRowB + ((((fr >> 2) ^ Tile<T>::swz(vkey)) << 4) | ((fr & 3) << 2))
+                          : vkey * kRowB + (((((fr & 3) >> 1) ^ Tile<T>::swz(vkey)) << 4) | ((fr & 1) << 3));
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));       // from here on vmcnt counts tile loads only
+    if constexpr (S > 2) {
+#pragma unroll 1
+      for (int it = together; it < S; ++it) {
+        locate(it);
+        issue(it);
+      }
+    }
+
+#pragma unroll 1
+    for (int it = 0; it < nit; ++it) {
+      if (S > 1 && it > 0) locate(it + S - 1);
+      // this wave's pieces of tile `it` have landed once at most those of the S - 2 tiles behind it are outstanding (the first has already)
+      if (S <= 2 || it + S - 1 >= nit) __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+      else if (it > 0) __builtin_amdgcn_s_waitcnt(vmcnt_imm(S <= 2 ? 0 : (S - 2) * kPieces));
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_s_waitcnt(0xC07F);           // lgkmcnt(0): tile it - 1 is read
+      if constexpr (NR > 1) __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      if (S > 1 && it > 0) issue(it + S - 1);
+      const int ti = it * NK + kg;
+      if (ti < ntl) {
+        const int t0 = s0 + kKeys * ti;
+        const char* tile = ring + (it % S) * kSlot;
+        asm volatile("" : "+v"(k_at), "+v"(v_at));  // (worked out per read from these two, not held)
+        // ---- S^T = C Q^T
+        f32x4_t sacc[kHalves][RTW];
+#pragma unroll
+        for (int j = 0; j < kHalves; ++j)
+#pragma unroll
+          for (int t = 0; t < RTW; ++t) sacc[j][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        constexpr int kReads = kHalves * kKS, kAhead = kF32 ? 4 : 8;
+        auto kread = [&](int i) {                   // read i: chunk quad i / kHalves, key half i % kHalves
+          const int ks = i / kHalves;
+          constexpr int kPer = kF32 ? 4 : 2;        // chunk quads that the swizzle mixes
+          return *reinterpret_cast<const uint4*>(tile + (k_at ^ ((ks % kPer) << 6)) + (ks / kPer) * (kPer << 6) + (i % kHalves) * 16 * kRowB);
+        };
+        uint4 kf[kReads];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) kf[i] = kread(i);
+#pragma unroll
+        for (int i = 0; i < kReads; ++i) {
+          if (i + kAhead < kReads) kf[i + kAhead] = kread(i + kAhead);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int t = 0; t < RTW; ++t) {
+            f32x4_t& c = sacc[i % kHalves][t];
+            if constexpr (kF32) {
+              const f32x4_t x = __builtin_bit_cast(f32x4_t, kf[i]), y = __builtin_bit_cast(f32x4_t, qf[i / kHalves][t]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], c, 0, 0, 0);
+            } else {
+              c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[i]), __builtin_bit_cast(bf16x8_t, qf[i / kHalves][t]), c, 0, 0, 0);
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        // ---- online softmax; lane (row fr, fq) owns the keys t0 + 16 j + 4 fq + e
+        const bool plain = t0 + kKeys <= min(L, s1);
+        uint4 pf[RTW], pl[RTW];
+        float pr32[4];
+#pragma unroll
+        for (int t = 0; t < RTW; ++t) {
+          float x[4 * kHalves];
+#pragma unroll
+          for (int j = 0; j < kHalves; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[4 * j + e] = sacc[j][t][e] * sl2;
+          if (!plain) {
+#pragma unroll
+            for (int j = 0; j < kHalves; ++j)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int p = t0 + 16 * j + 4 * fq + e;
+                bool seen = p < s1;
+                if (seen && p >= L) seen = (rowmask[t] >> (p - L)) & 1ull;
+                x[4 * j + e] = seen ? x[4 * j + e] : -INFINITY;
+              }
+          }
+          float mt = x[0];
+#pragma unroll
+          for (int e = 1; e < 4 * kHalves; ++e) mt = max_nan(mt, x[e]);
+          if (__builtin_amdgcn_ballot_w64(mt > m_run[t] + kSlack) != 0ull) {
+            const float m_new = fmaxf(m_run[t], quad_row_max(mt));
+            const float al = __builtin_amdgcn_exp2f(m_run[t] - m_new);
+            m_run[t] = m_new;
+            l_run[t] *= al;
+            lacc[t][0] *= al;
+#pragma unroll
+            for (int dt = 0; dt < kDT; ++dt) {
+              oacc[dt][t][0] *= al; oacc[dt][t][1] *= al;
+              oacc[dt][t][2] *= al; oacc[dt][t][3] *= al;
+              if constexpr (in_agprs(LD, sizeof(T), RTW)) {     // four at a time there and back: all at once are as many registers again
+                asm volatile("" : "+a"(oacc[dt][t]));
+                __builtin_amdgcn_sched_barrier(0);
+              }
+            }
+          }
+          float pr[4 * kHalves];
+#pragma unroll
+          for (int e = 0; e < 4 * kHalves; ++e) pr[e] = __builtin_amdgcn_exp2f(x[e] - m_run[t]);
+          if constexpr (kF32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pr32[e] = pr[e];
+            l_run[t] += (pr[0] + pr[1]) + (pr[2] + pr[3]);
+          } else {
+            pf[t] = make_uint4(pack_bf16x2(pr[0], pr[1]), pack_bf16x2(pr[2], pr[3]), pack_bf16x2(pr[4], pr[5]), pack_bf16x2(pr[6], pr[7]));
+            if constexpr (kSplitP) {
+              float hi[8];
+              unpack16(pf[t], hi);
+              pl[t] = make_uint4(pack_bf16x2(pr[0] - hi[0], pr[1] - hi[1]), pack_bf16x2(pr[2] - hi[2], pr[3] - hi[3]),
+                                 pack_bf16x2(pr[4] - hi[4], pr[5] - hi[5]), pack_bf16x2(pr[6] - hi[6], pr[7] - hi[7]));
+              l_run[t] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
+            } else {
+              const uint32_t one = 0x3F803F80u;     // the sum of the probabilities as the values are multiplied with them
+              lacc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, make_uint4(one, one, one, one)),
+                                                                __builtin_bit_cast(bf16x8_t, pf[t]), lacc[t], 0, 0, 0);
+            }
+          }
+        }
+        // ---- O^T += C^T P^T
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kF32) {
+          // (chunks 4 dt .. 4 dt + 3 of key 4 fq + e: the swizzle of the key mixes sixteen chunks, those of four column tiles)
+          float vf[kDT][4];
+          auto vread = [&](int dt) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              vf[dt][e] = *reinterpret_cast<const float*>(tile + ((v_at ^ (e << 4) ^ ((dt & 3) << 6)) + e * kRowB) + (dt >> 2) * 256);
+          };
+          constexpr int kVAhead = 2;
+#pragma unroll
+          for (int dt = 0; dt < kVAhead; ++dt) vread(dt);
+#pragma unroll
+          for (int dt = 0; dt < kDT; ++dt) {
+            if (dt + kVAhead < kDT) vread(dt + kVAhead);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) oacc[dt][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[dt][e], pr32[e], oacc[dt][0], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        } else {
+          s16x4_t vlo[kDT], vhi[kDT];
+          auto vread = [&](int dt) {
+            const char* p = tile + (v_at ^ ((dt & 3) << 5)) + (dt >> 2) * 128;
+            vlo[dt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(lds_ptr_t)p);
+            vhi[dt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(lds_ptr_t)(p + 16 * kRowB));
+          };
+          constexpr int kVAhead = 4;
+#pragma unroll
+          for (int dt = 0; dt < kVAhead; ++dt) vread(dt);
+#pragma unroll
+          for (int dt = 0; dt < kDT; ++dt) {
+            if (dt + kVAhead < kDT) vread(dt + kVAhead);
+            __builtin_amdgcn_sched_barrier(0);
+            const uint2 l2 = __builtin_bit_cast(uint2, vlo[dt]), h2 = __builtin_bit_cast(uint2, vhi[dt]);
+            const bf16x8_t va = __builtin_bit_cast(bf16x8_t, make_uint4(l2.x, l2.y, h2.x, h2.y));
+#pragma unroll
+            for (int t = 0; t < RTW; ++t) {
+              oacc[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8_t, pf[t]), oacc[dt][t], 0, 0, 0);
+              if constexpr (kSplitP) oacc[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8_t, pl[t]), oacc[dt][t], 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      }
+      if constexpr (S == 1) {                       // (rings of one slot, one wave: the others' loads are on their way meanwhile)
+        static_assert(S > 1 || NR == 1, "a slot alone belongs to one wave");
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_s_waitcnt(0xC07F);
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        locate(it + 1);
+        issue(it + 1);
+      }
+    }
+
+    // ---- the segment's partial result
+    const int64_t slot_row = (static_cast<int64_t>(blockIdx.x) + static_cast<int64_t>(b) * a.Hkv + seg.g) * a.block_rows;
+    if constexpr (NK == 1) {
+#pragma unroll
+      for (int t = 0; t < RTW; ++t) {
+        const float l = kF32 || kSplitP ? quad_row_sum(l_run[t]) : lacc[t][0];
+        if (rho[t] >= R) continue;
+        if (fq == 0) *reinterpret_cast<float2*>(a.part_ml + (slot_row + rho[t]) * 2) = make_float2(m_run[t], l);
+        float* dst = a.part_o + (slot_row + rho[t]) * LD + 4 * fq;
+#pragma unroll
+        for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = oacc[dt][t];
+      }
+    } else {
+      // the rings leave their sums in their own slots, the 16-byte pieces of a row swizzled, and every wave adds some rows in the order of the rings
+      static_assert(RTW == 1 && NR * 16 * LD * 4 <= S * kSlot, "a ring's slots hold its sums");
+      constexpr int C4 = LD / 4, kStep = C4 < 64 ? C4 : 64;
+      const float l = quad_row_sum(l_run[0]);
+      if constexpr (NR > 1) __syncthreads();        // (waves of a ring write where others may still read)
+      if (fq == 0) *reinterpret_cast<float2*>(ml_lds + 2 * (kg * NR * 16 + rho[0])) = make_float2(m_run[0], l);
+#pragma unroll
+      for (int dt = 0; dt < kDT; ++dt)
+        *reinterpret_cast<f32x4_t*>(ring + rho[0] * (4 * LD) + (((4 * dt + fq) ^ fr) << 4)) = oacc[dt][0];
+      __syncthreads();
+#pragma unroll 1
+      for (int x = wv * (64 / kStep) + lane / kStep; x < R * (C4 / kStep); x += 4 * (64 / kStep)) {
+        const int r = x / (C4 / kStep), c4 = x % (C4 / kStep) * kStep + lane % kStep;
+        float2 ml[NK];
+        float4 o[NK];
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+          ml[k] = *reinterpret_cast<const float2*>(ml_lds + 2 * (k * NR * 16 + r));
+          o[k] = *reinterpret_cast<const float4*>(smem + k * (S * kSlot) + r * (4 * LD) + ((c4 ^ (r & 15)) << 4));
+        }
+        float mm = ml[0].x;
+#pragma unroll
+        for (int k = 1; k < NK; ++k) mm = fmaxf(mm, ml[k].x);
+        float sum = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+          const float f = __builtin_amdgcn_exp2f(ml[k].x - mm);
+          sum = fmaf(f, ml[k].y, sum);
+          v.x = fmaf(f, o[k].x, v.x); v.y = fmaf(f, o[k].y, v.y);
+          v.z = fmaf(f, o[k].z, v.z); v.w = fmaf(f, o[k].w, v.w);
+        }
+        *reinterpret_cast<float4*>(a.part_o + (slot_row + r) * LD + 4 * c4) = v;
+        if (c4 == 0) *reinterpret_cast<float2*>(a.part_ml + (slot_row + r) * 2) = make_float2(mm, sum);
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ float load_value(const bf16_t* p) { return bf16_to_f32(*p); }
+__device__ __forceinline__ float load_value(const float* p) { return *p; }
+
+// One output row key by key, from the entries that it sees: for rows that are not finite, since the products above multiply what is masked with zero.
+template <typename T, int LD>
+__device__ __forceinline__ void latent_row_again(const LatentAttnArgs& a, int b, int row, float* lds) {
+  constexpr int E = LD / 64;
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int L = attn_ctx_len(a, b), i = row / a.Hq;
+  const uint64_t word = a.mask ? a.mask[static_cast<int64_t>(b) * a.mask_stride + i] : ((2ull << i) - 1ull);
+  const T* q = static_cast<const T*>(a.q) + (static_cast<int64_t>(b) * a.rows + row) * (LD + kPe);
+  float qv[E + 1], acc[E], m = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int e = 0; e <= E; ++e) qv[e] = load_value(q + 64 * e + lane);
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.f;
+  for (int p = wv; p < L + a.n_blk; p += 4) {
+    if (p >= L && !((word >> (p - L)) & 1ull)) continue;
+    int64_t at = static_cast<int64_t>(b) * a.l_max + p;
+    if (a.paged) {
+      const int in_seq = p / a.page_size;
+      at = static_cast<int64_t>(checked_page(a.page_table[static_cast<int64_t>(b) * a.max_pages + in_seq], a.n_pages, a.status)) * a.page_size + (p - in_seq * a.page_size);
+    }
+    const T* c = static_cast<const T*>(a.k) + at * (LD + kPe);
+    float cv[E + 1], s = 0.f;
+#pragma unroll
+    for (int e = 0; e <= E; ++e) {
+      cv[e] = load_value(c + 64 * e + lane);
+      s = fmaf(qv[e], cv[e], s);
+    }
+    s = wave_sum_dpp(s) * a.scale * 1.44269504088896340736f;
+    const float m_new = max_nan(m, s);
+    const float old = m == m_new ? 1.f : exp2f(m - m_new), w = s == -INFINITY ? 0.f : exp2f(s - m_new);
+    m = m_new;
+    sum = sum * old + w;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = acc[e] * old + w * cv[e];
+  }
+  __syncthreads();
+  float* mine = lds + wv * (LD + 2);
+#pragma unroll
+  for (int e = 0; e < E; ++e) mine[64 * e + lane] = acc[e];
+  if (lane == 0) {
+    mine[LD] = m;
+    mine[LD + 1] = sum;
+  }
+  __syncthreads();
+  float mm = -INFINITY;
+  for (int k = 0; k < 4; ++k) mm = max_nan(mm, lds[k * (LD + 2) + LD]);
+  float w[4], den = 0.f;
+  for (int k = 0; k < 4; ++k) {
+    const float mk = lds[k * (LD + 2) + LD];
+    w[k] = mk == -INFINITY ? 0.f : exp2f(mk - mm);          // (a wave that saw nothing, or scores of minus infinity only)
+    if (w[k] != 0.f) den += w[k] * lds[k * (LD + 2) + LD + 1];
+  }
+  T* out = static_cast<T*>(a.out) + (static_cast<int64_t>(b) * a.rows + row) * LD;
+  for (int d = threadIdx.x; d < LD; d += 256) {
+    float v = 0.f;
+    for (int k = 0; k < 4; ++k)
+      if (w[k] != 0.f) v += w[k] * lds[k * (LD + 2) + d];
+    v = den != 0.f ? v / den : mm == -INFINITY ? 0.f : v / den;
+    if constexpr (sizeof(T) == 2) out[d] = static_cast<bf16_t>(pack_bf16x2(v, v));
+    else out[d] = v;
+  }
+}
+
+// Merge the segments of an output row: exact log-sum-exp combination, a workgroup per row.  Groups of lanes take every NG-th segment of a
+// float4 column and are added in a fixed order; the weights are worked out by every wave for itself.
+constexpr int kCombEarly = 6;
+template <typename T, int LD>
+__global__ __launch_bounds__(256) void k_latent_combine(const LatentAttnArgs a) {
+  constexpr int C4 = LD / 4, NG = 256 / C4;
+  __shared__ float4 gs[NG][C4];
+  __shared__ float again[4 * (LD + 2)];
+  const int row = blockIdx.x, b = blockIdx.y;
+  const int lane = threadIdx.x & 63;
+  const int g = row / a.block_rows, r = row - g * a.block_rows, u = b * a.Hkv + g;
+  const int w_first = a.sched[2 * u], n = a.sched[2 * u + 1] - w_first + 1;
+  const int64_t first = (static_cast<int64_t>(w_first) + u) * a.block_rows + r;
+  const int sg = threadIdx.x / C4, c4 = threadIdx.x % C4;
+  const float* po = a.part_o + first * LD + c4 * 4;
+  const float* pm = a.part_ml + first * 2;
+  const int64_t po_step = static_cast<int64_t>(a.block_rows) * LD, pm_step = static_cast<int64_t>(a.block_rows) * 2;
+  float2 ml = *reinterpret_cast<const float2*>(pm + min(lane, n - 1) * pm_step);
+  float4 o[kCombEarly];
+#pragma unroll
+  for (int e = 0; e < kCombEarly; ++e) o[e] = *reinterpret_cast<const float4*>(po + min(sg + e * NG, n - 1) * po_step);
+  float mmax = ml.x;
+  for (int s = 64 + lane; s < n; s += 64) mmax = fmaxf(mmax, pm[s * pm_step]);
+  mmax = wave_max_dpp(mmax);
+  float den = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int q0 = 0; q0 < n; q0 += 64) {
+    if (q0 > 0) ml = *reinterpret_cast<const float2*>(pm + min(q0 + lane, n - 1) * pm_step);
+    const float w = q0 + lane < n ? exp2f(ml.x - mmax) : 0.f;
+    den += w != 0.f || ml.y != ml.y ? w * ml.y : 0.f;
+    const int k = min(64, n - q0);
+    for (int sb = 0; sb < k; sb += kCombEarly * NG) {          // (uniform: a shuffle reads lanes that take part only)
+      const int s = sb + sg;
+      if (q0 + sb > 0) {
+#pragma unroll
+        for (int e = 0; e < kCombEarly; ++e) o[e] = *reinterpret_cast<const float4*>(po + (q0 + min(s + e * NG, k - 1)) * po_step);
+      }
+#pragma unroll
+      for (int e = 0; e < kCombEarly; ++e) {
+        float we = __shfl(w, min(s + e * NG, k - 1), 64);
+        if (s + e * NG >= k) we = 0.f;
+        if (we != 0.f) {
+          acc.x = fmaf(we, o[e].x, acc.x); acc.y = fmaf(we, o[e].y, acc.y);
+          acc.z = fmaf(we, o[e].z, acc.z); acc.w = fmaf(we, o[e].w, acc.w);
+        }
+      }
+    }
+  }
+  gs[sg][c4] = acc;
+  den = wave_sum_dpp(den);
+  __syncthreads();
+  bool odd = false;
+  if (sg == 0) {
+    float4 sum = gs[0][c4];
+#pragma unroll
+    for (int k = 1; k < NG; ++k) {
+      const float4 v = gs[k][c4];
+      sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+    }
+    if (den == 0.f) sum = make_float4(0.f, 0.f, 0.f, 0.f);      // a row that sees nothing
+    else { sum.x /= den; sum.y /= den; sum.z /= den; sum.w /= den; }
+    T* dst = static_cast<T*>(a.out) + (static_cast<int64_t>(b) * a.rows + row) * LD + c4 * 4;
+    if constexpr (sizeof(T) == 2) {
+      const uint2 v = make_uint2(pack_bf16x2(sum.x, sum.y), pack_bf16x2(sum.z, sum.w));
+      __builtin_memcpy(dst, &v, sizeof(v));
+    } else {
+      __builtin_memcpy(dst, &sum, sizeof(sum));
+    }
+    odd = !(fabsf((sum.x + sum.y) + (sum.z + sum.w)) < INFINITY) || !(fabsf(den) < INFINITY);
+  }
+  if (__syncthreads_or(odd)) latent_row_again<T, LD>(a, b, row, again);
+}
+
+template <typename T, int LD, int RTW, int NR>
+hipError_t launch_ring(const LatentAttnArgs& a, hipStream_t s) {
+  constexpr int NK = 4 / NR, S = stages_of(LD, sizeof(T), NK);
+  const size_t lds = static_cast<size_t>(NK) * S * slot_bytes(LD, sizeof(T)) + (NK > 1 ? NK * NR * 16 * 8 : 0) + static_cast<size_t>(attn_sched_words(a.B)) * 4;
+  if (a.paged) {
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_latent_ring<T, LD, RTW, NR, NK, true>),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    if (attr != hipSuccess) return attr;
+    hipLaunchKernelGGL((k_latent_ring<T, LD, RTW, NR, NK, true>), dim3(a.wgrid), dim3(256), lds, s, a);
+  } else {
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_latent_ring<T, LD, RTW, NR, NK, false>),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    if (attr != hipSuccess) return attr;
+    hipLaunchKernelGGL((k_latent_ring<T, LD, RTW, NR, NK, false>), dim3(a.wgrid), dim3(256), lds, s, a);
+  }
+  return hipGetLastError();
+}
+
+template <typename T, int LD>
+hipError_t launch_ld(const LatentAttnArgs& a, hipStream_t s) {
+  hipError_t e;
+  if (a.block_rows <= 16) e = launch_ring<T, LD, 1, 1>(a, s);
+  else if (a.block_rows <= 32) e = launch_ring<T, LD, 1, 2>(a, s);
+  else e = launch_ring<T, LD, 1, 4>(a, s);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((k_latent_combine<T, LD>), dim3(a.rows, a.B), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_as(const LatentAttnArgs& a, hipStream_t s) {
+  switch (a.d) {
+    case 128: return launch_ld<T, 128>(a, s);
+    case 256: return launch_ld<T, 256>(a, s);
+    case 512: return launch_ld<T, 512>(a, s);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace
+
+bool latent_attn_plan(LatentAttnArgs& a, int num_cus) {
+  const int most = 64;
+  a.rows = a.Hq * a.n_q;
+  a.Hkv = (a.rows + most - 1) / most;
+  a.block_rows = ((a.rows + a.Hkv - 1) / a.Hkv + 15) & ~15;
+  a.Hkv = (a.rows + a.block_rows - 1) / a.block_rows;
+  a.pad = 2;
+  a.wide_from = INT_MAX;
+  a.use_mfma = 0;
+  if (a.B > kAttnMaxSeqs || a.l_max < a.n_blk) return false;
+  const int64_t units = static_cast<int64_t>(a.B) * a.Hkv;
+  const int64_t gmax = (a.l_max + kAttnGran - 1) / kAttnGran;
+  if (units * (gmax + a.pad) >= (1ll << 30)) return false;
+  const AttnLine line = attn_sched_line(static_cast<int>(a.B * gmax), a.B, a.Hkv, a.pad, a.wide_from, 0, num_cus);
+  a.wgrid = line.W;
+  if (line.T > kAttnSpread && a.wgrid < kAttnSpread) a.wgrid = kAttnSpread < num_cus ? kAttnSpread : num_cus;   // (fewer granules may take more workgroups)
+  return true;
+}
+
+static size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
+static size_t slot_rows(const LatentAttnArgs& a) { return (static_cast<size_t>(a.wgrid) + static_cast<size_t>(a.B) * a.Hkv) * a.block_rows; }
+
+size_t latent_attn_workspace_bytes(const LatentAttnArgs& a) {
+  return up256(slot_rows(a) * a.d * sizeof(float)) + up256(slot_rows(a) * 2 * sizeof(float)) + up256(static_cast<size_t>(a.B) * a.Hkv * 2 * sizeof(int));
+}
+
+void latent_attn_carve(LatentAttnArgs& a, void* workspace) {
+  char* p = static_cast<char*>(workspace);
+  a.part_o = reinterpret_cast<float*>(p);
+  p += up256(slot_rows(a) * a.d * sizeof(float));
+  a.part_ml = reinterpret_cast<float*>(p);
+  p += up256(slot_rows(a) * 2 * sizeof(float));
+  a.sched = reinterpret_cast<int*>(p);
+}
+
+hipError_t launch_latent_attn(const LatentAttnArgs& a, hipStream_t s) { return a.dtype == 1 ? launch_as<bf16_t>(a, s) : launch_as<float>(a, s); }
+
+}  // namespace sx

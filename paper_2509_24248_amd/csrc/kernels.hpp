@@ -298,6 +298,96 @@ void sample_plan(SampleArgs& a);
 size_t sample_carve(SampleArgs& a, void* base);
 hipError_t launch_sample(const SampleArgs& a, hipStream_t s);
 
+// ---- rotary positions, entries of a latent cache (rope.hip) ------------------------------------
+// Where an entry of a sequence lies.
+struct CachePlace {
+  int paged;
+  const int32_t* page_table;
+  int page_size, max_pages;
+  int64_t l_max, n_pages;
+};
+constexpr int kRopeLinear = 1, kRopeBands = 2, kRopeRamp = 3;
+struct RopeTableArgs {
+  int rot, scaling;
+  float theta, factor, low, high;
+  int orig_len;
+  uint64_t* turns;           // [rot / 2]
+};
+hipError_t launch_rope_table(const RopeTableArgs& a, hipStream_t s);
+struct RopeRowsArgs {
+  CachePlace kv;             // Hkv > 0
+  void *kc, *vc;
+  int f32, d, Hq, Hkv, B, T;
+  int rot, neighbours;       // rotated values of a head; pairs (2c, 2c + 1), else (c, c + rot / 2)
+  float amplitude;
+  const uint64_t* turns;
+  const void *q, *k, *v;     // token t of sequence b lies (b T + t) stride elements behind
+  int64_t q_stride, kv_stride, out_stride;
+  void* q_out;
+  const int32_t *pos, *offset, *count;     // offset, count: or nullptr
+  int* status;
+  int per, groups;           // rope_rows_plan: steps of a wave, waves of a token
+  int64_t tasks;             // waves
+};
+bool rope_rows_plan(RopeRowsArgs& a);
+hipError_t launch_rope_rows(const RopeRowsArgs& a, hipStream_t s);
+constexpr int kLatentRope = 64;            // rotated values of a latent entry
+struct LatentWriteArgs {
+  CachePlace kv;
+  void* c;
+  int f32, r, B, T, H;
+  const void* rows;          // [B][T] of r + 64 values, row_stride elements apart
+  int64_t row_stride;
+  const void* gain;          // [r] or nullptr: no norm
+  float eps;
+  const void* q_rows;        // 64 values of every head
+  int64_t q_stride, head_stride;
+  void* q_out;               // [B][T][H][r + 64], the last 64 written
+  int neighbours;
+  float amplitude;
+  const uint64_t* turns;
+  const int32_t *pos, *offset, *count;
+  int* status;
+  int64_t entries, tasks;    // latent_write_plan: waves that write entries, and all
+  int q_groups;              // waves of a token's queries
+};
+bool latent_write_plan(LatentWriteArgs& a);
+hipError_t launch_latent_write(const LatentWriteArgs& a, hipStream_t s);
+
+// ---- latent attention (attn_latent.hip) ------------------------------------------------------
+// k: the entries of one vector of latent + 64 values; d: the latent's width; Hkv: blocks of rows; n_q, Hq, q, out as in the call
+struct LatentAttnArgs : AttnArgs {
+  int block_rows;            // query rows of a block (the last may have fewer)
+  int rows;                  // Hq n_q
+};
+bool latent_attn_plan(LatentAttnArgs& a, int num_cus);
+size_t latent_attn_workspace_bytes(const LatentAttnArgs& a);
+void latent_attn_carve(LatentAttnArgs& a, void* workspace);
+hipError_t launch_latent_attn(const LatentAttnArgs& a, hipStream_t s);
+
+// ---- log probabilities (logprob.hip) ---------------------------------------------------------
+constexpr int kLogprobMaxTop = 32, kLogprobMaxTok = 64;
+struct LogprobArgs {
+  int f32, M, V;
+  int64_t ld;
+  const void* logits;
+  int rows_per_seq;
+  const float* temperature;  // [ceil(M / rows_per_seq)] or nullptr
+  int n_tok, n_top;
+  const int32_t* token;      // [M][n_tok]
+  float* logprob;            // [M][n_tok]
+  float* entropy;            // [M] or nullptr
+  int32_t* top_token;        // [M][n_top]
+  float* top_logprob;        // [M][n_top] or nullptr
+  int* status;
+  int wide, chunks;          // logprob_plan: chunks of 32 values a thread, else 8; chunks of a row
+  float4* stats;             // [M][chunks]: largest logit, how many equal it, sums
+  unsigned long long* best;  // [M][chunks][n_top]
+};
+void logprob_plan(LogprobArgs& a);
+size_t logprob_carve(LogprobArgs& a, void* base);
+hipError_t launch_logprob(const LogprobArgs& a, hipStream_t s);
+
 // ---- draft-step glue kernels -----------------------------------------------------------
 struct DraftDims {
   int dtype, D, Hq, Hkv, d, I, V;
@@ -339,6 +429,7 @@ struct CompactArgs {
 };
 bool kv_compact_supported(const CompactArgs& a);
 hipError_t launch_kv_compact(const CompactArgs& a, hipStream_t s);
+hipError_t launch_latent_compact(const CompactArgs& a, hipStream_t s);      // k: the entries, row_bytes of each; Hkv and v unused
 
 // ---- tree drafting: hand tokens and hidden states from one level to the next ----------------
 struct TreeGatherArgs {
