@@ -35,27 +35,114 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
 template <typename T> struct Tile;
-// XOR swizzle of a row's 16-byte chunks.  A bf16 row is an odd number of 128 bytes, so a key's parity already picks one half of the banks; the
-// permuted bits of the rest keep apart the sixteen keys of a K read (one chunk each) as well as the eight keys of a transpose read (an even chunk and
-// the next).  An fp32 row is a whole number of 256 bytes: the key itself.
+// A tile lies in LDS in groups of 8 keys (fp32: 4), a group in 1 KB blocks of 128 bytes (256) of each of them: what one load instruction brings in, lane l the 16-byte chunk
+// l % 8 (16) of key l / 8 (16), so that a lane's source is one offset for all blocks.  The chunks of a key's part are swizzled: the permuted bits of the key keep apart the
+// sixteen keys of a K read (one chunk each) as well as the eight keys of a transpose read (an even chunk and the next).
 template <> struct Tile<bf16_t> {
-  static constexpr int kKeys = 32;
+  static constexpr int kKeys = 32, kGroup = 8, kPart = 128;
   __host__ __device__ static constexpr int swz(int key) { return ((key >> 1 & 3) << 1) | (key >> 3 & 1); }
-  __host__ __device__ static constexpr int flip(int group) { return (group & 1) << 4; }       // of a piece's source, from group to group of 8 keys
+  __host__ __device__ static constexpr int flip(int group) { return (group & 1) << 4; }       // of a lane's source, from group to group
 };
 template <> struct Tile<float> {
-  static constexpr int kKeys = 16;
+  static constexpr int kKeys = 16, kGroup = 4, kPart = 256;
   __host__ __device__ static constexpr int swz(int key) { return key & 15; }
-  __host__ __device__ static constexpr int flip(int group) { return group << 6; }             // groups of 4 keys
+  __host__ __device__ static constexpr int flip(int group) { return group << 6; }
 };
 
 constexpr int slot_bytes(int ld, int e) { return (e == 2 ? 32 : 16) * (ld + kPe) * e; }
 // Slots of a ring: what the LDS of a compute unit holds beside the schedule's table and the merge's pairs.
 constexpr int kTableBytes = attn_sched_words(kAttnMaxSeqs) * 4 + 1024;
-constexpr int stages_of(int ld, int e, int nk) {
+__host__ __device__ constexpr int stages_of(int ld, int e, int nk) {
   const int most = (kLds - kTableBytes) / (nk * slot_bytes(ld, e));
   return most < 1 ? 1 : most > 4 ? 4 : most;
 }
+
+// Where the tiles of a segment come from.  Paged: a lane holds where 16 keys lie in the pool (in units of 16 entries), for 64 of them; the next 64 are on their way.
+template <typename T, int LD, bool PAGED>
+struct Source {
+  static constexpr int kKeys = Tile<T>::kKeys, kGroup = Tile<T>::kGroup, kPart = Tile<T>::kPart;
+  static constexpr int kRowB = (LD + kPe) * static_cast<int>(sizeof(T)), kBlocks = kRowB / kPart;    // 1 KB blocks of a group
+  static constexpr int kLanes = kPart / 16;                                                          // lanes of a key
+  const LatentAttnArgs& a;
+  int b, s0, s1;
+  uint32_t lane_off;           // of a lane's chunk behind the first key of its group
+  int ids, ids_next, chunk, id0, id1;
+  __device__ __forceinline__ Source(const LatentAttnArgs& args) : a(args) {
+    const int lane = threadIdx.x & 63, key = lane / kLanes;
+    lane_off = static_cast<uint32_t>(key * kRowB + (((lane % kLanes) ^ Tile<T>::swz(key)) << 4));
+  }
+  __device__ __forceinline__ int fetch(int c) const {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));                  // (worked out here, not held)
+    const int p = min(s0 + 16 * (64 * c + lane), s1 - 1) & ~15;
+    const int in_seq = static_cast<int>(static_cast<uint32_t>(p) / static_cast<uint32_t>(a.page_size));
+    const int page = checked_page(a.page_table[static_cast<int64_t>(b) * a.max_pages + in_seq], a.n_pages, a.status);
+    return page * (a.page_size >> 4) + ((p - in_seq * a.page_size) >> 4);
+  }
+  __device__ __forceinline__ void begin(int seq, int from, int to) {
+    b = seq; s0 = from; s1 = to;
+    ids = ids_next = chunk = id0 = id1 = 0;
+    if (PAGED) {
+      ids = fetch(0);
+      if (s1 - s0 > 1024) ids_next = fetch(1);
+    }
+  }
+  // Tile ti of the segment, in front of its entries or blocks.  (Calls go up by less than 1024 keys.)
+  __device__ __forceinline__ void locate(int ti) {
+    const int t0 = kKeys * ti;
+    if (!PAGED || s0 + t0 >= s1) return;
+    const int blk = t0 >> 4;
+    if (blk >> 6 != chunk) {
+      chunk = blk >> 6;
+      ids = ids_next;
+      if (s0 + 1024 * (chunk + 1) < s1) ids_next = fetch(chunk + 1);
+    }
+    id0 = __builtin_amdgcn_readlane(ids, blk & 63);
+    if (kKeys == 32) id1 = __builtin_amdgcn_readlane(ids, (blk & 63) + 1);
+  }
+  __device__ __forceinline__ const char* entry(int ti, int key) const {
+    if (!PAGED) return static_cast<const char*>(a.k) + (static_cast<int64_t>(b) * a.l_max + s0 + kKeys * ti + key) * kRowB;
+    return static_cast<const char*>(a.k) + (static_cast<int64_t>(key < 16 ? id0 : id1) * 16 + (key & 15)) * kRowB;
+  }
+  __device__ __forceinline__ bool whole(int ti) const { return s0 + kKeys * (ti + 1) <= s1; }
+  // Block `block` of a group of a whole tile whose first key lies at `base`.
+  __device__ __forceinline__ void load(const char* base, int group, int block, const char* slot) const {
+    load_to_lds16(base + block * kPart, lane_off ^ Tile<T>::flip(group), slot + (group * kBlocks + block) * 1024);
+  }
+  // A group of any tile; keys past the range repeat the last one and are masked later.
+  __device__ __forceinline__ void load_group(int ti, int group, const char* slot) const {
+    if (whole(ti)) {
+      const char* base = entry(ti, group * kGroup);
+#pragma unroll
+      for (int block = 0; block < kBlocks; ++block) load(base, group, block, slot);
+    } else {
+      int lane = threadIdx.x & 63;
+      asm volatile("" : "+v"(lane));
+      const int key = group * kGroup + lane / kLanes;
+      const char* at = entry(ti, min(key, s1 - 1 - s0 - kKeys * ti)) + (((lane % kLanes) ^ Tile<T>::swz(key)) << 4);
+#pragma unroll 1
+      for (int block = 0; block < kBlocks; ++block) load_to_lds16(at + block * kPart, slot + (group * kBlocks + block) * 1024);
+    }
+  }
+  // Operand addresses in a tile.  rows: chunk quad ks of key fr (+ 16 half).  columns: the transpose read of chunks 2 dt, 2 dt + 1 of key 4 fq + fr / 4 (+ 16 half); fp32: value
+  // 16 dt + fr of key 4 fq + e.
+  __device__ static __forceinline__ int place(int key) { return (key / kGroup) * (kBlocks * 1024) + key % kGroup * kPart; }
+  __device__ static __forceinline__ int rows_at(int fr, int fq) { return place(fr) + ((fq ^ Tile<T>::swz(fr)) << 4); }
+  __device__ static __forceinline__ int columns_at(int fr, int fq) {
+    if (sizeof(T) == 4) return place(4 * fq) + ((((fr >> 2) ^ Tile<T>::swz(4 * fq)) << 4) | ((fr & 3) << 2));
+    const int key = 4 * fq + (fr >> 2);
+    return place(key) + (((((fr & 3) >> 1) ^ Tile<T>::swz(key)) << 4) | ((fr & 1) << 3));
+  }
+  static constexpr int kHalf = (16 / kGroup) * kBlocks * 1024;                    // bytes between the halves of 16 keys
+  static constexpr int kQuads = kPart / 64;                                       // chunk quads of a block
+  __device__ static __forceinline__ const char* row_read(const char* tile, int rows_at, int ks, int half) {
+    return tile + (rows_at ^ (ks % kQuads << 6)) + (ks / kQuads) * 1024 + half * kHalf;
+  }
+  __device__ static __forceinline__ const char* column_read(const char* tile, int columns_at, int dt, int e) {
+    if (sizeof(T) == 4) return tile + ((columns_at ^ (e << 4) ^ ((dt & 3) << 6)) + e * kPart) + (dt >> 2) * 1024;
+    return tile + (columns_at ^ ((dt & 3) << 5)) + (dt >> 2) * 1024 + e * kHalf;
+  }
+};
 
 // Registers of a lane for accumulators and queries.  Up to 190 everything is done in 256 ordinary ones; beyond that the accumulators are in the other 256, which
 // only matrix instructions work on: see the rescaling.
@@ -67,14 +154,11 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
   static_assert(NR * NK == 4, "four waves");
   constexpr bool kF32 = sizeof(T) == 4;
   constexpr int S = stages_of(LD, sizeof(T), NK);
-  constexpr int kKeys = Tile<T>::kKeys, kGroup = kKeys / 4;
-  constexpr int kRowB = (LD + kPe) * static_cast<int>(sizeof(T)), kCPR = kRowB / 16;
+  constexpr int kKeys = Tile<T>::kKeys, kRowB = Source<T, LD, PAGED>::kRowB;
   constexpr int kSlot = slot_bytes(LD, sizeof(T));
-  constexpr int kPP = kGroup * kRowB / 1024;        // 1 KB pieces of a group of keys
   constexpr int kGroups = 4 / NR;                   // groups of a tile that a wave brings in
-  constexpr int kPieces = kGroups * kPP;
-  constexpr int kKS = kCPR / 4, kDT = LD / 16, kHalves = kKeys / 16;
-  static_assert(kPP * 1024 == kGroup * kRowB && kCPR % 8 == 0, "whole pieces");
+  constexpr int kPieces = kGroups * Source<T, LD, PAGED>::kBlocks;
+  constexpr int kKS = kRowB / 64, kDT = LD / 16, kHalves = kKeys / 16;
   // Probabilities of bf16 calls: two bf16 parts (16 bits) where the matrix instructions have the time, up to 64 rows; with 128 rows one, normalised with its own sum.
   constexpr bool kSplitP = !kF32 && RTW == 1;
   constexpr float kSlack = kF32 || kSplitP ? 8.f : 0.f;      // of the softmax reference, log2 units: see attn_mfma.hip
@@ -90,13 +174,7 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
   const AttnLine line = attn_sched_line(a, table);
   if (static_cast<int>(blockIdx.x) >= line.W) return;         // the whole workgroup leaves together
   const int x_hi = attn_sched_lo(line, blockIdx.x + 1);
-  // where a lane of a piece fetches from, behind the first key of its group
-  uint32_t lane_off[kPP];
-#pragma unroll
-  for (int p = 0; p < kPP; ++p) {
-    const int n = 64 * p + lane, row = n / kCPR, at = n % kCPR;
-    lane_off[p] = static_cast<uint32_t>(row * kRowB + ((at ^ Tile<T>::swz(row)) << 4));
-  }
+  Source<T, LD, PAGED> src(a);
   const float sl2 = a.scale * 1.44269504088896340736f;
   bool again = false;
   AttnSeg seg = attn_sched_next(a, table, true, line.pad, attn_sched_lo(line, blockIdx.x), x_hi);
@@ -128,62 +206,14 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
     if (again) __syncthreads();                     // the rings are free of the segment before
     again = true;
 
-    // ---- tiles.  Paged: a lane holds where 16 keys lie in the pool (in units of 16 entries), for 64 of them; the next 64 are on their way.
-    int ids = 0, ids_next = 0, chunk = 0;
-    auto fetch_ids = [&](int c) {
-      const int p = min(s0 + 16 * (64 * c + lane), s1 - 1) & ~15;
-      const int in_seq = static_cast<int>(static_cast<uint32_t>(p) / static_cast<uint32_t>(a.page_size));
-      const int page = checked_page(a.page_table[static_cast<int64_t>(b) * a.max_pages + in_seq], a.n_pages, a.status);
-      return page * (a.page_size >> 4) + ((p - in_seq * a.page_size) >> 4);
-    };
-    if (PAGED) {
-      ids = fetch_ids(0);
-      if (s1 - s0 > 1024) ids_next = fetch_ids(1);
-    }
-    const char* seq = static_cast<const char*>(a.k) + static_cast<int64_t>(b) * a.l_max * kRowB;
-    int id0 = 0, id1 = 0;                           // of a tile's first and second 16 keys
-    auto locate = [&](int it) {
-      const int t0 = kKeys * (it * NK + kg);
-      if (!PAGED || s0 + t0 >= s1) return;
-      const int blk = t0 >> 4;
-      if (blk >> 6 != chunk) {
-        chunk = blk >> 6;
-        ids = ids_next;
-        if (s0 + 1024 * (chunk + 1) < s1) ids_next = fetch_ids(chunk + 1);
-      }
-      id0 = __builtin_amdgcn_readlane(ids, blk & 63);
-      if (kHalves == 2) id1 = __builtin_amdgcn_readlane(ids, (blk & 63) + 1);
-    };
-    auto entry = [&](int t0, int key) -> const char* {        // of the tile from key t0 on
-      if (!PAGED) return seq + static_cast<int64_t>(t0 + key) * kRowB;
-      return static_cast<const char*>(a.k) + (static_cast<int64_t>(key < 16 ? id0 : id1) * 16 + (key & 15)) * kRowB;
-    };
+    src.begin(b, s0, s1);
+    auto locate = [&](int it) { src.locate(it * NK + kg); };
     auto issue = [&](int it) {                      // (after locate of the same tile)
-      const int t0 = s0 + kKeys * (it * NK + kg);
-      if (t0 >= s1) return;
+      const int ti = it * NK + kg;
+      if (ti >= ntl) return;
       char* slot = ring + (it % S) * kSlot;
 #pragma unroll
-      for (int u = 0; u < kGroups; ++u) {
-        const int gr = rr * kGroups + u;
-        char* to = slot + gr * (kPP * 1024);
-        if (t0 + kKeys <= s1) {
-          const char* base = entry(t0, gr * kGroup);
-#pragma unroll
-          for (int p = 0; p < kPP; ++p) {
-            uint32_t off = lane_off[p];
-            asm volatile("" : "+v"(off));           // (an instruction here, not a register for every group and piece)
-            load_to_lds16(base, off ^ Tile<T>::flip(gr), to + p * 1024);
-          }
-        } else {
-          int ln = lane;                            // (worked out here, once per segment at most)
-          asm volatile("" : "+v"(ln));
-#pragma unroll 1
-          for (int p = 0; p < kPP; ++p) {
-            const int n = 64 * p + ln, row = n / kCPR, key = gr * kGroup + row;
-            load_to_lds16(entry(t0, min(key, s1 - 1 - t0)) + (((n - row * kCPR) ^ Tile<T>::swz(key)) << 4), to + p * 1024);     // keys past the range are masked below
-          }
-        }
-      }
+      for (int u = 0; u < kGroups; ++u) src.load_group(ti, rr * kGroups + u, slot);
     };
 
     f32x4_t oacc[kDT][RTW], lacc[RTW];
@@ -204,11 +234,7 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
       locate(it);
       issue(it);
     }
-    // operand addresses: a K read is chunk 4 ks + fq of key fr, a column read the chunks 2 dt, 2 dt + 1 of key 4 fq + fr / 4 (fp32: column 16 dt + fr of key 4 fq + e)
-    int k_at = fr * kRowB + ((fq ^ Tile<T>::swz(fr)) << 4);
-    const int vkey = kF32 ? 4 * fq : 4 * fq + (fr >> 2);
-    int v_at = kF32 ? vkey * kRowB + ((((fr >> 2) ^ Tile<T>::swz(vkey)) << 4) | ((fr & 3) << 2))
-                          : vkey * kRowB + (((((fr & 3) >> 1) ^ Tile<T>::swz(vkey)) << 4) | ((fr & 1) << 3));
+    int k_at = src.rows_at(fr, fq), v_at = src.columns_at(fr, fq);
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));       // from here on vmcnt counts tile loads only
     if constexpr (S > 2) {
 #pragma unroll 1
@@ -241,11 +267,7 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
 #pragma unroll
           for (int t = 0; t < RTW; ++t) sacc[j][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         constexpr int kReads = kHalves * kKS, kAhead = kF32 ? 4 : 8;
-        auto kread = [&](int i) {                   // read i: chunk quad i / kHalves, key half i % kHalves
-          const int ks = i / kHalves;
-          constexpr int kPer = kF32 ? 4 : 2;        // chunk quads that the swizzle mixes
-          return *reinterpret_cast<const uint4*>(tile + (k_at ^ ((ks % kPer) << 6)) + (ks / kPer) * (kPer << 6) + (i % kHalves) * 16 * kRowB);
-        };
+        auto kread = [&](int i) { return *reinterpret_cast<const uint4*>(src.row_read(tile, k_at, i / kHalves, i % kHalves)); };
         uint4 kf[kReads];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) kf[i] = kread(i);
@@ -332,12 +354,10 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
         // ---- O^T += C^T P^T
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (kF32) {
-          // (chunks 4 dt .. 4 dt + 3 of key 4 fq + e: the swizzle of the key mixes sixteen chunks, those of four column tiles)
           float vf[kDT][4];
           auto vread = [&](int dt) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              vf[dt][e] = *reinterpret_cast<const float*>(tile + ((v_at ^ (e << 4) ^ ((dt & 3) << 6)) + e * kRowB) + (dt >> 2) * 256);
+            for (int e = 0; e < 4; ++e) vf[dt][e] = *reinterpret_cast<const float*>(src.column_read(tile, v_at, dt, e));
           };
           constexpr int kVAhead = 2;
 #pragma unroll
@@ -353,9 +373,8 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
         } else {
           s16x4_t vlo[kDT], vhi[kDT];
           auto vread = [&](int dt) {
-            const char* p = tile + (v_at ^ ((dt & 3) << 5)) + (dt >> 2) * 128;
-            vlo[dt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(lds_ptr_t)p);
-            vhi[dt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(lds_ptr_t)(p + 16 * kRowB));
+            vlo[dt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(lds_ptr_t)src.column_read(tile, v_at, dt, 0));
+            vhi[dt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(lds_ptr_t)src.column_read(tile, v_at, dt, 1));
           };
           constexpr int kVAhead = 4;
 #pragma unroll
@@ -433,6 +452,274 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
         *reinterpret_cast<float4*>(a.part_o + (slot_row + r) * LD + 4 * c4) = v;
         if (c4 == 0) *reinterpret_cast<float2*>(a.part_ml + (slot_row + r) * 2) = make_float2(mm, sum);
       }
+    }
+  }
+}
+
+// bf16, more rows than one wave's sixteen a ring: four waves of RTW 16-row tiles on one ring of four slots, software-pipelined.  With one wave to a SIMD nothing else fills
+// the time of the softmax, so the products of tile t + 1 with the queries are interleaved with the exponentials of tile t, the products of tile t's probabilities with
+// the maxima of tile t + 1, and the loads of tile t + 3 with the former; one barrier a tile.
+//
+// The reference of a row's exponentials is the maximum of its first tile and stays: floating-point probabilities lose nothing by being large, so up to
+// 2^kReach is fine, and the accumulators are never rescaled (256 registers that only matrix instructions work on, there and back, take longer than a tile).  A
+// segment with a score beyond that is taken again with its rows' true maxima, which the first pass has found.
+template <int LD, int RTW, bool PAGED>
+__global__ __launch_bounds__(256, in_agprs(LD, 2, RTW) ? 1 : 2) void k_latent_pipe(const LatentAttnArgs a) {
+  typedef Source<bf16_t, LD, PAGED> Src;
+  constexpr int S = 4, kSlot = slot_bytes(LD, 2), kKeys = 32;
+  static_assert(stages_of(LD, 2, 1) == S, "four slots");
+  constexpr int kKS = Src::kRowB / 64, kReads = 2 * kKS, kDT = LD / 16, kBlocks = Src::kBlocks;
+  constexpr bool kSplitP = RTW == 1;                // probabilities: see k_latent_ring
+  constexpr float kReach = 60.f;                    // log2; sums of 2^31 such probabilities times values of 2^30 stay in range
+  // With 128 rows of 512 columns the accumulators are all 256 registers that matrix instructions alone work on, and the compiler has no form that puts
+  // other results elsewhere: the scores' instructions are written out.
+  constexpr bool kWritten = LD == 512 && RTW == 2;
+  extern __shared__ uint4 smem4[];
+  char* smem = reinterpret_cast<char*>(smem4);
+  int* sched_lds = reinterpret_cast<int*>(smem + S * kSlot);
+  int* votes = sched_lds + attn_sched_words(a.B);
+  const int lane = threadIdx.x & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 15, fq = lane >> 4;
+  const AttnTable table = attn_sched_build(a, sched_lds);
+  const AttnLine line = attn_sched_line(a, table);
+  if (static_cast<int>(blockIdx.x) >= line.W) return;         // the whole workgroup leaves together
+  const int x_hi = attn_sched_lo(line, blockIdx.x + 1);
+  Src src(a);
+  const float sl2 = a.scale * 1.44269504088896340736f;
+  bool again = false;
+  AttnSeg seg = attn_sched_next(a, table, true, line.pad, attn_sched_lo(line, blockIdx.x), x_hi);
+  if (seg.next < x_hi) attn_sched_keep(a, table);
+  for (; seg.s1 > seg.s0; seg = attn_sched_next(a, table, false, line.pad, seg.next, x_hi)) {
+    attn_sched_publish(a, seg);
+    const int b = seg.b, row0 = seg.g * a.block_rows;
+    const int R = min(a.block_rows, a.rows - row0);
+    const int L = __builtin_amdgcn_readfirstlane(seg.L);
+    const int s0 = seg.s0, s1 = __builtin_amdgcn_readfirstlane(seg.s1);
+    const int ntl = (s1 - s0 + kKeys - 1) / kKeys;
+    uint4 qf[kKS][RTW];
+    const char* q0 = static_cast<const char*>(a.q) + (static_cast<int64_t>(b) * a.rows + row0) * Src::kRowB;
+#pragma unroll
+    for (int t = 0; t < RTW; ++t) {
+      const uint32_t off = static_cast<uint32_t>(min(16 * (wv * RTW + t) + fr, R - 1) * Src::kRowB + fq * 16);      // (rows past the last repeat it and are not stored)
+#pragma unroll
+      for (int ks = 0; ks < kKS; ++ks) qf[ks][t] = *reinterpret_cast<const uint4*>(q0 + off + 64 * ks);
+    }
+    float known[RTW];                               // second pass: the rows' maxima
+#pragma unroll 1
+    for (int pass = 0;; ++pass) {
+    if (again) __syncthreads();                     // the ring is free of the segment before
+    again = true;
+    src.begin(b, s0, s1);
+    auto slot_of = [&](int ti) { return smem + (ti & (S - 1)) * kSlot; };
+    auto issue = [&](int ti) {
+      if (ti >= ntl) return;
+      src.locate(ti);
+      src.load_group(ti, wv, slot_of(ti));
+    };
+    // (a short segment has all its tiles in flight at once, behind the queries; of a longer one the wait for the queries is not one for three tiles)
+    const int together = ntl < S ? S - 1 : 1;
+#pragma unroll 1
+    for (int ti = 0; ti < together; ++ti) issue(ti);
+    int k_at = Src::rows_at(fr, fq), v_at = Src::columns_at(fr, fq);
+    f32x4_t oacc[kDT][RTW];
+    float ref[RTW], l_run[RTW], most[RTW];          // reference, sum of the probabilities, largest score (times sl2: the first two)
+#pragma unroll
+    for (int t = 0; t < RTW; ++t) {
+      l_run[t] = 0.f;
+      most[t] = -INFINITY;
+#pragma unroll
+      for (int dt = 0; dt < kDT; ++dt) oacc[dt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));       // from here on vmcnt counts tile loads only
+#pragma unroll 1
+    for (int ti = together; ti < S - 1; ++ti) issue(ti);
+
+    f32x4_t sc[2][RTW], sn[2][RTW];                 // scores of tile t, of tile t + 1: key half, row tile
+    auto score = [&](f32x4_t& c, const uint4& k, const uint4& q, bool first) {
+      const bf16x8_t x = __builtin_bit_cast(bf16x8_t, k), y = __builtin_bit_cast(bf16x8_t, q);
+      if constexpr (kWritten) {
+        if (first) asm("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=&v"(c) : "v"(x), "v"(y));
+        else asm("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(x), "v"(y));
+      } else {
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, first ? f32x4_t{0.f, 0.f, 0.f, 0.f} : c, 0, 0, 0);
+      }
+    };
+    // the scores are there (the compiler does not know how long the written instructions take: eight passes, 11 wait states to an ordinary read)
+    auto scored = [&] {
+      if constexpr (kWritten) asm volatile("s_nop 15" : "+v"(sn[0][0]), "+v"(sn[1][0]), "+v"(sn[0][RTW - 1]), "+v"(sn[1][RTW - 1]));
+    };
+    auto mask_tile = [&](int ti) {                  // keys past the range and block entries that a row does not see
+      const int t0 = s0 + kKeys * ti;
+      if (t0 + kKeys <= min(L, s1)) return;
+      int ln = lane;                                // (worked out here, once or twice a segment, not held)
+      asm volatile("" : "+v"(ln));
+#pragma unroll
+      for (int t = 0; t < RTW; ++t) {
+        const int i = (row0 + min(16 * (wv * RTW + t) + (ln & 15), R - 1)) / a.Hq;
+        const uint64_t word = a.mask ? a.mask[static_cast<int64_t>(b) * a.mask_stride + i] : ((2ull << i) - 1ull);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int p = t0 + 16 * j + 4 * (ln >> 4) + e;
+            bool seen = p < s1;
+            if (seen && p >= L) seen = (word >> (p - L)) & 1ull;
+            sn[j][t][e] = seen ? sn[j][t][e] : -INFINITY;
+          }
+      }
+    };
+    constexpr int kAhead = kWritten ? 4 : LD == 128 && RTW == 2 ? 6 : 8, kVAhead = 4;
+    uint4 kf[kReads];
+    auto kread = [&](const char* tile, int i) { kf[i] = *reinterpret_cast<const uint4*>(Src::row_read(tile, k_at, i / 2, i % 2)); };
+
+    // ---- the first tile's scores
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) kread(smem, i);
+#pragma unroll
+    for (int i = 0; i < kReads; ++i) {
+      if (i + kAhead < kReads) kread(smem, i + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = 0; t < RTW; ++t) score(sn[i % 2][t], kf[i], qf[i / 2][t], i < 2);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    scored();
+    mask_tile(0);
+#pragma unroll
+    for (int t = 0; t < RTW; ++t) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) most[t] = max_nan(most[t], sn[e >> 2][t][e & 3]);
+      ref[t] = pass ? known[t] : fmaxf(-FLT_MAX, quad_row_max(most[t] * sl2));
+    }
+
+#pragma unroll 1
+    for (int ti = 0; ti < ntl; ++ti) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int t = 0; t < RTW; ++t) sc[j][t] = sn[j][t];
+      // tile ti + 1 has landed once at most this wave's blocks of tile ti + 2 are outstanding
+      if (ti + 2 < ntl) __builtin_amdgcn_s_waitcnt(vmcnt_imm(kBlocks));
+      else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_s_waitcnt(0xC07F);           // lgkmcnt(0): tile ti - 1 is read
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      const char* tile = slot_of(ti);
+      const char* next = slot_of(ti + 1);
+      asm volatile("" : "+v"(k_at), "+v"(v_at));    // (worked out per read from these two, not held)
+      uint4 pf[RTW], pl[RTW];
+      float pr[2];
+      auto weigh = [&](int n) {                     // exponential n of tile ti: row tile n / 8, key half n / 4 % 2
+        const int t = n / 8, e = n % 8;
+        pr[e & 1] = __builtin_amdgcn_exp2f(fmaf(sc[e >> 2][t][e & 3], sl2, -ref[t]));
+        if (!(e & 1)) return;
+        const uint32_t word = pack_bf16x2(pr[0], pr[1]);
+        const float x = __uint_as_float(word << 16), y = __uint_as_float(word & 0xFFFF0000u);
+        uint32_t* to = reinterpret_cast<uint32_t*>(&pf[t]);
+        to[e >> 1] = word;
+        if constexpr (kSplitP) {
+          reinterpret_cast<uint32_t*>(&pl[t])[e >> 1] = pack_bf16x2(pr[0] - x, pr[1] - y);
+          l_run[t] += pr[0] + pr[1];
+        } else {
+          l_run[t] += x + y;                        // the probabilities as the values are multiplied with them
+        }
+      };
+      s16x4_t vlo[kDT], vhi[kDT];
+      auto vread = [&](int dt) {
+        vlo[dt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(lds_ptr_t)Src::column_read(tile, v_at, dt, 0));
+        vhi[dt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(lds_ptr_t)Src::column_read(tile, v_at, dt, 1));
+      };
+      const bool more = ti + 1 < ntl;
+      if (more) {
+        // ---- scores of tile ti + 1, exponentials of tile ti, loads of tile ti + 3
+        const int tl = ti + S - 1;
+        const char* base = nullptr;
+        char* to = slot_of(tl);
+        if (tl < ntl) {
+          src.locate(tl);
+          if (src.whole(tl)) base = src.entry(tl, wv * Src::kGroup);
+          else src.load_group(tl, wv, to);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) kread(next, i);
+        constexpr int kEach = (8 * RTW + kReads - 1) / kReads;
+#pragma unroll
+        for (int i = 0; i < kReads; ++i) {
+          if (i + kAhead < kReads) kread(next, i + kAhead);
+          if (i >= kReads - kVAhead) vread(i - (kReads - kVAhead));
+          if (i % 4 == 0 && base) src.load(base, wv, i / 4, to);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int t = 0; t < RTW; ++t) score(sn[i % 2][t], kf[i], qf[i / 2][t], i < 2);
+#pragma unroll
+          for (int n = i * kEach; n < (i + 1) * kEach; ++n)
+            if (n < 8 * RTW) weigh(n);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        scored();
+        mask_tile(ti + 1);
+      } else {
+#pragma unroll
+        for (int dt = 0; dt < kVAhead; ++dt) vread(dt);
+#pragma unroll
+        for (int n = 0; n < 8 * RTW; ++n) weigh(n);
+      }
+      // ---- O^T += C^T P^T of tile ti, maxima of tile ti + 1
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int dt = 0; dt < kDT; ++dt) {
+        if (dt + kVAhead < kDT) vread(dt + kVAhead);
+        __builtin_amdgcn_sched_barrier(0);
+        const uint2 l2 = __builtin_bit_cast(uint2, vlo[dt]), h2 = __builtin_bit_cast(uint2, vhi[dt]);
+        const bf16x8_t va = __builtin_bit_cast(bf16x8_t, make_uint4(l2.x, l2.y, h2.x, h2.y));
+#pragma unroll
+        for (int t = 0; t < RTW; ++t) {
+          oacc[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8_t, pf[t]), oacc[dt][t], 0, 0, 0);
+          if constexpr (kSplitP) oacc[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8_t, pl[t]), oacc[dt][t], 0, 0, 0);
+        }
+        constexpr int kEach = (8 * RTW + kDT - 1) / kDT;
+#pragma unroll
+        for (int n = dt * kEach; n < (dt + 1) * kEach; ++n)
+          if (n < 8 * RTW) most[n / 8] = max_nan(most[n / 8], sn[n % 8 >> 2][n / 8][n & 3]);      // (of the last tile's again, behind it)
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    // (a maximum that is not a number counts as one out of reach: its row is worked out again by the merging kernel)
+    bool far = false;
+#pragma unroll
+    for (int t = 0; t < RTW; ++t) {
+      const float top = most[t] * sl2;
+      known[t] = top != top ? top : fmaxf(-FLT_MAX, quad_row_max(top));
+      far = far || !(known[t] - ref[t] <= kReach);
+    }
+    if (pass == 0) {                                // (static LDS, which the workgroup vote takes, has no room beside the slots)
+      const bool mine = __builtin_amdgcn_ballot_w64(far) != 0ull;
+      if (lane == 0) votes[wv] = mine;
+      __syncthreads();
+      if (votes[0] | votes[1] | votes[2] | votes[3]) continue;
+    }
+
+    // ---- the segment's partial result
+    const int64_t slot_row = (static_cast<int64_t>(blockIdx.x) + static_cast<int64_t>(b) * a.Hkv + seg.g) * a.block_rows;
+    int ln = lane;                                  // (as above)
+    asm volatile("" : "+v"(ln));
+#pragma unroll
+    for (int t = 0; t < RTW; ++t) {
+      const int rho = 16 * (wv * RTW + t) + (ln & 15), fq = ln >> 4;
+      const float l = quad_row_sum(l_run[t]);
+      if (rho >= R) continue;
+      if (fq == 0) *reinterpret_cast<float2*>(a.part_ml + (slot_row + rho) * 2) = make_float2(ref[t], l);
+      float* dst = a.part_o + (slot_row + rho) * LD + 4 * fq;
+#pragma unroll
+      for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = oacc[dt][t];
+    }
+    break;
     }
   }
 }
@@ -594,12 +881,28 @@ hipError_t launch_ring(const LatentAttnArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int LD, int RTW>
+hipError_t launch_pipe(const LatentAttnArgs& a, hipStream_t s) {
+  const size_t lds = static_cast<size_t>(4) * slot_bytes(LD, 2) + static_cast<size_t>(attn_sched_words(a.B) + 4) * 4;
+  if (a.paged) {
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_latent_pipe<LD, RTW, true>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    if (attr != hipSuccess) return attr;
+    hipLaunchKernelGGL((k_latent_pipe<LD, RTW, true>), dim3(a.wgrid), dim3(256), lds, s, a);
+  } else {
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_latent_pipe<LD, RTW, false>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    if (attr != hipSuccess) return attr;
+    hipLaunchKernelGGL((k_latent_pipe<LD, RTW, false>), dim3(a.wgrid), dim3(256), lds, s, a);
+  }
+  return hipGetLastError();
+}
+
 template <typename T, int LD>
 hipError_t launch_ld(const LatentAttnArgs& a, hipStream_t s) {
   hipError_t e;
   if (a.block_rows <= 16) e = launch_ring<T, LD, 1, 1>(a, s);
   else if (a.block_rows <= 32) e = launch_ring<T, LD, 1, 2>(a, s);
-  else e = launch_ring<T, LD, 1, 4>(a, s);
+  else if constexpr (sizeof(T) == 4) e = launch_ring<T, LD, 1, 4>(a, s);
+  else e = a.block_rows <= 64 ? launch_pipe<LD, 1>(a, s) : launch_pipe<LD, 2>(a, s);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((k_latent_combine<T, LD>), dim3(a.rows, a.B), dim3(256), 0, s, a);
   return hipGetLastError();
@@ -618,7 +921,10 @@ hipError_t launch_as(const LatentAttnArgs& a, hipStream_t s) {
 }  // namespace
 
 bool latent_attn_plan(LatentAttnArgs& a, int num_cus) {
-  const int most = 64;
+#ifndef LAT_MOST
+#define LAT_MOST 128
+#endif
+  const int most = a.dtype == 1 ? LAT_MOST : LAT_MOST < 64 ? LAT_MOST : 64;
   a.rows = a.Hq * a.n_q;
   a.Hkv = (a.rows + most - 1) / most;
   a.block_rows = ((a.rows + a.Hkv - 1) / a.Hkv + 15) & ~15;
