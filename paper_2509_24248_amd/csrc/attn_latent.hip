@@ -22,6 +22,7 @@
 
 #include <float.h>
 #include <limits.h>
+#include <algorithm>
 
 namespace sx {
 
@@ -36,12 +37,14 @@ __device__ __forceinline__ float max_nan(float a, float b) { return __builtin_el
 
 template <typename T> struct Tile;
 // A tile lies in LDS in groups of 8 keys (fp32: 4), a group in 1 KB blocks of 128 bytes (256) of each of them: what one load instruction brings in, lane l the 16-byte chunk
-// l % 8 (16) of key l / 8 (16), so that a lane's source is one offset for all blocks.  The chunks of a key's part are swizzled: the permuted bits of the key keep apart the
-// sixteen keys of a K read (one chunk each) as well as the eight keys of a transpose read (an even chunk and the next).
+// l % 8 (16) of key l / 8 (16), so that a lane's source is one offset for all blocks.  The chunks of a key's part are swizzled.  A row read takes a chunk of sixteen keys, four lanes' worth of
+// chunks at a time, and the LDS serves the lanes 0-3, 12-15, 20-27 of each 32 together, then the others: keys 0-3 and 12-15 of one chunk with 4-11 of its neighbour.  A transpose read takes an
+// even chunk and the next of eight keys.  With 2 (key / 2 % 4) + key / 4 % 2 neither has two lanes on a bank; with key / 8 for the last bit, which serves the transpose read alone, row reads took
+// twice their time and 35 % of all LDS cycles were conflicts.
 template <> struct Tile<bf16_t> {
   static constexpr int kKeys = 32, kGroup = 8, kPart = 128;
-  __host__ __device__ static constexpr int swz(int key) { return ((key >> 1 & 3) << 1) | (key >> 3 & 1); }
-  __host__ __device__ static constexpr int flip(int group) { return (group & 1) << 4; }       // of a lane's source, from group to group
+  __host__ __device__ static constexpr int swz(int key) { return ((key >> 1 & 3) << 1) | (key >> 2 & 1); }
+  __host__ __device__ static constexpr int flip(int) { return 0; }                            // of a lane's source, from group to group
 };
 template <> struct Tile<float> {
   static constexpr int kKeys = 16, kGroup = 4, kPart = 256;
@@ -65,11 +68,12 @@ struct Source {
   static constexpr int kLanes = kPart / 16;                                                          // lanes of a key
   const LatentAttnArgs& a;
   int b, s0, s1;
-  uint32_t lane_off;           // of a lane's chunk behind the first key of its group
+  int lane_key, lane_chunk;    // what a lane brings in of a group: key, and byte of its part
   int ids, ids_next, chunk, id0, id1;
   __device__ __forceinline__ Source(const LatentAttnArgs& args) : a(args) {
-    const int lane = threadIdx.x & 63, key = lane / kLanes;
-    lane_off = static_cast<uint32_t>(key * kRowB + (((lane % kLanes) ^ Tile<T>::swz(key)) << 4));
+    const int lane = threadIdx.x & 63;
+    lane_key = lane / kLanes;
+    lane_chunk = ((lane % kLanes) ^ Tile<T>::swz(lane_key)) << 4;
   }
   __device__ __forceinline__ int fetch(int c) const {
     int lane = threadIdx.x & 63;
@@ -87,12 +91,11 @@ struct Source {
       if (s1 - s0 > 1024) ids_next = fetch(1);
     }
   }
-  // Tile ti of the segment, in front of its entries or blocks.  (Calls go up by less than 1024 keys.)
+  // Tile ti of the segment, one that has keys, in front of its entries or blocks.  (Calls go up by less than 1024 keys.)
   __device__ __forceinline__ void locate(int ti) {
-    const int t0 = kKeys * ti;
-    if (!PAGED || s0 + t0 >= s1) return;
-    const int blk = t0 >> 4;
-    if (blk >> 6 != chunk) {
+    if (!PAGED) return;
+    const int blk = kKeys * ti >> 4;
+    if (__builtin_expect(blk >> 6 != chunk, 0)) {
       chunk = blk >> 6;
       ids = ids_next;
       if (s0 + 1024 * (chunk + 1) < s1) ids_next = fetch(chunk + 1);
@@ -104,25 +107,24 @@ struct Source {
     if (!PAGED) return static_cast<const char*>(a.k) + (static_cast<int64_t>(b) * a.l_max + s0 + kKeys * ti + key) * kRowB;
     return static_cast<const char*>(a.k) + (static_cast<int64_t>(key < 16 ? id0 : id1) * 16 + (key & 15)) * kRowB;
   }
-  __device__ __forceinline__ bool whole(int ti) const { return s0 + kKeys * (ti + 1) <= s1; }
-  // Block `block` of a group of a whole tile whose first key lies at `base`.
-  __device__ __forceinline__ void load(const char* base, int group, int block, const char* slot) const {
-    load_to_lds16(base + block * kPart, lane_off ^ Tile<T>::flip(group), slot + (group * kBlocks + block) * 1024);
+  // A group of a tile with keys (after locate): a base and a lane's offset.  Keys past the range repeat the group's last one, a group without any the tile's first: they are masked later.
+  // (No branch: between matrix instructions one costs 30 cycles.)
+  struct Group {
+    const char* base;
+    uint32_t off;
+  };
+  __device__ __forceinline__ Group group_of(int ti, int group) const {
+    const int last = s1 - 1 - s0 - kKeys * ti;
+    const int first = group * kGroup <= last ? group * kGroup : 0;
+    return {entry(ti, first), static_cast<uint32_t>(min(lane_key, last - first) * kRowB + (lane_chunk ^ Tile<T>::flip(group)))};
   }
-  // A group of any tile; keys past the range repeat the last one and are masked later.
+  __device__ __forceinline__ static void load(const Group& g, int group, int block, const char* slot) {
+    load_to_lds16(g.base + block * kPart, g.off, slot + (group * kBlocks + block) * 1024);
+  }
   __device__ __forceinline__ void load_group(int ti, int group, const char* slot) const {
-    if (whole(ti)) {
-      const char* base = entry(ti, group * kGroup);
+    const Group g = group_of(ti, group);
 #pragma unroll
-      for (int block = 0; block < kBlocks; ++block) load(base, group, block, slot);
-    } else {
-      int lane = threadIdx.x & 63;
-      asm volatile("" : "+v"(lane));
-      const int key = group * kGroup + lane / kLanes;
-      const char* at = entry(ti, min(key, s1 - 1 - s0 - kKeys * ti)) + (((lane % kLanes) ^ Tile<T>::swz(key)) << 4);
-#pragma unroll 1
-      for (int block = 0; block < kBlocks; ++block) load_to_lds16(at + block * kPart, slot + (group * kBlocks + block) * 1024);
-    }
+    for (int block = 0; block < kBlocks; ++block) load(g, group, block, slot);
   }
   // Operand addresses in a tile.  rows: chunk quad ks of key fr (+ 16 half).  columns: the transpose read of chunks 2 dt, 2 dt + 1 of key 4 fq + fr / 4 (+ 16 half); fp32: value
   // 16 dt + fr of key 4 fq + e.
@@ -189,6 +191,7 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
     const int nit = (ntl + NK - 1) / NK;
     char* ring = smem + kg * (S * kSlot);
 
+    src.begin(b, s0, s1);                           // (the page ids in front of the queries: the first tile waits for them)
     // ---- the rows' queries and mask words (rows past the last repeat it and are not stored)
     uint4 qf[kKS][RTW];
     uint64_t rowmask[RTW];
@@ -206,8 +209,9 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
     if (again) __syncthreads();                     // the rings are free of the segment before
     again = true;
 
-    src.begin(b, s0, s1);
-    auto locate = [&](int it) { src.locate(it * NK + kg); };
+    auto locate = [&](int it) {
+      if (it * NK + kg < ntl) src.locate(it * NK + kg);
+    };
     auto issue = [&](int it) {                      // (after locate of the same tile)
       const int ti = it * NK + kg;
       if (ti >= ntl) return;
@@ -405,60 +409,61 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
     }
 
     // ---- the segment's partial result
-    const int64_t slot_row = (static_cast<int64_t>(blockIdx.x) + static_cast<int64_t>(b) * a.Hkv + seg.g) * a.block_rows;
+    const int64_t slot = static_cast<int64_t>(blockIdx.x) + static_cast<int64_t>(b) * a.Hkv + seg.g;
+    const int tiles = a.block_rows / 16;            // row tiles of a block
     if constexpr (NK == 1) {
 #pragma unroll
       for (int t = 0; t < RTW; ++t) {
         const float l = kF32 || kSplitP ? quad_row_sum(l_run[t]) : lacc[t][0];
-        if (rho[t] >= R) continue;
-        if (fq == 0) *reinterpret_cast<float2*>(a.part_ml + (slot_row + rho[t]) * 2) = make_float2(m_run[t], l);
-        float* dst = a.part_o + (slot_row + rho[t]) * LD + 4 * fq;
+        const int tile = rr * RTW + t;
+        if (tile >= tiles) continue;
+        if (fq == 0) *reinterpret_cast<float2*>(a.part_ml + ((slot * tiles + tile) * 16 + fr) * 2) = make_float2(m_run[t], l);
+        float* dst = a.part_o + ((slot * tiles + tile) * kDT * 64 + lane) * 4;
 #pragma unroll
-        for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = oacc[dt][t];
+        for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + dt * 256) = oacc[dt][t];
       }
     } else {
-      // the rings leave their sums in their own slots, the 16-byte pieces of a row swizzled, and every wave adds some rows in the order of the rings
+      // the rings leave their sums in their own slots, and every wave adds some fragments in the order of the rings
       static_assert(RTW == 1 && NR * 16 * LD * 4 <= S * kSlot, "a ring's slots hold its sums");
-      constexpr int C4 = LD / 4, kStep = C4 < 64 ? C4 : 64;
       const float l = quad_row_sum(l_run[0]);
       if constexpr (NR > 1) __syncthreads();        // (waves of a ring write where others may still read)
-      if (fq == 0) *reinterpret_cast<float2*>(ml_lds + 2 * (kg * NR * 16 + rho[0])) = make_float2(m_run[0], l);
+      if (fq == 0) *reinterpret_cast<float2*>(ml_lds + 2 * ((kg * NR + rr) * 16 + fr)) = make_float2(m_run[0], l);
 #pragma unroll
-      for (int dt = 0; dt < kDT; ++dt)
-        *reinterpret_cast<f32x4_t*>(ring + rho[0] * (4 * LD) + (((4 * dt + fq) ^ fr) << 4)) = oacc[dt][0];
+      for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(ring + ((rr * kDT + dt) * 64 + lane) * 16) = oacc[dt][0];
       __syncthreads();
 #pragma unroll 1
-      for (int x = wv * (64 / kStep) + lane / kStep; x < R * (C4 / kStep); x += 4 * (64 / kStep)) {
-        const int r = x / (C4 / kStep), c4 = x % (C4 / kStep) * kStep + lane % kStep;
-        float2 ml[NK];
-        float4 o[NK];
+      for (int tile = 0; tile < tiles; ++tile) {
+        float f[NK], mm = -FLT_MAX, sum = 0.f;
 #pragma unroll
         for (int k = 0; k < NK; ++k) {
-          ml[k] = *reinterpret_cast<const float2*>(ml_lds + 2 * (k * NR * 16 + r));
-          o[k] = *reinterpret_cast<const float4*>(smem + k * (S * kSlot) + r * (4 * LD) + ((c4 ^ (r & 15)) << 4));
+          f[k] = ml_lds[2 * ((k * NR + tile) * 16 + fr)];
+          mm = fmaxf(mm, f[k]);
         }
-        float mm = ml[0].x;
-#pragma unroll
-        for (int k = 1; k < NK; ++k) mm = fmaxf(mm, ml[k].x);
-        float sum = 0.f;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int k = 0; k < NK; ++k) {
-          const float f = __builtin_amdgcn_exp2f(ml[k].x - mm);
-          sum = fmaf(f, ml[k].y, sum);
-          v.x = fmaf(f, o[k].x, v.x); v.y = fmaf(f, o[k].y, v.y);
-          v.z = fmaf(f, o[k].z, v.z); v.w = fmaf(f, o[k].w, v.w);
+          f[k] = __builtin_amdgcn_exp2f(f[k] - mm);
+          sum = fmaf(f[k], ml_lds[2 * ((k * NR + tile) * 16 + fr) + 1], sum);
         }
-        *reinterpret_cast<float4*>(a.part_o + (slot_row + r) * LD + 4 * c4) = v;
-        if (c4 == 0) *reinterpret_cast<float2*>(a.part_ml + (slot_row + r) * 2) = make_float2(mm, sum);
+        if (wv == 0 && fq == 0) *reinterpret_cast<float2*>(a.part_ml + ((slot * tiles + tile) * 16 + fr) * 2) = make_float2(mm, sum);
+#pragma unroll 2
+        for (int dt = wv; dt < kDT; dt += 4) {
+          f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < NK; ++k) {
+            const f32x4_t o = *reinterpret_cast<const f32x4_t*>(smem + k * (S * kSlot) + ((tile * kDT + dt) * 64 + lane) * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = fmaf(f[k], o[e], v[e]);
+          }
+          *reinterpret_cast<f32x4_t*>(a.part_o + (((slot * tiles + tile) * kDT + dt) * 64 + lane) * 4) = v;
+        }
       }
     }
   }
 }
 
 // bf16, more rows than one wave's sixteen a ring: four waves of RTW 16-row tiles on one ring of four slots, software-pipelined.  With one wave to a SIMD nothing else fills
-// the time of the softmax, so the products of tile t + 1 with the queries are interleaved with the exponentials of tile t, the products of tile t's probabilities with
-// the maxima of tile t + 1, and the loads of tile t + 3 with the former; one barrier a tile.
+// the time of the softmax, so the products of tile t's probabilities with its values are interleaved with the exponentials of tile t + 1, and the loads of tile t + 3
+// with the products of tile t + 1 with the queries in front of that; one barrier a tile.
 //
 // The reference of a row's exponentials is the maximum of its first tile and stays: floating-point probabilities lose nothing by being large, so up to
 // 2^kReach is fine, and the accumulators are never rescaled (256 registers that only matrix instructions work on, there and back, take longer than a tile).  A
@@ -497,6 +502,7 @@ __global__ __launch_bounds__(256, in_agprs(LD, 2, RTW) ? 1 : 2) void k_latent_pi
     const int L = __builtin_amdgcn_readfirstlane(seg.L);
     const int s0 = seg.s0, s1 = __builtin_amdgcn_readfirstlane(seg.s1);
     const int ntl = (s1 - s0 + kKeys - 1) / kKeys;
+    src.begin(b, s0, s1);                           // (the page ids in front of the queries: the first tile waits for them)
     uint4 qf[kKS][RTW];
     const char* q0 = static_cast<const char*>(a.q) + (static_cast<int64_t>(b) * a.rows + row0) * Src::kRowB;
 #pragma unroll
@@ -510,17 +516,15 @@ __global__ __launch_bounds__(256, in_agprs(LD, 2, RTW) ? 1 : 2) void k_latent_pi
     for (int pass = 0;; ++pass) {
     if (again) __syncthreads();                     // the ring is free of the segment before
     again = true;
-    src.begin(b, s0, s1);
+    if (pass) src.begin(b, s0, s1);
     auto slot_of = [&](int ti) { return smem + (ti & (S - 1)) * kSlot; };
+    // Every step asks for a tile, behind the last one for that again: the count of what is outstanding is then always the same.
     auto issue = [&](int ti) {
-      if (ti >= ntl) return;
-      src.locate(ti);
-      src.load_group(ti, wv, slot_of(ti));
+      const int t = min(ti, ntl - 1);
+      src.locate(t);
+      src.load_group(t, wv, slot_of(ti));
     };
-    // (a short segment has all its tiles in flight at once, behind the queries; of a longer one the wait for the queries is not one for three tiles)
-    const int together = ntl < S ? S - 1 : 1;
-#pragma unroll 1
-    for (int ti = 0; ti < together; ++ti) issue(ti);
+    issue(0);
     int k_at = Src::rows_at(fr, fq), v_at = Src::columns_at(fr, fq);
     f32x4_t oacc[kDT][RTW];
     float ref[RTW], l_run[RTW], most[RTW];          // reference, sum of the probabilities, largest score (times sl2: the first two)
@@ -531,11 +535,11 @@ __global__ __launch_bounds__(256, in_agprs(LD, 2, RTW) ? 1 : 2) void k_latent_pi
 #pragma unroll
       for (int dt = 0; dt < kDT; ++dt) oacc[dt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));       // from here on vmcnt counts tile loads only
-#pragma unroll 1
-    for (int ti = together; ti < S - 1; ++ti) issue(ti);
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));       // (the queries and the first tile) from here on vmcnt counts tile loads only
+    issue(1);
+    issue(2);
 
-    f32x4_t sc[2][RTW], sn[2][RTW];                 // scores of tile t, of tile t + 1: key half, row tile
+    f32x4_t sn[2][RTW];                             // scores of the next tile: key half, row tile
     auto score = [&](f32x4_t& c, const uint4& k, const uint4& q, bool first) {
       const bf16x8_t x = __builtin_bit_cast(bf16x8_t, k), y = __builtin_bit_cast(bf16x8_t, q);
       if constexpr (kWritten) {
@@ -551,7 +555,7 @@ __global__ __launch_bounds__(256, in_agprs(LD, 2, RTW) ? 1 : 2) void k_latent_pi
     };
     auto mask_tile = [&](int ti) {                  // keys past the range and block entries that a row does not see
       const int t0 = s0 + kKeys * ti;
-      if (t0 + kKeys <= min(L, s1)) return;
+      if (__builtin_expect(t0 + kKeys <= min(L, s1), 1)) return;
       int ln = lane;                                // (worked out here, once or twice a segment, not held)
       asm volatile("" : "+v"(ln));
 #pragma unroll
@@ -569,10 +573,28 @@ __global__ __launch_bounds__(256, in_agprs(LD, 2, RTW) ? 1 : 2) void k_latent_pi
           }
       }
     };
-    constexpr int kAhead = kWritten ? 4 : LD == 128 && RTW == 2 ? 6 : 8, kVAhead = 4;
+    constexpr int kAhead = 8, kVAhead = 4;
     uint4 kf[kReads];
     auto kread = [&](const char* tile, int i) { kf[i] = *reinterpret_cast<const uint4*>(Src::row_read(tile, k_at, i / 2, i % 2)); };
 
+    uint32_t pw[RTW][4], pn[RTW][4], rw[RTW][4], rn[RTW][4];          // probabilities of a tile and of the next, two to a word; what they are rounded by
+    float pr[2];
+    auto weigh = [&](int n, uint32_t (&p)[RTW][4], uint32_t (&rest)[RTW][4]) {      // exponential n: row tile n / 8, key half n / 4 % 2
+      const int t = n / 8, e = n % 8;
+      const float x = sn[e >> 2][t][e & 3];
+      most[t] = max_nan(most[t], x);
+      pr[e & 1] = __builtin_amdgcn_exp2f(fmaf(x, sl2, -ref[t]));
+      if (!(e & 1)) return;
+      const uint32_t word = pack_bf16x2(pr[0], pr[1]);
+      const float lo = __uint_as_float(word << 16), hi = __uint_as_float(word & 0xFFFF0000u);
+      p[t][e >> 1] = word;
+      if constexpr (kSplitP) {
+        rest[t][e >> 1] = pack_bf16x2(pr[0] - lo, pr[1] - hi);
+        l_run[t] += pr[0] + pr[1];
+      } else {
+        l_run[t] += lo + hi;                        // the probabilities as the values are multiplied with them
+      }
+    };
     // ---- the first tile's scores
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_s_waitcnt(0xC07F);
@@ -592,20 +614,21 @@ __global__ __launch_bounds__(256, in_agprs(LD, 2, RTW) ? 1 : 2) void k_latent_pi
     mask_tile(0);
 #pragma unroll
     for (int t = 0; t < RTW; ++t) {
+      float mt = sn[0][t][0];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) most[t] = max_nan(most[t], sn[e >> 2][t][e & 3]);
-      ref[t] = pass ? known[t] : fmaxf(-FLT_MAX, quad_row_max(most[t] * sl2));
+      for (int e = 1; e < 8; ++e) mt = max_nan(mt, sn[e >> 2][t][e & 3]);
+      ref[t] = pass ? known[t] : fmaxf(-FLT_MAX, quad_row_max(mt * sl2));
     }
+#pragma unroll
+    for (int n = 0; n < 8 * RTW; ++n) weigh(n, pw, rw);
 
 #pragma unroll 1
-    for (int ti = 0; ti < ntl; ++ti) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int t = 0; t < RTW; ++t) sc[j][t] = sn[j][t];
-      // tile ti + 1 has landed once at most this wave's blocks of tile ti + 2 are outstanding
-      if (ti + 2 < ntl) __builtin_amdgcn_s_waitcnt(vmcnt_imm(kBlocks));
-      else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    for (int ti = 0;; ++ti) {
+      const int tl = min(ti + S - 1, ntl - 1);
+      src.locate(tl);
+      const typename Src::Group group = src.group_of(tl, wv);
+      char* to = slot_of(ti + S - 1);
+      __builtin_amdgcn_s_waitcnt(vmcnt_imm(kBlocks));         // tile ti + 1 has landed: at most this wave's blocks of tile ti + 2 are outstanding
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_s_waitcnt(0xC07F);           // lgkmcnt(0): tile ti - 1 is read
       __builtin_amdgcn_s_barrier();
@@ -613,64 +636,28 @@ __global__ __launch_bounds__(256, in_agprs(LD, 2, RTW) ? 1 : 2) void k_latent_pi
       const char* tile = slot_of(ti);
       const char* next = slot_of(ti + 1);
       asm volatile("" : "+v"(k_at), "+v"(v_at));    // (worked out per read from these two, not held)
-      uint4 pf[RTW], pl[RTW];
-      float pr[2];
-      auto weigh = [&](int n) {                     // exponential n of tile ti: row tile n / 8, key half n / 4 % 2
-        const int t = n / 8, e = n % 8;
-        pr[e & 1] = __builtin_amdgcn_exp2f(fmaf(sc[e >> 2][t][e & 3], sl2, -ref[t]));
-        if (!(e & 1)) return;
-        const uint32_t word = pack_bf16x2(pr[0], pr[1]);
-        const float x = __uint_as_float(word << 16), y = __uint_as_float(word & 0xFFFF0000u);
-        uint32_t* to = reinterpret_cast<uint32_t*>(&pf[t]);
-        to[e >> 1] = word;
-        if constexpr (kSplitP) {
-          reinterpret_cast<uint32_t*>(&pl[t])[e >> 1] = pack_bf16x2(pr[0] - x, pr[1] - y);
-          l_run[t] += pr[0] + pr[1];
-        } else {
-          l_run[t] += x + y;                        // the probabilities as the values are multiplied with them
-        }
-      };
       s16x4_t vlo[kDT], vhi[kDT];
       auto vread = [&](int dt) {
         vlo[dt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(lds_ptr_t)Src::column_read(tile, v_at, dt, 0));
         vhi[dt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(lds_ptr_t)Src::column_read(tile, v_at, dt, 1));
       };
-      const bool more = ti + 1 < ntl;
-      if (more) {
-        // ---- scores of tile ti + 1, exponentials of tile ti, loads of tile ti + 3
-        const int tl = ti + S - 1;
-        const char* base = nullptr;
-        char* to = slot_of(tl);
-        if (tl < ntl) {
-          src.locate(tl);
-          if (src.whole(tl)) base = src.entry(tl, wv * Src::kGroup);
-          else src.load_group(tl, wv, to);
-        }
+      // ---- scores of tile ti + 1, loads of tile ti + 3.  (Behind the last tile: of what lies in the slot, all of it masked; a copy of the code without would be one
+      // of the products below as well, and the accumulators of two do not stay in place.)
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) kread(next, i);
-        constexpr int kEach = (8 * RTW + kReads - 1) / kReads;
+      for (int i = 0; i < kAhead; ++i) kread(next, i);
 #pragma unroll
-        for (int i = 0; i < kReads; ++i) {
-          if (i + kAhead < kReads) kread(next, i + kAhead);
-          if (i >= kReads - kVAhead) vread(i - (kReads - kVAhead));
-          if (i % 4 == 0 && base) src.load(base, wv, i / 4, to);
-          __builtin_amdgcn_sched_barrier(0);
+      for (int i = 0; i < kReads; ++i) {
+        if (i + kAhead < kReads) kread(next, i + kAhead);
+        if (i >= kReads - kVAhead) vread(i - (kReads - kVAhead));
+        if (i % 4 == 0) Src::load(group, wv, i / 4, to);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int t = 0; t < RTW; ++t) score(sn[i % 2][t], kf[i], qf[i / 2][t], i < 2);
-#pragma unroll
-          for (int n = i * kEach; n < (i + 1) * kEach; ++n)
-            if (n < 8 * RTW) weigh(n);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        scored();
-        mask_tile(ti + 1);
-      } else {
-#pragma unroll
-        for (int dt = 0; dt < kVAhead; ++dt) vread(dt);
-#pragma unroll
-        for (int n = 0; n < 8 * RTW; ++n) weigh(n);
+        for (int t = 0; t < RTW; ++t) score(sn[i % 2][t], kf[i], qf[i / 2][t], i < 2);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      // ---- O^T += C^T P^T of tile ti, maxima of tile ti + 1
+      scored();
+      mask_tile(ti + 1);
+      // ---- O^T += C^T P^T of tile ti, exponentials of tile ti + 1
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int dt = 0; dt < kDT; ++dt) {
@@ -680,16 +667,29 @@ __global__ __launch_bounds__(256, in_agprs(LD, 2, RTW) ? 1 : 2) void k_latent_pi
         const bf16x8_t va = __builtin_bit_cast(bf16x8_t, make_uint4(l2.x, l2.y, h2.x, h2.y));
 #pragma unroll
         for (int t = 0; t < RTW; ++t) {
-          oacc[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8_t, pf[t]), oacc[dt][t], 0, 0, 0);
-          if constexpr (kSplitP) oacc[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8_t, pl[t]), oacc[dt][t], 0, 0, 0);
+          const bf16x8_t p = __builtin_bit_cast(bf16x8_t, make_uint4(pw[t][0], pw[t][1], pw[t][2], pw[t][3]));
+          oacc[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, p, oacc[dt][t], 0, 0, 0);
+          if constexpr (kSplitP) {
+            const bf16x8_t r = __builtin_bit_cast(bf16x8_t, make_uint4(rw[t][0], rw[t][1], rw[t][2], rw[t][3]));
+            oacc[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, r, oacc[dt][t], 0, 0, 0);
+          }
         }
         constexpr int kEach = (8 * RTW + kDT - 1) / kDT;
 #pragma unroll
         for (int n = dt * kEach; n < (dt + 1) * kEach; ++n)
-          if (n < 8 * RTW) most[n / 8] = max_nan(most[n / 8], sn[n % 8 >> 2][n / 8][n & 3]);      // (of the last tile's again, behind it)
+          if (n < 8 * RTW) weigh(n, pn, rn);
         __builtin_amdgcn_sched_barrier(0);
       }
+#pragma unroll
+      for (int t = 0; t < RTW; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          pw[t][e] = pn[t][e];
+          if constexpr (kSplitP) rw[t][e] = rn[t][e];
+        }
+      if (ti + 1 >= ntl) break;
     }
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));       // (nothing is on its way to the ring any more)
     // (a maximum that is not a number counts as one out of reach: its row is worked out again by the merging kernel)
     bool far = false;
 #pragma unroll
@@ -706,18 +706,19 @@ __global__ __launch_bounds__(256, in_agprs(LD, 2, RTW) ? 1 : 2) void k_latent_pi
     }
 
     // ---- the segment's partial result
-    const int64_t slot_row = (static_cast<int64_t>(blockIdx.x) + static_cast<int64_t>(b) * a.Hkv + seg.g) * a.block_rows;
-    int ln = lane;                                  // (as above)
-    asm volatile("" : "+v"(ln));
+    const int64_t slot = static_cast<int64_t>(blockIdx.x) + static_cast<int64_t>(b) * a.Hkv + seg.g;
+    const int tiles = a.block_rows / 16;
 #pragma unroll
     for (int t = 0; t < RTW; ++t) {
-      const int rho = 16 * (wv * RTW + t) + (ln & 15), fq = ln >> 4;
       const float l = quad_row_sum(l_run[t]);
-      if (rho >= R) continue;
-      if (fq == 0) *reinterpret_cast<float2*>(a.part_ml + (slot_row + rho) * 2) = make_float2(ref[t], l);
-      float* dst = a.part_o + (slot_row + rho) * LD + 4 * fq;
+      const int rt = wv * RTW + t;
+      if (rt >= tiles) continue;
+      int ln = lane;                                // (as above)
+      asm volatile("" : "+v"(ln));
+      if (ln < 16) *reinterpret_cast<float2*>(a.part_ml + ((slot * tiles + rt) * 16 + ln) * 2) = make_float2(ref[t], l);
+      float* dst = a.part_o + (slot * tiles + rt) * (kDT * 256);
 #pragma unroll
-      for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = oacc[dt][t];
+      for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + dt * 256 + ln * 4) = oacc[dt][t];
     }
     break;
     }
@@ -727,19 +728,17 @@ __global__ __launch_bounds__(256, in_agprs(LD, 2, RTW) ? 1 : 2) void k_latent_pi
 __device__ __forceinline__ float load_value(const bf16_t* p) { return bf16_to_f32(*p); }
 __device__ __forceinline__ float load_value(const float* p) { return *p; }
 
-// One output row key by key, from the entries that it sees: for rows that are not finite, since the products above multiply what is masked with zero.
+// Sixteen columns of one output row key by key, from the entries that it sees: for rows that are not finite, since the products above multiply what is masked with zero.
 template <typename T, int LD>
-__device__ __forceinline__ void latent_row_again(const LatentAttnArgs& a, int b, int row, float* lds) {
+__device__ __forceinline__ void latent_row_again(const LatentAttnArgs& a, int b, int row, int dt, float (&lds)[4][18]) {
   constexpr int E = LD / 64;
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   const int L = attn_ctx_len(a, b), i = row / a.Hq;
   const uint64_t word = a.mask ? a.mask[static_cast<int64_t>(b) * a.mask_stride + i] : ((2ull << i) - 1ull);
   const T* q = static_cast<const T*>(a.q) + (static_cast<int64_t>(b) * a.rows + row) * (LD + kPe);
-  float qv[E + 1], acc[E], m = -INFINITY, sum = 0.f;
+  float qv[E + 1], acc = 0.f, m = -INFINITY, sum = 0.f;
 #pragma unroll
   for (int e = 0; e <= E; ++e) qv[e] = load_value(q + 64 * e + lane);
-#pragma unroll
-  for (int e = 0; e < E; ++e) acc[e] = 0.f;
   for (int p = wv; p < L + a.n_blk; p += 4) {
     if (p >= L && !((word >> (p - L)) & 1ull)) continue;
     int64_t at = static_cast<int64_t>(b) * a.l_max + p;
@@ -748,119 +747,150 @@ __device__ __forceinline__ void latent_row_again(const LatentAttnArgs& a, int b,
       at = static_cast<int64_t>(checked_page(a.page_table[static_cast<int64_t>(b) * a.max_pages + in_seq], a.n_pages, a.status)) * a.page_size + (p - in_seq * a.page_size);
     }
     const T* c = static_cast<const T*>(a.k) + at * (LD + kPe);
-    float cv[E + 1], s = 0.f;
+    float s = 0.f;
 #pragma unroll
-    for (int e = 0; e <= E; ++e) {
-      cv[e] = load_value(c + 64 * e + lane);
-      s = fmaf(qv[e], cv[e], s);
-    }
+    for (int e = 0; e <= E; ++e) s = fmaf(qv[e], load_value(c + 64 * e + lane), s);
     s = wave_sum_dpp(s) * a.scale * 1.44269504088896340736f;
     const float m_new = max_nan(m, s);
     const float old = m == m_new ? 1.f : exp2f(m - m_new), w = s == -INFINITY ? 0.f : exp2f(s - m_new);
     m = m_new;
     sum = sum * old + w;
-#pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = acc[e] * old + w * cv[e];
+    acc = acc * old + w * load_value(c + 16 * dt + (lane & 15));
   }
   __syncthreads();
-  float* mine = lds + wv * (LD + 2);
-#pragma unroll
-  for (int e = 0; e < E; ++e) mine[64 * e + lane] = acc[e];
+  if (lane < 16) lds[wv][lane] = acc;
   if (lane == 0) {
-    mine[LD] = m;
-    mine[LD + 1] = sum;
+    lds[wv][16] = m;
+    lds[wv][17] = sum;
   }
   __syncthreads();
   float mm = -INFINITY;
-  for (int k = 0; k < 4; ++k) mm = max_nan(mm, lds[k * (LD + 2) + LD]);
-  float w[4], den = 0.f;
+  for (int k = 0; k < 4; ++k) mm = max_nan(mm, lds[k][16]);
+  float den = 0.f, v = 0.f;
   for (int k = 0; k < 4; ++k) {
-    const float mk = lds[k * (LD + 2) + LD];
-    w[k] = mk == -INFINITY ? 0.f : exp2f(mk - mm);          // (a wave that saw nothing, or scores of minus infinity only)
-    if (w[k] != 0.f) den += w[k] * lds[k * (LD + 2) + LD + 1];
+    const float w = lds[k][16] == -INFINITY ? 0.f : exp2f(lds[k][16] - mm);          // (a wave that saw nothing, or scores of minus infinity only)
+    if (w == 0.f) continue;
+    den += w * lds[k][17];
+    v += w * lds[k][lane & 15];
   }
-  T* out = static_cast<T*>(a.out) + (static_cast<int64_t>(b) * a.rows + row) * LD;
-  for (int d = threadIdx.x; d < LD; d += 256) {
-    float v = 0.f;
-    for (int k = 0; k < 4; ++k)
-      if (w[k] != 0.f) v += w[k] * lds[k * (LD + 2) + d];
-    v = den != 0.f ? v / den : mm == -INFINITY ? 0.f : v / den;
-    if constexpr (sizeof(T) == 2) out[d] = static_cast<bf16_t>(pack_bf16x2(v, v));
-    else out[d] = v;
+  v = mm == -INFINITY ? 0.f : v / den;
+  if (threadIdx.x < 16) {
+    T* out = static_cast<T*>(a.out) + (static_cast<int64_t>(b) * a.rows + row) * LD + 16 * dt + lane;
+    if constexpr (sizeof(T) == 2) *out = static_cast<bf16_t>(pack_bf16x2(v, v));
+    else *out = v;
   }
 }
 
-// Merge the segments of an output row: exact log-sum-exp combination, a workgroup per row.  Groups of lanes take every NG-th segment of a
-// float4 column and are added in a fixed order; the weights are worked out by every wave for itself.
-constexpr int kCombEarly = 6;
-template <typename T, int LD>
+// Merge the segments of sixteen rows: exact log-sum-exp combination.  Partial results lie as the matrix instructions leave them, a 1 KB fragment for sixteen rows and
+// sixteen columns, and are read and added that way: (max, sum) pairs and fragments of a wave's segments in one round of requests, the WS waves that share a fragment's
+// segments in a fixed order.
+constexpr int kCombAhead = 8;
+template <typename T, int LD, int WS>
 __global__ __launch_bounds__(256) void k_latent_combine(const LatentAttnArgs a) {
-  constexpr int C4 = LD / 4, NG = 256 / C4;
-  __shared__ float4 gs[NG][C4];
-  __shared__ float again[4 * (LD + 2)];
-  const int row = blockIdx.x, b = blockIdx.y;
-  const int lane = threadIdx.x & 63;
-  const int g = row / a.block_rows, r = row - g * a.block_rows, u = b * a.Hkv + g;
+  constexpr int kDT = LD / 16, kPer = 4 / WS;
+  __shared__ f32x4_t part[4][64];
+  __shared__ float2 part_ml[4][16];
+  __shared__ float again[4][18];
+  __shared__ int odd_rows;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 15, fq = lane >> 4;
+  const int tiles = a.block_rows / 16;
+  const int b = blockIdx.y, g = blockIdx.x / tiles, tile = blockIdx.x - g * tiles, u = b * a.Hkv + g;
+  const int row = g * a.block_rows + tile * 16 + fr;
   const int w_first = a.sched[2 * u], n = a.sched[2 * u + 1] - w_first + 1;
-  const int64_t first = (static_cast<int64_t>(w_first) + u) * a.block_rows + r;
-  const int sg = threadIdx.x / C4, c4 = threadIdx.x % C4;
-  const float* po = a.part_o + first * LD + c4 * 4;
-  const float* pm = a.part_ml + first * 2;
-  const int64_t po_step = static_cast<int64_t>(a.block_rows) * LD, pm_step = static_cast<int64_t>(a.block_rows) * 2;
-  float2 ml = *reinterpret_cast<const float2*>(pm + min(lane, n - 1) * pm_step);
-  float4 o[kCombEarly];
+  const int64_t first = (static_cast<int64_t>(w_first) + u) * tiles + tile;
+  const float* pm = a.part_ml + first * 32 + fr * 2;
+  const float* po = a.part_o + first * (kDT * 256) + lane * 4;
+  const int64_t po_step = static_cast<int64_t>(tiles) * (kDT * 256), pm_step = static_cast<int64_t>(tiles) * 32;
+#pragma unroll 1
+  for (int d0 = blockIdx.z * kPer; d0 < kDT; d0 += gridDim.z * kPer) {
+    const int dt = d0 + wv / WS;
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    float m = -FLT_MAX, den = 0.f;
+#pragma unroll 1
+    for (int s0 = wv % WS; s0 < n; s0 += WS * kCombAhead) {
+      f32x4_t o[kCombAhead];
+      float2 ml[kCombAhead];
 #pragma unroll
-  for (int e = 0; e < kCombEarly; ++e) o[e] = *reinterpret_cast<const float4*>(po + min(sg + e * NG, n - 1) * po_step);
-  float mmax = ml.x;
-  for (int s = 64 + lane; s < n; s += 64) mmax = fmaxf(mmax, pm[s * pm_step]);
-  mmax = wave_max_dpp(mmax);
-  float den = 0.f;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int q0 = 0; q0 < n; q0 += 64) {
-    if (q0 > 0) ml = *reinterpret_cast<const float2*>(pm + min(q0 + lane, n - 1) * pm_step);
-    const float w = q0 + lane < n ? exp2f(ml.x - mmax) : 0.f;
-    den += w != 0.f || ml.y != ml.y ? w * ml.y : 0.f;
-    const int k = min(64, n - q0);
-    for (int sb = 0; sb < k; sb += kCombEarly * NG) {          // (uniform: a shuffle reads lanes that take part only)
-      const int s = sb + sg;
-      if (q0 + sb > 0) {
-#pragma unroll
-        for (int e = 0; e < kCombEarly; ++e) o[e] = *reinterpret_cast<const float4*>(po + (q0 + min(s + e * NG, k - 1)) * po_step);
+      for (int e = 0; e < kCombAhead; ++e) {
+        const int s = min(s0 + e * WS, n - 1);
+        o[e] = *reinterpret_cast<const f32x4_t*>(po + s * po_step + dt * 256);
+        ml[e] = *reinterpret_cast<const float2*>(pm + s * pm_step);
       }
+      float m_new = m;
 #pragma unroll
-      for (int e = 0; e < kCombEarly; ++e) {
-        float we = __shfl(w, min(s + e * NG, k - 1), 64);
-        if (s + e * NG >= k) we = 0.f;
-        if (we != 0.f) {
-          acc.x = fmaf(we, o[e].x, acc.x); acc.y = fmaf(we, o[e].y, acc.y);
-          acc.z = fmaf(we, o[e].z, acc.z); acc.w = fmaf(we, o[e].w, acc.w);
+      for (int e = 0; e < kCombAhead; ++e) m_new = fmaxf(m_new, ml[e].x);
+      const float old = __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      den *= old;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[c] *= old;
+#pragma unroll
+      for (int e = 0; e < kCombAhead; ++e) {
+        const float w = s0 + e * WS < n ? __builtin_amdgcn_exp2f(ml[e].x - m) : 0.f;
+        if (w != 0.f) {                             // (a weight of nothing counts nothing, whatever is there)
+          den = fmaf(w, ml[e].y, den);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[c] = fmaf(w, o[e][c], acc[c]);
         }
       }
     }
-  }
-  gs[sg][c4] = acc;
-  den = wave_sum_dpp(den);
-  __syncthreads();
-  bool odd = false;
-  if (sg == 0) {
-    float4 sum = gs[0][c4];
+    if constexpr (WS > 1) {
+      part[wv][lane] = acc;
+      if (fq == 0) part_ml[wv][fr] = make_float2(m, den);
+      __syncthreads();
+      if (wv % WS == 0) {
+        float2 ml[WS];
+        float top = m;
 #pragma unroll
-    for (int k = 1; k < NG; ++k) {
-      const float4 v = gs[k][c4];
-      sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+        for (int k = 0; k < WS; ++k) {
+          ml[k] = part_ml[wv + k][fr];
+          top = fmaxf(top, ml[k].x);
+        }
+        den = 0.f;
+        acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < WS; ++k) {
+          const float w = __builtin_amdgcn_exp2f(ml[k].x - top);
+          if (w == 0.f) continue;
+          den = fmaf(w, ml[k].y, den);
+          const f32x4_t v = part[wv + k][lane];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[c] = fmaf(w, v[c], acc[c]);
+        }
+      }
     }
-    if (den == 0.f) sum = make_float4(0.f, 0.f, 0.f, 0.f);      // a row that sees nothing
-    else { sum.x /= den; sum.y /= den; sum.z /= den; sum.w /= den; }
-    T* dst = static_cast<T*>(a.out) + (static_cast<int64_t>(b) * a.rows + row) * LD + c4 * 4;
-    if constexpr (sizeof(T) == 2) {
-      const uint2 v = make_uint2(pack_bf16x2(sum.x, sum.y), pack_bf16x2(sum.z, sum.w));
-      __builtin_memcpy(dst, &v, sizeof(v));
-    } else {
-      __builtin_memcpy(dst, &sum, sizeof(sum));
+    bool odd = false;
+    if (wv % WS == 0 && row < a.rows) {
+      const float inv = den == 0.f ? 0.f : 1.f / den;          // (a row that sees nothing)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[c] *= inv;
+      T* dst = static_cast<T*>(a.out) + (static_cast<int64_t>(b) * a.rows + row) * LD + 16 * dt + 4 * fq;
+      if constexpr (sizeof(T) == 2) {
+        const uint2 v = make_uint2(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]));
+        __builtin_memcpy(dst, &v, sizeof(v));
+      } else {
+        __builtin_memcpy(dst, &acc, sizeof(acc));
+      }
+      odd = !(fabsf((acc[0] + acc[1]) + (acc[2] + acc[3])) < INFINITY) || !(fabsf(den) < INFINITY);
     }
-    odd = !(fabsf((sum.x + sum.y) + (sum.z + sum.w)) < INFINITY) || !(fabsf(den) < INFINITY);
+    if (__syncthreads_or(odd)) {                       // rows that are not finite, one after the other, for every fragment of this step
+#pragma unroll 1
+      for (int f = 0; f < kPer; ++f) {
+        if (threadIdx.x == 0) odd_rows = 0;
+        __syncthreads();
+        if (odd && wv / WS == f) atomicOr(&odd_rows, 1 << fr);
+        __syncthreads();
+        int left = odd_rows;
+        while (left) {
+          const int r = __ffs(left) - 1;
+          left &= left - 1;
+          latent_row_again<T, LD>(a, b, g * a.block_rows + tile * 16 + r, d0 + f, again);
+        }
+        __syncthreads();
+      }
+    }
   }
-  if (__syncthreads_or(odd)) latent_row_again<T, LD>(a, b, row, again);
 }
 
 template <typename T, int LD, int RTW, int NR>
@@ -904,7 +934,16 @@ hipError_t launch_ld(const LatentAttnArgs& a, hipStream_t s) {
   else if constexpr (sizeof(T) == 4) e = launch_ring<T, LD, 1, 4>(a, s);
   else e = a.block_rows <= 64 ? launch_pipe<LD, 1>(a, s) : launch_pipe<LD, 2>(a, s);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_latent_combine<T, LD>), dim3(a.rows, a.B), dim3(256), 0, s, a);
+  // a fragment's segments to four waves where there are few fragments; many: several fragments a workgroup, some 4096 of those
+  const int64_t fragments = static_cast<int64_t>(a.Hkv) * (a.block_rows / 16) * a.B;
+  const unsigned tiles = static_cast<unsigned>(a.Hkv * (a.block_rows / 16));
+  constexpr int kDT = LD / 16;
+  if (fragments * kDT <= 4096) {
+    hipLaunchKernelGGL((k_latent_combine<T, LD, 4>), dim3(tiles, a.B, kDT), dim3(256), 0, s, a);
+  } else {
+    const unsigned z = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(kDT / 4, 4096 / fragments)));
+    hipLaunchKernelGGL((k_latent_combine<T, LD, 1>), dim3(tiles, a.B, z), dim3(256), 0, s, a);
+  }
   return hipGetLastError();
 }
 
