@@ -350,6 +350,7 @@ struct LatentWriteArgs {
   int* status;
   int64_t entries, tasks;    // latent_write_plan: waves that write entries, and all
   int q_groups;              // waves of a token's queries
+  int many;                  // eight tokens a wave, else one
 };
 bool latent_write_plan(LatentWriteArgs& a);
 hipError_t launch_latent_write(const LatentWriteArgs& a, hipStream_t s);

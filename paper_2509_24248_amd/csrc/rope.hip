@@ -123,12 +123,14 @@ enum { kHalves = 0, kNeighbours = 1, kHalvesOdd = 2 };       // kHalvesOdd: half
 template <typename T, int MODE>
 __global__ __launch_bounds__(kThreads) void k_rope_rows(const RopeRowsArgs a) {
   constexpr int N = Piece<T>::N;
+  arguments_at_once<sizeof(RopeRowsArgs)>();
   const int lane = threadIdx.x & 63;
-  const int64_t task = static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (task >= a.tasks) return;
-  const int64_t bt = task / a.groups;
-  const int group = static_cast<int>(task - bt * a.groups);
-  const int b = static_cast<int>(bt / a.T), t = static_cast<int>(bt - static_cast<int64_t>(b) * a.T);
+  const uint32_t task = blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // (fewer than 2^26)
+  if (task >= static_cast<uint32_t>(a.tasks)) return;
+  const uint32_t token = task / static_cast<uint32_t>(a.groups);
+  const int group = static_cast<int>(task - token * static_cast<uint32_t>(a.groups));
+  const int b = static_cast<int>(token / static_cast<uint32_t>(a.T)), t = static_cast<int>(token - static_cast<uint32_t>(b) * static_cast<uint32_t>(a.T));
+  const int64_t bt = token;
   if (a.count && t >= a.count[b]) return;
   const int LPR = a.d / (2 * N), RPW = 64 / LPR;
   const int sub = lane / LPR, i = lane - sub * LPR;
@@ -215,85 +217,108 @@ __global__ __launch_bounds__(kThreads) void k_rope_rows(const RopeRowsArgs a) {
   }
 }
 
-// Entries of a latent cache: a wave per token brings the latent's root mean square to one, multiplies with the gain and turns the key part;
-// behind those, waves that turn the queries' part of some heads of a token.
-template <typename T, bool PAIRS>
+// Entries of a latent cache: a wave brings the latents of U tokens to a root mean square of one, all its lanes on one after the other, multiplies with the gain and turns the key parts,
+// LPR lanes a token; behind those, waves that turn the queries' part of some heads of a token.  U = 8 where there are tokens enough: sines and cosines are the most of a token's
+// instructions, and with one token four lanes of 64 need them (4 prompts of 4111 tokens at most, 28 MB: 14.1 us with one).
+template <typename T, bool PAIRS, int U>
 __global__ __launch_bounds__(kThreads) void k_latent_write(const LatentWriteArgs a) {
   constexpr int N = Piece<T>::N, LPR = kLatentRope / (2 * N), RPW = 64 / LPR;       // lanes of a rotated part, parts of a wave
   constexpr int P = sizeof(T) == 2 ? 1 : 2;                                         // pieces of the latent of a lane, at most
+  static_assert(U <= RPW, "");
+  arguments_at_once<sizeof(LatentWriteArgs)>();
   const int lane = threadIdx.x & 63;
-  int64_t task = static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (task >= a.tasks) return;
-  const bool entry = task < a.entries;
-  int64_t bt = task;
-  int h0 = 0;
-  if (!entry) {
-    task -= a.entries;
-    bt = task / a.q_groups;
-    h0 = static_cast<int>(task - bt * a.q_groups) * RPW;
-  }
-  const int b = static_cast<int>(bt / a.T), t = static_cast<int>(bt - static_cast<int64_t>(b) * a.T);
-  if (a.count && t >= a.count[b]) return;
-  const int pos = a.pos[b];
+  uint32_t task = blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (task >= static_cast<uint32_t>(a.tasks)) return;
+  const bool entry = task < static_cast<uint32_t>(a.entries);
+  const uint32_t T_ = static_cast<uint32_t>(a.T), tokens = static_cast<uint32_t>(a.B) * T_;
   const int sub = lane / LPR, i = lane % LPR;
-  const int lo_at = PAIRS ? i * 2 * N : i * N, hi_at = PAIRS ? lo_at + N : lo_at + kLatentRope / 2;
-  const T* src = entry ? static_cast<const T*>(a.rows) + bt * a.row_stride + a.r
-                       : static_cast<const T*>(a.q_rows) + bt * a.q_stride + static_cast<int64_t>(min(h0 + sub, a.H - 1)) * a.head_stride;
-  uint4 raw[2], lat[P], gain[P];
-  raw[0] = *reinterpret_cast<const uint4*>(src + lo_at);
-  raw[1] = *reinterpret_cast<const uint4*>(src + hi_at);
-  const int pieces = a.r / N;
+  uint32_t bt;                                      // a lane's token
+  int h = 0;                                        // and head
+  bool mine;
   if (entry) {
-    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const T*>(a.rows) + bt * a.row_stride);
-#pragma unroll
-    for (int u = 0; u < P; ++u) {
-      const bool in = lane + u * 64 < pieces;
-      lat[u] = in ? p[lane + u * 64] : make_uint4(0, 0, 0, 0);
-      gain[u] = in && a.gain ? static_cast<const uint4*>(a.gain)[lane + u * 64] : make_uint4(0, 0, 0, 0);
-    }
+    bt = min(task * U + static_cast<uint32_t>(sub), tokens - 1);
+    mine = sub < U && task * U + static_cast<uint32_t>(sub) < tokens;
+  } else {
+    task -= static_cast<uint32_t>(a.entries);
+    bt = task / static_cast<uint32_t>(a.q_groups);
+    h = static_cast<int>(task - bt * static_cast<uint32_t>(a.q_groups)) * RPW + sub;
+    mine = h < a.H;
+    h = min(h, a.H - 1);
   }
-  const uint32_t turn = rotary_position(a.offset, pos, b, t, a.T, a.status);
+  const int b = static_cast<int>(bt / T_), t = static_cast<int>(bt - static_cast<uint32_t>(b) * T_);
+  const int pos = a.pos[b];
+  mine = mine && (!a.count || t < a.count[b]);
+  if (!__builtin_amdgcn_ballot_w64(mine)) return;
+  const int lo_at = PAIRS ? i * 2 * N : i * N, hi_at = PAIRS ? lo_at + N : lo_at + kLatentRope / 2;
+  const int pieces = a.r / N;
+  uint4 raw[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)}, lat[U][P], gain[P];
+  if (mine) {
+    const T* src = entry ? static_cast<const T*>(a.rows) + static_cast<int64_t>(bt) * a.row_stride + a.r
+                         : static_cast<const T*>(a.q_rows) + static_cast<int64_t>(bt) * a.q_stride + static_cast<int64_t>(h) * a.head_stride;
+    raw[0] = *reinterpret_cast<const uint4*>(src + lo_at);
+    raw[1] = *reinterpret_cast<const uint4*>(src + hi_at);
+  }
+  const uint64_t live = __builtin_amdgcn_ballot_w64(mine);
+  if (entry) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint4* p = reinterpret_cast<const uint4*>(static_cast<const T*>(a.rows) + static_cast<int64_t>(task * U + u) * a.row_stride);
+#pragma unroll
+      for (int k = 0; k < P; ++k) lat[u][k] = (live >> (u * LPR) & 1) && lane + k * 64 < pieces ? p[lane + k * 64] : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int k = 0; k < P; ++k) gain[k] = a.gain && lane + k * 64 < pieces ? static_cast<const uint4*>(a.gain)[lane + k * 64] : make_uint4(0, 0, 0, 0);
+  }
+  uint32_t turn = 0;
   Place at = {0, 0};
-  if (entry && !entry_place(a.kv, b, static_cast<int64_t>(pos) + t, a.status, at)) return;
-  float cs[N], sn[N];
+  if (mine) {
+    turn = rotary_position(a.offset, pos, b, t, a.T, a.status);
+    if (entry) mine = entry_place(a.kv, b, static_cast<int64_t>(pos) + t, a.status, at);
+  }
+  float cs[N], sn[N], lo[N], hi[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) turn_at(turn, a.turns[i * N + e], a.amplitude, cs[e], sn[e]);
-  float lo[N], hi[N];
   Piece<T>::get(raw[0], lo);
   Piece<T>::get(raw[1], hi);
   turn_pieces<N, PAIRS>(lo, hi, cs, sn, N);
-  T* dst;
-  if (!entry) {
-    if (h0 + sub >= a.H) return;
-    dst = static_cast<T*>(a.q_out) + (bt * a.H + h0 + sub) * (a.r + kLatentRope) + a.r;
-  } else {
-    T* row = static_cast<T*>(a.c) + (at.block * (a.kv.paged ? a.kv.page_size : a.kv.l_max) + at.at) * (a.r + kLatentRope);
+  const int64_t row = at.block * (a.kv.paged ? a.kv.page_size : a.kv.l_max) + at.at;       // of a lane's token in the pool
+  if (mine) {
+    T* dst = entry ? static_cast<T*>(a.c) + row * (a.r + kLatentRope) + a.r
+                   : static_cast<T*>(a.q_out) + (static_cast<int64_t>(bt) * a.H + h) * (a.r + kLatentRope) + a.r;
+    *reinterpret_cast<uint4*>(dst + lo_at) = Piece<T>::put(lo);
+    *reinterpret_cast<uint4*>(dst + hi_at) = Piece<T>::put(hi);
+  }
+  if (!entry) return;
+  const float per_value = 1.f / static_cast<float>(a.r);      // (a power of two)
+  const uint64_t placed = __builtin_amdgcn_ballot_w64(mine);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (!(placed >> (u * LPR) & 1)) continue;       // (uniform)
+    const int64_t to = static_cast<int64_t>(static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(row >> 32), u * LPR))) << 32 |
+                                            static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(row), u * LPR)));
     if (a.gain) {
       float x[P][N], ssq = 0.f;
 #pragma unroll
-      for (int u = 0; u < P; ++u) {
-        Piece<T>::get(lat[u], x[u]);
+      for (int k = 0; k < P; ++k) {
+        Piece<T>::get(lat[u][k], x[k]);
 #pragma unroll
-        for (int e = 0; e < N; ++e) ssq = fmaf(x[u][e], x[u][e], ssq);
+        for (int e = 0; e < N; ++e) ssq = fmaf(x[k][e], x[k][e], ssq);
       }
-      const float inv = 1.f / sqrtf(wave_sum_dpp(ssq) / static_cast<float>(a.r) + a.eps);
+      const float inv = rsqrtf(wave_sum_dpp(ssq) * per_value + a.eps);
 #pragma unroll
-      for (int u = 0; u < P; ++u) {
+      for (int k = 0; k < P; ++k) {
         float g[N];
-        Piece<T>::get(gain[u], g);
+        Piece<T>::get(gain[k], g);
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[u][e] = x[u][e] * inv * g[e];
-        lat[u] = Piece<T>::put(x[u]);
+        for (int e = 0; e < N; ++e) x[k][e] = x[k][e] * inv * g[e];
+        lat[u][k] = Piece<T>::put(x[k]);
       }
     }
+    uint4* dst = reinterpret_cast<uint4*>(static_cast<T*>(a.c) + to * (a.r + kLatentRope));
 #pragma unroll
-    for (int u = 0; u < P; ++u)
-      if (lane + u * 64 < pieces) reinterpret_cast<uint4*>(row)[lane + u * 64] = lat[u];
-    if (sub > 0) return;
-    dst = row + a.r;
+    for (int k = 0; k < P; ++k)
+      if (lane + k * 64 < pieces) dst[lane + k * 64] = lat[u][k];
   }
-  *reinterpret_cast<uint4*>(dst + lo_at) = Piece<T>::put(lo);
-  *reinterpret_cast<uint4*>(dst + hi_at) = Piece<T>::put(hi);
 }
 
 template <typename T>
@@ -310,13 +335,15 @@ hipError_t launch_rope_table(const RopeTableArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Waves from which on one takes several steps: 32 a compute unit.
+constexpr int64_t kRopeWaves = 8192;
 bool rope_rows_plan(RopeRowsArgs& a) {
   const int per_step = 64 / (a.d / (a.f32 ? 8 : 16));             // rows of a wave's step
   const int steps = (a.Hq + 2 * a.Hkv + per_step - 1) / per_step;
   const int64_t tokens = static_cast<int64_t>(a.B) * a.T;
   if (tokens > kLaunchWaves) return false;
-  // few tokens: a step per wave, so that the call is as short as one; many: all of a token's heads in one wave, which shares their sines and cosines
-  a.per = tokens * steps <= 4096 ? 1 : steps;
+  // few tokens: a step per wave, so that the call is as short as one; many: more of a token's heads in one wave, which shares their sines and cosines
+  a.per = static_cast<int>(std::min<int64_t>(steps, std::max<int64_t>(1, tokens * steps / kRopeWaves)));
   a.groups = (steps + a.per - 1) / a.per;
   a.tasks = tokens * a.groups;
   return a.tasks <= kLaunchWaves;
@@ -329,23 +356,33 @@ hipError_t launch_rope_rows(const RopeRowsArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Tokens from which a wave takes eight.
+constexpr int64_t kManyTokens = 4096;
 bool latent_write_plan(LatentWriteArgs& a) {
-  a.entries = static_cast<int64_t>(a.B) * a.T;
-  if (a.entries > kLaunchWaves) return false;
+  const int64_t tokens = static_cast<int64_t>(a.B) * a.T;
+  if (tokens > kLaunchWaves) return false;
+  a.many = tokens >= kManyTokens;
+  a.entries = a.many ? (tokens + 7) / 8 : tokens;
   const int rows = a.f32 ? 8 : 16;                                // rotated parts of a wave
   a.q_groups = (a.H + rows - 1) / rows;
-  a.tasks = a.entries * (1 + a.q_groups);
+  a.tasks = a.entries + tokens * a.q_groups;
   return a.tasks <= kLaunchWaves;
 }
 
-hipError_t launch_latent_write(const LatentWriteArgs& a, hipStream_t s) {
+template <typename T, bool PAIRS>
+static void launch_latent_as(const LatentWriteArgs& a, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>((a.tasks + 3) / 4)), block(kThreads);
+  if (a.many) hipLaunchKernelGGL((k_latent_write<T, PAIRS, 8>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((k_latent_write<T, PAIRS, 1>), grid, block, 0, s, a);
+}
+
+hipError_t launch_latent_write(const LatentWriteArgs& a, hipStream_t s) {
   if (a.f32) {
-    if (a.neighbours) hipLaunchKernelGGL((k_latent_write<float, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((k_latent_write<float, false>), grid, block, 0, s, a);
+    if (a.neighbours) launch_latent_as<float, true>(a, s);
+    else launch_latent_as<float, false>(a, s);
   } else {
-    if (a.neighbours) hipLaunchKernelGGL((k_latent_write<bf16_t, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((k_latent_write<bf16_t, false>), grid, block, 0, s, a);
+    if (a.neighbours) launch_latent_as<bf16_t, true>(a, s);
+    else launch_latent_as<bf16_t, false>(a, s);
   }
   return hipGetLastError();
 }
