@@ -381,9 +381,9 @@ struct LogprobArgs {
   int32_t* top_token;        // [M][n_top]
   float* top_logprob;        // [M][n_top] or nullptr
   int* status;
-  int wide, chunks;          // logprob_plan: chunks of 32 values a thread, else 8; chunks of a row
-  float4* stats;             // [M][chunks]: largest logit, how many equal it, sums
-  unsigned long long* best;  // [M][chunks][n_top]
+  int wide, parts;           // logprob_plan: parts of 32 values a lane, else 16; parts of a row
+  float4* stats;             // [M][parts]: largest logit, how many equal it, sums
+  float* groups;             // [M][parts][8]: the largest of eight lanes each
 };
 void logprob_plan(LogprobArgs& a);
 size_t logprob_carve(LogprobArgs& a, void* base);

@@ -4,12 +4,11 @@
 //   ln p_i = y_i - ln n - ln(1 + S / n),   H = ln n + ln(1 + S / n) - U / (n + S)
 // The best tokens' weight is counted, not summed: a row whose best token has nearly everything keeps the digits of what is left.
 //
-// Two launches.  k_logprob_chunk reads the logits once: a workgroup holds a chunk of a row in registers, 8 or 32 values a thread, takes its maximum, its sums and its
-// n_top best.  k_logprob_row, a workgroup per row, adds the chunks' sums, in their order, and selects among their best.
-//
-// The best of a chunk without sorting it: the n-th largest of the maxima of 32 groups of threads is a bound that at least n values meet, and about n (1 + n / 64) of 8192
-// do; those go to a list in LDS, where every one counts how many are before it.  Where more than the list holds do (many equal values, or a chunk sorted so that a
-// few groups have them all), the chunk is searched n times for the best that is left.
+// Two launches.  k_logprob_part reads the logits once: a wave holds 16 or 32 values a lane and takes its maximum, its sums and the maxima of its eight groups of eight lanes; no
+// barrier, no LDS.  k_logprob_row, a workgroup per row, adds the parts' sums, in their order, and finds the row's n_top best: the n-th largest of the maxima of
+// 64 sets of groups is a bound that at least n values meet and, in any order of the logits that does not conspire, few more; the groups that reach it (n and some) are read again, a
+// load instruction each, and what meets the bound goes to a list in LDS, where every one counts how many are before it.
+// A list that runs over (many equal values, or a few groups that hold all the best) is cut to its n best, whose last becomes the bound, and the groups go on.
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -23,9 +22,9 @@ namespace sx {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kGroups = 32;            // of eight threads
-constexpr int kList = 512;             // candidates of a chunk
-constexpr int kNarrow = 8, kWide = 32; // values of a thread
+constexpr int kNarrow = 16, kWide = 32;                    // values of a lane
+constexpr int kMostParts = 272;                            // parts of a row (512 logits x 16 ..)
+constexpr int kList = 1536;                                // candidates
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 
 typedef unsigned long long u64;
@@ -43,44 +42,12 @@ __device__ __forceinline__ int index_of(u64 key) { return static_cast<int>(0xFFF
 __device__ __forceinline__ float row_heat(const LogprobArgs& a, int r) {
   return a.temperature ? fminf(fmaxf(a.temperature[r / a.rows_per_seq], 0x1p-10f), 0x1p96f) : 1.f;
 }
-__device__ __forceinline__ u64 wave_max_u64(u64 v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const u64 w = __shfl_xor(v, o, 64);
-    v = w > v ? w : v;
-  }
-  return v;
-}
-// The n-th largest of the values that lanes 0 .. M - 1 hold (equal ones count apart), by counting.
-template <int M>
+// The n-th largest of a wave's values, equal ones counting apart: the least that fewer than n are above.
 __device__ __forceinline__ float nth_largest(float v, int n) {
-  const int lane = threadIdx.x & 63;
-  int before = 0;
+  int above = 0;
 #pragma unroll
-  for (int j = 0; j < M; ++j) {
-    const float x = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), j));
-    before += x > v || (x == v && j < lane);
-  }
-  const uint64_t it = __builtin_amdgcn_ballot_w64(lane < M && before == n - 1);
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), static_cast<int>(__builtin_ctzll(it))));
-}
-// The n-th largest of m <= 128 distinct keys of LDS, in every wave.
-__device__ __forceinline__ u64 nth_largest(const u64* v, int m, int n) {
-  const int lane = threadIdx.x & 63;
-  u64 mine[2], found = 0;
-  int before[2] = {0, 0};
-#pragma unroll
-  for (int u = 0; u < 2; ++u) mine[u] = lane + 64 * u < m ? v[lane + 64 * u] : 0;
-#pragma unroll 4
-  for (int j = 0; j < m; ++j) {
-    const u64 x = v[j];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) before[u] += x > mine[u] || (x == mine[u] && j < lane + 64 * u);
-  }
-#pragma unroll
-  for (int u = 0; u < 2; ++u)
-    if (lane + 64 * u < m && before[u] == n - 1) found = mine[u];
-  return wave_max_u64(found);
+  for (int j = 0; j < 64; ++j) above += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), j)) > v;
+  return -wave_max_dpp(above < n ? -v : -INFINITY);
 }
 // Places in a list of LDS for the lanes that want one: one atomic operation a wave.
 __device__ __forceinline__ int list_place(int* listed, bool wanted) {
@@ -104,38 +71,44 @@ __device__ __forceinline__ void rank_keys(const u64* list, int count, int n, u64
   for (int i = count + threadIdx.x; i < n; i += kThreads) out[i] = 0;
 }
 
-// The sums of a thread's values from the best one of the chunk: p = 2^((x - ref) unit), sum of p and of p (x - ref).  What is ruled out, infinitely far below, weighs nothing; with a
-// reference beyond 2^102 a distance can leave the range (FAR).
-template <int EPT, bool FAR>
-__device__ __forceinline__ void chunk_sums(const float (&x)[EPT], float ref, float unit, float& s, float& w) {
+// Maxima that hand a NaN on: the instruction takes three values and needs no quieting of its inputs, of which there would be one each.
+__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// A lane's 16 bytes of a row from value i on, ruled out where they are not of the row.
+template <typename T>
+__device__ __forceinline__ void load_piece(const T* row, int i, int V, float (&f)[16 / sizeof(T)]) {
+  constexpr int N = 16 / sizeof(T);
+  if (i >= 0 && i + N <= V) {
+    const uint4 v = *reinterpret_cast<const uint4*>(row + i);
+    if constexpr (sizeof(T) == 2) {
+      unpack16(v, f);
+    } else {
+      f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+    }
+  } else {
 #pragma unroll
-  for (int e = 0; e < EPT; ++e) {
-    float d = fmaxf(x[e], -FLT_MAX) - ref;
-    if (FAR) d = fmaxf(d, -FLT_MAX);
-    const float p = __builtin_amdgcn_exp2f(d * unit);
-    s += p;
-    w = fmaf(p, d, w);
+    for (int e = 0; e < N; ++e) f[e] = i + e >= 0 && i + e < V ? Elem<T>::load(row + i + e) : -INFINITY;
   }
 }
+// Parts begin at multiples of 16 bytes: values in front of the row.
+template <typename T> __device__ __forceinline__ int row_skew(const T* row) {
+  return static_cast<int>(reinterpret_cast<uintptr_t>(row) & 15) / static_cast<int>(sizeof(T));
+}
 
-// What a value costs here: 1 instruction for the maximum, 5 and an exponential for the sums, 2 for the candidates; what the best one's exclusion costs falls to the threads that hold one.
+// Bound by vector instructions before memory: 8.5 and an exponential a value (half a maximum, 2 that take the best one out, 6 for the sums).
 template <typename T, int EPT>
-__global__ __launch_bounds__(kThreads) void k_logprob_chunk(const LogprobArgs a) {
+__global__ __launch_bounds__(kThreads) void k_logprob_part(const LogprobArgs a) {
   constexpr int N = 16 / sizeof(T), U = EPT / N;
-  __shared__ float group_max[kGroups];
-  __shared__ float sums[kThreads / 64][3];
-  __shared__ u64 list[kList], best_of[kThreads / 64];
-  __shared__ int listed;
-  const int c = blockIdx.x, r = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  const int lane = threadIdx.x & 63, r = blockIdx.y;
+  const int part = blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (part >= a.parts) return;
   const T* row = static_cast<const T*>(a.logits) + static_cast<int64_t>(r) * a.ld;
-  // chunks begin at multiples of 16 bytes: `skew` values in front of the row
-  const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(row) & 15) / static_cast<int>(sizeof(T));
-  const int base = c * (kThreads * EPT) - skew;
+  const int base = part * (64 * EPT) - row_skew(row);
   float x[EPT];
-  if (base >= 0 && base + kThreads * EPT <= a.V) {
+  if (base >= 0 && base + 64 * EPT <= a.V) {
     uint4 v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const uint4*>(row + base + (u * kThreads + tid) * N);
+    for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const uint4*>(row + base + (u * 64 + lane) * N);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if constexpr (sizeof(T) == 2) {
@@ -148,130 +121,82 @@ __global__ __launch_bounds__(kThreads) void k_logprob_chunk(const LogprobArgs a)
         x[u * N + 2] = __uint_as_float(v[u].z); x[u * N + 3] = __uint_as_float(v[u].w);
       }
     }
-  } else {                                                // a row's first or last chunk
+  } else {                                                // a row's first or last part
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = base + (u * kThreads + tid) * N;
+      float f[N];
+      load_piece(row, base + (u * 64 + lane) * N, a.V, f);
 #pragma unroll
-      for (int e = 0; e < N; ++e) x[u * N + e] = i + e >= 0 && i + e < a.V ? Elem<T>::load(row + i + e) : -INFINITY;
+      for (int e = 0; e < N; ++e) x[u * N + e] = f[e];
     }
   }
-  if (tid == 0) listed = 0;
-  float mine = -INFINITY;
+  float mine = x[0];
 #pragma unroll
-  for (int e = 0; e < EPT; ++e) mine = fmaxf(mine, x[e]);         // (a NaN is passed over)
-  // maxima of eight lanes
-  float g = mine;
+  for (int e = 1; e < EPT; ++e) mine = max_nan(mine, x[e]);
+  if (__builtin_amdgcn_ballot_w64(mine != mine) != 0ull) {        // (uniform, rare) NaN counts as ruled out
+    mine = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) {
+      x[e] = x[e] != x[e] ? -INFINITY : x[e];
+      mine = max_nan(mine, x[e]);
+    }
+  }
+  float g = mine;                                         // of eight lanes
   g = fmaxf(g, row_lane<0xB1>(g));
   g = fmaxf(g, row_lane<0x4E>(g));
   g = fmaxf(g, row_lane<0x141>(g));
-  if ((lane & 7) == 0) group_max[tid >> 3] = g;
-  __syncthreads();
-  const float groups = group_max[lane & (kGroups - 1)];
-  const float top = wave_max_dpp(groups);
-  const float heat = row_heat(a, r), unit = kLog2e / heat;
+  const int64_t slot = static_cast<int64_t>(r) * a.parts + part;
+  if (a.n_top && (lane & 7) == 0) a.groups[slot * 8 + (lane >> 3)] = g;
+  const float top = quad_row_max(fmaxf(g, row_lane<0x128>(g)));
+  const float unit = kLog2e / row_heat(a, r);
   const float ref = top == -INFINITY ? 0.f : top;
-  float s = 0.f, w = 0.f, n = 0.f;
-  if (fabsf(ref) < 0x1p102f) chunk_sums<EPT, false>(x, ref, unit, s, w);
-  else chunk_sums<EPT, true>(x, ref, unit, s, w);
-  if (mine == top) {                                      // the thread that holds the best value, or several: that one is counted
-    s = w = 0.f;
+  // what equals the best one is counted and taken out; the sums are of p = 2^(d unit) and p d, d = x - ref, from -FLT_MAX on (what is ruled out weighs nothing)
+  float s = 0.f, w = 0.f;
+  int n = 0;
 #pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-      const bool is_top = x[e] == top;
-      const float d = fmaxf(fmaxf(x[e], -FLT_MAX) - ref, -FLT_MAX), p = __builtin_amdgcn_exp2f(d * unit);
-      n += is_top ? 1.f : 0.f;
-      s += is_top ? 0.f : p;
-      w += is_top ? 0.f : p * d;
-    }
-    if (top == -INFINITY) n = 0.f;
+  for (int e = 0; e < EPT; ++e) {
+    const bool is_top = x[e] == top;
+    n += static_cast<int>(__popcll(__builtin_amdgcn_ballot_w64(is_top)));
+    const float d = max_nan((is_top ? -INFINITY : x[e]) - ref, -FLT_MAX), p = __builtin_amdgcn_exp2f(d * unit);
+    s += p;
+    w = fmaf(p, d, w);
   }
   s = wave_sum_dpp(s);
   w = wave_sum_dpp(w);
-  n = wave_sum_dpp(n);
-  if (lane == 0) { sums[tid >> 6][0] = n; sums[tid >> 6][1] = s; sums[tid >> 6][2] = w * unit; }
-  const bool select = a.n_top > 0;
-  if (select) {
-    const float bound = a.n_top == 1 ? top : nth_largest<kGroups>(groups, a.n_top);
-    uint32_t meets = 0;
-    if (mine >= bound) {
-#pragma unroll
-      for (int e = 0; e < EPT; ++e) meets |= (x[e] >= bound ? 1u : 0u) << e;
-    }
-    if (bound == -INFINITY) {                             // (what is ruled out meets it as well)
-#pragma unroll
-      for (int e = 0; e < EPT; ++e) meets &= ~((x[e] == -INFINITY ? 1u : 0u) << e);
-    }
-    while (__builtin_amdgcn_ballot_w64(meets != 0) != 0ull) {
-      const bool has = meets != 0;
-      const int at = list_place(&listed, has);
-      if (has) {
-        const int e = __builtin_ctz(meets), i = base + (e / N * kThreads + tid) * N + e % N;
-        meets &= meets - 1;
-        if (at < kList) list[at] = key_of(Elem<T>::load(row + i), i);          // (read again: registers have no index)
-      }
-    }
-  }
-  __syncthreads();
-  const int64_t slot = static_cast<int64_t>(r) * a.chunks + c;
-  if (tid == 0) {
-    float4 t = make_float4(top, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int k = 0; k < kThreads / 64; ++k) { t.y += sums[k][0]; t.z += sums[k][1]; t.w += sums[k][2]; }
-    a.stats[slot] = t;
-  }
-  if (!select) return;
-  u64* out = a.best + slot * a.n_top;
-  if (listed <= kList) {
-    rank_keys(list, listed, a.n_top, out);
-    return;
-  }
-  u64 last = ~0ull;
-  for (int k = 0; k < a.n_top; ++k) {
-    u64 key = 0;
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-      const u64 ke = key_of(x[e], base + (e / N * kThreads + tid) * N + e % N);
-      if (x[e] > -INFINITY && ke < last && ke > key) key = ke;
-    }
-    key = wave_max_u64(key);
-    __syncthreads();
-    if (lane == 0) best_of[tid >> 6] = key;
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kThreads / 64; ++j) key = best_of[j] > key ? best_of[j] : key;
-    if (tid == 0) out[k] = key;
-    last = key;
-  }
+  if (lane == 0) a.stats[slot] = make_float4(top, top == -INFINITY ? 0.f : static_cast<float>(n), s, w * unit);
 }
 
-constexpr int kMostChunks = 128;
-
-template <typename T>
+template <typename T, int EPT>
 __global__ __launch_bounds__(kThreads) void k_logprob_row(const LogprobArgs a) {
-  __shared__ u64 heads[kMostChunks], list[kLogprobMaxTop * kLogprobMaxTop], ranked[kLogprobMaxTop];
-  __shared__ int listed;
+  constexpr int N = 16 / sizeof(T), U = EPT / N, kLanes = 8 * U;         // lanes that read a group again
+  constexpr int kPer = (kMostParts + 63) / 64, kGroupsPer = kMostParts * 8 / kThreads + 1;
+  static_assert(kLanes <= 64, "");
+  __shared__ float waves_max[kThreads / 64][64];
+  __shared__ uint16_t met[kMostParts * 8];
+  __shared__ u64 list[kList], ranked[kLogprobMaxTop];
+  __shared__ int listed, groups_met;
   arguments_at_once<sizeof(LogprobArgs)>();
-  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
-  const float4* stats = a.stats + static_cast<int64_t>(r) * a.chunks;
-  const u64* best = a.best + static_cast<int64_t>(r) * a.chunks * a.n_top;
-  // everything is asked for at once: the chunks' sums, their t-th best, the tokens' logits
-  constexpr int kPer = kMostChunks / 64;
+  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const T* row = static_cast<const T*>(a.logits) + static_cast<int64_t>(r) * a.ld;
+  const int64_t first = static_cast<int64_t>(r) * a.parts;
+  // everything is asked for at once: the parts' sums, the groups' maxima, the tokens' logits
   float4 st[kPer];
+  float gm[kGroupsPer];
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) st[k] = lane + 64 * k < a.chunks ? stats[lane + 64 * k] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
-  // ceil(n / t) chunks whose t-th best meet a bound hold n values that do; the least t that as many chunks as there are suffice for
-  const int t = a.n_top ? (a.n_top + a.chunks - 1) / a.chunks : 1;
-  if (a.n_top && tid < a.chunks) heads[tid] = best[static_cast<int64_t>(tid) * a.n_top + t - 1];
+  for (int k = 0; k < kPer; ++k) st[k] = lane + 64 * k < a.parts ? a.stats[first + lane + 64 * k] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  if (a.n_top) {
+#pragma unroll
+    for (int k = 0; k < kGroupsPer; ++k) gm[k] = tid + kThreads * k < a.parts * 8 ? a.groups[first * 8 + tid + kThreads * k] : -INFINITY;
+  }
   float mine = 0.f;
   bool known = false;
   if (tid < a.n_tok) {
     const int token = a.token[static_cast<int64_t>(r) * a.n_tok + tid];
     known = token >= 0 && token < a.V;
     if (!known && token != -1) report_status(a.status, kStatusBadToken);
-    if (known) mine = Elem<T>::load(static_cast<const T*>(a.logits) + static_cast<int64_t>(r) * a.ld + token);
+    if (known) mine = Elem<T>::load(row + token);
   }
-  if (tid == 0) listed = 0;
+  if (tid == 0) listed = groups_met = 0;
   const float heat = row_heat(a, r), unit = kLog2e / heat;
   float top = -INFINITY;
 #pragma unroll
@@ -300,15 +225,79 @@ __global__ __launch_bounds__(kThreads) void k_logprob_row(const LogprobArgs a) {
   if (tid < a.n_tok) a.logprob[static_cast<int64_t>(r) * a.n_tok + tid] = known ? logprob(mine) : __uint_as_float(0x7FC00000u);
   if (tid == 0 && a.entropy) a.entropy[r] = top == -INFINITY ? 0.f : norm - kLn2 * w / (n + s);
   if (a.n_top == 0) return;
+  // ---- the bound, and the groups that meet it
+  float best = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < kGroupsPer; ++k) best = fmaxf(best, gm[k]);
+  waves_max[wv][lane] = best;
   __syncthreads();
-  u64 bound = nth_largest(heads, a.chunks, (a.n_top + t - 1) / t);
-  if (bound == 0) bound = 1;
-  for (int i0 = 0; i0 < a.chunks * a.n_top; i0 += kThreads) {
-    const u64 key = i0 + tid < a.chunks * a.n_top ? best[i0 + tid] : 0;
-    const int at = list_place(&listed, key >= bound);
-    if (key >= bound) list[at] = key;
+#pragma unroll
+  for (int k = 0; k < kThreads / 64; ++k) best = fmaxf(best, waves_max[k][lane]);
+  const float bound = a.n_top == 1 ? wave_max_dpp(best) : nth_largest(best, a.n_top);
+#pragma unroll
+  for (int k = 0; k < kGroupsPer; ++k) {
+    const bool meets = gm[k] >= bound && gm[k] > -INFINITY;
+    const int at = list_place(&groups_met, meets);
+    if (meets) met[at] = static_cast<uint16_t>(tid + kThreads * k);
   }
   __syncthreads();
+  const int count = groups_met, skew = row_skew(row);
+  u64 least = 0;                                          // of the list's best, once it was cut
+  // group i of those: eight lanes of a part, U pieces of each
+  auto place_of = [&](int i) {
+    const int id = met[i];
+    return (id >> 3) * (64 * EPT) - skew + ((lane >> 3) * 64 + (id & 7) * 8 + (lane & 7)) * N;
+  };
+  auto keep = [&](const float (&f)[N], int at, bool mine) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const u64 key = key_of(f[e], at + e);
+      const bool in = mine && f[e] >= bound && f[e] > -INFINITY && key > least;
+      const int place = list_place(&listed, in);
+      if (in && place < kList) list[place] = key;
+    }
+  };
+  constexpr int kWaves = kThreads / 64;
+  constexpr int kTogether = 8;                            // groups of a wave that are asked for together
+#pragma unroll 1
+  for (int i0 = wv; i0 < count; i0 += kWaves * kTogether) {
+    float f[kTogether][N];
+#pragma unroll
+    for (int k = 0; k < kTogether; ++k) {
+      const int i = i0 + k * kWaves;
+      if (i < count && lane < kLanes) load_piece(row, place_of(i), a.V, f[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kTogether; ++k) {
+      const int i = i0 + k * kWaves;
+      if (i < count) keep(f[k], place_of(i), lane < kLanes);
+    }
+  }
+  __syncthreads();
+  if (listed > kList) {                                   // (uniform) again, a group a wave at a time
+    __syncthreads();
+    if (tid == 0) listed = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int i = 0; i < count; i += kWaves) {
+      if (i + wv < count) {
+        float f[N];
+        if (lane < kLanes) load_piece(row, place_of(i + wv), a.V, f);
+        keep(f, place_of(i + wv), lane < kLanes);
+      }
+      __syncthreads();
+      if (listed > kList - kWaves * 64 * N || i + kWaves >= count) {
+        const int have = listed;
+        __syncthreads();
+        rank_keys(list, have, a.n_top, ranked);
+        __syncthreads();
+        if (tid < a.n_top) list[tid] = ranked[tid];
+        if (tid == 0) listed = min(have, a.n_top);
+        if (have >= a.n_top) least = ranked[a.n_top - 1];
+        __syncthreads();
+      }
+    }
+  }
   rank_keys(list, listed, a.n_top, ranked);
   __syncthreads();
   if (tid < a.n_top) {
@@ -318,35 +307,39 @@ __global__ __launch_bounds__(kThreads) void k_logprob_row(const LogprobArgs a) {
   }
 }
 
-// chunks of a row, its alignment not known
-int chunks_of(int V, int per_thread) { return (V + 7 + kThreads * per_thread - 1) / (kThreads * per_thread); }
+// parts of a row, its alignment not known
+int parts_of(int V, int per_lane) { return (V + 7 + 64 * per_lane - 1) / (64 * per_lane); }
+
+template <typename T, int EPT>
+void launch_ept(const LogprobArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((k_logprob_part<T, EPT>), dim3(static_cast<unsigned>((a.parts + 3) / 4), static_cast<unsigned>(a.M)), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL((k_logprob_row<T, EPT>), dim3(static_cast<unsigned>(a.M)), dim3(kThreads), 0, s, a);
+}
 
 template <typename T>
 void launch_as(const LogprobArgs& a, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(a.chunks), static_cast<unsigned>(a.M));
-  if (a.wide) hipLaunchKernelGGL((k_logprob_chunk<T, kWide>), grid, dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((k_logprob_chunk<T, kNarrow>), grid, dim3(kThreads), 0, s, a);
-  hipLaunchKernelGGL(k_logprob_row<T>, dim3(static_cast<unsigned>(a.M)), dim3(kThreads), 0, s, a);
+  if (a.wide) launch_ept<T, kWide>(a, s);
+  else launch_ept<T, kNarrow>(a, s);
 }
 
 }  // namespace
 
 // Few rows are cut finer, so that they fill the chip too.
-constexpr int64_t kFewChunks = 512;
+constexpr int64_t kFewParts = 2048;
 void logprob_plan(LogprobArgs& a) {
-  a.wide = static_cast<int64_t>(a.M) * chunks_of(a.V, kWide) >= kFewChunks || chunks_of(a.V, kNarrow) > kMostChunks;
-  a.chunks = chunks_of(a.V, a.wide ? kWide : kNarrow);
+  a.wide = static_cast<int64_t>(a.M) * parts_of(a.V, kWide) >= kFewParts;
+  a.parts = parts_of(a.V, a.wide ? kWide : kNarrow);
 }
 
 size_t logprob_carve(LogprobArgs& a, void* base) {
-  // never less for more rows or a larger V: narrow chunks count four times those of kFewChunks at most
-  const int64_t wide = static_cast<int64_t>(a.M) * chunks_of(a.V, kWide), narrow = static_cast<int64_t>(a.M) * chunks_of(a.V, kNarrow);
-  const size_t chunks = static_cast<size_t>(std::max(wide, std::min(narrow, 4 * kFewChunks)));
+  // never less for more rows or a larger V: narrow parts count twice those of kFewParts at most
+  const int64_t wide = static_cast<int64_t>(a.M) * parts_of(a.V, kWide), narrow = static_cast<int64_t>(a.M) * parts_of(a.V, kNarrow);
+  const size_t parts = static_cast<size_t>(std::max(wide, std::min(narrow, 2 * kFewParts)));
   char* p = static_cast<char*>(base);
   a.stats = reinterpret_cast<float4*>(p);
-  const size_t stats = (chunks * sizeof(float4) + 255) & ~static_cast<size_t>(255);
-  a.best = reinterpret_cast<unsigned long long*>(p + stats);
-  return stats + ((chunks * a.n_top * sizeof(unsigned long long) + 255) & ~static_cast<size_t>(255));
+  const size_t stats = (parts * sizeof(float4) + 255) & ~static_cast<size_t>(255);
+  a.groups = reinterpret_cast<float*>(p + stats);
+  return stats + (a.n_top ? (parts * 8 * sizeof(float) + 255) & ~static_cast<size_t>(255) : 0);
 }
 
 hipError_t launch_logprob(const LogprobArgs& a, hipStream_t s) {
