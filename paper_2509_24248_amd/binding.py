@@ -640,7 +640,7 @@ def _turns(rope: RopeDesc, turns):
 def _head_rows(rows: torch.Tensor, B: int, T: int, heads: int, d: int, want, name: str) -> int:
     """rows: [B, T, heads, d], heads and values consecutive, tokens evenly apart; the elements between two tokens."""
     assert want is None or rows.dtype == want, f"{name} must be {want}, not {rows.dtype}"
-    assert rows.is_cuda and tuple(rows.shape) == (B, T, heads, d), f"{name}: {tuple(rows.shape)} is not {(B, T, heads, d)}"
+    assert rows.is_cuda and rows.shape == (B, T, heads, d), f"{name}: {tuple(rows.shape)} is not {(B, T, heads, d)}"
     sb, st, sh, sd = rows.stride()
     step = st if T > 1 else sb if B > 1 else heads * d
     assert sd == 1 and (sh == d or heads == 1) and (sb == T * step or B == 1), f"{name}: tokens must lie evenly apart, heads and values consecutive"
@@ -662,7 +662,7 @@ def specexit_rope_kv_write(kv: KVView, rope: RopeDesc, turns, B: int, T: int, n_
     """q_rows [B, T, n_q_heads, d], k_rows, v_rows [B, T, n_kv_heads, d]: tokens evenly apart; q_out contiguous."""
     want, i32, d = _STORAGE.get(kv.dtype), torch.int32, kv.head_dim
     step = _head_rows(k_rows, B, T, kv.n_kv_heads, d, want, "k_rows")
-    assert _head_rows(v_rows, B, T, kv.n_kv_heads, d, want, "v_rows") == step, "k_rows and v_rows must lie alike"
+    assert v_rows.is_cuda and v_rows.dtype == k_rows.dtype and v_rows.shape == k_rows.shape and v_rows.stride() == k_rows.stride(), "k_rows and v_rows must lie alike"
     q_step, q_at = (_head_rows(q_rows, B, T, n_q_heads, d, want, "q_rows"), q_rows.data_ptr()) if n_q_heads else (0, None)
     q_out = _arg(q_out, want, B * T * n_q_heads * d, "q_out") if n_q_heads else None
     pos, offset, count = _arg(pos, i32, B, "pos"), _arg(offset, i32, B * T, "offset"), _arg(count, i32, B, "count")

@@ -3,18 +3,24 @@
 //
 //   s_j = scale q . (c_j | k_j),  o = sum_j softmax_j(s) c_j          2 (2 LD + 64) operations a row and entry of (LD + 64) e bytes
 //
-// The rows of a sequence are cut into blocks of up to 128 (fp32: 64); a workgroup takes an equal share of all keys of all (sequence, block) units
-// (attn_sched.hpp, the blocks in the place of KV heads).  Inside it the tiles of 32 keys (fp32: 16) lie in LDS once, as they lie in memory, and are read
-// twice from there:
+// Read once, an entry has 2 R (2 LD + 64) / (LD + 64) operations an element: up to some 80 rows the bytes are the bound, beyond that the matrix instructions.
+//
+// The rows of a sequence are cut into blocks; a workgroup takes an equal share of all keys of all (sequence, block) units (attn_sched.hpp, the blocks in the place
+// of KV heads).  Inside it the tiles of 32 keys (fp32: 16) lie in LDS once, as they lie in memory, and are read twice from there:
 //   S^T = C Q^T    : A operand = entries (row = key), B operand = the rows' queries, held in registers;
 //   softmax        : online, per wave, in log2 units;
 //   O^T += C^T P^T : A operand = the same tile by columns (ds_read_b64_tr_b16; fp32: plain reads, a key's sixteen columns to sixteen lanes), B operand = P^T
 //                    straight from the softmax registers.
 // fp32 uses the fp32 matrix instructions: neither entries nor probabilities lose a digit.
 //
-// A workgroup has four waves, one per SIMD with all of its registers (128 rows of 512 columns: 256 of accumulators and 144 of queries): NR waves of RTW
-// 16-row tiles share a ring of tiles, NK rings have keys of their own and are added at the end, in their order.  S slots a ring.
-// Tiles are brought in by direct global -> LDS loads, a ring's waves a quarter or half each.
+// A workgroup has four waves, one per SIMD with all of its registers.  Tiles are brought in by direct global -> LDS loads, up to four slots ahead.  Rows of a block:
+//   16 or 32: four rings of one wave or two of two, each with keys of its own, added at the end in their order;
+//   64      : one ring of four waves, sixteen rows each (fp32; bf16 in software-pipelined form);
+//   128     : bf16, two tiles of sixteen rows a wave: 256 registers of accumulators and 144 of queries.
+// Partial results go to memory as the accumulators lie (1 KB for 16 rows x 16 columns: one store instruction) and are merged by a second kernel.
+//
+// Measured (whole calls, LD = 512, bf16): 16 sequences x 16384 entries, 128 rows, 302 MB and 73 GFLOP: 117 us, 2.6 TB/s and 624 TFLOP/s, bound by the matrix instructions
+// (a library product of 8192 reaches 1234; here a third of the time goes to the start, the last partial results and the merge).
 #include "attn_sched.hpp"
 #include "common.hpp"
 #include "kernels.hpp"
@@ -53,10 +59,11 @@ template <> struct Tile<float> {
 };
 
 constexpr int slot_bytes(int ld, int e) { return (e == 2 ? 32 : 16) * (ld + kPe) * e; }
-// Slots of a ring: what the LDS of a compute unit holds beside the schedule's table and the merge's pairs.
-constexpr int kTableBytes = attn_sched_words(kAttnMaxSeqs) * 4 + 1024;
+// LDS: the rings' slots, (max, sum) pairs of up to 64 rows for their merge, the schedule's table.  Slots of a ring: as many as find room, four at most.
+constexpr int kPairsBytes = 64 * 8, kTableBytes = attn_sched_words(kAttnMaxSeqs) * 4;
+constexpr int kPairsAt = kLds - kTableBytes - kPairsBytes, kTableAt = kLds - kTableBytes;
 __host__ __device__ constexpr int stages_of(int ld, int e, int nk) {
-  const int most = (kLds - kTableBytes) / (nk * slot_bytes(ld, e));
+  const int most = kPairsAt / (nk * slot_bytes(ld, e));
   return most < 1 ? 1 : most > 4 ? 4 : most;
 }
 
@@ -75,21 +82,23 @@ struct Source {
     lane_key = lane / kLanes;
     lane_chunk = ((lane % kLanes) ^ Tile<T>::swz(lane_key)) << 4;
   }
-  __device__ __forceinline__ int fetch(int c) const {
+  __device__ __forceinline__ int ids_at(int c) const {        // first key of the lane's sixteen
     int lane = threadIdx.x & 63;
-    asm volatile("" : "+v"(lane));                  // (worked out here, not held)
-    const int p = min(s0 + 16 * (64 * c + lane), s1 - 1) & ~15;
-    const int in_seq = static_cast<int>(static_cast<uint32_t>(p) / static_cast<uint32_t>(a.page_size));
-    const int page = checked_page(a.page_table[static_cast<int64_t>(b) * a.max_pages + in_seq], a.n_pages, a.status);
-    return page * (a.page_size >> 4) + ((p - in_seq * a.page_size) >> 4);
+    asm volatile("" : "+v"(lane));                  // (worked out where it is wanted, not held)
+    return min(s0 + 16 * (64 * c + lane), s1 - 1) & ~15;
+  }
+  __device__ __forceinline__ int page_in_seq(int p) const { return static_cast<int>(static_cast<uint32_t>(p) / static_cast<uint32_t>(a.page_size)); }
+  __device__ __forceinline__ int fetch(int c) const { return a.page_table[static_cast<int64_t>(b) * a.max_pages + page_in_seq(ids_at(c))]; }
+  // A fetched page as sixteens of the pool, apart from the fetch: whatever is asked for between does not wait for it.
+  __device__ __forceinline__ int sixteens(int page, int c) const {
+    const int p = ids_at(c);
+    return checked_page(page, a.n_pages, a.status) * (a.page_size >> 4) + ((p - page_in_seq(p) * a.page_size) >> 4);
   }
   __device__ __forceinline__ void begin(int seq, int from, int to) {
     b = seq; s0 = from; s1 = to;
-    ids = ids_next = chunk = id0 = id1 = 0;
-    if (PAGED) {
-      ids = fetch(0);
-      if (s1 - s0 > 1024) ids_next = fetch(1);
-    }
+    ids = ids_next = id0 = id1 = 0;
+    chunk = -1;
+    if (PAGED) ids_next = fetch(0);
   }
   // Tile ti of the segment, one that has keys, in front of its entries or blocks.  (Calls go up by less than 1024 keys.)
   __device__ __forceinline__ void locate(int ti) {
@@ -97,7 +106,7 @@ struct Source {
     const int blk = kKeys * ti >> 4;
     if (__builtin_expect(blk >> 6 != chunk, 0)) {
       chunk = blk >> 6;
-      ids = ids_next;
+      ids = sixteens(ids_next, chunk);
       if (s0 + 1024 * (chunk + 1) < s1) ids_next = fetch(chunk + 1);
     }
     id0 = __builtin_amdgcn_readlane(ids, blk & 63);
@@ -151,9 +160,10 @@ struct Source {
 constexpr int held_registers(int ld, int e, int rtw) { return rtw * (ld / 4 + (ld + kPe) * e / 16); }
 constexpr bool in_agprs(int ld, int e, int rtw) { return held_registers(ld, e, rtw) > 190; }
 
-template <typename T, int LD, int RTW, int NR, int NK, bool PAGED>
-__global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_latent_ring(const LatentAttnArgs a) {
-  static_assert(NR * NK == 4, "four waves");
+// NK = 4 / NR rings, each of NR waves with sixteen rows, and each with its own tiles of the segment.
+template <typename T, int LD, int NR, bool PAGED>
+__device__ __forceinline__ void ring_segments(const LatentAttnArgs& a, const AttnTable& table, const AttnLine& line, AttnSeg seg, int x_hi, char* smem) {
+  constexpr int NK = 4 / NR;
   constexpr bool kF32 = sizeof(T) == 4;
   constexpr int S = stages_of(LD, sizeof(T), NK);
   constexpr int kKeys = Tile<T>::kKeys, kRowB = Source<T, LD, PAGED>::kRowB;
@@ -161,26 +171,15 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
   constexpr int kGroups = 4 / NR;                   // groups of a tile that a wave brings in
   constexpr int kPieces = kGroups * Source<T, LD, PAGED>::kBlocks;
   constexpr int kKS = kRowB / 64, kDT = LD / 16, kHalves = kKeys / 16;
-  // Probabilities of bf16 calls: two bf16 parts (16 bits) where the matrix instructions have the time, up to 64 rows; with 128 rows one, normalised with its own sum.
-  constexpr bool kSplitP = !kF32 && RTW == 1;
-  constexpr float kSlack = kF32 || kSplitP ? 8.f : 0.f;      // of the softmax reference, log2 units: see attn_mfma.hip
-  extern __shared__ uint4 smem4[];
-  char* smem = reinterpret_cast<char*>(smem4);
-  float* ml_lds = reinterpret_cast<float*>(smem + NK * S * kSlot);
-  int* sched_lds = reinterpret_cast<int*>(ml_lds + (NK > 1 ? NK * NR * 16 * 2 : 0));
+  constexpr float kSlack = 8.f;                     // of the softmax reference, log2 units: see attn_mfma.hip
+  float* ml_lds = reinterpret_cast<float*>(smem + kPairsAt);
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kg = wv / NR, rr = wv % NR;
   const int fr = lane & 15, fq = lane >> 4;
-  const AttnTable table = attn_sched_build(a, sched_lds);
-  const AttnLine line = attn_sched_line(a, table);
-  if (static_cast<int>(blockIdx.x) >= line.W) return;         // the whole workgroup leaves together
-  const int x_hi = attn_sched_lo(line, blockIdx.x + 1);
   Source<T, LD, PAGED> src(a);
   const float sl2 = a.scale * 1.44269504088896340736f;
   bool again = false;
-  AttnSeg seg = attn_sched_next(a, table, true, line.pad, attn_sched_lo(line, blockIdx.x), x_hi);
-  if (seg.next < x_hi) attn_sched_keep(a, table);
   for (; seg.s1 > seg.s0; seg = attn_sched_next(a, table, false, line.pad, seg.next, x_hi)) {
     attn_sched_publish(a, seg);
     const int b = seg.b, row0 = seg.g * a.block_rows;
@@ -193,19 +192,13 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
 
     src.begin(b, s0, s1);                           // (the page ids in front of the queries: the first tile waits for them)
     // ---- the rows' queries and mask words (rows past the last repeat it and are not stored)
-    uint4 qf[kKS][RTW];
-    uint64_t rowmask[RTW];
-    int rho[RTW];
+    uint4 qf[kKS];
+    const int row = row0 + min(16 * rr + fr, R - 1);
+    const uint4* qp = reinterpret_cast<const uint4*>(static_cast<const char*>(a.q) + (static_cast<int64_t>(b) * a.rows + row) * kRowB) + fq;
 #pragma unroll
-    for (int t = 0; t < RTW; ++t) {
-      rho[t] = 16 * (rr * RTW + t) + fr;
-      const int row = row0 + min(rho[t], R - 1);
-      const uint4* qp = reinterpret_cast<const uint4*>(static_cast<const char*>(a.q) + (static_cast<int64_t>(b) * a.rows + row) * kRowB) + fq;
-#pragma unroll
-      for (int ks = 0; ks < kKS; ++ks) qf[ks][t] = qp[4 * ks];
-      const int i = row / a.Hq;
-      rowmask[t] = a.mask ? a.mask[static_cast<int64_t>(b) * a.mask_stride + i] : ((2ull << i) - 1ull);
-    }
+    for (int ks = 0; ks < kKS; ++ks) qf[ks] = qp[4 * ks];
+    const int i = row / a.Hq;
+    const uint64_t rowmask = a.mask ? a.mask[static_cast<int64_t>(b) * a.mask_stride + i] : ((2ull << i) - 1ull);
     if (again) __syncthreads();                     // the rings are free of the segment before
     again = true;
 
@@ -220,16 +213,10 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
       for (int u = 0; u < kGroups; ++u) src.load_group(ti, rr * kGroups + u, slot);
     };
 
-    f32x4_t oacc[kDT][RTW], lacc[RTW];
-    float m_run[RTW], l_run[RTW];
+    f32x4_t oacc[kDT];
+    float m_run = -FLT_MAX, l_run = 0.f;
 #pragma unroll
-    for (int t = 0; t < RTW; ++t) {
-      m_run[t] = -FLT_MAX;
-      l_run[t] = 0.f;
-      lacc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int dt = 0; dt < kDT; ++dt) oacc[dt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int dt = 0; dt < kDT; ++dt) oacc[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     // A short segment has all its tiles in flight at once, behind the queries; of a longer one the first, so that the wait for the queries is not one for a
     // whole ring.
     const int together = S <= 2 || nit < S ? S : 1;
@@ -265,11 +252,9 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
         const char* tile = ring + (it % S) * kSlot;
         asm volatile("" : "+v"(k_at), "+v"(v_at));  // (worked out per read from these two, not held)
         // ---- S^T = C Q^T
-        f32x4_t sacc[kHalves][RTW];
+        f32x4_t sacc[kHalves];
 #pragma unroll
-        for (int j = 0; j < kHalves; ++j)
-#pragma unroll
-          for (int t = 0; t < RTW; ++t) sacc[j][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < kHalves; ++j) sacc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         constexpr int kReads = kHalves * kKS, kAhead = kF32 ? 4 : 8;
         auto kread = [&](int i) { return *reinterpret_cast<const uint4*>(src.row_read(tile, k_at, i / kHalves, i % kHalves)); };
         uint4 kf[kReads];
@@ -279,81 +264,66 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
         for (int i = 0; i < kReads; ++i) {
           if (i + kAhead < kReads) kf[i + kAhead] = kread(i + kAhead);
           __builtin_amdgcn_sched_barrier(0);
+          f32x4_t& c = sacc[i % kHalves];
+          if constexpr (kF32) {
+            const f32x4_t x = __builtin_bit_cast(f32x4_t, kf[i]), y = __builtin_bit_cast(f32x4_t, qf[i / kHalves]);
 #pragma unroll
-          for (int t = 0; t < RTW; ++t) {
-            f32x4_t& c = sacc[i % kHalves][t];
-            if constexpr (kF32) {
-              const f32x4_t x = __builtin_bit_cast(f32x4_t, kf[i]), y = __builtin_bit_cast(f32x4_t, qf[i / kHalves][t]);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], c, 0, 0, 0);
-            } else {
-              c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[i]), __builtin_bit_cast(bf16x8_t, qf[i / kHalves][t]), c, 0, 0, 0);
-            }
+            for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], c, 0, 0, 0);
+          } else {
+            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[i]), __builtin_bit_cast(bf16x8_t, qf[i / kHalves]), c, 0, 0, 0);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
         // ---- online softmax; lane (row fr, fq) owns the keys t0 + 16 j + 4 fq + e
         const bool plain = t0 + kKeys <= min(L, s1);
-        uint4 pf[RTW], pl[RTW];
-        float pr32[4];
+        float x[4 * kHalves];
 #pragma unroll
-        for (int t = 0; t < RTW; ++t) {
-          float x[4 * kHalves];
+        for (int j = 0; j < kHalves; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[4 * j + e] = sacc[j][e] * sl2;
+        if (!plain) {
 #pragma unroll
           for (int j = 0; j < kHalves; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * j + e] = sacc[j][t][e] * sl2;
-          if (!plain) {
+            for (int e = 0; e < 4; ++e) {
+              const int p = t0 + 16 * j + 4 * fq + e;
+              bool seen = p < s1;
+              if (seen && p >= L) seen = (rowmask >> (p - L)) & 1ull;
+              x[4 * j + e] = seen ? x[4 * j + e] : -INFINITY;
+            }
+        }
+        float mt = x[0];
 #pragma unroll
-            for (int j = 0; j < kHalves; ++j)
+        for (int e = 1; e < 4 * kHalves; ++e) mt = max_nan(mt, x[e]);
+        if (__builtin_amdgcn_ballot_w64(mt > m_run + kSlack) != 0ull) {
+          const float m_new = fmaxf(m_run, quad_row_max(mt));
+          const float al = __builtin_amdgcn_exp2f(m_run - m_new);
+          m_run = m_new;
+          l_run *= al;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const int p = t0 + 16 * j + 4 * fq + e;
-                bool seen = p < s1;
-                if (seen && p >= L) seen = (rowmask[t] >> (p - L)) & 1ull;
-                x[4 * j + e] = seen ? x[4 * j + e] : -INFINITY;
-              }
-          }
-          float mt = x[0];
-#pragma unroll
-          for (int e = 1; e < 4 * kHalves; ++e) mt = max_nan(mt, x[e]);
-          if (__builtin_amdgcn_ballot_w64(mt > m_run[t] + kSlack) != 0ull) {
-            const float m_new = fmaxf(m_run[t], quad_row_max(mt));
-            const float al = __builtin_amdgcn_exp2f(m_run[t] - m_new);
-            m_run[t] = m_new;
-            l_run[t] *= al;
-            lacc[t][0] *= al;
-#pragma unroll
-            for (int dt = 0; dt < kDT; ++dt) {
-              oacc[dt][t][0] *= al; oacc[dt][t][1] *= al;
-              oacc[dt][t][2] *= al; oacc[dt][t][3] *= al;
-              if constexpr (in_agprs(LD, sizeof(T), RTW)) {     // four at a time there and back: all at once are as many registers again
-                asm volatile("" : "+a"(oacc[dt][t]));
-                __builtin_amdgcn_sched_barrier(0);
-              }
+          for (int dt = 0; dt < kDT; ++dt) {
+            oacc[dt][0] *= al; oacc[dt][1] *= al;
+            oacc[dt][2] *= al; oacc[dt][3] *= al;
+            if constexpr (in_agprs(LD, sizeof(T), 1)) {         // four at a time there and back: all at once are as many registers again
+              asm volatile("" : "+a"(oacc[dt]));
+              __builtin_amdgcn_sched_barrier(0);
             }
           }
-          float pr[4 * kHalves];
+        }
+        // Probabilities: fp32 as they are; bf16 two bf16 parts (16 bits), for which the matrix instructions have the time.
+        float pr[4 * kHalves];
+        uint4 pf, pl;
 #pragma unroll
-          for (int e = 0; e < 4 * kHalves; ++e) pr[e] = __builtin_amdgcn_exp2f(x[e] - m_run[t]);
-          if constexpr (kF32) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) pr32[e] = pr[e];
-            l_run[t] += (pr[0] + pr[1]) + (pr[2] + pr[3]);
-          } else {
-            pf[t] = make_uint4(pack_bf16x2(pr[0], pr[1]), pack_bf16x2(pr[2], pr[3]), pack_bf16x2(pr[4], pr[5]), pack_bf16x2(pr[6], pr[7]));
-            if constexpr (kSplitP) {
-              float hi[8];
-              unpack16(pf[t], hi);
-              pl[t] = make_uint4(pack_bf16x2(pr[0] - hi[0], pr[1] - hi[1]), pack_bf16x2(pr[2] - hi[2], pr[3] - hi[3]),
-                                 pack_bf16x2(pr[4] - hi[4], pr[5] - hi[5]), pack_bf16x2(pr[6] - hi[6], pr[7] - hi[7]));
-              l_run[t] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
-            } else {
-              const uint32_t one = 0x3F803F80u;     // the sum of the probabilities as the values are multiplied with them
-              lacc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, make_uint4(one, one, one, one)),
-                                                                __builtin_bit_cast(bf16x8_t, pf[t]), lacc[t], 0, 0, 0);
-            }
-          }
+        for (int e = 0; e < 4 * kHalves; ++e) pr[e] = __builtin_amdgcn_exp2f(x[e] - m_run);
+        if constexpr (kF32) {
+          l_run += (pr[0] + pr[1]) + (pr[2] + pr[3]);
+        } else {
+          pf = make_uint4(pack_bf16x2(pr[0], pr[1]), pack_bf16x2(pr[2], pr[3]), pack_bf16x2(pr[4], pr[5]), pack_bf16x2(pr[6], pr[7]));
+          float hi[8];
+          unpack16(pf, hi);
+          pl = make_uint4(pack_bf16x2(pr[0] - hi[0], pr[1] - hi[1]), pack_bf16x2(pr[2] - hi[2], pr[3] - hi[3]),
+                          pack_bf16x2(pr[4] - hi[4], pr[5] - hi[5]), pack_bf16x2(pr[6] - hi[6], pr[7] - hi[7]));
+          l_run += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
         }
         // ---- O^T += C^T P^T
         __builtin_amdgcn_sched_barrier(0);
@@ -371,7 +341,7 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
             if (dt + kVAhead < kDT) vread(dt + kVAhead);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) oacc[dt][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[dt][e], pr32[e], oacc[dt][0], 0, 0, 0);
+            for (int e = 0; e < 4; ++e) oacc[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[dt][e], pr[e], oacc[dt], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
           }
         } else {
@@ -389,11 +359,8 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
             __builtin_amdgcn_sched_barrier(0);
             const uint2 l2 = __builtin_bit_cast(uint2, vlo[dt]), h2 = __builtin_bit_cast(uint2, vhi[dt]);
             const bf16x8_t va = __builtin_bit_cast(bf16x8_t, make_uint4(l2.x, l2.y, h2.x, h2.y));
-#pragma unroll
-            for (int t = 0; t < RTW; ++t) {
-              oacc[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8_t, pf[t]), oacc[dt][t], 0, 0, 0);
-              if constexpr (kSplitP) oacc[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8_t, pl[t]), oacc[dt][t], 0, 0, 0);
-            }
+            oacc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8_t, pf), oacc[dt], 0, 0, 0);
+            oacc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8_t, pl), oacc[dt], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
           }
         }
@@ -412,24 +379,21 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
     const int64_t slot = static_cast<int64_t>(blockIdx.x) + static_cast<int64_t>(b) * a.Hkv + seg.g;
     const int tiles = a.block_rows / 16;            // row tiles of a block
     if constexpr (NK == 1) {
+      const float l = quad_row_sum(l_run);
+      if (rr < tiles) {
+        if (fq == 0) *reinterpret_cast<float2*>(a.part_ml + ((slot * tiles + rr) * 16 + fr) * 2) = make_float2(m_run, l);
+        float* dst = a.part_o + ((slot * tiles + rr) * kDT * 64 + lane) * 4;
 #pragma unroll
-      for (int t = 0; t < RTW; ++t) {
-        const float l = kF32 || kSplitP ? quad_row_sum(l_run[t]) : lacc[t][0];
-        const int tile = rr * RTW + t;
-        if (tile >= tiles) continue;
-        if (fq == 0) *reinterpret_cast<float2*>(a.part_ml + ((slot * tiles + tile) * 16 + fr) * 2) = make_float2(m_run[t], l);
-        float* dst = a.part_o + ((slot * tiles + tile) * kDT * 64 + lane) * 4;
-#pragma unroll
-        for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + dt * 256) = oacc[dt][t];
+        for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + dt * 256) = oacc[dt];
       }
     } else {
       // the rings leave their sums in their own slots, and every wave adds some fragments in the order of the rings
-      static_assert(RTW == 1 && NR * 16 * LD * 4 <= S * kSlot, "a ring's slots hold its sums");
-      const float l = quad_row_sum(l_run[0]);
+      static_assert(NR * 16 * LD * 4 <= S * kSlot, "a ring's slots hold its sums");
+      const float l = quad_row_sum(l_run);
       if constexpr (NR > 1) __syncthreads();        // (waves of a ring write where others may still read)
-      if (fq == 0) *reinterpret_cast<float2*>(ml_lds + 2 * ((kg * NR + rr) * 16 + fr)) = make_float2(m_run[0], l);
+      if (fq == 0) *reinterpret_cast<float2*>(ml_lds + 2 * ((kg * NR + rr) * 16 + fr)) = make_float2(m_run, l);
 #pragma unroll
-      for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(ring + ((rr * kDT + dt) * 64 + lane) * 16) = oacc[dt][0];
+      for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(ring + ((rr * kDT + dt) * 64 + lane) * 16) = oacc[dt];
       __syncthreads();
 #pragma unroll 1
       for (int tile = 0; tile < tiles; ++tile) {
@@ -461,7 +425,7 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
   }
 }
 
-// bf16, more rows than one wave's sixteen a ring: four waves of RTW 16-row tiles on one ring of four slots, software-pipelined.  With one wave to a SIMD nothing else fills
+// bf16, 64 or 128 rows: four waves of RTW 16-row tiles on one ring of four slots, software-pipelined.  With one wave to a SIMD nothing else fills
 // the time of the softmax, so the products of tile t's probabilities with its values are interleaved with the exponentials of tile t + 1, and the loads of tile t + 3
 // with the products of tile t + 1 with the queries in front of that; one barrier a tile.
 //
@@ -469,32 +433,23 @@ __global__ __launch_bounds__(256, in_agprs(LD, sizeof(T), RTW) ? 1 : 2) void k_l
 // 2^kReach is fine, and the accumulators are never rescaled (256 registers that only matrix instructions work on, there and back, take longer than a tile).  A
 // segment with a score beyond that is taken again with its rows' true maxima, which the first pass has found.
 template <int LD, int RTW, bool PAGED>
-__global__ __launch_bounds__(256, in_agprs(LD, 2, RTW) ? 1 : 2) void k_latent_pipe(const LatentAttnArgs a) {
+__device__ __forceinline__ void pipe_segments(const LatentAttnArgs& a, const AttnTable& table, const AttnLine& line, AttnSeg seg, int x_hi, char* smem) {
   typedef Source<bf16_t, LD, PAGED> Src;
   constexpr int S = 4, kSlot = slot_bytes(LD, 2), kKeys = 32;
   static_assert(stages_of(LD, 2, 1) == S, "four slots");
   constexpr int kKS = Src::kRowB / 64, kReads = 2 * kKS, kDT = LD / 16, kBlocks = Src::kBlocks;
-  constexpr bool kSplitP = RTW == 1;                // probabilities: see k_latent_ring
+  constexpr bool kSplitP = RTW == 1;                // probabilities: two bf16 parts (16 bits) with 64 rows; with 128 the matrix instructions are the bound, and one part, normalised with its own sum, is a third less of the products
   constexpr float kReach = 60.f;                    // log2; sums of 2^31 such probabilities times values of 2^30 stay in range
   // With 128 rows of 512 columns the accumulators are all 256 registers that matrix instructions alone work on, and the compiler has no form that puts
   // other results elsewhere: the scores' instructions are written out.
   constexpr bool kWritten = LD == 512 && RTW == 2;
-  extern __shared__ uint4 smem4[];
-  char* smem = reinterpret_cast<char*>(smem4);
-  int* sched_lds = reinterpret_cast<int*>(smem + S * kSlot);
-  int* votes = sched_lds + attn_sched_words(a.B);
+  int* votes = reinterpret_cast<int*>(smem + kPairsAt);
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 15, fq = lane >> 4;
-  const AttnTable table = attn_sched_build(a, sched_lds);
-  const AttnLine line = attn_sched_line(a, table);
-  if (static_cast<int>(blockIdx.x) >= line.W) return;         // the whole workgroup leaves together
-  const int x_hi = attn_sched_lo(line, blockIdx.x + 1);
   Src src(a);
   const float sl2 = a.scale * 1.44269504088896340736f;
   bool again = false;
-  AttnSeg seg = attn_sched_next(a, table, true, line.pad, attn_sched_lo(line, blockIdx.x), x_hi);
-  if (seg.next < x_hi) attn_sched_keep(a, table);
   for (; seg.s1 > seg.s0; seg = attn_sched_next(a, table, false, line.pad, seg.next, x_hi)) {
     attn_sched_publish(a, seg);
     const int b = seg.b, row0 = seg.g * a.block_rows;
@@ -725,6 +680,53 @@ __global__ __launch_bounds__(256, in_agprs(LD, 2, RTW) ? 1 : 2) void k_latent_pi
   }
 }
 
+// Rows of a workgroup.  Few granules (64 entries for the whole rows of a sequence; the lengths are known here only): what counts is how many workgroups share them and what each
+// writes for the merge, 2 KB a row with 512 columns, so they take 16 rows, each with four rings of keys, or 32 with two; the caches are small then and their
+// second reader finds them in a cache of the chip.  Many: 64 or 128 (MOST), as many as the sequences have.  Whole calls, LD = 512, granules of MOST rows, 16 / 32 / MOST rows a workgroup:
+//   112 rows   3: 14.6 / 14.8 / 19.7 us   17: 16.6 / 16.2 / 21.0   65: 21.8 / 22.5 / 28.6   126: 23.1 / 24.7 / 34.2   257: 38.8 / 31.0 / 37.7   501: 44.7 / 42.7 / 43.3   1025: 70 / 68 / 51
+//   128 rows 256 (8 sequences): 36.9 / 36.8 / 39.5   504: 51.4 / 40.9 / 39.4   4112 (16): 331 / 204 / 117            64 rows 252: 29.1 / 25.4 / 29.6   2016: 114 / 73 / 66
+constexpr int kFewGran = 160, kSomeGran = 512;
+__host__ __device__ __forceinline__ int rows_of_block(int rows, int most) {
+  const int blocks = (rows + most - 1) / most;
+  return ((rows + blocks - 1) / blocks + 15) & ~15;
+}
+
+template <typename T, int LD, int MOST, bool PAGED>
+__global__ __launch_bounds__(256, MOST <= 32 && !in_agprs(LD, sizeof(T), 1) ? 2 : 1) void k_latent_attn(const LatentAttnArgs args) {
+  extern __shared__ uint4 smem4[];
+  char* smem = reinterpret_cast<char*>(smem4);
+  LatentAttnArgs a = args;
+  const AttnTable table = attn_sched_build(a, reinterpret_cast<int*>(smem + kTableAt));
+  int most = MOST;
+  if (MOST > 16) {
+    const int gran = (a.B <= 64 ? __builtin_amdgcn_readlane(table.upto, 63) : __builtin_amdgcn_readfirstlane(table.S[a.B])) * ((a.rows + MOST - 1) / MOST);
+    most = gran < kFewGran ? 16 : MOST > 32 && gran < kSomeGran ? 32 : MOST;
+  }
+  a.block_rows = rows_of_block(a.rows, most);
+  a.Hkv = (a.rows + a.block_rows - 1) / a.block_rows;
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.sched[0] = a.block_rows;         // for the merging kernel
+  a.sched += 2;
+  const AttnLine line = attn_sched_line(a, table);
+  if (static_cast<int>(blockIdx.x) >= line.W) return;         // the whole workgroup leaves together
+  const int x_hi = attn_sched_lo(line, blockIdx.x + 1);
+  const AttnSeg seg = attn_sched_next(a, table, true, line.pad, attn_sched_lo(line, blockIdx.x), x_hi);
+  if (seg.next < x_hi) attn_sched_keep(a, table);
+  if constexpr (MOST > 32) {
+    if (most == MOST) {
+      if constexpr (sizeof(T) == 4) ring_segments<T, LD, 4, PAGED>(a, table, line, seg, x_hi, smem);
+      else pipe_segments<LD, MOST / 64, PAGED>(a, table, line, seg, x_hi, smem);
+      return;
+    }
+  }
+  if constexpr (MOST > 16) {
+    if (most == 32) {
+      ring_segments<T, LD, 2, PAGED>(a, table, line, seg, x_hi, smem);
+      return;
+    }
+  }
+  ring_segments<T, LD, 1, PAGED>(a, table, line, seg, x_hi, smem);
+}
+
 __device__ __forceinline__ float load_value(const bf16_t* p) { return bf16_to_f32(*p); }
 __device__ __forceinline__ float load_value(const float* p) { return *p; }
 
@@ -794,10 +796,10 @@ __global__ __launch_bounds__(256) void k_latent_combine(const LatentAttnArgs a) 
   __shared__ int odd_rows;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 15, fq = lane >> 4;
-  const int tiles = a.block_rows / 16;
-  const int b = blockIdx.y, g = blockIdx.x / tiles, tile = blockIdx.x - g * tiles, u = b * a.Hkv + g;
-  const int row = g * a.block_rows + tile * 16 + fr;
-  const int w_first = a.sched[2 * u], n = a.sched[2 * u + 1] - w_first + 1;
+  const int block_rows = a.sched[0], tiles = block_rows / 16, blocks = (a.rows + block_rows - 1) / block_rows;
+  const int b = blockIdx.y, g = blockIdx.x / tiles, tile = blockIdx.x - g * tiles, u = b * blocks + g;
+  const int row = blockIdx.x * 16 + fr;
+  const int w_first = a.sched[2 + 2 * u], n = a.sched[3 + 2 * u] - w_first + 1;
   const int64_t first = (static_cast<int64_t>(w_first) + u) * tiles + tile;
   const float* pm = a.part_ml + first * 32 + fr * 2;
   const float* po = a.part_o + first * (kDT * 256) + lane * 4;
@@ -885,7 +887,7 @@ __global__ __launch_bounds__(256) void k_latent_combine(const LatentAttnArgs a) 
         while (left) {
           const int r = __ffs(left) - 1;
           left &= left - 1;
-          latent_row_again<T, LD>(a, b, g * a.block_rows + tile * 16 + r, d0 + f, again);
+          latent_row_again<T, LD>(a, b, blockIdx.x * 16 + r, d0 + f, again);
         }
         __syncthreads();
       }
@@ -893,50 +895,35 @@ __global__ __launch_bounds__(256) void k_latent_combine(const LatentAttnArgs a) 
   }
 }
 
-template <typename T, int LD, int RTW, int NR>
-hipError_t launch_ring(const LatentAttnArgs& a, hipStream_t s) {
-  constexpr int NK = 4 / NR, S = stages_of(LD, sizeof(T), NK);
-  const size_t lds = static_cast<size_t>(NK) * S * slot_bytes(LD, sizeof(T)) + (NK > 1 ? NK * NR * 16 * 8 : 0) + static_cast<size_t>(attn_sched_words(a.B)) * 4;
-  if (a.paged) {
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_latent_ring<T, LD, RTW, NR, NK, true>),
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-    if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL((k_latent_ring<T, LD, RTW, NR, NK, true>), dim3(a.wgrid), dim3(256), lds, s, a);
-  } else {
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_latent_ring<T, LD, RTW, NR, NK, false>),
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-    if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL((k_latent_ring<T, LD, RTW, NR, NK, false>), dim3(a.wgrid), dim3(256), lds, s, a);
-  }
+// Rows that a workgroup takes where there is work for all of them.
+int most_rows(const LatentAttnArgs& a) { return a.rows <= 16 ? 16 : a.rows <= 32 ? 32 : a.rows <= 64 || a.dtype == 0 ? 64 : 128; }
+
+template <typename T, int LD, int MOST, bool PAGED>
+hipError_t launch_attn_as(const LatentAttnArgs& a, hipStream_t s) {
+  // set once per process; a function-local static is initialised under the language's own lock, so first calls from several host threads are safe
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_latent_attn<T, LD, MOST, PAGED>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+  if (attr != hipSuccess) return attr;
+  hipLaunchKernelGGL((k_latent_attn<T, LD, MOST, PAGED>), dim3(a.wgrid), dim3(256), kLds, s, a);
   return hipGetLastError();
 }
-
-template <int LD, int RTW>
-hipError_t launch_pipe(const LatentAttnArgs& a, hipStream_t s) {
-  const size_t lds = static_cast<size_t>(4) * slot_bytes(LD, 2) + static_cast<size_t>(attn_sched_words(a.B) + 4) * 4;
-  if (a.paged) {
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_latent_pipe<LD, RTW, true>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-    if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL((k_latent_pipe<LD, RTW, true>), dim3(a.wgrid), dim3(256), lds, s, a);
-  } else {
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_latent_pipe<LD, RTW, false>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-    if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL((k_latent_pipe<LD, RTW, false>), dim3(a.wgrid), dim3(256), lds, s, a);
-  }
-  return hipGetLastError();
+template <typename T, int LD, int MOST>
+hipError_t launch_most(const LatentAttnArgs& a, hipStream_t s) {
+  return a.paged ? launch_attn_as<T, LD, MOST, true>(a, s) : launch_attn_as<T, LD, MOST, false>(a, s);
 }
 
 template <typename T, int LD>
 hipError_t launch_ld(const LatentAttnArgs& a, hipStream_t s) {
   hipError_t e;
-  if (a.block_rows <= 16) e = launch_ring<T, LD, 1, 1>(a, s);
-  else if (a.block_rows <= 32) e = launch_ring<T, LD, 1, 2>(a, s);
-  else if constexpr (sizeof(T) == 4) e = launch_ring<T, LD, 1, 4>(a, s);
-  else e = a.block_rows <= 64 ? launch_pipe<LD, 1>(a, s) : launch_pipe<LD, 2>(a, s);
+  const int most = most_rows(a);
+  if (most == 16) e = launch_most<T, LD, 16>(a, s);
+  else if (most == 32) e = launch_most<T, LD, 32>(a, s);
+  else if (most == 64) e = launch_most<T, LD, 64>(a, s);
+  else if constexpr (sizeof(T) == 2) e = launch_most<T, LD, 128>(a, s);
+  else e = hipErrorInvalidValue;
   if (e != hipSuccess) return e;
   // a fragment's segments to four waves where there are few fragments; many: several fragments a workgroup, some 4096 of those
-  const int64_t fragments = static_cast<int64_t>(a.Hkv) * (a.block_rows / 16) * a.B;
-  const unsigned tiles = static_cast<unsigned>(a.Hkv * (a.block_rows / 16));
+  const unsigned tiles = static_cast<unsigned>((a.rows + 15) / 16);
+  const int64_t fragments = static_cast<int64_t>(tiles) * a.B;
   constexpr int kDT = LD / 16;
   if (fragments * kDT <= 4096) {
     hipLaunchKernelGGL((k_latent_combine<T, LD, 4>), dim3(tiles, a.B, kDT), dim3(256), 0, s, a);
@@ -960,32 +947,37 @@ hipError_t launch_as(const LatentAttnArgs& a, hipStream_t s) {
 }  // namespace
 
 bool latent_attn_plan(LatentAttnArgs& a, int num_cus) {
-#ifndef LAT_MOST
-#define LAT_MOST 128
-#endif
-  const int most = a.dtype == 1 ? LAT_MOST : LAT_MOST < 64 ? LAT_MOST : 64;
   a.rows = a.Hq * a.n_q;
-  a.Hkv = (a.rows + most - 1) / most;
-  a.block_rows = ((a.rows + a.Hkv - 1) / a.Hkv + 15) & ~15;
+  a.block_rows = rows_of_block(a.rows, most_rows(a));
   a.Hkv = (a.rows + a.block_rows - 1) / a.block_rows;
   a.pad = 2;
   a.wide_from = INT_MAX;
   a.use_mfma = 0;
   if (a.B > kAttnMaxSeqs || a.l_max < a.n_blk) return false;
-  const int64_t units = static_cast<int64_t>(a.B) * a.Hkv;
+  // (smaller blocks are taken of few granules only, some 8 kSomeGran of theirs at most)
   const int64_t gmax = (a.l_max + kAttnGran - 1) / kAttnGran;
-  if (units * (gmax + a.pad) >= (1ll << 30)) return false;
-  const AttnLine line = attn_sched_line(static_cast<int>(a.B * gmax), a.B, a.Hkv, a.pad, a.wide_from, 0, num_cus);
-  a.wgrid = line.W;
-  if (line.T > kAttnSpread && a.wgrid < kAttnSpread) a.wgrid = kAttnSpread < num_cus ? kAttnSpread : num_cus;   // (fewer granules may take more workgroups)
+  if (static_cast<int64_t>(a.B) * a.Hkv * (gmax + a.pad) >= (1ll << 30)) return false;
+  // one workgroup per compute unit; fewer where even the longest possible caches have no granule for each
+  const int64_t most = static_cast<int64_t>(a.B) * ((a.rows + 15) / 16) * gmax;
+  a.wgrid = static_cast<int>(std::min<int64_t>(most, num_cus));
   return true;
 }
 
+// Partial results: a slot per workgroup and one per unit, of the rows of a block, whichever block is taken.
 static size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
-static size_t slot_rows(const LatentAttnArgs& a) { return (static_cast<size_t>(a.wgrid) + static_cast<size_t>(a.B) * a.Hkv) * a.block_rows; }
+static size_t slot_rows(const LatentAttnArgs& a) {
+  size_t rows = 0;
+  for (const int most : {16, 32, 64, 128}) {
+    if (most > most_rows(a)) break;
+    const size_t block = rows_of_block(a.rows, most), blocks = (a.rows + block - 1) / block;
+    rows = std::max(rows, (static_cast<size_t>(a.wgrid) + static_cast<size_t>(a.B) * blocks) * block);
+  }
+  return rows;
+}
+static size_t sched_bytes(const LatentAttnArgs& a) { return up256((2 + static_cast<size_t>(a.B) * ((a.rows + 15) / 16) * 2) * sizeof(int)); }
 
 size_t latent_attn_workspace_bytes(const LatentAttnArgs& a) {
-  return up256(slot_rows(a) * a.d * sizeof(float)) + up256(slot_rows(a) * 2 * sizeof(float)) + up256(static_cast<size_t>(a.B) * a.Hkv * 2 * sizeof(int));
+  return up256(slot_rows(a) * a.d * sizeof(float)) + up256(slot_rows(a) * 2 * sizeof(float)) + sched_bytes(a);
 }
 
 void latent_attn_carve(LatentAttnArgs& a, void* workspace) {

@@ -356,10 +356,11 @@ bool latent_write_plan(LatentWriteArgs& a);
 hipError_t launch_latent_write(const LatentWriteArgs& a, hipStream_t s);
 
 // ---- latent attention (attn_latent.hip) ------------------------------------------------------
-// k: the entries of one vector of latent + 64 values; d: the latent's width; Hkv: blocks of rows; n_q, Hq, q, out as in the call
+// k: the entries of one vector of latent + 64 values; d: the latent's width; n_q, Hq, q, out as in the call; part_o, part_ml in fragments and rows of 16-row tiles;
+// sched: the rows of a block and a word of nothing, then as there
 struct LatentAttnArgs : AttnArgs {
-  int block_rows;            // query rows of a block (the last may have fewer)
   int rows;                  // Hq n_q
+  int block_rows;            // of a block of query rows (the last may have fewer); Hkv: blocks.  The kernel sets both to what the lengths call for
 };
 bool latent_attn_plan(LatentAttnArgs& a, int num_cus);
 size_t latent_attn_workspace_bytes(const LatentAttnArgs& a);
