@@ -23,7 +23,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kNarrow = 16, kWide = 32;                    // values of a lane
-constexpr int kMostParts = 272;                            // parts of a row (512 logits x 16 ..)
+constexpr int kMostParts = 272;                            // parts of a row at most: 2^18 logits, 1024 a part
 constexpr int kList = 1536;                                // candidates
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 
@@ -286,9 +286,9 @@ __global__ __launch_bounds__(kThreads) void k_logprob_row(const LogprobArgs a) {
         keep(f, place_of(i + wv), lane < kLanes);
       }
       __syncthreads();
-      if (listed > kList - kWaves * 64 * N || i + kWaves >= count) {
-        const int have = listed;
-        __syncthreads();
+      const int have = listed;                            // (read by all in front of the next barrier: a wave that goes on adds to it)
+      __syncthreads();
+      if (have > kList - kWaves * 64 * N || i + kWaves >= count) {
         rank_keys(list, have, a.n_top, ranked);
         __syncthreads();
         if (tid < a.n_top) list[tid] = ranked[tid];
