@@ -197,8 +197,10 @@ __device__ __forceinline__ void ring_segments(const LatentAttnArgs& a, const Att
     const uint4* qp = reinterpret_cast<const uint4*>(static_cast<const char*>(a.q) + (static_cast<int64_t>(b) * a.rows + row) * kRowB) + fq;
 #pragma unroll
     for (int ks = 0; ks < kKS; ++ks) qf[ks] = qp[4 * ks];
+    // (a load either way, without a mask of a query's bytes: a branch would wait for the queries in front of the first tiles)
     const int i = row / a.Hq;
-    const uint64_t rowmask = a.mask ? a.mask[static_cast<int64_t>(b) * a.mask_stride + i] : ((2ull << i) - 1ull);
+    const uint64_t* mask_at = a.mask ? a.mask + static_cast<int64_t>(b) * a.mask_stride : static_cast<const uint64_t*>(a.q);
+    uint64_t rowmask = mask_at[a.mask ? i : 0];
     if (again) __syncthreads();                     // the rings are free of the segment before
     again = true;
 
@@ -227,6 +229,8 @@ __device__ __forceinline__ void ring_segments(const LatentAttnArgs& a, const Att
     }
     int k_at = src.rows_at(fr, fq), v_at = src.columns_at(fr, fq);
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));       // from here on vmcnt counts tile loads only
+    __builtin_amdgcn_sched_barrier(0);
+    if (!a.mask) rowmask = (2ull << i) - 1ull;
     if constexpr (S > 2) {
 #pragma unroll 1
       for (int it = together; it < S; ++it) {
@@ -409,17 +413,19 @@ __device__ __forceinline__ void ring_segments(const LatentAttnArgs& a, const Att
           sum = fmaf(f[k], ml_lds[2 * ((k * NR + tile) * 16 + fr) + 1], sum);
         }
         if (wv == 0 && fq == 0) *reinterpret_cast<float2*>(a.part_ml + ((slot * tiles + tile) * 16 + fr) * 2) = make_float2(mm, sum);
-#pragma unroll 2
-        for (int dt = wv; dt < kDT; dt += 4) {
-          f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+        constexpr int kEach = kDT / 4;              // fragments of a wave, all read together
+        f32x4_t v[kEach];
 #pragma unroll
-          for (int k = 0; k < NK; ++k) {
-            const f32x4_t o = *reinterpret_cast<const f32x4_t*>(smem + k * (S * kSlot) + ((tile * kDT + dt) * 64 + lane) * 16);
+        for (int k = 0; k < NK; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = fmaf(f[k], o[e], v[e]);
+          for (int u = 0; u < kEach; ++u) {
+            const f32x4_t o = *reinterpret_cast<const f32x4_t*>(smem + k * (S * kSlot) + ((tile * kDT + wv * kEach + u) * 64 + lane) * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[u][e] = k ? fmaf(f[k], o[e], v[u][e]) : f[k] * o[e];
           }
-          *reinterpret_cast<f32x4_t*>(a.part_o + (((slot * tiles + tile) * kDT + dt) * 64 + lane) * 4) = v;
-        }
+        float* dst = a.part_o + (((slot * tiles + tile) * kDT + wv * kEach) * 64 + lane) * 4;
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) *reinterpret_cast<f32x4_t*>(dst + u * 256) = v[u];
       }
     }
   }
@@ -785,11 +791,11 @@ __device__ __forceinline__ void latent_row_again(const LatentAttnArgs& a, int b,
 
 // Merge the segments of sixteen rows: exact log-sum-exp combination.  Partial results lie as the matrix instructions leave them, a 1 KB fragment for sixteen rows and
 // sixteen columns, and are read and added that way: (max, sum) pairs and fragments of a wave's segments in one round of requests, the WS waves that share a fragment's
-// segments in a fixed order.
-constexpr int kCombAhead = 8;
+// segments in a fixed order.  (What is not there is not asked for: with the last segment again in its place the merge of 272 segments of 128 rows x 512 columns, 71 MB, took 17.3
+// us, 15.4 this way; with four waves a fragment there 24.6.)
 template <typename T, int LD, int WS>
 __global__ __launch_bounds__(256) void k_latent_combine(const LatentAttnArgs a) {
-  constexpr int kDT = LD / 16, kPer = 4 / WS;
+  constexpr int kDT = LD / 16, kPer = 4 / WS, kCombAhead = WS == 1 ? 8 : 12;
   __shared__ f32x4_t part[4][64];
   __shared__ float2 part_ml[4][16];
   __shared__ float again[4][18];
@@ -799,7 +805,7 @@ __global__ __launch_bounds__(256) void k_latent_combine(const LatentAttnArgs a) 
   const int block_rows = a.sched[0], tiles = block_rows / 16, blocks = (a.rows + block_rows - 1) / block_rows;
   const int b = blockIdx.y, g = blockIdx.x / tiles, tile = blockIdx.x - g * tiles, u = b * blocks + g;
   const int row = blockIdx.x * 16 + fr;
-  const int w_first = a.sched[2 + 2 * u], n = a.sched[3 + 2 * u] - w_first + 1;
+  const int w_first = a.sched[2 + 2 * u], n = __builtin_amdgcn_readfirstlane(a.sched[3 + 2 * u] - w_first + 1);
   const int64_t first = (static_cast<int64_t>(w_first) + u) * tiles + tile;
   const float* pm = a.part_ml + first * 32 + fr * 2;
   const float* po = a.part_o + first * (kDT * 256) + lane * 4;
@@ -815,10 +821,17 @@ __global__ __launch_bounds__(256) void k_latent_combine(const LatentAttnArgs a) 
       float2 ml[kCombAhead];
 #pragma unroll
       for (int e = 0; e < kCombAhead; ++e) {
-        const int s = min(s0 + e * WS, n - 1);
+        o[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        ml[e] = make_float2(-FLT_MAX, 0.f);
+      }
+#pragma unroll
+      for (int e = 0; e < kCombAhead; ++e) {
+        const int s = s0 + e * WS;
+        if (s >= n) break;                          // (uniform)
         o[e] = *reinterpret_cast<const f32x4_t*>(po + s * po_step + dt * 256);
         ml[e] = *reinterpret_cast<const float2*>(pm + s * pm_step);
       }
+      __builtin_amdgcn_sched_barrier(0);
       float m_new = m;
 #pragma unroll
       for (int e = 0; e < kCombAhead; ++e) m_new = fmaxf(m_new, ml[e].x);
@@ -829,7 +842,8 @@ __global__ __launch_bounds__(256) void k_latent_combine(const LatentAttnArgs a) 
       for (int c = 0; c < 4; ++c) acc[c] *= old;
 #pragma unroll
       for (int e = 0; e < kCombAhead; ++e) {
-        const float w = s0 + e * WS < n ? __builtin_amdgcn_exp2f(ml[e].x - m) : 0.f;
+        if (s0 + e * WS >= n) break;
+        const float w = __builtin_amdgcn_exp2f(ml[e].x - m);
         if (w != 0.f) {                             // (a weight of nothing counts nothing, whatever is there)
           den = fmaf(w, ml[e].y, den);
 #pragma unroll
@@ -925,7 +939,7 @@ hipError_t launch_ld(const LatentAttnArgs& a, hipStream_t s) {
   const unsigned tiles = static_cast<unsigned>((a.rows + 15) / 16);
   const int64_t fragments = static_cast<int64_t>(tiles) * a.B;
   constexpr int kDT = LD / 16;
-  if (fragments * kDT <= 4096) {
+  if (fragments * kDT < 4096) {
     hipLaunchKernelGGL((k_latent_combine<T, LD, 4>), dim3(tiles, a.B, kDT), dim3(256), 0, s, a);
   } else {
     const unsigned z = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(kDT / 4, 4096 / fragments)));
