@@ -160,6 +160,22 @@ struct Source {
 constexpr int held_registers(int ld, int e, int rtw) { return rtw * (ld / 4 + (ld + kPe) * e / 16); }
 constexpr bool in_agprs(int ld, int e, int rtw) { return held_registers(ld, e, rtw) > 190; }
 
+// Until at most `blocks` blocks of GROUPS loads each are outstanding (a constant where it is called: the instruction has no other form).
+template <int GROUPS>
+__device__ __forceinline__ void wait_blocks(int blocks) {
+  switch (blocks) {
+    case 8: __builtin_amdgcn_s_waitcnt(vmcnt_imm(8 * GROUPS)); break;
+    case 7: __builtin_amdgcn_s_waitcnt(vmcnt_imm(7 * GROUPS)); break;
+    case 6: __builtin_amdgcn_s_waitcnt(vmcnt_imm(6 * GROUPS)); break;
+    case 5: __builtin_amdgcn_s_waitcnt(vmcnt_imm(5 * GROUPS)); break;
+    case 4: __builtin_amdgcn_s_waitcnt(vmcnt_imm(4 * GROUPS)); break;
+    case 3: __builtin_amdgcn_s_waitcnt(vmcnt_imm(3 * GROUPS)); break;
+    case 2: __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * GROUPS)); break;
+    case 1: __builtin_amdgcn_s_waitcnt(vmcnt_imm(GROUPS)); break;
+    default: __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+  }
+}
+
 // NK = 4 / NR rings, each of NR waves with sixteen rows, and each with its own tiles of the segment.
 template <typename T, int LD, int NR, bool PAGED>
 __device__ __forceinline__ void ring_segments(const LatentAttnArgs& a, const AttnTable& table, const AttnLine& line, AttnSeg seg, int x_hi, char* smem) {
@@ -211,8 +227,27 @@ __device__ __forceinline__ void ring_segments(const LatentAttnArgs& a, const Att
       const int ti = it * NK + kg;
       if (ti >= ntl) return;
       char* slot = ring + (it % S) * kSlot;
+      if constexpr (S == 1) {                       // one part of all keys after the other, as the products take them
+        typename Source<T, LD, PAGED>::Group g[kGroups];
 #pragma unroll
-      for (int u = 0; u < kGroups; ++u) src.load_group(ti, rr * kGroups + u, slot);
+        for (int u = 0; u < kGroups; ++u) g[u] = src.group_of(ti, u);
+#pragma unroll
+        for (int block = 0; block < src.kBlocks; ++block)
+#pragma unroll
+          for (int u = 0; u < kGroups; ++u) src.load(g[u], u, block, slot);
+      } else {
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u) src.load_group(ti, rr * kGroups + u, slot);
+      }
+    };
+    // A ring of one slot: its wave takes a part of the tile as soon as that is there.  (What was asked for in front of the tile comes first.)
+    auto landed = [&](int block) {
+      if constexpr (S == 1) {
+        if (block >= src.kBlocks) return;
+        wait_blocks<kGroups>(src.kBlocks - 1 - block);
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        __builtin_amdgcn_sched_barrier(0);
+      }
     };
 
     f32x4_t oacc[kDT];
@@ -228,9 +263,7 @@ __device__ __forceinline__ void ring_segments(const LatentAttnArgs& a, const Att
       issue(it);
     }
     int k_at = src.rows_at(fr, fq), v_at = src.columns_at(fr, fq);
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));       // from here on vmcnt counts tile loads only
-    __builtin_amdgcn_sched_barrier(0);
-    if (!a.mask) rowmask = (2ull << i) - 1ull;
+    if constexpr (S > 1) __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));           // from here on vmcnt counts tile loads only
     if constexpr (S > 2) {
 #pragma unroll 1
       for (int it = together; it < S; ++it) {
@@ -243,8 +276,8 @@ __device__ __forceinline__ void ring_segments(const LatentAttnArgs& a, const Att
     for (int it = 0; it < nit; ++it) {
       if (S > 1 && it > 0) locate(it + S - 1);
       // this wave's pieces of tile `it` have landed once at most those of the S - 2 tiles behind it are outstanding (the first has already)
-      if (S <= 2 || it + S - 1 >= nit) __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-      else if (it > 0) __builtin_amdgcn_s_waitcnt(vmcnt_imm(S <= 2 ? 0 : (S - 2) * kPieces));
+      if (S == 2 || (S > 2 && it + S - 1 >= nit)) __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+      else if (S > 2 && it > 0) __builtin_amdgcn_s_waitcnt(vmcnt_imm(S <= 2 ? 0 : (S - 2) * kPieces));
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_s_waitcnt(0xC07F);           // lgkmcnt(0): tile it - 1 is read
       if constexpr (NR > 1) __builtin_amdgcn_s_barrier();
@@ -259,13 +292,16 @@ __device__ __forceinline__ void ring_segments(const LatentAttnArgs& a, const Att
         f32x4_t sacc[kHalves];
 #pragma unroll
         for (int j = 0; j < kHalves; ++j) sacc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        constexpr int kReads = kHalves * kKS, kAhead = kF32 ? 4 : 8;
+        constexpr int kReads = kHalves * kKS, kAhead = kF32 ? 4 : 8, kOfBlock = 4;          // reads; those of a 1 KB block of every group
+        static_assert(kHalves * src.kQuads == kOfBlock && kAhead % kOfBlock == 0, "");
+        landed(kAhead / kOfBlock - 1);
         auto kread = [&](int i) { return *reinterpret_cast<const uint4*>(src.row_read(tile, k_at, i / kHalves, i % kHalves)); };
         uint4 kf[kReads];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) kf[i] = kread(i);
 #pragma unroll
         for (int i = 0; i < kReads; ++i) {
+          if (i % kOfBlock == 0) landed((i + kAhead) / kOfBlock);
           if (i + kAhead < kReads) kf[i + kAhead] = kread(i + kAhead);
           __builtin_amdgcn_sched_barrier(0);
           f32x4_t& c = sacc[i % kHalves];
@@ -286,13 +322,15 @@ __device__ __forceinline__ void ring_segments(const LatentAttnArgs& a, const Att
 #pragma unroll
           for (int e = 0; e < 4; ++e) x[4 * j + e] = sacc[j][e] * sl2;
         if (!plain) {
+          asm volatile("" : "+v"(rowmask));         // (chosen here, not in front of the loop)
+          const uint64_t word = a.mask ? rowmask : (2ull << i) - 1ull;
 #pragma unroll
           for (int j = 0; j < kHalves; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const int p = t0 + 16 * j + 4 * fq + e;
               bool seen = p < s1;
-              if (seen && p >= L) seen = (rowmask >> (p - L)) & 1ull;
+              if (seen && p >= L) seen = (word >> (p - L)) & 1ull;
               x[4 * j + e] = seen ? x[4 * j + e] : -INFINITY;
             }
         }
