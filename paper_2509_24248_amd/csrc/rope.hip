@@ -100,7 +100,8 @@ struct Place {
   int64_t block;
   int at;
 };
-__device__ __forceinline__ bool entry_place(const CachePlace& kv, int b, int64_t p, int* status, Place& out) {
+// (`page`: the page table's word for p, which the caller has asked for, if p is in the cache)
+__device__ __forceinline__ bool entry_place(const CachePlace& kv, int b, int64_t p, int page, int* status, Place& out) {
   if (p < 0 || p >= kv.l_max) {
     report_status(status, kStatusBadLength);
     return false;
@@ -111,7 +112,6 @@ __device__ __forceinline__ bool entry_place(const CachePlace& kv, int b, int64_t
     return true;
   }
   const uint32_t in_seq = static_cast<uint32_t>(p) / static_cast<uint32_t>(kv.page_size);
-  const int page = kv.page_table[static_cast<int64_t>(b) * kv.max_pages + in_seq];
   out.block = page;
   out.at = static_cast<int>(p - static_cast<int64_t>(in_seq) * kv.page_size);
   return page_in_pool(page, kv.n_pages, status);
@@ -136,10 +136,13 @@ __global__ __launch_bounds__(kThreads) void k_rope_rows(const RopeRowsArgs a) {
   const int sub = lane / LPR, i = lane - sub * LPR;
   const int rows = a.Hq + 2 * a.Hkv;
   const int pos = a.pos[b];
+  const int64_t p = static_cast<int64_t>(pos) + t;
+  int page = -1;
+  if (a.Hkv && a.kv.paged && p >= 0 && p < a.kv.l_max) page = a.kv.page_table[static_cast<int64_t>(b) * a.kv.max_pages + static_cast<uint32_t>(p) / static_cast<uint32_t>(a.kv.page_size)];
   const uint32_t turn = rotary_position(a.offset, pos, b, t, a.T, a.status);
   Place at = {0, 0};
   bool stored = false;
-  if (a.Hkv) stored = entry_place(a.kv, b, static_cast<int64_t>(pos) + t, a.status, at);
+  if (a.Hkv) stored = entry_place(a.kv, b, p, page, a.status, at);
   if (sub >= RPW) return;
   // pairs i N .. i N + N - 1; in kHalvesOdd i, i + LPR, ..
   const int half = a.rot / 2;
@@ -249,6 +252,13 @@ __global__ __launch_bounds__(kThreads) void k_latent_write(const LatentWriteArgs
   const int pos = a.pos[b];
   mine = mine && (!a.count || t < a.count[b]);
   if (!__builtin_amdgcn_ballot_w64(mine)) return;
+  // frequencies and the entry's page are asked for beside the rows, not behind them
+  uint64_t turns[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) turns[e] = a.turns[i * N + e];
+  const int64_t p = static_cast<int64_t>(pos) + t;
+  int page = -1;
+  if (entry && mine && a.kv.paged && p >= 0 && p < a.kv.l_max) page = a.kv.page_table[static_cast<int64_t>(b) * a.kv.max_pages + static_cast<uint32_t>(p) / static_cast<uint32_t>(a.kv.page_size)];
   const int lo_at = PAIRS ? i * 2 * N : i * N, hi_at = PAIRS ? lo_at + N : lo_at + kLatentRope / 2;
   const int pieces = a.r / N;
   uint4 raw[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)}, lat[U][P], gain[P];
@@ -273,11 +283,11 @@ __global__ __launch_bounds__(kThreads) void k_latent_write(const LatentWriteArgs
   Place at = {0, 0};
   if (mine) {
     turn = rotary_position(a.offset, pos, b, t, a.T, a.status);
-    if (entry) mine = entry_place(a.kv, b, static_cast<int64_t>(pos) + t, a.status, at);
+    if (entry) mine = entry_place(a.kv, b, p, page, a.status, at);
   }
   float cs[N], sn[N], lo[N], hi[N];
 #pragma unroll
-  for (int e = 0; e < N; ++e) turn_at(turn, a.turns[i * N + e], a.amplitude, cs[e], sn[e]);
+  for (int e = 0; e < N; ++e) turn_at(turn, turns[e], a.amplitude, cs[e], sn[e]);
   Piece<T>::get(raw[0], lo);
   Piece<T>::get(raw[1], hi);
   turn_pieces<N, PAIRS>(lo, hi, cs, sn, N);
