@@ -19,8 +19,8 @@
 //   128     : bf16, two tiles of sixteen rows a wave: 256 registers of accumulators and 144 of queries.
 // Partial results go to memory as the accumulators lie (1 KB for 16 rows x 16 columns: one store instruction) and are merged by a second kernel.
 //
-// Measured (whole calls, LD = 512, bf16): 16 sequences x 16384 entries, 128 rows, 302 MB and 73 GFLOP: 117 us, 2.6 TB/s and 624 TFLOP/s, bound by the matrix instructions
-// (a library product of 8192 reaches 1234; here a third of the time goes to the start, the last partial results and the merge).
+// Measured (whole calls, LD = 512, bf16): 16 sequences x 16448 entries, 128 rows, 303 MB and 73 GFLOP: 97 us, 3.1 TB/s and 755 TFLOP/s, bound by the matrix instructions
+// (a library product of 8192 reaches 1257; here a third of the time goes to the start, the last partial results and the merge).
 #include "attn_sched.hpp"
 #include "common.hpp"
 #include "kernels.hpp"
@@ -727,8 +727,8 @@ __device__ __forceinline__ void pipe_segments(const LatentAttnArgs& a, const Att
 // Rows of a workgroup.  Few granules (64 entries for the whole rows of a sequence; the lengths are known here only): what counts is how many workgroups share them and what each
 // writes for the merge, 2 KB a row with 512 columns, so they take 16 rows, each with four rings of keys, or 32 with two; the caches are small then and their
 // second reader finds them in a cache of the chip.  Many: 64 or 128 (MOST), as many as the sequences have.  Whole calls, LD = 512, granules of MOST rows, 16 / 32 / MOST rows a workgroup:
-//   112 rows   3: 14.6 / 14.8 / 19.7 us   17: 16.6 / 16.2 / 21.0   65: 21.8 / 22.5 / 28.6   126: 23.1 / 24.7 / 34.2   257: 38.8 / 31.0 / 37.7   501: 44.7 / 42.7 / 43.3   1025: 70 / 68 / 51
-//   128 rows 256 (8 sequences): 36.9 / 36.8 / 39.5   504: 51.4 / 40.9 / 39.4   4112 (16): 331 / 204 / 117            64 rows 252: 29.1 / 25.4 / 29.6   2016: 114 / 73 / 66
+//   112 rows   3: 12.9 / 13.4 / 18.9 us   17: 15.4 / 16.1 / 20.2   65: 18.1 / 20.2 / 24.2   126: 20.9 / 21.5 / 28.1   160: 28.4 / 25.2 / 30.6   257: 35.0 / 28.2 / 31.3   501: 38.0 / 40.6 / 41.7
+//   1025: 61 / 63 / 46         128 rows 256 (8 sequences): 34.9 / 35.3 / 39.3   504: 46.1 / 40.3 / 39.3   4112 (16): 314 / 165 / 97         64 rows 252: 26.2 / 23.3 / 24.8   2016: 84 / 57 / 51
 constexpr int kFewGran = 160, kSomeGran = 512;
 __host__ __device__ __forceinline__ int rows_of_block(int rows, int most) {
   const int blocks = (rows + most - 1) / most;
