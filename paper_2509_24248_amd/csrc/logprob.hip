@@ -25,7 +25,7 @@ constexpr int kThreads = 256;
 constexpr int kNarrow = 16, kWide = 32;                    // values of a lane
 constexpr int kMostParts = 272;                            // parts of a row at most: 2^18 logits, 1024 a part
 constexpr int kList = 1536;                                // candidates
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
+constexpr float kLog2e = 1.44269504088896340736f, kLog2eRest = 1.9259630e-8f, kLn2 = 0.693147180559945309417f;
 
 typedef unsigned long long u64;
 
@@ -217,13 +217,16 @@ __global__ __launch_bounds__(kThreads) void k_logprob_row(const LogprobArgs a) {
   n = wave_sum_dpp(n);
   s = wave_sum_dpp(s);
   w = wave_sum_dpp(w);
-  const float norm = logf(n) + log1pf(s / n);             // ln of the sum of the weights
+  // The exponents' unit was rounded, log2(e) (1 - off) / T in its place: to first order the sum is off by off times its weights' logarithms, which w has.  (A row whose weights
+  // lie 15 units below the best one otherwise has 1e-6 in all its log probabilities.  The entropy is left as that of the rounded unit: off times the logarithms' variance.)
+  const float off = (fmaf(-unit, heat, kLog2e) + kLog2eRest) * kLn2;
+  const float norm = logf(n) + log1pf(fmaxf(fmaf(off * kLn2, w, s), 0.f) / n);             // ln of the sum of the weights
   auto logprob = [&](float x) {
     if (x != x || x == -INFINITY || top == -INFINITY) return -INFINITY;
     return (x == top ? 0.f : 2.f * ((0.5f * x - 0.5f * top) / heat)) - norm;       // (halves: their difference stays in range)
   };
   if (tid < a.n_tok) a.logprob[static_cast<int64_t>(r) * a.n_tok + tid] = known ? logprob(mine) : __uint_as_float(0x7FC00000u);
-  if (tid == 0 && a.entropy) a.entropy[r] = top == -INFINITY ? 0.f : norm - kLn2 * w / (n + s);
+  if (tid == 0 && a.entropy) a.entropy[r] = top == -INFINITY ? 0.f : logf(n) + log1pf(s / n) - kLn2 * w / (n + s);
   if (a.n_top == 0) return;
   // ---- the bound, and the groups that meet it
   float best = -INFINITY;
