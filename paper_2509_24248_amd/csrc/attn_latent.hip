@@ -155,6 +155,13 @@ struct Source {
   }
 };
 
+// The lane's number, worked out where it is wanted, not held.
+__device__ __forceinline__ int lane_here() {
+  int none = 0;
+  asm volatile("" : "+v"(none));
+  return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, none));
+}
+
 // Registers of a lane for accumulators and queries.  Up to 190 everything is done in 256 ordinary ones; beyond that the accumulators are in the other 256, which
 // only matrix instructions work on: see the rescaling.
 constexpr int held_registers(int ld, int e, int rtw) { return rtw * (ld / 4 + (ld + kPe) * e / 16); }
@@ -216,7 +223,7 @@ __device__ __forceinline__ void ring_segments(const LatentAttnArgs& a, const Att
     // (a load either way, without a mask of a query's bytes: a branch would wait for the queries in front of the first tiles)
     const int i = row / a.Hq;
     const uint64_t* mask_at = a.mask ? a.mask + static_cast<int64_t>(b) * a.mask_stride : static_cast<const uint64_t*>(a.q);
-    uint64_t rowmask = mask_at[a.mask ? i : 0];
+    const uint64_t rowmask = mask_at[a.mask ? i : 0];
     if (again) __syncthreads();                     // the rings are free of the segment before
     again = true;
 
@@ -322,8 +329,9 @@ __device__ __forceinline__ void ring_segments(const LatentAttnArgs& a, const Att
 #pragma unroll
           for (int e = 0; e < 4; ++e) x[4 * j + e] = sacc[j][e] * sl2;
         if (!plain) {
-          asm volatile("" : "+v"(rowmask));         // (chosen here, not in front of the loop)
-          const uint64_t word = a.mask ? rowmask : (2ull << i) - 1ull;
+          int given = __builtin_amdgcn_readfirstlane(a.mask != nullptr);
+          asm volatile("" : "+s"(given));           // (chosen here, not in front of the loop)
+          const uint64_t word = given ? rowmask : (2ull << i) - 1ull;
 #pragma unroll
           for (int j = 0; j < kHalves; ++j)
 #pragma unroll
@@ -555,10 +563,10 @@ __device__ __forceinline__ void pipe_segments(const LatentAttnArgs& a, const Att
     auto mask_tile = [&](int ti) {                  // keys past the range and block entries that a row does not see
       const int t0 = s0 + kKeys * ti;
       if (__builtin_expect(t0 + kKeys <= min(L, s1), 1)) return;
-      int ln = lane;                                // (worked out here, once or twice a segment, not held)
-      asm volatile("" : "+v"(ln));
 #pragma unroll
       for (int t = 0; t < RTW; ++t) {
+        const int ln = lane_here();                 // (once or twice a segment; of each row tile anew, for what is worked out from it is not held then)
+        __builtin_amdgcn_sched_barrier(0);
         const int i = (row0 + min(16 * (wv * RTW + t) + (ln & 15), R - 1)) / a.Hq;
         const uint64_t word = a.mask ? a.mask[static_cast<int64_t>(b) * a.mask_stride + i] : ((2ull << i) - 1ull);
 #pragma unroll
@@ -699,7 +707,7 @@ __device__ __forceinline__ void pipe_segments(const LatentAttnArgs& a, const Att
     }
     if (pass == 0) {                                // (static LDS, which the workgroup vote takes, has no room beside the slots)
       const bool mine = __builtin_amdgcn_ballot_w64(far) != 0ull;
-      if (lane == 0) votes[wv] = mine;
+      if (lane_here() == 0) votes[wv] = mine;
       __syncthreads();
       if (votes[0] | votes[1] | votes[2] | votes[3]) continue;
     }
@@ -712,8 +720,7 @@ __device__ __forceinline__ void pipe_segments(const LatentAttnArgs& a, const Att
       const float l = quad_row_sum(l_run[t]);
       const int rt = wv * RTW + t;
       if (rt >= tiles) continue;
-      int ln = lane;                                // (as above)
-      asm volatile("" : "+v"(ln));
+      const int ln = lane_here();
       if (ln < 16) *reinterpret_cast<float2*>(a.part_ml + ((slot * tiles + rt) * 16 + ln) * 2) = make_float2(ref[t], l);
       float* dst = a.part_o + (slot * tiles + rt) * (kDT * 256);
 #pragma unroll
