@@ -838,6 +838,8 @@ __device__ __forceinline__ void latent_row_again(const LatentAttnArgs& a, int b,
 // sixteen columns, and are read and added that way: (max, sum) pairs and fragments of a wave's segments in one round of requests, the WS waves that share a fragment's
 // segments in a fixed order.  (What is not there is not asked for: with the last segment again in its place the merge of 272 segments of 128 rows x 512 columns, 71 MB, took 17.3
 // us, 15.4 this way; with four waves a fragment there 24.6.)
+// A segment's sum counts whatever its weight: it is finite or, of a key that the row sees (what is masked weighs nothing), NaN, and maxima pass NaN over, so that a segment
+// whose scores are all NaN is left with the lowest maximum.
 template <typename T, int LD, int WS>
 __global__ __launch_bounds__(256) void k_latent_combine(const LatentAttnArgs a) {
   constexpr int kDT = LD / 16, kPer = 4 / WS, kCombAhead = WS == 1 ? 8 : 12;
@@ -889,8 +891,8 @@ __global__ __launch_bounds__(256) void k_latent_combine(const LatentAttnArgs a) 
       for (int e = 0; e < kCombAhead; ++e) {
         if (s0 + e * WS >= n) break;
         const float w = __builtin_amdgcn_exp2f(ml[e].x - m);
+        den = fmaf(w, ml[e].y, den);
         if (w != 0.f) {                             // (a weight of nothing counts nothing, whatever is there)
-          den = fmaf(w, ml[e].y, den);
 #pragma unroll
           for (int c = 0; c < 4; ++c) acc[c] = fmaf(w, o[e][c], acc[c]);
         }
@@ -913,8 +915,8 @@ __global__ __launch_bounds__(256) void k_latent_combine(const LatentAttnArgs a) 
 #pragma unroll
         for (int k = 0; k < WS; ++k) {
           const float w = __builtin_amdgcn_exp2f(ml[k].x - top);
-          if (w == 0.f) continue;
           den = fmaf(w, ml[k].y, den);
+          if (w == 0.f) continue;
           const f32x4_t v = part[wv + k][lane];
 #pragma unroll
           for (int c = 0; c < 4; ++c) acc[c] = fmaf(w, v[c], acc[c]);
