@@ -123,6 +123,10 @@ __host__ __device__ __forceinline__ float attn_sched_rcp(int x) {
 __host__ __device__ __forceinline__ int attn_sched_div(int a, int b) {
   return static_cast<int>((static_cast<float>(a) + 0.5f) * attn_sched_rcp(b));
 }
+// The same of any numbers: a is at most 2 T + 512 where T, the line's length, chooses the way, and less than 2^32.
+__host__ __device__ __forceinline__ int attn_sched_quotient(int T, uint32_t a, int b) {
+  return T < (1 << 20) - 512 ? attn_sched_div(static_cast<int>(a), b) : static_cast<int>(a / static_cast<uint32_t>(b));
+}
 __host__ __device__ __forceinline__ AttnLine attn_sched_line(int gran, int B, int Hkv, int pad, int wide_from, int spread, int wgrid) {
   AttnLine l;
   l.T = gran * Hkv;
@@ -133,14 +137,15 @@ __host__ __device__ __forceinline__ AttnLine attn_sched_line(int gran, int B, in
     const int units = B * Hkv;
     l.T += units * pad;
     want = (l.T + 1) >> 1;
-    if (!wide || want < kAttnSpread) {                                    // (T < 2^21)
+    if (!wide || want < kAttnSpread) {
       const int most = (l.T + kAttnSpread - 1) / kAttnSpread;             // the largest share
-      want = spread ? kAttnSpread : units * attn_sched_div(l.T + units * most - 1, units * most);
-      if (want > kAttnSpread) want = attn_sched_div(l.T + most - 1, most);
+      // (more units than workgroups: no whole number for each, and the product may pass 32 bits)
+      want = spread ? kAttnSpread : units > kAttnSpread ? kAttnSpread + 1 : units * attn_sched_quotient(l.T, static_cast<uint32_t>(l.T) + units * most - 1, units * most);
+      if (want > kAttnSpread) want = attn_sched_quotient(l.T, static_cast<uint32_t>(l.T) + most - 1, most);
     }
   }
   l.W = want < 1 ? 1 : want < wgrid ? want : wgrid;
-  l.q = l.T < 1 << 21 ? attn_sched_div(l.T, l.W) : static_cast<int>(static_cast<uint32_t>(l.T) / static_cast<uint32_t>(l.W));
+  l.q = attn_sched_quotient(l.T, l.T, l.W);
   l.r = l.T - l.q * l.W;                                                  // (q is at least 1: W <= T)
   return l;
 }
