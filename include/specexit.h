@@ -534,7 +534,10 @@ int32_t specexit_latent_kv_compact(const specexit_latent_kv_view *kv, int32_t n_
  *   entropy[r] = - sum p ln p (may be NULL);
  *   top_token[r, k], top_logprob[r, k] (may be NULL): the n_top best by (logit descending, index ascending); -1 and -infinity behind the last above -infinity.
  * NaN logits count as -infinity.  If some are +infinity, those share the probability; a row without any logit above -infinity has log probabilities of -infinity and entropy 0.
- * At least one of entropy, n_tok and n_top is asked for.  The same row gives the same bits whatever else is in the call only where M * V lies on the same side of 4 million logits. */
+ * At least one of entropy, n_tok and n_top is asked for. 
+ * The same row gives the same bits whatever else is in the call if it begins as many bytes behind a multiple of 16 (the rows of one call do where ld is a multiple of
+ * 16 bytes) and M ceil((V + 7) / 2048) is below 2048 in both calls or in neither: from there on a row is summed in parts of 2048 logits, below in parts of 1024, and parts
+ * begin at multiples of 16 bytes. */
 #define SPECEXIT_LOGPROB_MAX_TOK 64
 #define SPECEXIT_LOGPROB_MAX_TOP 32
 int32_t specexit_token_logprobs(int32_t dtype, int32_t M, int32_t V, const void *logits /*[M,ld]*/, int64_t ld, int32_t rows_per_seq,
