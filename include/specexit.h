@@ -475,8 +475,10 @@ size_t specexit_sample_workspace_bytes(int32_t dtype, int32_t M, int32_t V);
 
 /* ---- rotary positions (the target's queries and keys in front of its verification attention) ----
  * specexit_rope_table writes the frequencies of a rotation, f_c / 2 pi as fractions of 2^64, to turns [rot_dim / 2] on the device: once per
- * model; the calls below read it and take rot_dim, interleaved and amplitude from the same descriptor.  An angle at position p
- * is off by p (2^-64 turns + 2^-48 f_c) at most. */
+ * model; the calls below read it and take rot_dim, interleaved and amplitude from the same descriptor.  Sine and cosine at position p are
+ * those of an angle that is off by p (2^-64 turns + 2^-48 f_c) and by 2^-32 turns (1.5e-9; the product of position and frequency is cut there, downward),
+ * worked out in 32 bits: 2^-21 of themselves.  (The sine of a pair that has turned by 10^-7 has two digits then; what it adds to the other value of its pair
+ * is right to a fortieth of an fp32 rounding of that.) */
 int32_t specexit_rope_table(const specexit_rope_desc *rope, uint64_t *turns /*[rot_dim/2]*/, void *stream);
 
 /* Rotates the heads of rows.  Head h of token t of sequence b lies (b * T + t) * token_stride + h * head_dim elements behind rows, its result at
