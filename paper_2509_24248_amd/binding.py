@@ -647,6 +647,14 @@ def _head_rows(rows: torch.Tensor, B: int, T: int, heads: int, d: int, want, nam
     return step
 
 
+def _holds(kv, B: int) -> None:
+    """A view says nothing of how many sequences its cache (or page table) has; what the helpers above made a view of does."""
+    keep = getattr(kv, "_keep", None)
+    if keep is not None:
+        n = (keep[0] if keep[-1] is None else keep[-1]).shape[0]
+        assert n >= B, f"the cache has {n} sequences, {B} are read or written"
+
+
 def specexit_rope(dtype: int, rope: RopeDesc, turns, B: int, T: int, n_heads: int, head_dim: int, rows, out, pos, offset=None, count=None,
                   flags: int = 0, stream=None) -> None:
     """rows, out: [B, T, n_heads, head_dim], tokens evenly apart (slices of a fused projection's output will do); out may be rows."""
@@ -661,6 +669,7 @@ def specexit_rope_kv_write(kv: KVView, rope: RopeDesc, turns, B: int, T: int, n_
                            count=None, flags: int = 0, stream=None) -> None:
     """q_rows [B, T, n_q_heads, d], k_rows, v_rows [B, T, n_kv_heads, d]: tokens evenly apart; q_out contiguous."""
     want, i32, d = _STORAGE.get(kv.dtype), torch.int32, kv.head_dim
+    _holds(kv, B)
     step = _head_rows(k_rows, B, T, kv.n_kv_heads, d, want, "k_rows")
     assert v_rows.is_cuda and v_rows.dtype == k_rows.dtype and v_rows.shape == k_rows.shape and v_rows.stride() == k_rows.stride(), "k_rows and v_rows must lie alike"
     q_step, q_at = (_head_rows(q_rows, B, T, n_q_heads, d, want, "q_rows"), q_rows.data_ptr()) if n_q_heads else (0, None)
@@ -675,6 +684,7 @@ def specexit_latent_kv_write(kv: LatentKVView, rope: RopeDesc, turns, B: int, T:
     """rows [B, T, latent_dim + 64], tokens evenly apart; q_rows [B, T, n_q_heads, 64], tokens and heads evenly apart; q_out [B, T, n_q_heads,
     latent_dim + 64] contiguous, its last 64 values are written."""
     want, i32, w = _STORAGE.get(kv.dtype), torch.int32, kv.latent_dim + kv.rope_dim
+    _holds(kv, B)
     step = _head_rows(rows.unsqueeze(2), B, T, 1, w, want, "rows")
     gain = _arg(gain, want, kv.latent_dim, "gain")
     q_at, q_step, head_step = None, 0, 0
@@ -697,6 +707,7 @@ def specexit_latent_verify_attn_workspace_bytes(kv: LatentKVView, B: int, n_q: i
 
 def specexit_latent_verify_attn(kv: LatentKVView, B: int, n_q: int, n_q_heads: int, q, ctx_len, mask, scale: float, out, workspace,
                                 flags: int = 0, stream=None) -> None:
+    _holds(kv, B)
     want, n = _STORAGE.get(kv.dtype), B * n_q * n_q_heads
     q, out = _arg(q, want, n * (kv.latent_dim + kv.rope_dim), "q"), _arg(out, want, n * kv.latent_dim, "out")
     ctx_len = _arg(ctx_len, torch.int32, B, "ctx_len")
@@ -707,6 +718,7 @@ def specexit_latent_verify_attn(kv: LatentKVView, B: int, n_q: int, n_q_heads: i
 
 def specexit_latent_kv_compact(kv: LatentKVView, n_layers: int, layer_stride_bytes: int, B: int, n_q: int, ctx_len, accept_path, accept_len,
                                last_node=None, block_hidden=None, D: int = 0, hidden_next=None, flags: int = 0, stream=None) -> None:
+    _holds(kv, B)
     i32, want = torch.int32, _STORAGE.get(kv.dtype)
     ctx_len, accept_path = _arg(ctx_len, i32, B, "ctx_len"), _arg(accept_path, i32, B * n_q, "accept_path")
     accept_len, last_node = _arg(accept_len, i32, B, "accept_len"), _arg(last_node, i32, B, "last_node")
