@@ -671,7 +671,7 @@ def specexit_rope_kv_write(kv: KVView, rope: RopeDesc, turns, B: int, T: int, n_
     want, i32, d = _STORAGE.get(kv.dtype), torch.int32, kv.head_dim
     _holds(kv, B)
     step = _head_rows(k_rows, B, T, kv.n_kv_heads, d, want, "k_rows")
-    assert v_rows.is_cuda and v_rows.dtype == k_rows.dtype and v_rows.shape == k_rows.shape and v_rows.stride() == k_rows.stride(), "k_rows and v_rows must lie alike"
+    assert _head_rows(v_rows, B, T, kv.n_kv_heads, d, want, "v_rows") == step, "k_rows and v_rows must lie alike"
     q_step, q_at = (_head_rows(q_rows, B, T, n_q_heads, d, want, "q_rows"), q_rows.data_ptr()) if n_q_heads else (0, None)
     q_out = _arg(q_out, want, B * T * n_q_heads * d, "q_out") if n_q_heads else None
     pos, offset, count = _arg(pos, i32, B, "pos"), _arg(offset, i32, B * T, "offset"), _arg(count, i32, B, "count")

@@ -64,3 +64,15 @@ def test_more_sequences_than_the_cache_has(paged):
 
 class Null:                                        # a stream by its handle
     cuda_stream = 0
+
+
+def test_keys_and_values_of_one_token_may_lie_anyhow():
+    """With one token of one sequence the strides of those two dimensions say nothing."""
+    from paper_2509_24248_amd import binding as sx
+    kv = sx.kv_view(f(1, 2, 48, 64), f(1, 2, 48, 64))
+    k, v = f(1, 1, 6, 64)[:, :, :2], f(1, 1, 2, 64)
+    assert k.stride() != v.stride()
+    write = lambda a, b: sx.specexit_rope_kv_write(kv, sx.rope_desc(64, theta=0.5), turns(64), 1, a.shape[1], 0, None, a, b, None, i(1), stream=Null)
+    stopped_by_the_library(sx, "theta", write, k, v)
+    rejected("must lie alike", write, f(1, 3, 6, 64)[:, :, :2], f(1, 3, 2, 64))
+    rejected("v_rows must be torch.float32", write, k, v.double())
