@@ -739,6 +739,8 @@ def specexit_token_logprobs(dtype: int, M: int, V: int, logits, entropy=None, to
     assert logits.is_cuda and logits.dim() == 2 and logits.shape[0] == M and logits.shape[1] >= V and logits.stride(1) == 1
     ld = logits.stride(0) if M > 1 else logits.shape[1]
     n_tok, n_top = (0 if t is None else t.shape[1] if t.dim() == 2 else 1 for t in (token, top_token))
+    for t, n, name in ((logprob, n_tok, "logprob"), (top_logprob, n_top, "top_logprob")):
+        assert t is None or (t.shape[1] == n if t.dim() == 2 else n > 0), f"{name}: {tuple(t.shape)} for {n} tokens a row"
     token, logprob = _arg(token, i32, M * n_tok, "token"), _arg(logprob, f32, M * n_tok, "logprob")
     entropy, temperature = _arg(entropy, f32, M, "entropy"), _arg(temperature, f32, -(-M // max(rows_per_seq, 1)), "temperature")
     top_token, top_logprob = _arg(top_token, i32, M * n_top, "top_token"), _arg(top_logprob, f32, M * n_top, "top_logprob")

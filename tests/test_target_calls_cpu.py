@@ -76,3 +76,17 @@ def test_keys_and_values_of_one_token_may_lie_anyhow():
     stopped_by_the_library(sx, "theta", write, k, v)
     rejected("must lie alike", write, f(1, 3, 6, 64)[:, :, :2], f(1, 3, 2, 64))
     rejected("v_rows must be torch.float32", write, k, v.double())
+
+
+def test_log_probabilities_without_their_tokens():
+    """An output whose width is not that of what it belongs to would be left as it is, or be laid out another way."""
+    from paper_2509_24248_amd import binding as sx
+    M, V = 4, 100
+    call = lambda **kw: sx.specexit_token_logprobs(sx.F32, M, V, f(M, V), f(M), rows_per_seq=0, stream=Null, **kw)
+    rejected("logprob: \\(4, 1\\) for 0 tokens", call, logprob=f(M, 1))
+    rejected("logprob: \\(4,\\) for 0 tokens", call, logprob=f(M))
+    rejected("logprob: \\(4, 3\\) for 1 tokens", call, token=i(M, 1), logprob=f(M, 3))
+    rejected("top_logprob: \\(4, 5\\) for 0 tokens", call, top_logprob=f(M, 5))
+    rejected("top_logprob: \\(4, 5\\) for 2 tokens", call, top_token=i(M, 2), top_logprob=f(M, 5))
+    for kw in (dict(token=i(M, 2), logprob=f(M, 2)), dict(token=i(M), logprob=f(M)), dict(top_token=i(M, 5)), dict(token=i(M, 0), logprob=f(M, 0)), dict(token=i(M, 1), logprob=f(2 * M, 1))):
+        stopped_by_the_library(sx, "rows_per_seq", call, **kw)
