@@ -299,6 +299,7 @@ def kv_view(k: torch.Tensor, v: torch.Tensor, page_table: Optional[torch.Tensor]
         kv.page_table = page_table.data_ptr()
         kv.page_size, kv.max_pages_per_seq = k.shape[2], page_table.shape[1]
         kv.l_max, kv.n_pages = page_table.shape[1] * k.shape[2], k.shape[0]
+    kv._sequences = k.shape[0] if page_table is None else page_table.shape[0]
     kv._keep = (k, v, page_table)      # the view holds raw addresses: keep their tensors alive with it
     return kv
 
@@ -618,6 +619,7 @@ def latent_kv_view(c: torch.Tensor, rope_dim: int = 64, page_table: Optional[tor
         kv.page_table = page_table.data_ptr()
         kv.page_size, kv.max_pages_per_seq = c.shape[1], page_table.shape[1]
         kv.l_max, kv.n_pages = page_table.shape[1] * c.shape[1], c.shape[0]
+    kv._sequences = c.shape[0] if page_table is None else page_table.shape[0]
     kv._keep = (c, page_table)
     return kv
 
@@ -648,11 +650,8 @@ def _head_rows(rows: torch.Tensor, B: int, T: int, heads: int, d: int, want, nam
 
 
 def _holds(kv, B: int) -> None:
-    """A view says nothing of how many sequences its cache (or page table) has; what the helpers above made a view of does."""
-    keep = getattr(kv, "_keep", None)
-    if keep is not None:
-        n = (keep[0] if keep[-1] is None else keep[-1]).shape[0]
-        assert n >= B, f"the cache has {n} sequences, {B} are read or written"
+    """The library takes a view at its word for how many sequences its cache (or page table) has: the helpers above note it (0.1 us a call)."""
+    assert getattr(kv, "_sequences", B) >= B, f"the cache has {kv._sequences} sequences, {B} are read or written"
 
 
 def specexit_rope(dtype: int, rope: RopeDesc, turns, B: int, T: int, n_heads: int, head_dim: int, rows, out, pos, offset=None, count=None,
@@ -731,6 +730,14 @@ def specexit_token_logprobs_workspace_bytes(dtype: int, M: int, V: int, n_top: i
     return int(LIB.specexit_token_logprobs_workspace_bytes(dtype, M, V, n_top))
 
 
+def _columns(t: Optional[torch.Tensor], flat: int = 1) -> int:
+    """n of a tensor [M, n]; of one of another shape what it may be taken for, at least one."""
+    if t is None:
+        return 0
+    shape = t.shape
+    return shape[1] if len(shape) == 2 else max(flat, 1)
+
+
 def specexit_token_logprobs(dtype: int, M: int, V: int, logits, entropy=None, token=None, logprob=None, top_token=None, top_logprob=None,
                             temperature=None, rows_per_seq: int = 1, workspace=None, flags: int = 0, stream=None) -> None:
     """logits: [M, >= V], rows evenly apart; token (int32), logprob: [M, n_tok]; top_token (int32), top_logprob: [M, n_top]."""
@@ -738,9 +745,9 @@ def specexit_token_logprobs(dtype: int, M: int, V: int, logits, entropy=None, to
     assert want is None or logits.dtype == want, f"logits must be {want}"
     assert logits.is_cuda and logits.dim() == 2 and logits.shape[0] == M and logits.shape[1] >= V and logits.stride(1) == 1
     ld = logits.stride(0) if M > 1 else logits.shape[1]
-    n_tok, n_top = (0 if t is None else t.shape[1] if t.dim() == 2 else 1 for t in (token, top_token))
-    for t, n, name in ((logprob, n_tok, "logprob"), (top_logprob, n_top, "top_logprob")):
-        assert t is None or (t.shape[1] == n if t.dim() == 2 else n > 0), f"{name}: {tuple(t.shape)} for {n} tokens a row"
+    n_tok, n_top = _columns(token), _columns(top_token)
+    assert logprob is None or _columns(logprob, n_tok) == n_tok, f"logprob: {tuple(logprob.shape)} for {n_tok} tokens a row"
+    assert top_logprob is None or _columns(top_logprob, n_top) == n_top, f"top_logprob: {tuple(top_logprob.shape)} for {n_top} tokens a row"
     token, logprob = _arg(token, i32, M * n_tok, "token"), _arg(logprob, f32, M * n_tok, "logprob")
     entropy, temperature = _arg(entropy, f32, M, "entropy"), _arg(temperature, f32, -(-M // max(rows_per_seq, 1)), "temperature")
     top_token, top_logprob = _arg(top_token, i32, M * n_top, "top_token"), _arg(top_logprob, f32, M * n_top, "top_logprob")
