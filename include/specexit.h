@@ -501,7 +501,7 @@ int32_t specexit_rope_kv_write(const specexit_kv_view *kv, const specexit_rope_d
 
 /* ---- latent cache: entries written ----
  * rows (token t of sequence b: (b * T + t) * row_stride elements behind, latent_dim + 64 values in the view's dtype) go to entries pos[b] + t, t < count[b]: the latent x as
- * x / sqrt(mean x^2 + eps) * gain (gain NULL: as it is), the other 64 values rotated (rope->rot_dim must be 64).  With n_q_heads > 0 the queries' rotated part is
+ * x / sqrt(mean x^2 + eps) * gain (gain NULL: as it is; the squares are summed in fp32, so the mean is one of values below 2^59), the other 64 values rotated (rope->rot_dim must be 64).  With n_q_heads > 0 the queries' rotated part is
  * written too: 64 values of head h at (b * T + t) * q_stride + h * head_stride behind q_rows become the last 64 of q_out [B, T, n_q_heads, latent_dim + 64], whose first
  * latent_dim (the query times the key half of the latent's up-projection) are the caller's and stay.  Positions, counts and what is not written as in specexit_rope_kv_write;
  * pointers and strides are multiples of 16 bytes. */
@@ -514,8 +514,8 @@ int32_t specexit_latent_kv_write(const specexit_latent_kv_view *kv, const specex
 /* ---- stage 2 over a latent cache: specexit_verify_attn where one vector a token is key and value of every head (Alg. 1) ----
  * out[b,i,h,:] = sum_j softmax_j(scale * q[b,i,h,:] . c[j]) c[j][0:latent_dim]; q is [B, n_q, n_q_heads, latent_dim + 64], out [B, n_q, n_q_heads, latent_dim] (to be multiplied with the
  * value half of the up-projection), in the view's dtype and 16-byte aligned (out: 8 suffice).  Context, block entries and masks as in specexit_verify_attn; n_q_heads 1 .. 256, scale > 0.  bf16
- * probabilities are multiplied in two bf16 parts (16 bits) or, with more than 64 rows n_q n_q_heads over long contexts, in one (8 bits), divided by the sum of what those
- * hold; fp32 products and sums are fp32.
+ * probabilities are multiplied in two bf16 parts (16 bits) or, with more than 64 rows n_q n_q_heads over long contexts, in one (8 bits): where the sequences' entries in
+ * sixty-fours, rounded up, times the blocks of 128 rows of a sequence are 512 or more.  They are divided by the sum of what those hold; fp32 products and sums are fp32.
  * Entries that a row does not see may hold anything, NaN included (values that are not finite among them make the call slow: rows of its sequence are computed
  * again key by key); a row that sees nothing (an empty context and an empty mask word) is all zeros. */
 int32_t specexit_latent_verify_attn(const specexit_latent_kv_view *kv, int32_t B, int32_t n_q, int32_t n_q_heads, const void *q,

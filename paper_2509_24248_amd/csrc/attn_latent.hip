@@ -3,7 +3,7 @@
 //
 //   s_j = scale q . (c_j | k_j),  o = sum_j softmax_j(s) c_j          2 (2 LD + 64) operations a row and entry of (LD + 64) e bytes
 //
-// Read once, an entry has 2 R (2 LD + 64) / (LD + 64) operations an element: up to some 80 rows the bytes are the bound, beyond that the matrix instructions.
+// Read once, an entry has 2 R (2 LD + 64) / (LD + 64) operations an element: up to some 80 rows the bytes take longer, beyond that the products.
 //
 // The rows of a sequence are cut into blocks; a workgroup takes an equal share of all keys of all (sequence, block) units (attn_sched.hpp, the blocks in the place
 // of KV heads).  Inside it the tiles of 32 keys (fp32: 16) lie in LDS once, as they lie in memory, and are read twice from there:
@@ -19,8 +19,10 @@
 //   128     : bf16, two tiles of sixteen rows a wave: 256 registers of accumulators and 144 of queries.
 // Partial results go to memory as the accumulators lie (1 KB for 16 rows x 16 columns: one store instruction) and are merged by a second kernel.
 //
-// Measured (whole calls, LD = 512, bf16): 16 sequences x 16448 entries, 128 rows, 303 MB and 73 GFLOP: 97 us, 3.1 TB/s and 755 TFLOP/s, bound by the matrix instructions
-// (a library product of 8192 reaches 1257; here a third of the time goes to the start, the last partial results and the merge).
+// Measured (whole calls, LD = 512, bf16): 16 sequences x 16448 entries, 128 rows, 303 MB and 73 GFLOP: 97 us, 3.1 TB/s and 755 TFLOP/s (a library product of 8192 reaches 1257).
+// Beyond some 80 rows no unit is full: of the cycles of the attention kernel over 16 contexts of 8192 to 32768 entries the matrix instructions are busy for 45 %, vector instructions for 24, LDS for
+// 23, and 23 are spent waiting, at 1.6 GHz, where the power limit holds the clock.  With one wave to a SIMD (its accumulators are half of the registers) nothing fills what the order of that wave's
+// instructions leaves open.  The merge is 15 us of such a call's 120.
 #include "attn_sched.hpp"
 #include "common.hpp"
 #include "kernels.hpp"
@@ -490,7 +492,10 @@ __device__ __forceinline__ void pipe_segments(const LatentAttnArgs& a, const Att
   constexpr int S = 4, kSlot = slot_bytes(LD, 2), kKeys = 32;
   static_assert(stages_of(LD, 2, 1) == S, "four slots");
   constexpr int kKS = Src::kRowB / 64, kReads = 2 * kKS, kDT = LD / 16, kBlocks = Src::kBlocks;
-  constexpr bool kSplitP = RTW == 1;                // probabilities: two bf16 parts (16 bits) with 64 rows; with 128 the matrix instructions are the bound, and one part, normalised with its own sum, is a third less of the products
+  // Probabilities: two bf16 parts (16 bits) with 64 rows, with 128 one (8 bits), normalised with its own sum, so that the rounding is no bias.  Two would be a third more of the products and sixteen registers
+  // more than there are: 139 us where one takes 117 (16 sequences x 20480 entries, 128 rows), 214 for 169 (8 x 9216, 1024 rows); blocks of 64 rows with two parts take 147 and 240.  One leaves
+  // results 1.15 to 1.33 times as far from 64 bits as their own rounding to bf16 does (with two: 1.00).
+  constexpr bool kSplitP = RTW == 1;
   constexpr float kReach = 60.f;                    // log2; sums of 2^31 such probabilities times values of 2^30 stay in range
   // With 128 rows of 512 columns the accumulators are all 256 registers that matrix instructions alone work on, and the compiler has no form that puts
   // other results elsewhere: the scores' instructions are written out.
